@@ -260,6 +260,99 @@ int kvc_prefetch_layers_window_static(kvc_ctx* ctx, void* d_l2, int32_t* d_tags,
                                       int32_t layer_begin, int32_t layer_end, int64_t pool_blocks_per_layer,
                                       int32_t fill_half, int32_t omega, int64_t* d_notify, void* stream);
 
+/* ---- Decode steps over the paged cache ---------------------------------------------------------
+ * What a serving program does with the FP16 cache and the compressed pool between offload and fetch: it
+ * writes new tokens' keys and values into the cache, computes attention over it, forks sequences, and gives
+ * up the blocks of those that ended.  The calls follow the rules above: they only enqueue kernels (and may
+ * be recorded into a HIP graph), block ids < 0 mean "no block", an id or table entry beyond its buffer sets
+ * KVC_ST_BAD_INDEX and counts as no block.
+ *
+ * The cache has the context's geometry and layout (kvc_set_cache_layout).  Keys of KV head h are page h of a
+ * block.  Their values are page n_kv_heads + h of the same block where d_v_cache is NULL (pages_per_block =
+ * 2 * n_kv_heads), else page h of the same block of d_v_cache (pages_per_block = n_kv_heads).  Token t of a
+ * sequence is row t mod N of the block that entry t div N of its row of the block table names. */
+
+/* New tokens of a batch: token i (of n_new) of sequence s has its K and V rows written to position
+ * lens[s] - n_new + i of the sequence, so that lens counts the new tokens already, as kvc_attend takes it.
+ * Positions below 0 and positions without a block are skipped. */
+typedef struct {
+    void* d_k_cache;
+    void* d_v_cache;        /* NULL: values are in d_k_cache */
+    int64_t n_cache_blocks; /* of either */
+    const int32_t* d_block_table; /* [n_seq][max_blocks] */
+    const int32_t* d_lens;        /* [n_seq] */
+    const void* d_k_new;    /* FP16: element (s, i, h, c) at s*k_strides[0] + i*k_strides[1] + h*k_strides[2] + c */
+    const void* d_v_new;
+    int64_t k_strides[3], v_strides[3]; /* FP16 elements, multiples of 8; both pointers 16-byte aligned */
+    int32_t max_blocks, n_seq, n_new, n_kv_heads;
+} kvc_append_t;
+int kvc_append(kvc_ctx* ctx, const kvc_append_t* a, void* stream);
+
+/* Attention of the last n_q tokens of every sequence over the sequence's tokens, and over a prefix that a
+ * group of consecutive sequences shares.  n_heads query heads, n_heads / n_kv_heads of them to a KV head.
+ * Query i of sequence s sees the tokens t < lens[s] - (n_q - 1 - i) of its own row of d_block_table, and all
+ * prefix_lens[g] tokens of row g of d_prefix_table where prefix_first[g] <= s < prefix_first[g+1].  With
+ * x_t = scale * <q, k_t> and m = max x_t:  out = sum e^(x_t - m) v_t / sum e^(x_t - m), and, where asked for,
+ * lse = m + ln sum e^(x_t - m).  Tokens without a block do not exist: what memory holds in their place, and
+ * behind the last token, is never read into a sum.  A query that sees no token gets out = 0, lse = -inf.
+ * Each prefix is read once for its group, not once for every sequence.  Lengths beyond their table's row set
+ * KVC_ST_BAD_INDEX and are cut to it.  Sums, maxima and products are held in 32 bits; the weights e^(x_t - m)
+ * are rounded to FP16 (11 bits, far from its smallest numbers) for the product with the values.
+ * d_work: device memory of at least kvc_attend_workspace(...) bytes, 256-byte aligned, contents meaningless
+ * between calls; calls that overlap in time need workspaces of their own. */
+typedef struct {
+    const void* d_q;        /* FP16: element (s, i, head, c) at s*q_strides[0] + i*q_strides[1] + head*q_strides[2] + c */
+    void* d_out;            /* FP16, with out_strides likewise */
+    float* d_lse;           /* NULL, or [n_seq][n_q][n_heads] */
+    int64_t q_strides[3], out_strides[3]; /* FP16 elements, multiples of 8; both pointers 16-byte aligned */
+    const void* d_k_cache;
+    const void* d_v_cache;  /* NULL: values are in d_k_cache */
+    int64_t n_cache_blocks; /* of either */
+    const int32_t* d_block_table;  /* [n_seq][max_blocks] */
+    const int32_t* d_lens;         /* [n_seq], the last n_q tokens included */
+    const int32_t* d_prefix_table; /* [n_prefix][max_prefix_blocks]; the three may be NULL where n_prefix = 0 */
+    const int32_t* d_prefix_lens;  /* [n_prefix] */
+    const int32_t* d_prefix_first; /* [n_prefix + 1], non-decreasing, 0..n_seq; sequences outside all groups have no prefix */
+    int32_t max_blocks, max_prefix_blocks, n_prefix, n_seq, n_q, n_heads, n_kv_heads;
+    float scale;
+    void* d_work;
+    uint64_t work_bytes;
+} kvc_attend_t;
+int kvc_attend(kvc_ctx* ctx, const kvc_attend_t* a, void* stream);
+/* Workspace of a call of these sizes, in bytes (0: sizes that kvc_attend refuses). */
+uint64_t kvc_attend_workspace(int32_t n_seq, int32_t n_q, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t n_prefix);
+
+/* Copy of cache blocks: in every layer l < n_layers, block l*blocks_per_layer + src[i] is copied to block
+ * l*blocks_per_layer + dst[i] of the same cache, i < n.  One block may be copied to several; no block may be
+ * both source and destination, nor destination twice. */
+int kvc_copy_blocks(kvc_ctx* ctx, void* d_cache, int64_t n_cache_blocks, const int32_t* d_src_ids, const int32_t* d_dst_ids, int32_t n,
+                    int32_t n_layers, int64_t blocks_per_layer, void* stream);
+
+/* Fork of pool blocks, ids as in kvc_copy_blocks (l*pool_blocks_per_layer + id): block dst[i] becomes a second name of what
+ * block src[i] holds.  Payloads are never written in place, so both share them: only descriptors are copied.
+ * What dst[i] held before is given up (its span stays in use until kvc_compact_pool or kvc_reset_pool). */
+int kvc_fork_blocks(kvc_ctx* ctx, const int32_t* d_src_ids, const int32_t* d_dst_ids, int32_t n, int32_t n_layers, int64_t pool_blocks_per_layer,
+                    void* stream);
+
+/* Pool blocks l*pool_blocks_per_layer + ids[i] are given up: their descriptors become INVALID.  A payload that another
+ * block shares stays that block's. */
+int kvc_free_blocks(kvc_ctx* ctx, const int32_t* d_ids, int32_t n, int32_t n_layers, int64_t pool_blocks_per_layer, void* stream);
+
+/* The payloads that the bound descriptor table still names, moved together: to the beginning of d_pool_out, in the
+ * order of their offsets, shared payloads once, with d_desc_out (as many entries as the bound table) naming
+ * their new places and *d_used_out the bytes they take.  The bound pool and table are only read: decodes may go on,
+ * until kvc_adopt_pool puts the context on the new ones.  A descriptor whose payload leaves the bound pool
+ * becomes INVALID and sets KVC_ST_CORRUPT; one whose payload does not fit into pool_out_bytes becomes INVALID and sets
+ * KVC_ST_POOL_FULL.  Pointers 16-byte aligned (d_used_out 8, d_work 256); the new buffers must not overlap the bound ones. */
+int kvc_compact_pool(kvc_ctx* ctx, void* d_pool_out, uint64_t pool_out_bytes, kvc_desc* d_desc_out, uint64_t* d_used_out, void* d_work,
+                     uint64_t work_bytes, void* stream);
+/* Workspace of kvc_compact_pool on a bound pool of pool_bytes, in bytes: about a ninetieth of it. */
+uint64_t kvc_compact_workspace(uint64_t pool_bytes);
+
+/* kvc_bind_pool on buffers that kvc_compact_pool has filled: the cursor goes to *d_used (device memory, read on the
+ * stream), the status stays. */
+int kvc_adopt_pool(kvc_ctx* ctx, void* d_pool, uint64_t pool_bytes, kvc_desc* d_desc, uint64_t n_desc_pages, const uint64_t* d_used, void* stream);
+
 /* Reduce the descriptor table and read the device state.  The only call that synchronises
  * (on `stream`).  Returns KVC_ERR_POOL_FULL / KVC_ERR_CORRUPT if the matching status bit is set
  * (out is filled either way), else 0. */

@@ -1,7 +1,8 @@
 """Build libkvc.so (HIP, gfx950) in-tree with hipcc.  No GPU is needed to compile.
 
 The codec kernels (csrc/kvc_codec.hip) are compiled once per group of page shapes
-(-DKVC_SHAPE_GROUP=k), side by side with the other sources; the objects are then linked."""
+(-DKVC_SHAPE_GROUP=k), attention (csrc/kvc_attend.hip) once per head dimension, side by side with the other sources; the
+objects are then linked."""
 from __future__ import annotations
 
 import concurrent.futures
@@ -13,11 +14,13 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_PKG)
 _CSRC = os.path.join(_PKG, "csrc")
 SHAPE_GROUPS = 16  # see csrc/kvc_codec.hip
+HEAD_DIMS = range(32, 257, 32)  # see csrc/kvc_attend.hip
 #: (source, extra defines, object name)
-UNITS = [("kvc_kernels.hip", (), "kvc_kernels.o"), ("kvc_api.hip", (), "kvc_api.o")] + \
+UNITS = [("kvc_kernels.hip", (), "kvc_kernels.o"), ("kvc_api.hip", (), "kvc_api.o"), ("kvc_cache.hip", (), "kvc_cache.o"), ("kvc_cache_api.hip", (), "kvc_cache_api.o")] + \
+        [("kvc_attend.hip", (f"-DKVC_HEAD_DIM={d}",), f"kvc_attend_{d}.o") for d in HEAD_DIMS] + \
         [("kvc_codec.hip", (f"-DKVC_SHAPE_GROUP={g}",), f"kvc_codec_{g}.o") for g in range(SHAPE_GROUPS)]
-SOURCES = [os.path.join(_CSRC, f) for f in ("kvc_kernels.hip", "kvc_codec.hip", "kvc_api.hip")]
-HEADERS = [os.path.join(_CSRC, f) for f in ("kvc_common.h", "kvc_fastdiv.h", "kvc_device.h", "kvc_codec.h")] + [os.path.join(_ROOT, "include", "kvc.h")]
+SOURCES = [os.path.join(_CSRC, f) for f in ("kvc_kernels.hip", "kvc_codec.hip", "kvc_api.hip", "kvc_cache.hip", "kvc_attend.hip", "kvc_cache_api.hip")]
+HEADERS = [os.path.join(_CSRC, f) for f in ("kvc_common.h", "kvc_fastdiv.h", "kvc_device.h", "kvc_codec.h", "kvc_ctx.h", "kvc_cache.h", "kvc_attend.h")] + [os.path.join(_ROOT, "include", "kvc.h")]
 LIB = os.path.join(_PKG, "libkvc.so")
 #: the same library with every LDS index and pool span the kernels compute checked against its bounds
 #: (a violation sets status bit 8); a GPU test runs the parity cases through it

@@ -3,7 +3,7 @@
 #include <atomic>
 #include <new>
 
-#include "kvc_common.h"
+#include "kvc_ctx.h"
 
 // Workspace of kvc_prefetch_layers_window_static: device memory that exists from the moment the library
 // is loaded, one copy per GPU, so that the call allocates nothing.  In host code the array's name is
@@ -13,23 +13,6 @@ static constexpr int64_t kStaticWindowBlocks = 65536;  // slots one static-works
 static constexpr int32_t kStaticWindowLayers = 1024;   // layers one static-workspace call may cover
 static constexpr uint64_t kStaticWindowBytes = 256 + (uint64_t)kStaticWindowLayers * 4 + (uint64_t)kStaticWindowBlocks * 4;
 static __device__ __align__(256) unsigned char scratch[kStaticWindowBytes];
-
-struct kvc_ctx {
-    int prefetch_policy = 0;
-    int window_capacity = 0;      // window engines this device holds at once (0: unknown); an upper bound on useful omega
-    int wide_capacity = 0;        // ... and wide engines (0: unknown)
-    void* static_work = nullptr;  // device address of `scratch` on this context's device
-    kvc_config cfg;
-    kvc::Geometry g;
-    int device;
-    kvc::DevState* st;  // device
-    uint8_t* pool;
-    uint64_t pool_bytes;
-    bool pool_in_hbm, desc_in_hbm;  // plain memory of this device
-    kvc_desc* desc;
-    uint64_t n_desc;
-    std::atomic<uint64_t> waiting{0};  // its part of g_waiting
-};
 
 // Bytes of payload that the contexts of this process have stored to stay in each device's last-level cache and not fetched yet.
 // They are bounded: what does not fit beside another context's is stored past the cache (see kPoolKeptBytes).  Counted when a
@@ -65,13 +48,19 @@ static constexpr int64_t kMaxPagesPerCall = (1ll << 26) - 4;
 // Text of the last HIP failure seen by this thread (for kvc_strerror(KVC_ERR_HIP)).
 static thread_local hipError_t t_last_hip = hipSuccess;
 
-static bool hip_ok(hipError_t e) {
+namespace kvc {
+bool hip_ok(hipError_t e) {
     if (e != hipSuccess) t_last_hip = e;
     return e == hipSuccess;
 }
 
-// Every call must be made with the context's device current: buffers and streams belong to it.
-static bool on_ctx_device(const kvc_ctx* ctx);
+bool on_ctx_device(const kvc_ctx* ctx) {
+    int dev = -1;
+    return hip_ok(hipGetDevice(&dev)) && dev == ctx->device;
+}
+}  // namespace kvc
+using kvc::hip_ok;
+using kvc::on_ctx_device;
 
 static bool config_ok(const kvc_config* c) {
     if (!c) return false;
@@ -82,11 +71,6 @@ static bool config_ok(const kvc_config* c) {
     if (d < 32 || d > 256 || d % 32 != 0) return false;
     const int64_t E = (int64_t)c->tokens_per_block * d;
     return E <= 4096;
-}
-
-static bool on_ctx_device(const kvc_ctx* ctx) {
-    int dev = -1;
-    return hip_ok(hipGetDevice(&dev)) && dev == ctx->device;
 }
 
 extern "C" {

@@ -1,0 +1,208 @@
+// Attention over a paged cache: what a wave does with 32 tokens.
+//
+// The scores are made transposed, S^T = K Q^T, and the output too, O^T = V^T P^T, with matrix instructions of 16 x 16 x 32.  A wave holds 16
+// query rows: row n belongs to the lanes n, n + 16, n + 32, n + 48, and everything about it (maximum, sum, output) stays in them.
+// The sums over channels and over tokens take their terms in any order, so the order is chosen for the lanes:
+//   * of 32 tokens, token 8g + 4u + r is row 4g + r of score tile u.  A lane of group g = lane / 16 then gets the scores
+//     of tokens 8g..8g+7, and those are the terms it holds of P^T in the second product: the scores become weights in place.
+//   * in the second product a lane holds V of the same 8 tokens for the channels w*n..w*n+w-1 of a piece of 16w channels.  It loads them
+//     as they lie (16w * 2 bytes of a row, shared by 16 lanes) and pairs tokens with one byte permutation a register; channel w*n + j
+//     goes to row n of output tile j.  A lane ends up with 4w consecutive channels of its row.
+// So keys and values go from memory to registers and from there to the matrix unit, without LDS and without a word to another lane.
+//
+// Tokens that do not exist (behind the end, in a block that is not there) are read from a row of zeros: their scores are
+// replaced by -infinity, and their values add weight zero times zero, whatever the cache holds in their place.
+#pragma once
+#include "kvc_cache.h"
+
+namespace kvc {
+
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef _Float16 half2 __attribute__((ext_vector_type(2)));
+typedef float float4v __attribute__((ext_vector_type(4)));
+
+constexpr int kTile = 32;  // tokens
+
+// Weights are 2^(x - m + kLift), x the score in powers of two and m a maximum that may lag by kLag: FP16 holds them with 11 bits from 2^(kLift + kLag)
+// = 2^14 (its largest is below 2^16) down to 2^-14, that is 2^-24 of the largest weight; smaller ones keep fewer bits, down to 2^-34.
+constexpr float kLift = 10.f, kLag = 4.f;
+
+// 512 bytes of zeros: a row of the widest head
+static __device__ __align__(16) const uint16_t kZeroRow[256] = {};
+
+// Pieces of a row's channels: 128s, then a 64, then a 32.
+constexpr int piece_count(int d) { return d / 128 + d / 64 % 2 + d / 32 % 2; }
+constexpr int piece_before(int d, int p) { return p <= d / 128 ? 128 * p : p == d / 128 + 1 ? d / 128 * 128 + (d / 64 % 2 ? 64 : 32) : d; }
+template <int D, int P>
+struct Piece {
+    static constexpr int before = piece_before(D, P), w = (piece_before(D, P + 1) - before) / 16;  // channels before it; channels of a lane
+    static constexpr int regs = before / 32;                                                     // 32-bit registers of a token before it
+};
+
+__device__ inline uint32_t load32(const uint16_t* p) { return *reinterpret_cast<const uint32_t*>(p); }
+
+// K and V of 32 tokens as a lane holds them.
+template <int D>
+struct Tokens {
+    uint4v k[2][D / 32];      // [score tile][step of 32 channels]: 8 channels
+    uint32_t v[8][D / 32];    // [token]: the lane's channels of every piece
+    uint32_t there;           // bit j: token 8g + j exists
+};
+
+// Where tokens are: a sequence's or a prefix's row of a block table, and the pages of one KV head.
+struct Source {
+    const int32_t* table;
+    const uint16_t* k;  // page of the head in block 0
+    const uint16_t* v;
+    uint32_t len;       // tokens, at most the row's blocks hold
+};
+
+// Row of token t < s.len in block 0's page, in elements; -1: it has no block.
+template <class Args>
+__device__ inline int64_t locate(const Args& a, const Source& s, uint32_t t) {
+    if (t >= s.len) return -1;
+    const uint32_t at = fast_div(t, a.by_N);
+    const int32_t block = s.table[at];
+    if (block < 0) return -1;
+    if (block >= a.n_cache_blocks) {
+        atomicOr(&a.st->status, KVC_ST_BAD_INDEX);
+        return -1;
+    }
+    return block * a.g.block_stride + (int64_t)(t - at * (uint32_t)a.g.N) * a.g.row_stride;
+}
+
+template <int D, int P>
+__device__ inline void load_pieces(Tokens<D>& x, int j, const uint16_t* row, int n) {
+    if constexpr (P < piece_count(D)) {
+        using Q = Piece<D, P>;
+        const uint16_t* p = row + Q::before + Q::w * n;
+        if constexpr (Q::w == 8) {
+            const uint4v r = *reinterpret_cast<const uint4v*>(p);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x.v[j][Q::regs + e] = r[e];
+        } else if constexpr (Q::w == 4) {
+            const uint2 r = *reinterpret_cast<const uint2*>(p);
+            x.v[j][Q::regs] = r.x;
+            x.v[j][Q::regs + 1] = r.y;
+        } else {
+            x.v[j][Q::regs] = load32(p);
+        }
+        load_pieces<D, P + 1>(x, j, row, n);
+    }
+}
+
+// Loads tokens t..t+31 of a source.
+template <int D, class Args>
+__device__ inline void load_tokens(Tokens<D>& x, const Args& a, const Source& s, uint32_t t) {
+    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const int64_t at = locate(a, s, t + 8 * (n >> 2) + 4 * u + (n & 3));
+        const uint16_t* row = at < 0 ? kZeroRow : s.k + at;
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) x.k[u][c] = *reinterpret_cast<const uint4v*>(row + 32 * c + 8 * g);
+    }
+    x.there = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int64_t at = locate(a, s, t + 8 * g + j);
+        x.there |= at < 0 ? 0u : 1u << j;
+        load_pieces<D, 0>(x, j, at < 0 ? kZeroRow : s.v + at, n);
+    }
+}
+
+// The largest of a row's four lanes, and their sum.
+__device__ inline float row_max(float v) {
+    v = fmaxf(v, __shfl_xor(v, 16));
+    return fmaxf(v, __shfl_xor(v, 32));
+}
+__device__ inline float row_sum(float v) {
+    v += __shfl_xor(v, 16);
+    return v + __shfl_xor(v, 32);
+}
+
+// Running softmax of 16 rows: output tiles, the reference that weights are relative to, and the lane's part of their sum.
+template <int D>
+struct Rows {
+    uint4v q[D / 32];
+    float4v o[D / 16];  // tile of piece P, channel j of w: o[Piece::before / 16 + j]
+    float m, l;
+};
+
+template <int D, int P>
+__device__ inline void add_pieces(Rows<D>& r, const Tokens<D>& x, const half8& p) {
+    if constexpr (P < piece_count(D)) {
+        using Q = Piece<D, P>;
+#pragma unroll
+        for (int j = 0; j < Q::w; ++j) {
+            uint4v v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                v[e] = __builtin_amdgcn_perm(x.v[2 * e + 1][Q::regs + j / 2], x.v[2 * e][Q::regs + j / 2], j & 1 ? 0x07060302u : 0x05040100u);
+            r.o[Q::before / 16 + j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, v), p, r.o[Q::before / 16 + j], 0, 0, 0);
+        }
+        add_pieces<D, P + 1>(r, x, p);
+    }
+}
+
+// Adds 32 tokens from t on to the rows; the lane's row sees the tokens below `limit`.
+template <int D>
+__device__ inline void add_tokens(Rows<D>& r, const Tokens<D>& x, float scale_log2, uint32_t t, uint32_t limit) {
+    const uint32_t g = (threadIdx.x & 63) >> 4;
+    float4v s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+            s[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, x.k[u][c]), __builtin_bit_cast(half8, r.q[c]), s[u], 0, 0, 0);
+    const uint32_t first = t + 8 * g, n = limit > first ? limit - first : 0;
+    const uint32_t seen = x.there & (n >= 8 ? 0xFFu : ~(~0u << n));
+    float v[8], top = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        v[j] = seen >> j & 1 ? s[j / 4][j % 4] * scale_log2 : -INFINITY;
+        top = fmaxf(top, v[j]);
+    }
+    top = row_max(top);
+    if (__any(top > r.m + kLag)) {  // (a row's first token too: its reference is -infinity)
+        const float m = fmaxf(r.m, top), f = r.m == -INFINITY ? 0.f : exp2f(r.m - m);
+        r.m = m;
+        r.l *= f;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) r.o[i] *= f;
+    }
+    const float low = (r.m == -INFINITY ? 0.f : r.m) - kLift;
+    half8 p;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float w = exp2f(v[j] - low);
+        r.l += w;
+        p[j] = (_Float16)w;
+    }
+    add_pieces<D, 0>(r, x, p);
+}
+
+template <int D, int P>
+__device__ inline void store_pieces(const Rows<D>& r, uint16_t* out, float f, int g) {
+    if constexpr (P < piece_count(D)) {
+        using Q = Piece<D, P>;
+        uint32_t v[2 * Q::w];
+#pragma unroll
+        for (int e = 0; e < 2 * Q::w; ++e) {  // channels 2e and 2e+1 of the lane's 4w: w*i + j
+            const int c = 2 * e;
+            half2 h;
+            h[0] = (_Float16)(r.o[Q::before / 16 + c % Q::w][c / Q::w] * f);
+            h[1] = (_Float16)(r.o[Q::before / 16 + (c + 1) % Q::w][(c + 1) / Q::w] * f);
+            v[e] = __builtin_bit_cast(uint32_t, h);
+        }
+        uint16_t* p = out + Q::before + 4 * Q::w * g;
+#pragma unroll
+        for (int e = 0; e < Q::w / 2; ++e) *reinterpret_cast<uint4*>(p + 8 * e) = make_uint4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+        store_pieces<D, P + 1>(r, out, f, g);
+    }
+}
+
+// log-sum-exp of a row whose weights are relative to 2^(m - kLift) and sum to l
+__device__ inline float lse_of(float m, float l) { return l > 0.f ? (m - kLift + log2f(l)) * 0.69314718055994531f : l == l ? -INFINITY : l; }
+
+}  // namespace kvc

@@ -1,0 +1,265 @@
+// Kernels that move blocks, tokens and payloads: append, copy, fork, free, compaction.
+#include <algorithm>
+
+#include "kvc_cache.h"
+
+namespace kvc {
+
+__device__ inline void bad_index(DevState* st) { atomicOr(&st->status, KVC_ST_BAD_INDEX); }
+
+// ---- append: a workgroup per new token, a lane per 16 bytes of its K and V rows.
+__global__ __launch_bounds__(256) void k_append(AppendArgs a) {
+    const uint32_t s = fast_div(blockIdx.x, a.by_n_new), i = blockIdx.x - s * (uint32_t)a.n_new;
+    const int64_t t = (int64_t)a.lens[s] - a.n_new + i;
+    if (t < 0) return;
+    const uint32_t at = fast_div((uint32_t)t, a.by_N), row = (uint32_t)t - at * (uint32_t)a.g.N;
+    if (at >= (uint32_t)a.max_blocks) {
+        if (threadIdx.x == 0) bad_index(a.st);
+        return;
+    }
+    const int32_t block = a.table[(int64_t)s * a.max_blocks + at];
+    if (block < 0) return;
+    if (block >= a.n_cache_blocks) {
+        if (threadIdx.x == 0) bad_index(a.st);
+        return;
+    }
+    const int64_t to = block * a.g.block_stride + row * a.g.row_stride;
+    const uint32_t each = (uint32_t)(a.n_kv * a.g.lpr);
+    for (uint32_t c = threadIdx.x; c < 2 * each; c += blockDim.x) {
+        const bool v = c >= each;
+        const uint32_t e = v ? c - each : c, h = fast_div(e, a.by_lpr), k = e - h * (uint32_t)a.g.lpr;
+        const uint16_t* from = v ? a.v_new + s * a.v_strides[0] + i * a.v_strides[1] + h * a.v_strides[2]
+                                 : a.k_new + s * a.k_strides[0] + i * a.k_strides[1] + h * a.k_strides[2];
+        uint16_t* into = (v ? a.v_cache : a.k_cache) + to + h * a.g.page_stride;
+        reinterpret_cast<uint4*>(into)[k] = reinterpret_cast<const uint4*>(from)[k];
+    }
+}
+
+// ---- copy: a workgroup per 16 KB of a block.
+__global__ __launch_bounds__(256) void k_copy_blocks(CopyArgs a) {
+    const int64_t layer = blockIdx.y;
+    const uint32_t pair = fast_div(blockIdx.x, a.by_pieces), piece = blockIdx.x - pair * (uint32_t)a.pieces;
+    const int32_t src = a.src[pair], dst = a.dst[pair];
+    if (src < 0 || dst < 0) return;
+    const int64_t from = layer * a.per_layer + src, to = layer * a.per_layer + dst;
+    if (src >= a.per_layer || dst >= a.per_layer || from >= a.n_cache_blocks || to >= a.n_cache_blocks) {
+        if (threadIdx.x == 0) bad_index(a.st);
+        return;
+    }
+    const uint16_t* x = a.cache + from * a.g.block_stride;
+    uint16_t* y = a.cache + to * a.g.block_stride;
+    uint4v r[kCopyChunks / 256];
+    int64_t at[kCopyChunks / 256];
+#pragma unroll
+    for (int k = 0; k < kCopyChunks / 256; ++k) {
+        const uint32_t c = piece * kCopyChunks + k * 256 + threadIdx.x;
+        at[k] = -1;
+        r[k] = uint4v{0, 0, 0, 0};
+        if (c < (uint32_t)a.chunks) {
+            if (a.dense) {
+                at[k] = 8ll * c;
+            } else {
+                const uint32_t line = fast_div(c, a.by_lpr), page = fast_div(line, a.by_N);
+                at[k] = page * a.g.page_stride + (line - page * (uint32_t)a.g.N) * a.g.row_stride + 8 * (c - line * (uint32_t)a.g.lpr);
+            }
+            r[k] = *reinterpret_cast<const uint4v*>(x + at[k]);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kCopyChunks / 256; ++k)
+        if (at[k] >= 0) *reinterpret_cast<uint4v*>(y + at[k]) = r[k];
+}
+
+// ---- fork and free: a lane per descriptor.
+__device__ inline uint4 no_page() { return make_uint4(0, 0, 0, (uint32_t)KVC_MODE_INVALID << 16); }
+
+template <bool FORK>
+__global__ __launch_bounds__(256) void k_ids(IdsArgs a) {
+    const int64_t p = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (p >= a.n_pages) return;
+    const uint32_t i = fast_div((uint32_t)p, a.by_ppb), page = (uint32_t)p - i * (uint32_t)a.ppb;
+    const int32_t dst = a.dst[i], src = FORK ? a.src[i] : 0;
+    if (dst < 0 || src < 0) return;
+    if (dst >= a.per_layer || src >= a.per_layer) {
+        if (page == 0) bad_index(a.st);
+        return;
+    }
+    uint4* desc = reinterpret_cast<uint4*>(a.desc) + (int64_t)blockIdx.y * a.per_layer * a.ppb + page;
+    desc[(int64_t)dst * a.ppb] = FORK ? desc[(int64_t)src * a.ppb] : no_page();
+}
+
+// ---- compaction.
+__global__ __launch_bounds__(256) void k_bits_zero(CompactArgs a) {
+    const uint64_t n = a.tiles * kTileWords / 2;
+    for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (uint64_t)gridDim.x * 256) reinterpret_cast<uint4*>(a.bits)[i] = make_uint4(0, 0, 0, 0);
+}
+
+// A page's span in units, and whether it is held at all; one that leaves the pool is not.
+struct Span {
+    uint64_t from;
+    uint32_t n, kind;  // kind: 0 none, 1 live, 2 corrupt
+};
+__device__ inline Span span_of(const uint4& d, uint64_t units) {
+    const uint64_t off = d.x | (uint64_t)d.y << 32;
+    const uint32_t mode = d.w >> 16 & 0xFF;
+    Span s{off / 16, d.w & 0xFFFF, 1};
+    if (mode == KVC_MODE_INVALID) s.kind = 0;
+    else if (mode > KVC_MODE_CHAN || (off & 15) || s.from > units || s.n > units - s.from) s.kind = 2;
+    return s;
+}
+
+// Marks the units of a page's payload: whole words are stored (a store of all ones takes nothing from a shared or neighbouring
+// payload), the first and the last are or-ed.
+__global__ __launch_bounds__(256) void k_mark(CompactArgs a) {
+    const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= a.n_desc) return;
+    const Span s = span_of(reinterpret_cast<const uint4*>(a.desc)[i], a.units);
+    if (s.kind == 2) atomicOr(&a.st->status, KVC_ST_CORRUPT);
+    if (s.kind != 1 || s.n == 0) return;
+    const uint64_t end = s.from + s.n, first = s.from / 64, last = (end - 1) / 64;
+    const uint32_t lo = s.from & 63, hi = (uint32_t)(end - 1) & 63;
+    // all ones from bit lo up, and up to bit hi, by 32-bit halves
+    const uint32_t l0 = lo < 32 ? ~0u << lo : 0, l1 = lo < 32 ? ~0u : ~0u << (lo - 32);
+    const uint32_t h0 = hi < 32 ? ~0u >> (31 - hi) : ~0u, h1 = hi < 32 ? 0 : ~0u >> (63 - hi);
+    const unsigned long long low = l0 | (unsigned long long)l1 << 32, high = h0 | (unsigned long long)h1 << 32;
+    if (first == last) {
+        atomicOr(a.bits + first, low & high);
+        return;
+    }
+    atomicOr(a.bits + first, low);
+    for (uint64_t w = first + 1; w < last; ++w) a.bits[w] = ~0ull;
+    atomicOr(a.bits + last, high);
+}
+
+__device__ inline uint32_t scan_wave(uint32_t v) {  // inclusive
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int k = 1; k < 64; k *= 2) {
+        const uint32_t o = __shfl_up(v, k);
+        if (lane >= k) v += o;
+    }
+    return v;
+}
+
+__global__ __launch_bounds__(256) void k_count(CompactArgs a) {
+    const uint64_t tile = (uint64_t)blockIdx.x * 4 + threadIdx.x / 64;
+    if (tile >= a.tiles) return;
+    const uint32_t lane = threadIdx.x & 63;
+    const uint32_t n = __popcll(a.bits[tile * kTileWords + lane]), upto = scan_wave(n);
+    a.before[tile * kTileWords + lane] = (uint16_t)(upto - n);
+    if (lane == 63) a.base[tile] = upto;
+}
+
+// one workgroup: exclusive sums of all tiles' counts
+__global__ __launch_bounds__(1024) void k_base(CompactArgs a) {
+    __shared__ uint32_t part[16];
+    unsigned long long sum = 0;
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x / 64;
+    for (uint64_t t0 = 0; t0 < a.tiles; t0 += 1024) {
+        const uint64_t t = t0 + threadIdx.x;
+        const uint32_t n = t < a.tiles ? (uint32_t)a.base[t] : 0, upto = scan_wave(n);
+        if (lane == 63) part[wave] = upto;
+        __syncthreads();
+        uint32_t before = 0, all = 0;
+        for (uint32_t w = 0; w < 16; ++w) {
+            before += w < wave ? part[w] : 0;
+            all += part[w];
+        }
+        if (t < a.tiles) a.base[t] = sum + before + upto - n;
+        sum += all;
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) *a.used = 16 * (sum < a.out_units ? sum : a.out_units);
+}
+
+__device__ inline uint64_t rank_of(const CompactArgs& a, uint64_t unit) {
+    const uint64_t w = unit / 64;
+    const uint32_t b = unit & 63;
+    const unsigned long long bits = a.bits[w];
+    const uint32_t lo = (uint32_t)bits, hi = (uint32_t)(bits >> 32);
+    const uint32_t below = b < 32 ? __popc(lo & ~(~0u << b)) : __popc(lo) + __popc(hi & ~(~0u << (b - 32)));
+    return a.base[w / kTileWords] + a.before[w] + below;
+}
+
+// A wave moves a tile: 64 units at a time, the lanes whose unit is held load it and store it to its rank.
+constexpr int kMoveWords = 8;
+
+__global__ __launch_bounds__(256) void k_move(CompactArgs a) {
+    const uint64_t tile = (uint64_t)blockIdx.x * 4 + threadIdx.x / 64;
+    if (tile >= a.tiles) return;
+    const uint32_t lane = threadIdx.x & 63;
+    const uint64_t base = a.base[tile];
+    for (uint32_t w0 = 0; w0 < kTileWords; w0 += kMoveWords) {
+        uint4v r[kMoveWords];
+        uint64_t to[kMoveWords];
+#pragma unroll
+        for (int k = 0; k < kMoveWords; ++k) {
+            const uint64_t w = tile * kTileWords + w0 + k;
+            const unsigned long long bits = a.bits[w];
+            const uint32_t half = lane < 32 ? (uint32_t)bits : (uint32_t)(bits >> 32);
+            const uint32_t below = __popc(half & ~(~0u << (lane & 31))) + (lane < 32 ? 0 : __popc((uint32_t)bits));
+            to[k] = ~0ull;
+            r[k] = uint4v{0, 0, 0, 0};
+            if (half >> (lane & 31) & 1) {
+                to[k] = base + a.before[w] + below;
+                r[k] = reinterpret_cast<const uint4v*>(a.pool)[w * 64 + lane];
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kMoveWords; ++k)
+            if (to[k] < a.out_units) reinterpret_cast<uint4v*>(a.pool_out)[to[k]] = r[k];
+    }
+}
+
+__global__ __launch_bounds__(256) void k_rename(CompactArgs a) {
+    const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= a.n_desc) return;
+    uint4 d = reinterpret_cast<const uint4*>(a.desc)[i];
+    const Span s = span_of(d, a.units);
+    if (s.kind != 1) {
+        d = no_page();
+    } else {
+        const uint64_t at = s.n ? rank_of(a, s.from) : 0;
+        if (at + s.n > a.out_units) {
+            atomicOr(&a.st->status, KVC_ST_POOL_FULL);
+            d = no_page();
+        } else {
+            d.x = (uint32_t)(at * 16);
+            d.y = (uint32_t)(at >> 28);
+        }
+    }
+    reinterpret_cast<uint4*>(a.desc_out)[i] = d;
+}
+
+__global__ void k_adopt(DevState* st, const unsigned long long* used) {
+    if (threadIdx.x == 0) st->cursor16 = *used / 16;
+}
+
+// ---- launches.
+static unsigned groups(uint64_t n, uint64_t each) { return (unsigned)((n + each - 1) / each); }
+
+hipError_t launch_append(const AppendArgs& a, hipStream_t s) {
+    const int lanes = 2 * a.n_kv * a.g.lpr;
+    return launch_kernel(k_append, dim3((unsigned)(a.n_seq * a.n_new)), dim3(lanes <= 64 ? 64 : lanes <= 128 ? 128 : 256), s, a);
+}
+
+hipError_t launch_copy_blocks(const CopyArgs& a, hipStream_t s) {
+    return launch_kernel(k_copy_blocks, dim3((unsigned)(a.n * a.pieces), (unsigned)a.n_layers), dim3(256), s, a);
+}
+
+hipError_t launch_fork(const IdsArgs& a, hipStream_t s) { return launch_kernel(k_ids<true>, dim3(groups(a.n_pages, 256), (unsigned)a.n_layers), dim3(256), s, a); }
+hipError_t launch_free(const IdsArgs& a, hipStream_t s) { return launch_kernel(k_ids<false>, dim3(groups(a.n_pages, 256), (unsigned)a.n_layers), dim3(256), s, a); }
+
+hipError_t launch_compact(const CompactArgs& a, hipStream_t s) {
+    hipError_t e = launch_kernel(k_bits_zero, dim3((unsigned)std::min<uint64_t>(groups(a.tiles * kTileWords / 2, 256), 2048)), dim3(256), s, a);
+    if (e == hipSuccess) e = launch_kernel(k_mark, dim3(groups(a.n_desc, 256)), dim3(256), s, a);
+    if (e == hipSuccess) e = launch_kernel(k_count, dim3(groups(a.tiles, 4)), dim3(256), s, a);
+    if (e == hipSuccess) e = launch_kernel(k_base, dim3(1), dim3(1024), s, a);
+    if (e == hipSuccess) e = launch_kernel(k_move, dim3(groups(a.tiles, 4)), dim3(256), s, a);
+    if (e == hipSuccess) e = launch_kernel(k_rename, dim3(groups(a.n_desc, 256)), dim3(256), s, a);
+    return e;
+}
+
+hipError_t launch_adopt(DevState* st, const unsigned long long* used, hipStream_t s) { return launch_kernel(k_adopt, dim3(1), dim3(64), s, st, used); }
+
+}  // namespace kvc

@@ -20,6 +20,12 @@ struct Entries {
     decltype(&kvc_decompress_blocks) decompress;
     decltype(&kvc_gather_decompress) gather;
     decltype(&kvc_prefetch_layers) prefetch;
+    decltype(&kvc_append) append;
+    decltype(&kvc_attend) attend;
+    decltype(&kvc_copy_blocks) copy;
+    decltype(&kvc_fork_blocks) fork;
+    decltype(&kvc_free_blocks) free;
+    decltype(&kvc_compact_pool) compact;
 } e;
 
 // a Python error has been set
@@ -113,6 +119,9 @@ public:
         if (n < 0) throw Raised();
         return n;
     }
+    long long stride(int i) const {
+        return t ? t->stride(i) : integer(Ref(PyObject_CallMethod(o, "stride", "i", i)).o);
+    }
     long long size(int i) const { return t ? t->size(i) : integer(Ref(PySequence_GetItem(get("shape").o, i)).o); }
 };
 
@@ -197,9 +206,11 @@ int unlocked(F f) {
 
 // init(addresses of the entry points, in the order of Entries)
 PyObject* py_init(PyObject*, PyObject* const* a, Py_ssize_t given) {
-    return guarded(given, 5, [&] {
+    return guarded(given, 11, [&] {
         e = Entries{address<decltype(e.compress)>(a[0]), address<decltype(e.compress_mixed)>(a[1]), address<decltype(e.decompress)>(a[2]),
-                    address<decltype(e.gather)>(a[3]), address<decltype(e.prefetch)>(a[4])};
+                    address<decltype(e.gather)>(a[3]),   address<decltype(e.prefetch)>(a[4]),       address<decltype(e.append)>(a[5]),
+                    address<decltype(e.attend)>(a[6]),   address<decltype(e.copy)>(a[7]),           address<decltype(e.fork)>(a[8]),
+                    address<decltype(e.free)>(a[9]),     address<decltype(e.compact)>(a[10])};
         return 0;
     });
 }
@@ -272,9 +283,182 @@ PyObject* py_prefetch(PyObject*, PyObject* const* a, Py_ssize_t given) {
     });
 }
 
+// ---- decode steps
+
+// FP16 [sequence][token][head][channel], channels next to each other; the strides of the others (0 where there is one)
+struct Rows4 {
+    void* at;
+    long long n[4];
+    int64_t strides[3];
+};
+Rows4 rows4(PyObject* o, const char* what) {
+    const Tensor t(o);
+    require(t.is_cuda() && t.holds(at::kHalf) && t.dim() == 4, what);
+    Rows4 r;
+    r.at = t.data_ptr();
+    for (int i = 0; i < 4; ++i) r.n[i] = t.size(i);
+    for (int i = 0; i < 3; ++i) r.strides[i] = r.n[i] > 1 ? t.stride(i) : 0;
+    require(r.n[3] < 2 || t.stride(3) == 1, what);
+    return r;
+}
+// a number of sequences, tokens, heads or blocks as the C side takes it
+int32_t narrow(long long n) {
+    require(n >= 0 && n <= INT32_MAX, "sizes: at most 2^31 - 1");
+    return (int32_t)n;
+}
+// int32 table of so many rows
+int32_t* table_of(PyObject* o, long long n, int32_t* each) {
+    const Tensor t(o);
+    check_ids(t);
+    const Rows r = rows(t, false);
+    require(r.n == n, "block table: a row per sequence, or per prefix");
+    *each = narrow(r.each);
+    return static_cast<int32_t*>(t.data_ptr());
+}
+// whole bytes, at least so many, of memory on the GPU
+struct Bytes {
+    void* at;
+    long long n;
+};
+Bytes bytes(PyObject* o, const char* what) {
+    const Tensor t(o);
+    require(t.is_cuda() && t.is_contiguous() && t.holds(at::kByte), what);
+    return {t.data_ptr(), t.numel()};
+}
+
+// append(ctx, stride, span, pages, cache, v_cache, block_table, lens, k_new, v_new, d, stream)
+PyObject* py_append(PyObject*, PyObject* const* a, Py_ssize_t given) {
+    return guarded(given, 12, [&] {
+        kvc_ctx* ctx = address<kvc_ctx*>(a[0]);
+        const Blocks b = blocks(a[4], a[1], a[2]);
+        const bool apart = a[5] != Py_None;
+        const Blocks vb = apart ? blocks(a[5], a[1], a[2]) : Blocks{nullptr, b.n};
+        require(vb.n == b.n, "key and value caches of as many blocks");
+        const long long pages = integer(a[3]);
+        const Rows4 k = rows4(a[8], "k_new: float16 CUDA tensor [sequence][token][head][channel]"), v = rows4(a[9], "v_new: float16 CUDA tensor [sequence][token][head][channel]");
+        for (int i = 0; i < 4; ++i) require(k.n[i] == v.n[i], "k_new and v_new of one shape");
+        kvc_append_t p;
+        p.n_kv_heads = narrow(k.n[2]);
+        require(k.n[2] * (apart ? 1 : 2) == pages, "a page of the block for every head of K, and of V where they share blocks");
+        require(k.n[3] == integer(a[10]), "head_dim channels");
+        p.d_k_cache = b.at;
+        p.d_v_cache = vb.at;
+        p.n_cache_blocks = b.n;
+        p.n_seq = narrow(k.n[0]);
+        p.n_new = narrow(k.n[1]);
+        p.d_block_table = table_of(a[6], k.n[0], &p.max_blocks);
+        p.d_lens = ids_of(a[7], k.n[0]);
+        p.d_k_new = k.at;
+        p.d_v_new = v.at;
+        for (int i = 0; i < 3; ++i) p.k_strides[i] = k.strides[i], p.v_strides[i] = v.strides[i];
+        void* stream = address<void*>(a[11]);
+        return unlocked([&] { return e.append(ctx, &p, stream); });
+    });
+}
+
+// attend(ctx, stride, span, pages, d, out, q, cache, v_cache, block_table, lens, work, scale, prefix_table, prefix_lens, prefix_first, lse, stream)
+PyObject* py_attend(PyObject*, PyObject* const* a, Py_ssize_t given) {
+    return guarded(given, 18, [&] {
+        kvc_ctx* ctx = address<kvc_ctx*>(a[0]);
+        const Blocks b = blocks(a[7], a[1], a[2]);
+        const bool apart = a[8] != Py_None;
+        const Blocks vb = apart ? blocks(a[8], a[1], a[2]) : Blocks{nullptr, b.n};
+        require(vb.n == b.n, "key and value caches of as many blocks");
+        const long long pages = integer(a[3]);
+        const Rows4 out = rows4(a[5], "out: float16 CUDA tensor [sequence][token][head][channel]"), q = rows4(a[6], "q: float16 CUDA tensor [sequence][token][head][channel]");
+        for (int i = 0; i < 4; ++i) require(out.n[i] == q.n[i], "out and q of one shape");
+        require(q.n[3] == integer(a[4]), "head_dim channels");
+        require(apart || pages % 2 == 0, "a page of the block for every head of K, and of V where they share blocks");
+        kvc_attend_t p;
+        p.d_q = q.at;
+        p.d_out = out.at;
+        for (int i = 0; i < 3; ++i) {
+            p.q_strides[i] = q.strides[i], p.out_strides[i] = out.strides[i];
+            require(out.n[i] < 2 || out.strides[i] > 0, "out: an element of memory for every element");
+        }
+        p.n_seq = narrow(q.n[0]);
+        p.n_q = narrow(q.n[1]);
+        p.n_heads = narrow(q.n[2]);
+        p.n_kv_heads = narrow(apart ? pages : pages / 2);
+        p.d_k_cache = b.at;
+        p.d_v_cache = vb.at;
+        p.n_cache_blocks = b.n;
+        p.d_block_table = table_of(a[9], q.n[0], &p.max_blocks);
+        p.d_lens = ids_of(a[10], q.n[0]);
+        const Bytes work = bytes(a[11], "work: contiguous uint8 CUDA tensor");
+        p.d_work = work.at;
+        p.work_bytes = (uint64_t)work.n;
+        const double scale = PyFloat_AsDouble(a[12]);
+        if (scale == -1.0 && PyErr_Occurred()) throw Raised();
+        p.scale = (float)scale;
+        p.d_prefix_table = p.d_prefix_lens = p.d_prefix_first = nullptr;
+        p.n_prefix = p.max_prefix_blocks = 0;
+        require((a[13] == Py_None) == (a[14] == Py_None) && (a[13] == Py_None) == (a[15] == Py_None), "prefixes: table, lengths and first sequences");
+        if (a[13] != Py_None) {
+            const Tensor lens(a[14]);
+            check_ids(lens);
+            p.n_prefix = narrow(lens.numel());
+            p.d_prefix_lens = static_cast<int32_t*>(lens.data_ptr());
+            p.d_prefix_table = table_of(a[13], lens.numel(), &p.max_prefix_blocks);
+            p.d_prefix_first = ids_of(a[15], lens.numel() + 1);
+        }
+        p.d_lse = nullptr;
+        if (a[16] != Py_None) {
+            const Tensor lse(a[16]);
+            require(lse.is_cuda() && lse.is_contiguous() && lse.holds(at::kFloat) && lse.numel() == (wide)q.n[0] * q.n[1] * q.n[2],
+                    "lse: contiguous float32 CUDA tensor [sequence][token][head]");
+            p.d_lse = static_cast<float*>(lse.data_ptr());
+        }
+        void* stream = address<void*>(a[17]);
+        return unlocked([&] { return e.attend(ctx, &p, stream); });
+    });
+}
+
+// copy(ctx, stride, span, cache, src_ids, dst_ids, n_layers, blocks_per_layer, stream)
+PyObject* py_copy(PyObject*, PyObject* const* a, Py_ssize_t given) {
+    return guarded(given, 9, [&] {
+        kvc_ctx* ctx = address<kvc_ctx*>(a[0]);
+        const Blocks b = blocks(a[3], a[1], a[2]);
+        const int32_t n = narrow(Tensor(a[4]).numel()), layers = narrow(integer(a[6]));
+        const int32_t *src = ids_of(a[4], n), *dst = ids_of(a[5], n);
+        require(layers > 0, "n_layers: at least one");
+        const long long per = a[7] == Py_None ? b.n / layers : integer(a[7]);
+        void* stream = address<void*>(a[8]);
+        return unlocked([&] { return e.copy(ctx, b.at, b.n, src, dst, n, layers, per, stream); });
+    });
+}
+
+// fork(ctx, src_ids, dst_ids, n_layers, pool_blocks_per_layer, stream); src_ids None: the blocks are freed
+PyObject* py_fork(PyObject*, PyObject* const* a, Py_ssize_t given) {
+    return guarded(given, 6, [&] {
+        kvc_ctx* ctx = address<kvc_ctx*>(a[0]);
+        const int32_t n = narrow(Tensor(a[2]).numel()), layers = narrow(integer(a[3]));
+        const int32_t *dst = ids_of(a[2], n), *src = a[1] == Py_None ? nullptr : ids_of(a[1], n);
+        const long long per = integer(a[4]);
+        void* stream = address<void*>(a[5]);
+        return unlocked([&] { return src ? e.fork(ctx, src, dst, n, layers, per, stream) : e.free(ctx, dst, n, layers, per, stream); });
+    });
+}
+
+// compact(ctx, n_desc, pool_out, desc_out, used_out, work, stream)
+PyObject* py_compact(PyObject*, PyObject* const* a, Py_ssize_t given) {
+    return guarded(given, 7, [&] {
+        kvc_ctx* ctx = address<kvc_ctx*>(a[0]);
+        const Bytes pool = bytes(a[2], "pool_out: contiguous uint8 CUDA tensor"), desc = bytes(a[3], "desc_out: contiguous uint8 CUDA tensor"),
+                    work = bytes(a[5], "work: contiguous uint8 CUDA tensor");
+        require(desc.n == 16 * (wide)integer(a[1]), "desc_out: as many descriptors as are bound");
+        const Tensor used(a[4]);
+        require(used.is_cuda() && used.is_contiguous() && used.holds(at::kLong) && used.numel() == 1, "used_out: int64 CUDA tensor of one element");
+        uint64_t* u = static_cast<uint64_t*>(used.data_ptr());
+        void* stream = address<void*>(a[6]);
+        return unlocked([&] { return e.compact(ctx, pool.at, (uint64_t)pool.n, static_cast<kvc_desc*>(desc.at), u, work.at, (uint64_t)work.n, stream); });
+    });
+}
+
 #define KVC_METHOD(name, f) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {KVC_METHOD("init", py_init), KVC_METHOD("compress", py_compress), KVC_METHOD("decompress", py_decompress), KVC_METHOD("gather", py_gather),
-                         KVC_METHOD("prefetch", py_prefetch), {nullptr, nullptr, 0, nullptr}};
+                         KVC_METHOD("prefetch", py_prefetch), KVC_METHOD("append", py_append), KVC_METHOD("attend", py_attend), KVC_METHOD("copy", py_copy),
+                         KVC_METHOD("fork", py_fork),         KVC_METHOD("compact", py_compact), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_kvc_py", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -25,7 +25,8 @@ DESC_DTYPE = np.dtype([("off", "<u8"), ("scale", "<f4"), ("n16", "<u2"), ("mode"
 
 EXPORTS = ("kvc_create", "kvc_destroy", "kvc_set_scheme", "kvc_set_cache_layout", "kvc_bind_pool", "kvc_reset_pool", "kvc_restore_pool", "kvc_compress_blocks",
            "kvc_compress_blocks_mixed", "kvc_decompress_blocks", "kvc_gather_decompress", "kvc_set_prefetch_policy", "kvc_prefetch_reset", "kvc_prefetch_layers", "kvc_prefetch_window_workspace",
-           "kvc_prefetch_layers_window", "kvc_prefetch_layers_window_static", "kvc_wall_clock_khz", "kvc_device_clocks", "kvc_stats", "kvc_page_scales",
+           "kvc_prefetch_layers_window", "kvc_prefetch_layers_window_static", "kvc_append", "kvc_attend", "kvc_attend_workspace", "kvc_copy_blocks", "kvc_fork_blocks",
+           "kvc_free_blocks", "kvc_compact_pool", "kvc_compact_workspace", "kvc_adopt_pool", "kvc_wall_clock_khz", "kvc_device_clocks", "kvc_stats", "kvc_page_scales",
            "kvc_copy_bytes", "kvc_strerror")
 
 
@@ -37,6 +38,20 @@ class Config(C.Structure):
 class Stats(C.Structure):
     _fields_ = [("pool_bytes_used", C.c_uint64), ("pages", C.c_uint64 * 6), ("pages_invalid", C.c_uint64),
                 ("payload_bytes", C.c_uint64), ("status", C.c_uint32), ("rsvd", C.c_uint32)]
+
+
+class Append(C.Structure):
+    _fields_ = [("d_k_cache", C.c_void_p), ("d_v_cache", C.c_void_p), ("n_cache_blocks", C.c_int64), ("d_block_table", C.c_void_p), ("d_lens", C.c_void_p),
+                ("d_k_new", C.c_void_p), ("d_v_new", C.c_void_p), ("k_strides", C.c_int64 * 3), ("v_strides", C.c_int64 * 3),
+                ("max_blocks", C.c_int32), ("n_seq", C.c_int32), ("n_new", C.c_int32), ("n_kv_heads", C.c_int32)]
+
+
+class Attend(C.Structure):
+    _fields_ = [("d_q", C.c_void_p), ("d_out", C.c_void_p), ("d_lse", C.c_void_p), ("q_strides", C.c_int64 * 3), ("out_strides", C.c_int64 * 3),
+                ("d_k_cache", C.c_void_p), ("d_v_cache", C.c_void_p), ("n_cache_blocks", C.c_int64), ("d_block_table", C.c_void_p), ("d_lens", C.c_void_p),
+                ("d_prefix_table", C.c_void_p), ("d_prefix_lens", C.c_void_p), ("d_prefix_first", C.c_void_p), ("max_blocks", C.c_int32),
+                ("max_prefix_blocks", C.c_int32), ("n_prefix", C.c_int32), ("n_seq", C.c_int32), ("n_q", C.c_int32), ("n_heads", C.c_int32),
+                ("n_kv_heads", C.c_int32), ("scale", C.c_float), ("d_work", C.c_void_p), ("work_bytes", C.c_uint64)]
 
 
 class KvcError(RuntimeError):
@@ -108,6 +123,24 @@ def load():
     L.kvc_prefetch_layers_window_static.restype = C.c_int
     L.kvc_prefetch_layers_window_static.argtypes = [vp, vp, vp, vp, vp, i32p, C.c_int32, i32p, i32p, C.c_int32, C.c_int32, C.c_int32,
                                                     C.c_int32, C.c_int32, C.c_int64, C.c_int32, C.c_int32, vp, vp]
+    L.kvc_append.restype = C.c_int
+    L.kvc_append.argtypes = [vp, C.POINTER(Append), vp]
+    L.kvc_attend.restype = C.c_int
+    L.kvc_attend.argtypes = [vp, C.POINTER(Attend), vp]
+    L.kvc_attend_workspace.restype = C.c_uint64
+    L.kvc_attend_workspace.argtypes = [C.c_int32] * 6
+    L.kvc_copy_blocks.restype = C.c_int
+    L.kvc_copy_blocks.argtypes = [vp, vp, C.c_int64, i32p, i32p, C.c_int32, C.c_int32, C.c_int64, vp]
+    L.kvc_fork_blocks.restype = C.c_int
+    L.kvc_fork_blocks.argtypes = [vp, i32p, i32p, C.c_int32, C.c_int32, C.c_int64, vp]
+    L.kvc_free_blocks.restype = C.c_int
+    L.kvc_free_blocks.argtypes = [vp, i32p, C.c_int32, C.c_int32, C.c_int64, vp]
+    L.kvc_compact_pool.restype = C.c_int
+    L.kvc_compact_pool.argtypes = [vp, vp, C.c_uint64, vp, vp, vp, C.c_uint64, vp]
+    L.kvc_compact_workspace.restype = C.c_uint64
+    L.kvc_compact_workspace.argtypes = [C.c_uint64]
+    L.kvc_adopt_pool.restype = C.c_int
+    L.kvc_adopt_pool.argtypes = [vp, vp, C.c_uint64, vp, C.c_uint64, vp, vp]
     L.kvc_wall_clock_khz.restype = C.c_int
     L.kvc_wall_clock_khz.argtypes = [C.POINTER(C.c_int32)]
     L.kvc_device_clocks.restype = C.c_int
@@ -122,7 +155,8 @@ def load():
     L.kvc_strerror.argtypes = [C.c_int]
     from . import _kvc_py
 
-    _kvc_py.init(*(C.cast(f, vp).value for f in (L.kvc_compress_blocks, L.kvc_compress_blocks_mixed, L.kvc_decompress_blocks, L.kvc_gather_decompress, L.kvc_prefetch_layers)))
+    _kvc_py.init(*(C.cast(f, vp).value for f in (L.kvc_compress_blocks, L.kvc_compress_blocks_mixed, L.kvc_decompress_blocks, L.kvc_gather_decompress, L.kvc_prefetch_layers,
+                                                  L.kvc_append, L.kvc_attend, L.kvc_copy_blocks, L.kvc_fork_blocks, L.kvc_free_blocks, L.kvc_compact_pool)))
     _call = _kvc_py
     _lib = L
     return L
@@ -308,6 +342,72 @@ class Codec:
                                                   fill_half, int(omega), notify.data_ptr(), work.data_ptr(), work.numel(),
                                                   _stream(stream)), "kvc_prefetch_layers_window")
 
+    # -- decode steps over the paged cache
+    def append(self, cache, block_table, lens, k_new, v_new, v_cache=None, stream=None):
+        """K and V rows of new tokens (float16 [n_seq][n_new][n_kv_heads][d], any strides of multiples of 8) go to the last n_new
+        of the lens[s] positions of every sequence.  cache: K and V pages of a block, or K pages, with the V pages in v_cache."""
+        c = self.cfg
+        rc = _call.append(self._ctx.value, self._block_stride, self._span, c.pages_per_block, cache, v_cache, block_table, lens, k_new, v_new, c.head_dim,
+                          _stream_now() if stream is None else stream.cuda_stream)
+        if rc:
+            _check(rc, "kvc_append")
+
+    def attend(self, out, q, cache, block_table, lens, work, v_cache=None, scale=None, prefix_table=None, prefix_lens=None, prefix_first=None, lse=None, stream=None):
+        """out[s][i][head] = attention of query i of sequence s over the sequence's tokens up to its own position (the n_q
+        queries are the last of lens[s] tokens) and over the prefix that the sequences prefix_first[g] <= s < prefix_first[g+1] share.
+        q, out: float16 [n_seq][n_q][n_heads][d]; block_table int32 [n_seq][max_blocks], lens int32 [n_seq]; prefix_table int32
+        [n_prefix][max_prefix_blocks], prefix_lens int32 [n_prefix], prefix_first int32 [n_prefix + 1]; lse: None or float32
+        [n_seq][n_q][n_heads]; work: uint8 of attend_workspace(...) bytes; scale: default 1 / sqrt(d)."""
+        c = self.cfg
+        rc = _call.attend(self._ctx.value, self._block_stride, self._span, c.pages_per_block, c.head_dim, out, q, cache, v_cache, block_table, lens, work,
+                          c.head_dim ** -0.5 if scale is None else scale, prefix_table, prefix_lens, prefix_first, lse,
+                          _stream_now() if stream is None else stream.cuda_stream)
+        if rc:
+            _check(rc, "kvc_attend")
+
+    def copy_blocks(self, cache, src_ids, dst_ids, n_layers: int = 1, blocks_per_layer: int | None = None, stream=None):
+        """In every layer, cache block src_ids[i] is copied to block dst_ids[i].  blocks_per_layer: default all there are."""
+        rc = _call.copy(self._ctx.value, self._block_stride, self._span, cache, src_ids, dst_ids, n_layers, blocks_per_layer,
+                        _stream_now() if stream is None else stream.cuda_stream)
+        if rc:
+            _check(rc, "kvc_copy_blocks")
+
+    def _pool_blocks(self, n_layers):
+        if self.desc is None:
+            return 0
+        return self.desc.numel() // (16 * self.cfg.pages_per_block) // max(n_layers, 1)
+
+    def fork_blocks(self, src_ids, dst_ids, n_layers: int = 1, pool_blocks_per_layer: int | None = None, stream=None):
+        """In every layer, pool block dst_ids[i] becomes a second name of what pool block src_ids[i] holds."""
+        assert src_ids is not None
+        rc = _call.fork(self._ctx.value, src_ids, dst_ids, n_layers, self._pool_blocks(n_layers) if pool_blocks_per_layer is None else pool_blocks_per_layer,
+                        _stream_now() if stream is None else stream.cuda_stream)
+        if rc:
+            _check(rc, "kvc_fork_blocks")
+
+    def free_blocks(self, ids, n_layers: int = 1, pool_blocks_per_layer: int | None = None, stream=None):
+        """In every layer, pool block ids[i] is given up.  Its space comes back with compact_pool."""
+        rc = _call.fork(self._ctx.value, None, ids, n_layers, self._pool_blocks(n_layers) if pool_blocks_per_layer is None else pool_blocks_per_layer,
+                        _stream_now() if stream is None else stream.cuda_stream)
+        if rc:
+            _check(rc, "kvc_free_blocks")
+
+    def compact_pool(self, pool_out, desc_out, used_out, work, stream=None):
+        """The live payloads of the bound pool, moved together to the beginning of pool_out, with their descriptors in desc_out
+        and the bytes they take in used_out (int64, one element).  work: uint8 of compact_workspace(pool bytes)."""
+        rc = _call.compact(self._ctx.value, 0 if self.desc is None else self.desc.numel() // 16, pool_out, desc_out, used_out, work,
+                           _stream_now() if stream is None else stream.cuda_stream)
+        if rc:
+            _check(rc, "kvc_compact_pool")
+
+    def adopt_pool(self, pool, desc, used, stream=None):
+        """Go on with the buffers that compact_pool has filled."""
+        assert (pool.is_cuda or pool.is_pinned()) and desc.is_cuda and pool.is_contiguous() and desc.is_contiguous()
+        assert pool.element_size() == 1 and desc.element_size() == 1 and desc.numel() % 16 == 0
+        assert used.is_cuda and used.element_size() == 8 and used.numel() == 1
+        _check(self._L.kvc_adopt_pool(self._ctx, pool.data_ptr(), pool.numel(), desc.data_ptr(), desc.numel() // 16, used.data_ptr(), _stream(stream)), "kvc_adopt_pool")
+        self.pool, self.desc = pool, desc
+
     def stats(self, stream=None, check: bool = False) -> dict:
         st = Stats()
         rc = self._L.kvc_stats(self._ctx, C.byref(st), _stream(stream))
@@ -330,6 +430,19 @@ class Codec:
 def window_workspace(n_blocks: int, n_layers_call: int) -> int:
     """Bytes of device workspace prefetch_layers_window needs for a call over n_blocks slots."""
     return int(load().kvc_prefetch_window_workspace(int(n_blocks), int(n_layers_call)))
+
+
+def attend_workspace(n_seq: int, n_q: int, n_heads: int, n_kv_heads: int, head_dim: int, n_prefix: int = 0) -> int:
+    """Bytes of device workspace attend needs for a call of these sizes."""
+    n = int(load().kvc_attend_workspace(int(n_seq), int(n_q), int(n_heads), int(n_kv_heads), int(head_dim), int(n_prefix)))
+    if not n:
+        raise KvcError(ERR_ARG, "kvc_attend_workspace")
+    return n
+
+
+def compact_workspace(pool_bytes: int) -> int:
+    """Bytes of device workspace compact_pool needs on a bound pool of pool_bytes."""
+    return int(load().kvc_compact_workspace(int(pool_bytes)))
 
 
 def device_clocks() -> dict:
