@@ -19,6 +19,7 @@ namespace kvc {
 
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef _Float16 half2 __attribute__((ext_vector_type(2)));
+typedef uint32_t uint2v __attribute__((ext_vector_type(2)));
 typedef float float4v __attribute__((ext_vector_type(4)));
 
 constexpr int kTile = 32;  // tokens
@@ -39,16 +40,6 @@ struct Piece {
     static constexpr int regs = before / 32;                                                     // 32-bit registers of a token before it
 };
 
-__device__ inline uint32_t load32(const uint16_t* p) { return *reinterpret_cast<const uint32_t*>(p); }
-
-// K and V of 32 tokens as a lane holds them.
-template <int D>
-struct Tokens {
-    uint4v k[2][D / 32];      // [score tile][step of 32 channels]: 8 channels
-    uint32_t v[8][D / 32];    // [token]: the lane's channels of every piece
-    uint32_t there;           // bit j: token 8g + j exists
-};
-
 // Where tokens are: a sequence's or a prefix's row of a block table, and the pages of one KV head.
 struct Source {
     const int32_t* table;
@@ -57,18 +48,61 @@ struct Source {
     uint32_t len;       // tokens, at most the row's blocks hold
 };
 
-// Row of token t < s.len in block 0's page, in elements; -1: it has no block.
-template <class Args>
-__device__ inline int64_t locate(const Args& a, const Source& s, uint32_t t) {
-    if (t >= s.len) return -1;
-    const uint32_t at = fast_div(t, a.by_N);
-    const int32_t block = s.table[at];
-    if (block < 0) return -1;
-    if (block >= a.n_cache_blocks) {
-        atomicOr(&a.st->status, KVC_ST_BAD_INDEX);
-        return -1;
+// Blocks of the 32 tokens from t on that a lane needs, as the table names them; -1: none, or the token is behind the end.
+// EIGHT: N is a multiple of 8, so that 8 tokens from a multiple of 8 on share a block.
+template <bool EIGHT>
+struct Blocks {
+    int32_t k[EIGHT ? 1 : 2], v[EIGHT ? 1 : 8];
+};
+__device__ inline int32_t block_of(const AttendArgs& a, const Source& s, uint32_t t) { return t < s.len ? s.table[fast_div(t, a.by_N)] : -1; }
+template <bool EIGHT>
+__device__ inline Blocks<EIGHT> find_blocks(const AttendArgs& a, const Source& s, uint32_t t) {
+    const uint32_t lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    Blocks<EIGHT> b;
+    if constexpr (EIGHT) {
+        b.k[0] = block_of(a, s, t + 8 * (n >> 2));
+        b.v[0] = block_of(a, s, t + 8 * g);
+    } else {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) b.k[u] = block_of(a, s, t + 8 * (n >> 2) + 4 * u + (n & 3));
+#pragma unroll
+        for (int j = 0; j < 8; ++j) b.v[j] = block_of(a, s, t + 8 * g + j);
     }
-    return block * a.g.block_stride + (int64_t)(t - at * (uint32_t)a.g.N) * a.g.row_stride;
+    return b;
+}
+__device__ inline bool in_cache(const AttendArgs& a, int32_t block) {
+    if (block < a.n_cache_blocks) return block >= 0;
+    atomicOr(&a.st->status, KVC_ST_BAD_INDEX);
+    return false;
+}
+// row of token t in its block, in elements
+__device__ inline int64_t place(const AttendArgs& a, int32_t block, uint32_t t) {
+    return block * a.g.block_stride + (int64_t)((t - fast_div(t, a.by_N) * (uint32_t)a.g.N) * (uint32_t)a.g.row_stride);
+}
+
+// K and V of 32 tokens as a lane holds them.
+template <int D>
+struct Tokens {
+    uint4v k[2][D / 32];    // [score tile][step of 32 channels]: 8 channels
+    uint32_t v[8][D / 32];  // [token]: the lane's channels of every piece
+};
+
+template <int D, bool EIGHT>
+__device__ inline void load_keys(Tokens<D>& x, const AttendArgs& a, const Source& s, const Blocks<EIGHT>& b, uint32_t t) {
+    const uint32_t lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    const uint32_t first = t + 8 * (n >> 2) + (n & 3);
+    int64_t at = 0;
+    bool have = false;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        if (u == 0 || !EIGHT) {
+            have = in_cache(a, b.k[EIGHT ? 0 : u]);
+            at = place(a, b.k[EIGHT ? 0 : u], first + 4 * u);
+        }
+        const uint16_t* row = have && first + 4 * u < s.len ? s.k + at + (EIGHT ? 4 * u * a.g.row_stride : 0) : kZeroRow;
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) x.k[u][c] = *reinterpret_cast<const uint4v*>(row + 32 * c + 8 * g);
+    }
 }
 
 template <int D, int P>
@@ -81,45 +115,51 @@ __device__ inline void load_pieces(Tokens<D>& x, int j, const uint16_t* row, int
 #pragma unroll
             for (int e = 0; e < 4; ++e) x.v[j][Q::regs + e] = r[e];
         } else if constexpr (Q::w == 4) {
-            const uint2 r = *reinterpret_cast<const uint2*>(p);
-            x.v[j][Q::regs] = r.x;
-            x.v[j][Q::regs + 1] = r.y;
+            const uint2v r = *reinterpret_cast<const uint2v*>(p);
+            x.v[j][Q::regs] = r[0];
+            x.v[j][Q::regs + 1] = r[1];
         } else {
-            x.v[j][Q::regs] = load32(p);
+            x.v[j][Q::regs] = *reinterpret_cast<const uint32_t*>(p);
         }
         load_pieces<D, P + 1>(x, j, row, n);
     }
 }
 
-// Loads tokens t..t+31 of a source.
-template <int D, class Args>
-__device__ inline void load_tokens(Tokens<D>& x, const Args& a, const Source& s, uint32_t t) {
-    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-        const int64_t at = locate(a, s, t + 8 * (n >> 2) + 4 * u + (n & 3));
-        const uint16_t* row = at < 0 ? kZeroRow : s.k + at;
-#pragma unroll
-        for (int c = 0; c < D / 32; ++c) x.k[u][c] = *reinterpret_cast<const uint4v*>(row + 32 * c + 8 * g);
-    }
-    x.there = 0;
+// -> bit j: token t + 8g + j exists
+template <int D, bool EIGHT>
+__device__ inline uint32_t load_values(Tokens<D>& x, const AttendArgs& a, const Source& s, const Blocks<EIGHT>& b, uint32_t t) {
+    const uint32_t lane = threadIdx.x & 63, n = lane & 15, first = t + 8 * (lane >> 4);
+    uint32_t there = 0;
+    int64_t at = 0;
+    bool have = false;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        const int64_t at = locate(a, s, t + 8 * g + j);
-        x.there |= at < 0 ? 0u : 1u << j;
-        load_pieces<D, 0>(x, j, at < 0 ? kZeroRow : s.v + at, n);
+        if (j == 0 || !EIGHT) {
+            have = in_cache(a, b.v[EIGHT ? 0 : j]);
+            at = place(a, b.v[EIGHT ? 0 : j], first + j);
+        }
+        const bool here = have && first + j < s.len;
+        there |= here ? 1u << j : 0u;
+        load_pieces<D, 0>(x, j, here ? s.v + at + (EIGHT ? j * a.g.row_stride : 0) : kZeroRow, n);
     }
+    return there;
 }
 
+// The two halves of a wave, and the two rows of 16 lanes of each half, change places: what a lane and its partners hold, joined.
+__device__ inline float both16(float v, bool sum) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return sum ? __uint_as_float(r[0]) + __uint_as_float(r[1]) : fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ inline float both32(float v, bool sum) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return sum ? __uint_as_float(r[0]) + __uint_as_float(r[1]) : fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
 // The largest of a row's four lanes, and their sum.
-__device__ inline float row_max(float v) {
-    v = fmaxf(v, __shfl_xor(v, 16));
-    return fmaxf(v, __shfl_xor(v, 32));
-}
-__device__ inline float row_sum(float v) {
-    v += __shfl_xor(v, 16);
-    return v + __shfl_xor(v, 32);
-}
+__device__ inline float row_max(float v) { return both32(both16(v, false), false); }
+__device__ inline float row_sum(float v) { return both32(both16(v, true), true); }
+
+// 2^x by the hardware's instruction alone: what would be a subnormal number is zero.
+__device__ inline float power2(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // Running softmax of 16 rows: output tiles, the reference that weights are relative to, and the lane's part of their sum.
 template <int D>
@@ -129,34 +169,29 @@ struct Rows {
     float m, l;
 };
 
-template <int D, int P>
-__device__ inline void add_pieces(Rows<D>& r, const Tokens<D>& x, const half8& p) {
-    if constexpr (P < piece_count(D)) {
-        using Q = Piece<D, P>;
+template <int D>
+__device__ inline void clear(Rows<D>& r) {
 #pragma unroll
-        for (int j = 0; j < Q::w; ++j) {
-            uint4v v;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                v[e] = __builtin_amdgcn_perm(x.v[2 * e + 1][Q::regs + j / 2], x.v[2 * e][Q::regs + j / 2], j & 1 ? 0x07060302u : 0x05040100u);
-            r.o[Q::before / 16 + j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, v), p, r.o[Q::before / 16 + j], 0, 0, 0);
-        }
-        add_pieces<D, P + 1>(r, x, p);
-    }
+    for (int i = 0; i < D / 16; ++i) r.o[i] = float4v{0.f, 0.f, 0.f, 0.f};
+    r.m = -INFINITY;
+    r.l = 0.f;
 }
 
-// Adds 32 tokens from t on to the rows; the lane's row sees the tokens below `limit`.
 template <int D>
-__device__ inline void add_tokens(Rows<D>& r, const Tokens<D>& x, float scale_log2, uint32_t t, uint32_t limit) {
-    const uint32_t g = (threadIdx.x & 63) >> 4;
-    float4v s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+__device__ inline void scores(float4v (&s)[2], const Rows<D>& r, const Tokens<D>& x) {
+    s[0] = s[1] = float4v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int c = 0; c < D / 32; ++c)
 #pragma unroll
         for (int u = 0; u < 2; ++u)
             s[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, x.k[u][c]), __builtin_bit_cast(half8, r.q[c]), s[u], 0, 0, 0);
-    const uint32_t first = t + 8 * g, n = limit > first ? limit - first : 0;
-    const uint32_t seen = x.there & (n >= 8 ? 0xFFu : ~(~0u << n));
+}
+
+// Scores of tokens t + 8g.. become weights, of those below the row's limit that exist; the row's reference follows their maximum.
+template <int D>
+__device__ inline half8 weights(Rows<D>& r, const float4v (&s)[2], float scale_log2, uint32_t there, uint32_t t, uint32_t limit) {
+    const uint32_t first = t + 8 * ((threadIdx.x & 63) >> 4), n = limit > first ? limit - first : 0;
+    const uint32_t seen = there & (n >= 8 ? 0xFFu : ~(~0u << n));
     float v[8], top = -INFINITY;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -165,7 +200,7 @@ __device__ inline void add_tokens(Rows<D>& r, const Tokens<D>& x, float scale_lo
     }
     top = row_max(top);
     if (__any(top > r.m + kLag)) {  // (a row's first token too: its reference is -infinity)
-        const float m = fmaxf(r.m, top), f = r.m == -INFINITY ? 0.f : exp2f(r.m - m);
+        const float m = fmaxf(r.m, top), f = r.m == -INFINITY ? 0.f : power2(r.m - m);
         r.m = m;
         r.l *= f;
 #pragma unroll
@@ -175,11 +210,29 @@ __device__ inline void add_tokens(Rows<D>& r, const Tokens<D>& x, float scale_lo
     half8 p;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        const float w = exp2f(v[j] - low);
+        const float w = power2(v[j] - low);
         r.l += w;
         p[j] = (_Float16)w;
     }
-    add_pieces<D, 0>(r, x, p);
+    return p;
+}
+
+template <int D, int R, int P = 0>
+__device__ inline void add_values(Rows<D> (&r)[R], const Tokens<D>& x, const half8 (&p)[R]) {
+    if constexpr (P < piece_count(D)) {
+        using Q = Piece<D, P>;
+#pragma unroll
+        for (int j = 0; j < Q::w; ++j) {
+            uint4v v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                v[e] = __builtin_amdgcn_perm(x.v[2 * e + 1][Q::regs + j / 2], x.v[2 * e][Q::regs + j / 2], j & 1 ? 0x07060302u : 0x05040100u);
+#pragma unroll
+            for (int i = 0; i < R; ++i)
+                r[i].o[Q::before / 16 + j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, v), p[i], r[i].o[Q::before / 16 + j], 0, 0, 0);
+        }
+        add_values<D, R, P + 1>(r, x, p);
+    }
 }
 
 template <int D, int P>
@@ -202,7 +255,24 @@ __device__ inline void store_pieces(const Rows<D>& r, uint16_t* out, float f, in
     }
 }
 
-// log-sum-exp of a row whose weights are relative to 2^(m - kLift) and sum to l
-__device__ inline float lse_of(float m, float l) { return l > 0.f ? (m - kLift + log2f(l)) * 0.69314718055994531f : l == l ? -INFINITY : l; }
+// The same channels as they are summed, in 32 bits.
+template <int D, int P = 0>
+__device__ inline void store_sums(const Rows<D>& r, float* out, int g) {
+    if constexpr (P < piece_count(D)) {
+        using Q = Piece<D, P>;
+        float* p = out + Q::before + 4 * Q::w * g;
+#pragma unroll
+        for (int e = 0; e < Q::w; ++e) {
+            float4v v;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = r.o[Q::before / 16 + (4 * e + i) % Q::w][(4 * e + i) / Q::w];
+            *reinterpret_cast<float4v*>(p + 4 * e) = v;
+        }
+        store_sums<D, P + 1>(r, out, g);
+    }
+}
+
+// log-sum-exp of a row whose weights are relative to 2^m and sum to l
+__device__ inline float lse_of(float m, float l) { return l > 0.f ? (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f : l == l ? -INFINITY : l; }
 
 }  // namespace kvc

@@ -1,4 +1,9 @@
 // Attention over the paged cache, compiled once per head dimension (-DKVC_HEAD_DIM=d).
+//
+// Work is divided evenly, whatever the lengths are: what a call has to do is a list of units (a sequence, a KV head and some of
+// its query rows; or a prefix, a KV head and some rows of its group), each of so many tiles of tokens, and worker w of W takes the tiles from w * T / W to
+// (w + 1) * T / W of all T.  A unit that one worker has alone is finished there; the pieces of others are left as sums and joined
+// by k_join.  Lengths are on the device, so each workgroup adds them up for itself.
 #include "kvc_attend.h"
 
 #ifndef KVC_HEAD_DIM
@@ -10,64 +15,508 @@ namespace kvc {
 __device__ inline uint32_t length_of(const AttendArgs& a, int32_t len, int32_t blocks) {
     const int64_t most = (int64_t)blocks * a.g.N;
     if (len > most) {
-        if (threadIdx.x == 0) atomicOr(&a.st->status, KVC_ST_BAD_INDEX);
+        atomicOr(&a.st->status, KVC_ST_BAD_INDEX);
         return (uint32_t)most;
     }
     return len < 0 ? 0 : (uint32_t)len;
 }
+__device__ inline uint32_t own_length(const AttendArgs& a, int s) { return length_of(a, a.lens[s], a.max_blocks); }
+__device__ inline uint32_t prefix_length(const AttendArgs& a, int g) { return length_of(a, a.prefix_lens[g], a.max_prefix_blocks); }
 
-// Group of sequence s: the prefix whose range of sequences holds it, or -1.
+// Sequences of prefix g.
+struct Range {
+    int begin, end;
+};
+__device__ inline Range group_of_prefix(const AttendArgs& a, int g) {
+    Range r;
+    r.begin = min(max(a.prefix_first[g], 0), a.n_seq);
+    r.end = min(max(a.prefix_first[g + 1], r.begin), a.n_seq);
+    return r;
+}
+// The prefix that sequence s has, or -1: the last one that begins at or before it, if that holds it.
 __device__ inline int prefix_of(const AttendArgs& a, int s) {
-    for (int g = 0; g < a.n_prefix; ++g)
-        if (s >= a.prefix_first[g] && s < a.prefix_first[g + 1]) return g;
-    return -1;
+    int lo = 0, hi = a.n_prefix;  // first[lo..hi) may be at or before s
+    while (lo < hi) {
+        const int mid = (lo + hi) / 2;
+        if (a.prefix_first[mid] <= s) lo = mid + 1;
+        else hi = mid;
+    }
+    return lo > 0 && s < group_of_prefix(a, lo - 1).end && s >= group_of_prefix(a, lo - 1).begin ? lo - 1 : -1;
 }
 
-// A wave per sequence, KV head and 16 query rows: the prefix's tokens, then the sequence's.
-template <int D>
-__global__ __launch_bounds__(64, 1) void k_attend(AttendArgs a) {
-    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
-    const int s = blockIdx.x, h = blockIdx.y, row = blockIdx.z * 16 + n;
-    const bool have = row < a.rows;
-    const int head = h * a.group + (have ? row / a.n_q : 0), i = have ? row % a.n_q : 0;
-    Rows<D> r;
-    const uint16_t* q = a.q + s * a.q_strides[0] + i * a.q_strides[1] + head * a.q_strides[2];
+// ---- dividing the work: sums of f(0..n-1), with the items dealt to the 256 threads of a workgroup in runs of `each`.
+struct Sums {
+    uint32_t before[256], wave[4], all, each;
+};
+template <class F>
+__device__ inline void add_up(Sums& s, uint32_t n, F f) {
+    const uint32_t t = threadIdx.x, lane = t & 63, each = (n + 255) / 256;
+    uint32_t sum = 0;
+    for (uint32_t i = t * each; i < n && i < (t + 1) * each; ++i) sum += f(i);
+    uint32_t upto = sum;
 #pragma unroll
-    for (int c = 0; c < D / 32; ++c) r.q[c] = *reinterpret_cast<const uint4v*>(q + 32 * c + 8 * g);
+    for (int k = 1; k < 64; k *= 2) {
+        const uint32_t o = __shfl_up(upto, k);
+        if (lane >= (uint32_t)k) upto += o;
+    }
+    if (lane == 63) s.wave[t / 64] = upto;
+    __syncthreads();
+    uint32_t base = 0;
+    for (uint32_t w = 0; w < t / 64; ++w) base += s.wave[w];
+    s.before[t] = base + upto - sum;
+    if (t == 255) s.all = base + upto, s.each = each;
+    __syncthreads();
+}
+// The item that holds position p < s.all, and the sum before it.
+struct Item {
+    uint32_t i, start;
+};
+template <class F>
+__device__ inline Item find_item(const Sums& s, uint32_t n, uint32_t p, F f) {
+    uint32_t lo = 0;  // the last run that begins at or before p (runs of no work begin where the next does)
 #pragma unroll
-    for (int c = 0; c < D / 16; ++c) r.o[c] = float4v{0.f, 0.f, 0.f, 0.f};
-    r.m = -INFINITY;
-    r.l = 0.f;
-    const int prefix = prefix_of(a, s);
-    for (int part = prefix < 0 ? 1 : 0; part < 2; ++part) {
-        Source src;
-        src.k = a.k_cache + h * a.g.page_stride;
-        src.v = a.v_cache + h * a.g.page_stride;
-        uint32_t limit;
-        if (part == 0) {
-            src.table = a.prefix_table + (int64_t)prefix * a.max_prefix_blocks;
-            src.len = limit = length_of(a, a.prefix_lens[prefix], a.max_prefix_blocks);
-        } else {
-            src.table = a.table + (int64_t)s * a.max_blocks;
-            src.len = length_of(a, a.lens[s], a.max_blocks);
-            const int64_t sees = (int64_t)a.lens[s] - (a.n_q - 1 - i);
-            limit = sees < 0 ? 0 : sees < src.len ? (uint32_t)sees : src.len;
+    for (uint32_t k = 128; k; k /= 2)
+        if (s.before[lo + k] <= p) lo += k;
+    Item r{lo * s.each, s.before[lo]};
+    while (r.i + 1 < n) {
+        const uint32_t v = f(r.i);
+        if (p - r.start < v) break;
+        r.start += v;
+        ++r.i;
+    }
+    return r;
+}
+__device__ inline uint32_t uniform(uint32_t v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// tiles a worker takes
+__device__ inline uint32_t share(uint32_t tiles, uint32_t workers) { return max(1u, (tiles + workers - 1) / workers); }
+
+// ---- the sequences' own tokens.  A worker is a wave: tiles of 32 tokens go from memory to its registers, keys of the next tile while this
+// one's scores become weights, values while the next scores are made, so that a tile is always on its way; the block table is read one
+// tile further ahead.  R: tiles of 16 rows that share the tokens.
+struct Place {
+    uint32_t s, u, t, tiles, len;  // sequence; unit u of it (head and row tile); tile t of `tiles`
+};
+
+template <int D, int R, bool EIGHT>
+__global__ __launch_bounds__(256, D * R <= 128 ? 2 : 1) void k_own(AttendArgs a) {
+    __shared__ Sums sums;
+    const auto tiles_of = [&](uint32_t s) { return (own_length(a, s) + kTile - 1) / kTile; };
+    add_up(sums, a.n_seq, tiles_of);
+    if (blockIdx.x == 0) {
+        const uint32_t t = threadIdx.x;
+        uint32_t at = sums.before[t];
+        for (uint32_t i = t * sums.each; i < (uint32_t)a.n_seq && i < (t + 1) * sums.each; ++i) {
+            a.own_start[i] = at;
+            at += tiles_of(i);
         }
-        for (uint32_t t = 0; t < src.len; t += kTile) {
-            Tokens<D> x;
-            load_tokens<D>(x, a, src, t);
-            add_tokens<D>(r, x, a.scale_log2, t, limit);
+        if (t == 0) a.own_start[a.n_seq] = sums.all;
+    }
+    const uint32_t units = a.n_kv * a.own_tiles, all = sums.all * units, each = share(all, a.own_workers);
+    const uint32_t worker = uniform(blockIdx.x * 4 + threadIdx.x / 64), begin = worker * each;
+    if (begin >= all) return;
+    const uint32_t end = min(begin + each, all);
+
+    Place c;
+    {
+        const Item it = find_item(sums, a.n_seq, begin / units, tiles_of);
+        c.s = uniform(it.i);
+        c.len = uniform(own_length(a, c.s));
+        c.tiles = (c.len + kTile - 1) / kTile;
+        const uint32_t rel = begin - uniform(it.start) * units;
+        c.u = rel / c.tiles;
+        c.t = rel - c.u * c.tiles;
+    }
+    const auto advance = [&](Place& p) {  // (there is a next tile)
+        if (++p.t < p.tiles) return;
+        p.t = 0;
+        if (++p.u < units) return;
+        p.u = 0;
+        do {
+            ++p.s;
+            p.len = uniform(own_length(a, p.s));
+        } while (p.len == 0);
+        p.tiles = (p.len + kTile - 1) / kTile;
+    };
+    const auto source = [&](const Place& p) {
+        const uint32_t h = p.u / a.own_tiles;
+        return Source{a.table + (int64_t)p.s * a.max_blocks, a.k_cache + h * a.g.page_stride, a.v_cache + h * a.g.page_stride, p.len};
+    };
+
+    const uint32_t lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    Rows<D> r[R];
+    uint32_t limit[R];
+    const auto open = [&](const Place& p) {
+        const uint32_t h = p.u / a.own_tiles, rt = p.u - h * a.own_tiles;
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            clear(r[j]);
+            const uint32_t row = min((rt * R + j) * 16 + n, (uint32_t)a.rows - 1);  // (rows beyond the last are computed with it, and not stored)
+            const uint32_t in = fast_div(row, a.by_n_q), i = row - in * a.n_q;
+            const uint16_t* q = a.q + p.s * a.q_strides[0] + i * a.q_strides[1] + (h * a.group + in) * a.q_strides[2];
+#pragma unroll
+            for (int k = 0; k < D / 32; ++k) r[j].q[k] = *reinterpret_cast<const uint4v*>(q + 32 * k + 8 * g);
+            const uint32_t later = a.n_q - 1 - i, len = (uint32_t)a.lens[p.s];
+            limit[j] = min(len > later ? len - later : 0, p.len);
+        }
+    };
+    const auto close = [&](const Place& p, uint32_t first_tile) {
+        const uint32_t h = p.u / a.own_tiles, rt = p.u - h * a.own_tiles;
+        const bool whole = first_tile == 0 && p.t + 1 == p.tiles, alone = whole && prefix_of(a, p.s) < 0;
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            const float l = row_sum(r[j].l);
+            const uint32_t row = (rt * R + j) * 16 + n;
+            if (row >= (uint32_t)a.rows) continue;
+            const uint32_t in = fast_div(row, a.by_n_q), i = row - in * a.n_q, head = h * a.group + in;
+            if (alone) {
+                store_pieces<D, 0>(r[j], a.out + p.s * a.out_strides[0] + i * a.out_strides[1] + head * a.out_strides[2], l == 0.f ? 0.f : 1.f / l, g);
+                if (a.lse && g == 0) a.lse[((int64_t)p.s * a.n_q + i) * a.n_heads + head] = lse_of(r[j].m - kLift, l);
+            } else {
+                const int64_t slot = whole ? ((int64_t)p.s * a.n_kv + h) * a.rows + row
+                                           : a.own_slots + (int64_t)(2 * worker + (first_tile == 0 ? 1 : 0)) * (16 * R) + 16 * j + n;
+                store_sums<D>(r[j], a.sums + slot * D, g);
+                if (g == 0) a.stats[slot] = float2v{r[j].m - kLift, l};
+            }
+        }
+    };
+
+    // c: the tile computed; c1: the one loaded; c2: the one whose blocks are looked up
+    Place c1 = c, c2 = c;
+    uint32_t left = end - begin, first_tile = c.t;
+    Tokens<D> x;
+    Blocks<EIGHT> b = find_blocks<EIGHT>(a, source(c), c.t * kTile);
+    open(c);
+    load_keys<D, EIGHT>(x, a, source(c), b, c.t * kTile);
+    uint32_t there = load_values<D, EIGHT>(x, a, source(c), b, c.t * kTile);
+    if (left > 1) {
+        advance(c1);
+        b = find_blocks<EIGHT>(a, source(c1), c1.t * kTile);
+        c2 = c1;
+    }
+    for (;;) {
+        float4v s[R][2];
+#pragma unroll
+        for (int j = 0; j < R; ++j) scores(s[j], r[j], x);
+        Blocks<EIGHT> ahead = b;
+        if (left > 1) {
+            load_keys<D, EIGHT>(x, a, source(c1), b, c1.t * kTile);
+            if (left > 2) {
+                advance(c2);
+                ahead = find_blocks<EIGHT>(a, source(c2), c2.t * kTile);
+            }
+        }
+        half8 p[R];
+#pragma unroll
+        for (int j = 0; j < R; ++j) p[j] = weights(r[j], s[j], a.scale_log2, there, c.t * kTile, limit[j]);
+        add_values<D, R>(r, x, p);
+        if (left > 1) there = load_values<D, EIGHT>(x, a, source(c1), b, c1.t * kTile);
+        if (left == 1 || c1.t == 0) {
+            close(c, first_tile);
+            if (left == 1) break;
+            open(c1);
+            first_tile = 0;
+        }
+        c = c1;
+        c1 = c2;
+        b = ahead;
+        --left;
+    }
+}
+
+// ---- prefixes.  A worker is a workgroup: 128 * RB rows of a group (32 * RB a wave) share tiles of 64 tokens in LDS.
+constexpr int kPrefixTile = 64;
+typedef float float16v __attribute__((ext_vector_type(16)));
+typedef short short4v __attribute__((ext_vector_type(4)));
+
+// A tile is [token][chunk] with chunks of 16 bytes; chunk c of token t lies at place c ^ turn(t) of its row, so that lanes that read one chunk of
+// consecutive tokens meet in no bank (rows are loaded whole, so that the order within a row is free).
+template <int D>
+__device__ inline uint32_t turn(uint32_t t) {
+    constexpr int C = D / 8;
+    return C % 16 == 0 ? t & 15 : C % 8 == 0 ? t >> 1 & 7 : t >> 2 & 3;
+}
+
+template <int D, int RB>
+struct PrefixRows {
+    uint4v q[RB][D / 16];
+    float16v o[RB][D / 32];
+    float m[RB], l[RB];
+};
+
+template <int D, int RB>
+__global__ __launch_bounds__(256, 1) void k_prefix(AttendArgs a) {
+    constexpr int C = D / 8, kLoads = C / 4, kRows = 128 * RB;
+    __shared__ Sums sums;
+    __shared__ __align__(16) uint4v tile[2][2][kPrefixTile * C];  // [stage][keys, values]
+    const auto row_tiles = [&](uint32_t g) {
+        const Range r = group_of_prefix(a, g);
+        return ((uint32_t)(r.end - r.begin) * a.rows + kRows - 1) / kRows;
+    };
+    const auto tiles_of = [&](uint32_t g) { return (prefix_length(a, g) + kPrefixTile - 1) / kPrefixTile; };
+    const auto work_of = [&](uint32_t g) { return row_tiles(g) * tiles_of(g); };
+    add_up(sums, a.n_prefix, work_of);
+    if (blockIdx.x == 0) {
+        const uint32_t t = threadIdx.x;
+        uint32_t at = sums.before[t];
+        for (uint32_t i = t * sums.each; i < (uint32_t)a.n_prefix && i < (t + 1) * sums.each; ++i) {
+            a.prefix_start[i] = at;
+            at += work_of(i);
+        }
+        if (t == 0) a.prefix_start[a.n_prefix] = sums.all;
+    }
+    const uint32_t all = sums.all * a.n_kv, each = share(all, a.prefix_workers);
+    // workgroups go to the XCDs in turn: an XCD's take neighbouring shares, which read the same tokens
+    const uint32_t worker = a.prefix_workers % 8 ? blockIdx.x : blockIdx.x % 8 * (a.prefix_workers / 8) + blockIdx.x / 8, begin = worker * each;
+    if (begin >= all) return;
+    uint32_t left = min(each, all - begin);
+
+    const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x / 64), n = lane & 31, h2 = lane >> 5;
+    // what this lane loads of a tile: chunk at[j] of the tile is chunk from[j] of its token's row
+    uint32_t token[kLoads], from[kLoads];
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+        const uint32_t i = (wave * kLoads + j) * 64 + lane;
+        token[j] = i / C;
+        from[j] = (i % C) ^ turn<D>(token[j]);
+    }
+
+    uint32_t g, u, t, tiles, rts;
+    Range seqs;
+    {
+        const Item it = find_item(sums, a.n_prefix, begin / a.n_kv, work_of);
+        g = uniform(it.i);
+        tiles = uniform(tiles_of(g));
+        rts = uniform(row_tiles(g));
+        const uint32_t rel = begin - uniform(it.start) * a.n_kv;
+        u = rel / tiles;
+        t = rel - u * tiles;
+    }
+    for (;;) {
+        const uint32_t h = u / rts, rt = u - h * rts, len = uniform(prefix_length(a, g)), first_tile = t, n_tiles = min(tiles - t, left);
+        seqs = group_of_prefix(a, g);
+        const uint32_t rows = (uint32_t)(seqs.end - seqs.begin) * a.rows;
+        const int32_t* table = a.prefix_table + (int64_t)g * a.max_prefix_blocks;
+        const uint16_t *keys = a.k_cache + h * a.g.page_stride, *values = a.v_cache + h * a.g.page_stride;
+
+        PrefixRows<D, RB> r;
+#pragma unroll
+        for (int b = 0; b < RB; ++b) {
+            const uint32_t rr = min(rt * kRows + (wave * RB + b) * 32 + n, rows - 1), s = fast_div(rr, a.by_rows), row = rr - s * a.rows;
+            const uint32_t in = fast_div(row, a.by_n_q), i = row - in * a.n_q;
+            const uint16_t* q = a.q + (seqs.begin + s) * a.q_strides[0] + i * a.q_strides[1] + (h * a.group + in) * a.q_strides[2];
+#pragma unroll
+            for (int c = 0; c < D / 16; ++c) r.q[b][c] = *reinterpret_cast<const uint4v*>(q + 16 * c + 8 * h2);
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) r.o[b][c][e] = 0.f;
+            r.m[b] = -INFINITY;
+            r.l[b] = 0.f;
+        }
+        // block of token `lane` of tile i, -1: it has none
+        const auto look_up = [&](uint32_t i) {
+            const uint32_t k = i * kPrefixTile + lane;
+            const int32_t block = k < len ? table[fast_div(k, a.by_N)] : -1;
+            return in_cache(a, block) ? block : -1;
+        };
+        const auto load = [&](uint32_t i, int32_t blocks, int stage) {
+#pragma unroll
+            for (int j = 0; j < kLoads; ++j) {
+                const int32_t block = __shfl(blocks, token[j]);
+                const uint32_t k = i * kPrefixTile + token[j];
+                const int64_t at = place(a, block, k) + 8 * from[j];
+                const uint16_t* kp = block < 0 ? kZeroRow + 8 * from[j] : keys + at;
+                const uint16_t* vp = block < 0 ? kZeroRow + 8 * from[j] : values + at;
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)kp, (__attribute__((address_space(3))) void*)&tile[stage][0][(wave * kLoads + j) * 64], 16, 0, 0);
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)vp, (__attribute__((address_space(3))) void*)&tile[stage][1][(wave * kLoads + j) * 64], 16, 0, 0);
+            }
+        };
+        int32_t blocks = look_up(t);
+        __syncthreads();  // (the tiles of the last piece have been read)
+        load(t, blocks, 0);
+        for (uint32_t i = 0; i < n_tiles; ++i) {
+            const int stage = i & 1;
+            const unsigned long long there = __ballot(blocks >= 0);
+            if (i + 1 < n_tiles) blocks = look_up(t + i + 1);
+            __builtin_amdgcn_s_waitcnt(0);  // this wave's part of the tile is in LDS
+            __syncthreads();                // all of it is, and the other stage has been read
+            if (i + 1 < n_tiles) load(t + i + 1, blocks, stage ^ 1);
+#pragma unroll
+            for (int sub = 0; sub < 2; ++sub) {
+                float16v s[RB];
+#pragma unroll
+                for (int b = 0; b < RB; ++b)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) s[b][e] = 0.f;
+                const uint32_t krow = 32 * sub + n;
+#pragma unroll
+                for (int c = 0; c < D / 16; ++c) {
+                    const uint4v k = tile[stage][0][krow * C + ((2 * c + h2) ^ turn<D>(krow))];
+#pragma unroll
+                    for (int b = 0; b < RB; ++b)
+                        s[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, k), __builtin_bit_cast(half8, r.q[b][c]), s[b], 0, 0, 0);
+                }
+                half8 p[RB][2];
+                const uint32_t here = (uint32_t)(there >> (32 * sub)) >> (4 * h2);
+#pragma unroll
+                for (int b = 0; b < RB; ++b) {
+                    float v[16], top = -INFINITY;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        v[e] = here >> (8 * (e / 4) + e % 4) & 1 ? s[b][e] * a.scale_log2 : -INFINITY;
+                        top = fmaxf(top, v[e]);
+                    }
+                    top = both32(top, false);
+                    if (__any(top > r.m[b] + kLag)) {
+                        const float m = fmaxf(r.m[b], top), f = r.m[b] == -INFINITY ? 0.f : power2(r.m[b] - m);
+                        r.m[b] = m;
+                        r.l[b] *= f;
+#pragma unroll
+                        for (int c = 0; c < D / 32; ++c) r.o[b][c] *= f;
+                    }
+                    const float low = (r.m[b] == -INFINITY ? 0.f : r.m[b]) - kLift;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const float w = power2(v[e] - low);
+                        r.l[b] += w;
+                        p[b][e / 8][e % 8] = (_Float16)w;
+                    }
+                }
+                // values: lane group i of 16 reads, of 4 tokens, 16 channels, and gets one channel of the 4 tokens
+                const uint32_t l16 = lane & 15, vrow = 4 * h2 + l16 / 4, vc = (lane >> 4 & 1) * 2 + (l16 & 3) / 2;
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int c = 0; c < D / 32; ++c) {
+                        short4v part[2];
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const uint32_t row = 32 * sub + 16 * k + 8 * e + vrow;
+                            const uint4v* at = &tile[stage][1][row * C + ((4 * c + vc) ^ turn<D>(row))];
+                            part[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(reinterpret_cast<const char*>(at) + 8 * (l16 & 1)));
+                        }
+                        const half8 v = __builtin_bit_cast(half8, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+                        for (int b = 0; b < RB; ++b) r.o[b][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p[b][k], r.o[b][c], 0, 0, 0);
+                    }
+            }
+        }
+        const bool whole = first_tile == 0 && n_tiles == tiles;
+#pragma unroll
+        for (int b = 0; b < RB; ++b) {
+            const float l = both32(r.l[b], true);
+            const uint32_t in_tile = (wave * RB + b) * 32 + n, rr = rt * kRows + in_tile;
+            if (rr >= rows) continue;
+            const uint32_t s = fast_div(rr, a.by_rows), row = rr - s * a.rows;
+            const int64_t slot = whole ? a.prefix_whole + ((int64_t)(seqs.begin + s) * a.n_kv + h) * a.rows + row
+                                       : a.prefix_slots + (int64_t)(2 * worker + (first_tile == 0 ? 1 : 0)) * kRows + in_tile;
+            float* out = a.sums + slot * D + 4 * h2;
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    *reinterpret_cast<float4v*>(out + 32 * c + 8 * e) = float4v{r.o[b][c][4 * e], r.o[b][c][4 * e + 1], r.o[b][c][4 * e + 2], r.o[b][c][4 * e + 3]};
+            if (h2 == 0) a.stats[slot] = float2v{r.m[b] - kLift, l};
+        }
+        left -= n_tiles;
+        if (left == 0) break;
+        t = 0;
+        if (++u == rts * a.n_kv) {
+            u = 0;
+            do ++g;
+            while (uniform(work_of(g)) == 0);
+            tiles = uniform(tiles_of(g));
+            rts = uniform(row_tiles(g));
         }
     }
-    const float l = row_sum(r.l);
-    if (!have) return;
-    store_pieces<D, 0>(r, a.out + s * a.out_strides[0] + i * a.out_strides[1] + head * a.out_strides[2], l == 0.f ? 0.f : 1.f / l, g);
-    if (a.lse && g == 0) a.lse[((int64_t)s * a.n_q + i) * a.n_heads + head] = lse_of(r.m, l);
+}
+
+// ---- joining pieces: D / 8 threads to a row, 8 channels each.
+template <int D>
+struct Join {
+    float m = -INFINITY, l = 0.f;
+    float4v o[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+
+    __device__ void add(const AttendArgs& a, int64_t slot, uint32_t c) {
+        const float2v st = a.stats[slot];
+        const float4v* p = reinterpret_cast<const float4v*>(a.sums + slot * D + 8 * c);
+        const float4v x = p[0], y = p[1];
+        if (st[0] == -INFINITY) return;  // (a piece in which the row saw no token)
+        const float top = fmaxf(m, st[0]), f = m == -INFINITY ? 0.f : power2(m - top), w = power2(st[0] - top);
+        m = top;
+        l = l * f + st[1] * w;
+        o[0] = o[0] * f + x * w;
+        o[1] = o[1] * f + y * w;
+    }
+    // A unit of `tiles` tiles from `start` on: in `whole` if one worker had it, else in the workers' slots.
+    __device__ void add_unit(const AttendArgs& a, uint32_t start, uint32_t tiles, uint32_t each, int64_t whole, int64_t slots, uint32_t rows, uint32_t row, uint32_t c) {
+        const uint32_t w0 = start / each, w1 = (start + tiles - 1) / each;
+        if (w0 == w1) {
+            add(a, whole, c);
+            return;
+        }
+        for (uint32_t w = w0; w <= w1; ++w) add(a, slots + (int64_t)(2 * w + (w == w0 ? 1 : 0)) * rows + row, c);
+    }
+};
+
+template <int D>
+__global__ __launch_bounds__(256) void k_join(AttendArgs a) {
+    const uint32_t own_rows = a.own_rows, prefix_rows = a.prefix_rows;
+    constexpr uint32_t kEach = D / 8, kRows = 256 / kEach;
+    const uint32_t in_group = threadIdx.x / kEach, c = threadIdx.x % kEach;
+    const int64_t id = (int64_t)blockIdx.x * kRows + in_group;
+    if (in_group >= kRows || id >= (int64_t)a.n_seq * a.n_kv * a.rows) return;
+    const uint32_t unit = fast_div((uint32_t)id, a.by_rows), row = (uint32_t)id - unit * a.rows, s = unit / a.n_kv, h = unit - s * a.n_kv;
+    const int g = a.n_prefix ? prefix_of(a, s) : -1;
+    Join<D> j;
+    const uint32_t before = a.own_start[s], tiles = a.own_start[s + 1] - before;
+    if (tiles) {
+        const uint32_t units = a.n_kv * a.own_tiles, each = share(a.own_start[a.n_seq] * units, a.own_workers);
+        const uint32_t start = before * units + (h * a.own_tiles + row / own_rows) * tiles;
+        if (g < 0 && start / each == (start + tiles - 1) / each) return;  // finished by its worker
+        j.add_unit(a, start, tiles, each, id, a.own_slots, own_rows, row % own_rows, c);
+    }
+    if (g >= 0) {
+        const Range seqs = group_of_prefix(a, g);
+        const uint32_t ptiles = (prefix_length(a, g) + kPrefixTile - 1) / kPrefixTile;
+        if (ptiles) {
+            const uint32_t rts = ((uint32_t)(seqs.end - seqs.begin) * a.rows + prefix_rows - 1) / prefix_rows;
+            const uint32_t rr = (s - seqs.begin) * a.rows + row, each = share(a.prefix_start[a.n_prefix] * a.n_kv, a.prefix_workers);
+            const uint32_t start = a.prefix_start[g] * a.n_kv + (h * rts + rr / prefix_rows) * ptiles;
+            j.add_unit(a, start, ptiles, each, a.prefix_whole + id, a.prefix_slots, prefix_rows, rr % prefix_rows, c);
+        }
+    }
+    const uint32_t in = fast_div(row, a.by_n_q), i = row - in * a.n_q, head = h * a.group + in;
+    const float f = j.l == 0.f ? 0.f : 1.f / j.l;
+    uint4v v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        half2 x;
+        x[0] = (_Float16)(j.o[e / 2][e % 2 * 2] * f);
+        x[1] = (_Float16)(j.o[e / 2][e % 2 * 2 + 1] * f);
+        v[e] = __builtin_bit_cast(uint32_t, x);
+    }
+    *reinterpret_cast<uint4v*>(a.out + s * a.out_strides[0] + i * a.out_strides[1] + head * a.out_strides[2] + 8 * c) = v;
+    if (a.lse && c == 0) a.lse[((int64_t)s * a.n_q + i) * a.n_heads + head] = lse_of(j.m, j.l);
+}
+
+template <int D, int R>
+static hipError_t launch_own(const AttendArgs& a, hipStream_t s) {
+    const dim3 grid(a.own_workers / 4);
+    return a.g.N % 8 == 0 ? launch_kernel(k_own<D, R, true>, grid, dim3(256), s, a) : launch_kernel(k_own<D, R, false>, grid, dim3(256), s, a);
 }
 
 template <>
 hipError_t launch_attend<KVC_HEAD_DIM>(const AttendArgs& a, hipStream_t s) {
-    return launch_kernel(k_attend<KVC_HEAD_DIM>, dim3((unsigned)a.n_seq, (unsigned)a.n_kv, (unsigned)((a.rows + 15) / 16)), dim3(64), s, a);
+    constexpr int D = KVC_HEAD_DIM, RB = D <= 128 ? 2 : 1;
+    hipError_t e;
+    if constexpr (D <= 192) e = a.own_rows == 32 ? launch_own<D, 2>(a, s) : launch_own<D, 1>(a, s);
+    else e = launch_own<D, 1>(a, s);
+    if (e == hipSuccess && a.n_prefix) e = launch_kernel(k_prefix<D, RB>, dim3(a.prefix_workers), dim3(256), s, a);
+    constexpr uint32_t rows = 256 / (D / 8);
+    if (e == hipSuccess) e = launch_kernel(k_join<D>, dim3((unsigned)(((int64_t)a.n_seq * a.n_kv * a.rows + rows - 1) / rows)), dim3(256), s, a);
+    return e;
 }
 
 }  // namespace kvc

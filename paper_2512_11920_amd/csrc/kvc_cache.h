@@ -7,6 +7,8 @@ namespace kvc {
 
 typedef uint32_t uint4v __attribute__((ext_vector_type(4)));  // (arrays of the runtime's uint4 end up in memory)
 
+typedef float float2v __attribute__((ext_vector_type(2)));
+
 struct AppendArgs {
     uint16_t* k_cache;
     uint16_t* v_cache;  // already at the first value page
@@ -88,9 +90,40 @@ struct AttendArgs {
     int32_t rows;   // query rows of one sequence and KV head: group * n_q
     float scale_log2;  // scale * log2(e)
     Geometry g;
-    FastDiv by_N, by_rows;
+    FastDiv by_N, by_rows, by_n_q;
     DevState* st;
+    // the workspace, see AttendPlan
+    uint32_t own_tiles;  // row tiles of one sequence and KV head
+    uint32_t own_workers, prefix_workers, own_rows, prefix_rows;
+    uint32_t* own_start;     // [n_seq + 1]
+    uint32_t* prefix_start;  // [n_prefix + 1]
+    float* sums;             // [slots][d]
+    float2v* stats;          // [slots]: reference and sum of the weights
+    int64_t own_slots, prefix_whole, prefix_slots;   // first slots of what the own part shares, and of the prefix part's
 };
+
+// Workers of a call and what they need of the workspace.  Each worker may share a unit at either end of its part, so it has two slots for sums
+// of so many rows; rows whose own and prefix parts each have one worker still have to be joined, so there is a slot for each row of either.
+struct AttendPlan {
+    uint32_t own_rows, prefix_rows;  // of a worker
+    uint32_t own_workers, prefix_workers;
+    uint64_t rows, slots, starts;    // query rows; slots; bytes of the sums of tiles
+    uint64_t bytes;
+};
+constexpr uint32_t kOwnWorkers = 2048, kPrefixWorkers = 256;  // waves, workgroups: what the GPU holds at once
+
+inline AttendPlan plan_attend(int64_t n_seq, int64_t n_q, int64_t n_heads, int64_t n_kv, int d, int64_t n_prefix) {
+    AttendPlan p;
+    p.own_rows = n_heads / n_kv * n_q <= 16 || d > 192 ? 16 : 32;  // (32 rows of wider heads do not fit into the registers)
+    p.prefix_rows = d <= 128 ? 256 : 128;
+    p.own_workers = kOwnWorkers;
+    p.prefix_workers = n_prefix ? kPrefixWorkers : 0;
+    p.rows = (uint64_t)(n_seq * n_heads * n_q);
+    p.slots = p.rows + 2ull * p.own_workers * p.own_rows + (n_prefix ? p.rows + 2ull * p.prefix_workers * p.prefix_rows : 0);
+    p.starts = round_256((uint64_t)(n_seq + 1) * 4) + round_256((uint64_t)(n_prefix + 1) * 4);
+    p.bytes = p.starts + round_256(p.slots * 8) + p.slots * (uint64_t)d * 4;
+    return p;
+}
 
 hipError_t launch_append(const AppendArgs& a, hipStream_t s);
 hipError_t launch_copy_blocks(const CopyArgs& a, hipStream_t s);

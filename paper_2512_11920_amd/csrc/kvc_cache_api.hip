@@ -54,7 +54,8 @@ int kvc_append(kvc_ctx* ctx, const kvc_append_t* p, void* stream) {
 
 uint64_t kvc_attend_workspace(int32_t n_seq, int32_t n_q, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t n_prefix) {
     if (n_seq < 0 || n_q < 1 || n_kv_heads < 1 || n_heads < n_kv_heads || n_heads % n_kv_heads || head_dim < 32 || head_dim > 256 || head_dim % 32 || n_prefix < 0) return 0;
-    return 256;
+    if ((int64_t)n_seq * n_heads > (int64_t)INT32_MAX / n_q) return 0;
+    return plan_attend(n_seq, n_q, n_heads, n_kv_heads, head_dim, n_prefix).bytes;
 }
 
 int kvc_attend(kvc_ctx* ctx, const kvc_attend_t* p, void* stream) {
@@ -66,11 +67,17 @@ int kvc_attend(kvc_ctx* ctx, const kvc_attend_t* p, void* stream) {
     if (!aligned(p->d_q, 16) || !aligned(p->d_out, 16) || !aligned(p->d_k_cache, 16) || !aligned(p->d_v_cache, 16)) return KVC_ERR_ARG;
     if (!strides_ok(p->q_strides) || !strides_ok(p->out_strides)) return KVC_ERR_ARG;
     if (p->n_prefix > 0 && (!p->d_prefix_table || !p->d_prefix_lens || !p->d_prefix_first)) return KVC_ERR_ARG;
-    // rows are counted in 31 bits, tokens too
+    // rows are counted in 31 bits, and so are a row's tokens and the tiles of all units
     if ((int64_t)p->n_seq * p->n_heads > (int64_t)INT32_MAX / p->n_q) return KVC_ERR_ARG;
-    if ((int64_t)p->max_blocks * ctx->g.N > INT32_MAX || (int64_t)p->max_prefix_blocks * ctx->g.N > INT32_MAX) return KVC_ERR_ARG;
-    const uint64_t need = kvc_attend_workspace(p->n_seq, p->n_q, p->n_heads, p->n_kv_heads, ctx->g.d, p->n_prefix);
-    if (!p->d_work || !aligned(p->d_work, 256) || p->work_bytes < need) return KVC_ERR_ARG;
+    const int64_t own_tokens = (int64_t)p->max_blocks * ctx->g.N, prefix_tokens = (int64_t)p->max_prefix_blocks * ctx->g.N;
+    if (own_tokens > INT32_MAX - 256 || prefix_tokens > INT32_MAX - 256) return KVC_ERR_ARG;
+    const AttendPlan plan = plan_attend(p->n_seq, p->n_q, p->n_heads, p->n_kv_heads, ctx->g.d, p->n_prefix);
+    const int64_t rows = (int64_t)(p->n_heads / p->n_kv_heads) * p->n_q, own_tiles = (rows + plan.own_rows - 1) / plan.own_rows;
+    const int64_t prefix_tiles = (rows * p->n_seq + plan.prefix_rows - 1) / plan.prefix_rows + p->n_prefix;
+    const auto product = [](int64_t a, int64_t b, int64_t c) { return (__int128)a * b * c; };
+    if (product(own_tiles * p->n_kv_heads, p->n_seq, own_tokens / 32 + 1) > INT32_MAX) return KVC_ERR_ARG;
+    if (p->n_prefix && product(prefix_tiles, p->n_kv_heads, prefix_tokens / 64 + 1) > INT32_MAX) return KVC_ERR_ARG;
+    if (!p->d_work || !aligned(p->d_work, 256) || p->work_bytes < plan.bytes) return KVC_ERR_ARG;
     AttendArgs a;
     a.q = static_cast<const uint16_t*>(p->d_q);
     a.out = static_cast<uint16_t*>(p->d_out);
@@ -97,7 +104,21 @@ int kvc_attend(kvc_ctx* ctx, const kvc_attend_t* p, void* stream) {
     a.g = ctx->g;
     a.by_N = make_fast_div((uint32_t)ctx->g.N);
     a.by_rows = make_fast_div((uint32_t)a.rows);
+    a.by_n_q = make_fast_div((uint32_t)a.n_q);
     a.st = ctx->st;
+    a.own_tiles = (uint32_t)own_tiles;
+    a.own_workers = plan.own_workers;
+    a.prefix_workers = plan.prefix_workers;
+    uint8_t* w = static_cast<uint8_t*>(p->d_work);
+    a.own_start = reinterpret_cast<uint32_t*>(w);
+    a.prefix_start = reinterpret_cast<uint32_t*>(w + round_256((uint64_t)(p->n_seq + 1) * 4));
+    a.stats = reinterpret_cast<float2v*>(w + plan.starts);
+    a.sums = reinterpret_cast<float*>(w + plan.starts + round_256(plan.slots * 8));
+    a.own_rows = plan.own_rows;
+    a.prefix_rows = plan.prefix_rows;
+    a.own_slots = (int64_t)plan.rows;
+    a.prefix_whole = a.own_slots + 2ll * plan.own_workers * plan.own_rows;
+    a.prefix_slots = a.prefix_whole + (int64_t)plan.rows;
     hipStream_t s = static_cast<hipStream_t>(stream);
     switch (ctx->g.d) {
         case 32: return launched(launch_attend<32>(a, s));
