@@ -33,7 +33,7 @@ __device__ inline Range group_of_prefix(const AttendArgs& a, int g) {
     r.end = min(max(a.prefix_first[g + 1], r.begin), a.n_seq);
     return r;
 }
-// The prefix that sequence s has, or -1: the last one that begins at or before it, if that holds it.
+// The prefix that sequence s has, or -1: the last one that begins at or before it, if the next one does not.
 __device__ inline int prefix_of(const AttendArgs& a, int s) {
     int lo = 0, hi = a.n_prefix;  // first[lo..hi) may be at or before s
     while (lo < hi) {
@@ -41,7 +41,7 @@ __device__ inline int prefix_of(const AttendArgs& a, int s) {
         if (a.prefix_first[mid] <= s) lo = mid + 1;
         else hi = mid;
     }
-    return lo > 0 && s < group_of_prefix(a, lo - 1).end && s >= group_of_prefix(a, lo - 1).begin ? lo - 1 : -1;
+    return lo > 0 && s < a.prefix_first[lo] ? lo - 1 : -1;
 }
 
 // ---- dividing the work: sums of f(0..n-1), with the items dealt to the 256 threads of a workgroup in runs of `each`.
@@ -432,73 +432,98 @@ __global__ __launch_bounds__(256, 1) void k_prefix(AttendArgs a) {
     }
 }
 
-// ---- joining pieces: D / 8 threads to a row, 8 channels each.
-template <int D>
-struct Join {
-    float m = -INFINITY, l = 0.f;
-    float4v o[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+// ---- joining pieces: D / 8 threads to a row, 8 channels each.  A row's pieces are read kAtOnce at a time: each read goes to memory, and takes as
+// long as all of them together.
+constexpr uint32_t kAtOnce = 8;
 
-    __device__ void add(const AttendArgs& a, int64_t slot, uint32_t c) {
-        const float2v st = a.stats[slot];
-        const float4v* p = reinterpret_cast<const float4v*>(a.sums + slot * D + 8 * c);
-        const float4v x = p[0], y = p[1];
-        if (st[0] == -INFINITY) return;  // (a piece in which the row saw no token)
-        const float top = fmaxf(m, st[0]), f = m == -INFINITY ? 0.f : power2(m - top), w = power2(st[0] - top);
-        m = top;
-        l = l * f + st[1] * w;
-        o[0] = o[0] * f + x * w;
-        o[1] = o[1] * f + y * w;
+// Where the pieces of a unit are, for one of its rows: `n` workers from w0 on have one each, or one has it whole.
+struct Pieces {
+    int64_t whole, slots;
+    uint32_t n = 0, w0 = 0, rows = 0;
+
+    __device__ void find(uint32_t start, uint32_t tiles, uint32_t each) {
+        w0 = start / each;
+        n = (start + tiles - 1) / each - w0 + 1;
     }
-    // A unit of `tiles` tiles from `start` on: in `whole` if one worker had it, else in the workers' slots.
-    __device__ void add_unit(const AttendArgs& a, uint32_t start, uint32_t tiles, uint32_t each, int64_t whole, int64_t slots, uint32_t rows, uint32_t row, uint32_t c) {
-        const uint32_t w0 = start / each, w1 = (start + tiles - 1) / each;
-        if (w0 == w1) {
-            add(a, whole, c);
-            return;
-        }
-        for (uint32_t w = w0; w <= w1; ++w) add(a, slots + (int64_t)(2 * w + (w == w0 ? 1 : 0)) * rows + row, c);
-    }
+    __device__ int64_t slot(uint32_t k) const { return n == 1 ? whole : slots + (int64_t)(2 * (w0 + k) + (k == 0 ? 1 : 0)) * rows; }
 };
 
 template <int D>
 __global__ __launch_bounds__(256) void k_join(AttendArgs a) {
-    const uint32_t own_rows = a.own_rows, prefix_rows = a.prefix_rows;
     constexpr uint32_t kEach = D / 8, kRows = 256 / kEach;
     const uint32_t in_group = threadIdx.x / kEach, c = threadIdx.x % kEach;
     const int64_t id = (int64_t)blockIdx.x * kRows + in_group;
     if (in_group >= kRows || id >= (int64_t)a.n_seq * a.n_kv * a.rows) return;
     const uint32_t unit = fast_div((uint32_t)id, a.by_rows), row = (uint32_t)id - unit * a.rows, s = unit / a.n_kv, h = unit - s * a.n_kv;
+    Pieces own, shared;
+    const uint32_t before = a.own_start[s], tiles = a.own_start[s + 1] - before, all = a.own_start[a.n_seq];
     const int g = a.n_prefix ? prefix_of(a, s) : -1;
-    Join<D> j;
-    const uint32_t before = a.own_start[s], tiles = a.own_start[s + 1] - before;
     if (tiles) {
-        const uint32_t units = a.n_kv * a.own_tiles, each = share(a.own_start[a.n_seq] * units, a.own_workers);
-        const uint32_t start = before * units + (h * a.own_tiles + row / own_rows) * tiles;
-        if (g < 0 && start / each == (start + tiles - 1) / each) return;  // finished by its worker
-        j.add_unit(a, start, tiles, each, id, a.own_slots, own_rows, row % own_rows, c);
+        const uint32_t units = a.n_kv * a.own_tiles, rt = row / a.own_rows;
+        own.find(before * units + (h * a.own_tiles + rt) * tiles, tiles, share(all * units, a.own_workers));
+        if (g < 0 && own.n == 1) return;  // finished by its worker
+        own.whole = id;
+        own.rows = a.own_rows;
+        own.slots = a.own_slots + (row - rt * a.own_rows);
     }
     if (g >= 0) {
         const Range seqs = group_of_prefix(a, g);
         const uint32_t ptiles = (prefix_length(a, g) + kPrefixTile - 1) / kPrefixTile;
         if (ptiles) {
-            const uint32_t rts = ((uint32_t)(seqs.end - seqs.begin) * a.rows + prefix_rows - 1) / prefix_rows;
-            const uint32_t rr = (s - seqs.begin) * a.rows + row, each = share(a.prefix_start[a.n_prefix] * a.n_kv, a.prefix_workers);
-            const uint32_t start = a.prefix_start[g] * a.n_kv + (h * rts + rr / prefix_rows) * ptiles;
-            j.add_unit(a, start, ptiles, each, a.prefix_whole + id, a.prefix_slots, prefix_rows, rr % prefix_rows, c);
+            const uint32_t rts = ((uint32_t)(seqs.end - seqs.begin) * a.rows + a.prefix_rows - 1) / a.prefix_rows;
+            const uint32_t rr = (s - seqs.begin) * a.rows + row, rt = rr / a.prefix_rows;
+            shared.find(a.prefix_start[g] * a.n_kv + (h * rts + rt) * ptiles, ptiles, share(a.prefix_start[a.n_prefix] * a.n_kv, a.prefix_workers));
+            shared.whole = a.prefix_whole + id;
+            shared.rows = a.prefix_rows;
+            shared.slots = a.prefix_slots + (rr - rt * a.prefix_rows);
+        }
+    }
+    float m = -INFINITY, l = 0.f;
+    float4v o[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    const uint32_t n = own.n + shared.n;
+    for (uint32_t k0 = 0; k0 < n; k0 += kAtOnce) {
+        float2v st[kAtOnce];
+        float4v x[kAtOnce][2];
+#pragma unroll
+        for (uint32_t j = 0; j < kAtOnce; ++j) {
+            const uint32_t k = min(k0 + j, n - 1);
+            const int64_t slot = k < own.n ? own.slot(k) : shared.slot(k - own.n);
+            st[j] = a.stats[slot];
+            const float4v* p = reinterpret_cast<const float4v*>(a.sums + slot * D + 8 * c);
+            x[j][0] = p[0];
+            x[j][1] = p[1];
+            if (k0 + j >= n) st[j][0] = -INFINITY;
+        }
+        float top = m;
+#pragma unroll
+        for (uint32_t j = 0; j < kAtOnce; ++j) top = fmaxf(top, st[j][0]);
+        if (top == -INFINITY) continue;  // pieces in which the row saw no token
+        const float f = power2(m - top);
+        m = top;
+        l *= f;
+        o[0] *= f;
+        o[1] *= f;
+#pragma unroll
+        for (uint32_t j = 0; j < kAtOnce; ++j) {
+            const float w = power2(st[j][0] - top);
+            if (st[j][0] == -INFINITY) continue;  // (their sums are zeros, or another piece's)
+            l += st[j][1] * w;
+            o[0] += x[j][0] * w;
+            o[1] += x[j][1] * w;
         }
     }
     const uint32_t in = fast_div(row, a.by_n_q), i = row - in * a.n_q, head = h * a.group + in;
-    const float f = j.l == 0.f ? 0.f : 1.f / j.l;
+    const float f = l == 0.f ? 0.f : 1.f / l;
     uint4v v;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         half2 x;
-        x[0] = (_Float16)(j.o[e / 2][e % 2 * 2] * f);
-        x[1] = (_Float16)(j.o[e / 2][e % 2 * 2 + 1] * f);
+        x[0] = (_Float16)(o[e / 2][e % 2 * 2] * f);
+        x[1] = (_Float16)(o[e / 2][e % 2 * 2 + 1] * f);
         v[e] = __builtin_bit_cast(uint32_t, x);
     }
     *reinterpret_cast<uint4v*>(a.out + s * a.out_strides[0] + i * a.out_strides[1] + head * a.out_strides[2] + 8 * c) = v;
-    if (a.lse && c == 0) a.lse[((int64_t)s * a.n_q + i) * a.n_heads + head] = lse_of(j.m, j.l);
+    if (a.lse && c == 0) a.lse[((int64_t)s * a.n_q + i) * a.n_heads + head] = lse_of(m, l);
 }
 
 template <int D, int R>
