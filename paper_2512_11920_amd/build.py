@@ -15,9 +15,12 @@ _ROOT = os.path.dirname(_PKG)
 _CSRC = os.path.join(_PKG, "csrc")
 SHAPE_GROUPS = 16  # see csrc/kvc_codec.hip
 HEAD_DIMS = range(32, 257, 32)  # see csrc/kvc_attend.hip
+#: matrix products leave their results in ordinary vector registers, where the softmax reads them: without it attention moved each score
+#: from an accumulation register first, two instructions a score
+VECTOR_RESULTS = ("-mllvm", "-amdgpu-mfma-vgpr-form")
 #: (source, extra defines, object name)
 UNITS = [("kvc_kernels.hip", (), "kvc_kernels.o"), ("kvc_api.hip", (), "kvc_api.o"), ("kvc_cache.hip", (), "kvc_cache.o"), ("kvc_cache_api.hip", (), "kvc_cache_api.o")] + \
-        [("kvc_attend.hip", (f"-DKVC_HEAD_DIM={d}",), f"kvc_attend_{d}.o") for d in HEAD_DIMS] + \
+        [("kvc_attend.hip", (f"-DKVC_HEAD_DIM={d}", *VECTOR_RESULTS), f"kvc_attend_{d}.o") for d in HEAD_DIMS] + \
         [("kvc_codec.hip", (f"-DKVC_SHAPE_GROUP={g}",), f"kvc_codec_{g}.o") for g in range(SHAPE_GROUPS)]
 SOURCES = [os.path.join(_CSRC, f) for f in ("kvc_kernels.hip", "kvc_codec.hip", "kvc_api.hip", "kvc_cache.hip", "kvc_attend.hip", "kvc_cache_api.hip")]
 HEADERS = [os.path.join(_CSRC, f) for f in ("kvc_common.h", "kvc_fastdiv.h", "kvc_device.h", "kvc_codec.h", "kvc_ctx.h", "kvc_cache.h", "kvc_attend.h")] + [os.path.join(_ROOT, "include", "kvc.h")]

@@ -52,20 +52,35 @@ template <class F>
 __device__ inline void add_up(Sums& s, uint32_t n, F f) {
     const uint32_t t = threadIdx.x, lane = t & 63, each = (n + 255) / 256;
     uint32_t sum = 0;
-    for (uint32_t i = t * each; i < n && i < (t + 1) * each; ++i) sum += f(i);
+    if (t < 256)
+        for (uint32_t i = t * each; i < n && i < (t + 1) * each; ++i) sum += f(i);
     uint32_t upto = sum;
 #pragma unroll
     for (int k = 1; k < 64; k *= 2) {
         const uint32_t o = __shfl_up(upto, k);
         if (lane >= (uint32_t)k) upto += o;
     }
-    if (lane == 63) s.wave[t / 64] = upto;
+    if (lane == 63 && t < 256) s.wave[t / 64] = upto;
     __syncthreads();
-    uint32_t base = 0;
-    for (uint32_t w = 0; w < t / 64; ++w) base += s.wave[w];
-    s.before[t] = base + upto - sum;
-    if (t == 255) s.all = base + upto, s.each = each;
+    if (t < 256) {
+        uint32_t base = 0;
+        for (uint32_t w = 0; w < t / 64; ++w) base += s.wave[w];
+        s.before[t] = base + upto - sum;
+        if (t == 255) s.all = base + upto, s.each = each;
+    }
     __syncthreads();
+}
+// The sum before every item, and of all, for k_join.
+template <class F>
+__device__ inline void write_starts(const Sums& s, uint32_t* start, uint32_t n, F f) {
+    const uint32_t t = threadIdx.x;
+    if (t >= 256) return;
+    uint32_t at = s.before[t];
+    for (uint32_t i = t * s.each; i < n && i < (t + 1) * s.each; ++i) {
+        start[i] = at;
+        at += f(i);
+    }
+    if (t == 0) start[n] = s.all;
 }
 // The item that holds position p < s.all, and the sum before it.
 struct Item {
@@ -103,15 +118,7 @@ __global__ __launch_bounds__(256, D * R <= 128 ? 2 : 1) void k_own(AttendArgs a)
     __shared__ Sums sums;
     const auto tiles_of = [&](uint32_t s) { return (own_length(a, s) + kTile - 1) / kTile; };
     add_up(sums, a.n_seq, tiles_of);
-    if (blockIdx.x == 0) {
-        const uint32_t t = threadIdx.x;
-        uint32_t at = sums.before[t];
-        for (uint32_t i = t * sums.each; i < (uint32_t)a.n_seq && i < (t + 1) * sums.each; ++i) {
-            a.own_start[i] = at;
-            at += tiles_of(i);
-        }
-        if (t == 0) a.own_start[a.n_seq] = sums.all;
-    }
+    if (blockIdx.x == 0) write_starts(sums, a.own_start, a.n_seq, tiles_of);
     const uint32_t units = a.n_kv * a.own_tiles, all = sums.all * units, each = share(all, a.own_workers);
     const uint32_t worker = uniform(blockIdx.x * 4 + threadIdx.x / 64), begin = worker * each;
     if (begin >= all) return;
@@ -224,47 +231,43 @@ __global__ __launch_bounds__(256, D * R <= 128 ? 2 : 1) void k_own(AttendArgs a)
     }
 }
 
-// ---- prefixes.  A worker is a workgroup: 128 * RB rows of a group (32 * RB a wave) share tiles of 64 tokens in LDS.
-constexpr int kPrefixTile = 64;
+// ---- prefixes.  A worker is a workgroup: 32 rows of a group a wave share tiles of 32 tokens in LDS, of which four are there: the present one, two on their way ...
+constexpr int kStages = 4;
 typedef float float16v __attribute__((ext_vector_type(16)));
 typedef short short4v __attribute__((ext_vector_type(4)));
+#define KVC_LDS(p) (__attribute__((address_space(3))) void*)(p)
 
-// A tile is [token][chunk] with chunks of 16 bytes; chunk c of token t lies at place c ^ turn(t) of its row, so that lanes that read one chunk of
-// consecutive tokens meet in no bank (rows are loaded whole, so that the order within a row is free).
+// How keys and values of 32 tokens lie in LDS, in chunks of 16 bytes, C to a row.  The lanes that read one chunk of 16 consecutive tokens shall meet in no
+// bank (16 chunks wide): the low bits of a chunk's number are turned by its token, and where whole rows would still begin in one
+// bank, every fourth row is followed by four chunks of padding.  (Only low bits are turned, so that addresses of other chunks are a constant away.)
 template <int D>
-__device__ inline uint32_t turn(uint32_t t) {
-    constexpr int C = D / 8;
-    return C % 16 == 0 ? t & 15 : C % 8 == 0 ? t >> 1 & 7 : t >> 2 & 3;
-}
-
-template <int D, int RB>
-struct PrefixRows {
-    uint4v q[RB][D / 16];
-    float16v o[RB][D / 32];
-    float m[RB], l[RB];
+struct Layout {
+    static constexpr uint32_t C = D / 8, kMask = C % 16 == 0 || C % 8 != 0 ? 3 : 7, kPad = C % 16 == 0 ? 4 : 0;
+    static constexpr uint32_t kChunks = 32 * C + 8 * kPad;
+    __host__ __device__ static constexpr uint32_t turn(uint32_t t) { return C % 16 == 0 ? t & 3 : C % 8 == 0 ? t >> 1 & 7 : t >> 2 & 3; }
+    __host__ __device__ static constexpr uint32_t row(uint32_t t) { return t * C + t / 4 * kPad; }
 };
 
-template <int D, int RB>
-__global__ __launch_bounds__(256, 1) void k_prefix(AttendArgs a) {
-    constexpr int C = D / 8, kLoads = C / 4, kRows = 128 * RB;
+// Waits until at most N of the wave's loads are on their way.
+template <uint32_t N>
+__device__ inline void wait_for_loads() {
+    __builtin_amdgcn_s_waitcnt((N & 15) | N >> 4 << 14 | 7 << 4 | 15 << 8);
+}
+
+template <int D, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, WAVES / 4) void k_prefix(AttendArgs a) {
+    using L = Layout<D>;
+    constexpr uint32_t C = L::C, kLoads = (C + WAVES - 1) / WAVES, kRows = 32 * WAVES, kVariants = (L::kMask + 1) / 2;
     __shared__ Sums sums;
-    __shared__ __align__(16) uint4v tile[2][2][kPrefixTile * C];  // [stage][keys, values]
+    __shared__ __align__(16) uint4v tile[kStages][2][L::kChunks];  // [stage][keys, values]
     const auto row_tiles = [&](uint32_t g) {
         const Range r = group_of_prefix(a, g);
         return ((uint32_t)(r.end - r.begin) * a.rows + kRows - 1) / kRows;
     };
-    const auto tiles_of = [&](uint32_t g) { return (prefix_length(a, g) + kPrefixTile - 1) / kPrefixTile; };
+    const auto tiles_of = [&](uint32_t g) { return (prefix_length(a, g) + kTile - 1) / kTile; };
     const auto work_of = [&](uint32_t g) { return row_tiles(g) * tiles_of(g); };
     add_up(sums, a.n_prefix, work_of);
-    if (blockIdx.x == 0) {
-        const uint32_t t = threadIdx.x;
-        uint32_t at = sums.before[t];
-        for (uint32_t i = t * sums.each; i < (uint32_t)a.n_prefix && i < (t + 1) * sums.each; ++i) {
-            a.prefix_start[i] = at;
-            at += work_of(i);
-        }
-        if (t == 0) a.prefix_start[a.n_prefix] = sums.all;
-    }
+    if (blockIdx.x == 0) write_starts(sums, a.prefix_start, a.n_prefix, work_of);
     const uint32_t all = sums.all * a.n_kv, each = share(all, a.prefix_workers);
     // workgroups go to the XCDs in turn: an XCD's take neighbouring shares, which read the same tokens
     const uint32_t worker = a.prefix_workers % 8 ? blockIdx.x : blockIdx.x % 8 * (a.prefix_workers / 8) + blockIdx.x / 8, begin = worker * each;
@@ -272,17 +275,30 @@ __global__ __launch_bounds__(256, 1) void k_prefix(AttendArgs a) {
     uint32_t left = min(each, all - begin);
 
     const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x / 64), n = lane & 31, h2 = lane >> 5;
-    // what this lane loads of a tile: chunk at[j] of the tile is chunk from[j] of its token's row
-    uint32_t token[kLoads], from[kLoads];
+    // A tile comes in C loads of 64 chunks, the first half of them keys; a wave makes kLoads (where they are more than there are, some twice).  Of
+    // load j this lane's is chunk `from` of token `token`.
+    uint32_t token[kLoads], from[kLoads], number[kLoads];
 #pragma unroll
-    for (int j = 0; j < kLoads; ++j) {
-        const uint32_t i = (wave * kLoads + j) * 64 + lane;
+    for (uint32_t j = 0; j < kLoads; ++j) {
+        number[j] = (wave * kLoads + j) % C;
+        const uint32_t i = number[j] % (C / 2) * 64 + lane;
         token[j] = i / C;
-        from[j] = (i % C) ^ turn<D>(token[j]);
+        from[j] = 8 * (i % C ^ L::turn(token[j]));
     }
+    // What this lane reads of a tile of keys: row n, chunk 2c + h2; of values: a group of 16 lanes reads 16 channels of 4 tokens and gets
+    // a channel's 4 tokens each, so rows 4 * h2 + l16 / 4 (+ 8, 16, 24), 8 bytes of chunk 4c + vc.
+    const uint32_t l16 = lane & 15, vrow = 4 * h2 + l16 / 4, vc = (lane >> 4 & 1) * 2 + (l16 & 3) / 2;
+    uint32_t key_at[kVariants], value_at[2][kVariants == 2 ? 1 : 2];
+#pragma unroll
+    for (uint32_t v = 0; v < kVariants; ++v) key_at[v] = 16 * (L::row(n) + ((2 * v + h2) ^ L::turn(n)));
+#pragma unroll
+    for (uint32_t e = 0; e < 2; ++e)
+#pragma unroll
+        for (uint32_t v = 0; v < (kVariants == 2 ? 1 : 2); ++v) value_at[e][v] = 16 * (L::row(8 * e + vrow) + ((4 * v + vc) ^ L::turn(8 * e + vrow))) + 8 * (l16 & 1);
 
+    const float scale = fabsf(a.scale_log2);
+    const uint32_t flip = a.scale_log2 < 0.f ? 0x80008000u : 0u;  // a negative scale is the queries' sign
     uint32_t g, u, t, tiles, rts;
-    Range seqs;
     {
         const Item it = find_item(sums, a.n_prefix, begin / a.n_kv, work_of);
         g = uniform(it.i);
@@ -294,130 +310,125 @@ __global__ __launch_bounds__(256, 1) void k_prefix(AttendArgs a) {
     }
     for (;;) {
         const uint32_t h = u / rts, rt = u - h * rts, len = uniform(prefix_length(a, g)), first_tile = t, n_tiles = min(tiles - t, left);
-        seqs = group_of_prefix(a, g);
+        const Range seqs = group_of_prefix(a, g);
         const uint32_t rows = (uint32_t)(seqs.end - seqs.begin) * a.rows;
         const int32_t* table = a.prefix_table + (int64_t)g * a.max_prefix_blocks;
         const uint16_t *keys = a.k_cache + h * a.g.page_stride, *values = a.v_cache + h * a.g.page_stride;
+        const uint32_t in_tile = wave * 32 + n, rr = rt * kRows + in_tile;  // the lane's row, of the tile and of the group
 
-        PrefixRows<D, RB> r;
+        uint4v q[D / 16];
+        float16v o[D / 32];
+        float m = -INFINITY, l = 0.f;
+        {
+            const uint32_t r = min(rr, rows - 1), sq = fast_div(r, a.by_rows), row = r - sq * a.rows, in = fast_div(row, a.by_n_q), i = row - in * a.n_q;
+            const uint16_t* p = a.q + (seqs.begin + sq) * a.q_strides[0] + i * a.q_strides[1] + (h * a.group + in) * a.q_strides[2];
 #pragma unroll
-        for (int b = 0; b < RB; ++b) {
-            const uint32_t rr = min(rt * kRows + (wave * RB + b) * 32 + n, rows - 1), s = fast_div(rr, a.by_rows), row = rr - s * a.rows;
-            const uint32_t in = fast_div(row, a.by_n_q), i = row - in * a.n_q;
-            const uint16_t* q = a.q + (seqs.begin + s) * a.q_strides[0] + i * a.q_strides[1] + (h * a.group + in) * a.q_strides[2];
-#pragma unroll
-            for (int c = 0; c < D / 16; ++c) r.q[b][c] = *reinterpret_cast<const uint4v*>(q + 16 * c + 8 * h2);
+            for (int c = 0; c < D / 16; ++c) q[c] = *reinterpret_cast<const uint4v*>(p + 16 * c + 8 * h2) ^ flip;
 #pragma unroll
             for (int c = 0; c < D / 32; ++c)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) r.o[b][c][e] = 0.f;
-            r.m[b] = -INFINITY;
-            r.l[b] = 0.f;
+                for (int e = 0; e < 16; ++e) o[c][e] = 0.f;
         }
-        // block of token `lane` of tile i, -1: it has none
-        const auto look_up = [&](uint32_t i) {
-            const uint32_t k = i * kPrefixTile + lane;
-            const int32_t block = k < len ? table[fast_div(k, a.by_N)] : -1;
-            return in_cache(a, block) ? block : -1;
-        };
-        const auto load = [&](uint32_t i, int32_t blocks, int stage) {
+        const auto look_up = [&](uint32_t i) { const uint32_t k = (t + i) * kTile + n; return i < n_tiles && k < len ? table[fast_div(k, a.by_N)] : -1; };
+        // loads tile i, whose token n lies in `block`; -> which of its tokens exist
+        const auto load = [&](uint32_t i, int32_t block) {
+            const bool there = in_cache(a, block);
+            const int64_t at = there ? place(a, block, (t + i) * kTile + n) : -1;
+            const int lo = (int)at, hi = (int)(at >> 32);
 #pragma unroll
-            for (int j = 0; j < kLoads; ++j) {
-                const int32_t block = __shfl(blocks, token[j]);
-                const uint32_t k = i * kPrefixTile + token[j];
-                const int64_t at = place(a, block, k) + 8 * from[j];
-                const uint16_t* kp = block < 0 ? kZeroRow + 8 * from[j] : keys + at;
-                const uint16_t* vp = block < 0 ? kZeroRow + 8 * from[j] : values + at;
-                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)kp, (__attribute__((address_space(3))) void*)&tile[stage][0][(wave * kLoads + j) * 64], 16, 0, 0);
-                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)vp, (__attribute__((address_space(3))) void*)&tile[stage][1][(wave * kLoads + j) * 64], 16, 0, 0);
+            for (uint32_t j = 0; j < kLoads; ++j) {
+                const int64_t row = (uint32_t)__shfl(lo, token[j]) | (int64_t)__shfl(hi, token[j]) << 32;
+                const bool is_value = number[j] >= C / 2;
+                const uint32_t first = number[j] % (C / 2) * 64;
+                const uint16_t* p = row < 0 ? kZeroRow : (is_value ? values : keys) + row;
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(p + from[j]),
+                                                 KVC_LDS(&tile[i % kStages][is_value][first + first / C / 4 * L::kPad]), 16, 0, 0);
             }
+            return (uint32_t)__ballot(there);
         };
-        int32_t blocks = look_up(t);
+
+        // Tiles 0..2 on their way, and the blocks of tiles 3 and 4; mask[k]: the tokens of tile i + k that exist.  What comes back comes in order: the
+        // present tile and the block number of the one to be loaded next are there when only what the last two steps asked for is missing.
+        uint32_t mask[3];
+        int32_t next[2], block[3];
+#pragma unroll
+        for (uint32_t i = 0; i < 3; ++i) block[i] = look_up(i);
+        next[0] = look_up(3);
         __syncthreads();  // (the tiles of the last piece have been read)
-        load(t, blocks, 0);
+        mask[0] = load(0, block[0]);
+        mask[1] = load(1, block[1]);
+        next[1] = look_up(4);
+        mask[2] = load(2, block[2]);
         for (uint32_t i = 0; i < n_tiles; ++i) {
-            const int stage = i & 1;
-            const unsigned long long there = __ballot(blocks >= 0);
-            if (i + 1 < n_tiles) blocks = look_up(t + i + 1);
-            __builtin_amdgcn_s_waitcnt(0);  // this wave's part of the tile is in LDS
-            __syncthreads();                // all of it is, and the other stage has been read
-            if (i + 1 < n_tiles) load(t + i + 1, blocks, stage ^ 1);
+            // tile i is there, and every wave is done with tile i - 1, whose place tile i + 3 takes
+            wait_for_loads<2 * kLoads + 1>();
+            __syncthreads();
+            const uint32_t coming = load(i + 3, next[0]);
+            next[0] = next[1];
+            next[1] = look_up(i + 5);
+            float16v s;
 #pragma unroll
-            for (int sub = 0; sub < 2; ++sub) {
-                float16v s[RB];
+            for (int e = 0; e < 16; ++e) s[e] = 0.f;
+            const char* kt = reinterpret_cast<const char*>(&tile[i % kStages][0][0]);
+            const char* vt = reinterpret_cast<const char*>(&tile[i % kStages][1][0]);
 #pragma unroll
-                for (int b = 0; b < RB; ++b)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) s[b][e] = 0.f;
-                const uint32_t krow = 32 * sub + n;
-#pragma unroll
-                for (int c = 0; c < D / 16; ++c) {
-                    const uint4v k = tile[stage][0][krow * C + ((2 * c + h2) ^ turn<D>(krow))];
-#pragma unroll
-                    for (int b = 0; b < RB; ++b)
-                        s[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, k), __builtin_bit_cast(half8, r.q[b][c]), s[b], 0, 0, 0);
-                }
-                half8 p[RB][2];
-                const uint32_t here = (uint32_t)(there >> (32 * sub)) >> (4 * h2);
-#pragma unroll
-                for (int b = 0; b < RB; ++b) {
-                    float v[16], top = -INFINITY;
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        v[e] = here >> (8 * (e / 4) + e % 4) & 1 ? s[b][e] * a.scale_log2 : -INFINITY;
-                        top = fmaxf(top, v[e]);
-                    }
-                    top = both32(top, false);
-                    if (__any(top > r.m[b] + kLag)) {
-                        const float m = fmaxf(r.m[b], top), f = r.m[b] == -INFINITY ? 0.f : power2(r.m[b] - m);
-                        r.m[b] = m;
-                        r.l[b] *= f;
-#pragma unroll
-                        for (int c = 0; c < D / 32; ++c) r.o[b][c] *= f;
-                    }
-                    const float low = (r.m[b] == -INFINITY ? 0.f : r.m[b]) - kLift;
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const float w = power2(v[e] - low);
-                        r.l[b] += w;
-                        p[b][e / 8][e % 8] = (_Float16)w;
-                    }
-                }
-                // values: lane group i of 16 reads, of 4 tokens, 16 channels, and gets one channel of the 4 tokens
-                const uint32_t l16 = lane & 15, vrow = 4 * h2 + l16 / 4, vc = (lane >> 4 & 1) * 2 + (l16 & 3) / 2;
-#pragma unroll
-                for (int k = 0; k < 2; ++k)
-#pragma unroll
-                    for (int c = 0; c < D / 32; ++c) {
-                        short4v part[2];
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const uint32_t row = 32 * sub + 16 * k + 8 * e + vrow;
-                            const uint4v* at = &tile[stage][1][row * C + ((4 * c + vc) ^ turn<D>(row))];
-                            part[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(reinterpret_cast<const char*>(at) + 8 * (l16 & 1)));
-                        }
-                        const half8 v = __builtin_bit_cast(half8, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-                        for (int b = 0; b < RB; ++b) r.o[b][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p[b][k], r.o[b][c], 0, 0, 0);
-                    }
+            for (uint32_t c = 0; c < D / 16; ++c) {
+                const uint4v k = *reinterpret_cast<const uint4v*>(kt + key_at[c % kVariants] + 32 * (c - c % kVariants));
+                s = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, k), __builtin_bit_cast(half8, q[c]), s, 0, 0, 0);
             }
+            if (mask[0] != ~0u) {
+                const uint32_t here = mask[0] >> (4 * h2);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[e] = here >> (8 * (e / 4) + e % 4) & 1 ? s[e] : -INFINITY;
+            }
+            float top = fmaxf(s[0], s[1]);
+#pragma unroll
+            for (int e = 2; e < 16; ++e) top = fmaxf(top, s[e]);
+            top = both32(top, false) * scale;
+            if (__any(top > m + kLag)) {
+                const float to = fmaxf(m, top), f = m == -INFINITY ? 0.f : power2(m - to);
+                m = to;
+                l *= f;
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) o[c] *= f;
+            }
+            half8 p[2];
+            const float low = kLift - (m == -INFINITY ? 0.f : m);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const float w = power2(fmaf(s[e], scale, low));
+                l += w;
+                p[e / 8][e % 8] = (_Float16)w;
+            }
+#pragma unroll
+            for (uint32_t k = 0; k < 2; ++k)
+#pragma unroll
+                for (uint32_t c = 0; c < D / 32; ++c) {
+                    short4v part[2];
+#pragma unroll
+                    for (uint32_t e = 0; e < 2; ++e)
+                        part[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)KVC_LDS(
+                            vt + value_at[e][kVariants == 2 ? 0 : c % 2] + 16 * L::row(16 * k) + 64 * (kVariants == 2 ? c : c - c % 2)));
+                    const half8 v = __builtin_bit_cast(half8, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
+                    o[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p[k], o[c], 0, 0, 0);
+                }
+            mask[0] = mask[1];
+            mask[1] = mask[2];
+            mask[2] = coming;
         }
         const bool whole = first_tile == 0 && n_tiles == tiles;
-#pragma unroll
-        for (int b = 0; b < RB; ++b) {
-            const float l = both32(r.l[b], true);
-            const uint32_t in_tile = (wave * RB + b) * 32 + n, rr = rt * kRows + in_tile;
-            if (rr >= rows) continue;
-            const uint32_t s = fast_div(rr, a.by_rows), row = rr - s * a.rows;
-            const int64_t slot = whole ? a.prefix_whole + ((int64_t)(seqs.begin + s) * a.n_kv + h) * a.rows + row
+        const float sum = both32(l, true);
+        if (rr < rows) {
+            const uint32_t sq = fast_div(rr, a.by_rows), row = rr - sq * a.rows;
+            const int64_t slot = whole ? a.prefix_whole + ((int64_t)(seqs.begin + sq) * a.n_kv + h) * a.rows + row
                                        : a.prefix_slots + (int64_t)(2 * worker + (first_tile == 0 ? 1 : 0)) * kRows + in_tile;
             float* out = a.sums + slot * D + 4 * h2;
 #pragma unroll
             for (int c = 0; c < D / 32; ++c)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    *reinterpret_cast<float4v*>(out + 32 * c + 8 * e) = float4v{r.o[b][c][4 * e], r.o[b][c][4 * e + 1], r.o[b][c][4 * e + 2], r.o[b][c][4 * e + 3]};
-            if (h2 == 0) a.stats[slot] = float2v{r.m[b] - kLift, l};
+                    *reinterpret_cast<float4v*>(out + 32 * c + 8 * e) = float4v{o[c][4 * e], o[c][4 * e + 1], o[c][4 * e + 2], o[c][4 * e + 3]};
+            if (h2 == 0) a.stats[slot] = float2v{m - kLift, sum};
         }
         left -= n_tiles;
         if (left == 0) break;
@@ -468,7 +479,7 @@ __global__ __launch_bounds__(256) void k_join(AttendArgs a) {
     }
     if (g >= 0) {
         const Range seqs = group_of_prefix(a, g);
-        const uint32_t ptiles = (prefix_length(a, g) + kPrefixTile - 1) / kPrefixTile;
+        const uint32_t ptiles = (prefix_length(a, g) + kTile - 1) / kTile;
         if (ptiles) {
             const uint32_t rts = ((uint32_t)(seqs.end - seqs.begin) * a.rows + a.prefix_rows - 1) / a.prefix_rows;
             const uint32_t rr = (s - seqs.begin) * a.rows + row, rt = rr / a.prefix_rows;
@@ -534,11 +545,11 @@ static hipError_t launch_own(const AttendArgs& a, hipStream_t s) {
 
 template <>
 hipError_t launch_attend<KVC_HEAD_DIM>(const AttendArgs& a, hipStream_t s) {
-    constexpr int D = KVC_HEAD_DIM, RB = D <= 128 ? 2 : 1;
+    constexpr int D = KVC_HEAD_DIM, W = prefix_waves(D);
     hipError_t e;
     if constexpr (D <= 192) e = a.own_rows == 32 ? launch_own<D, 2>(a, s) : launch_own<D, 1>(a, s);
     else e = launch_own<D, 1>(a, s);
-    if (e == hipSuccess && a.n_prefix) e = launch_kernel(k_prefix<D, RB>, dim3(a.prefix_workers), dim3(256), s, a);
+    if (e == hipSuccess && a.n_prefix) e = launch_kernel(k_prefix<D, W>, dim3(a.prefix_workers), dim3(64 * W), s, a);
     constexpr uint32_t rows = 256 / (D / 8);
     if (e == hipSuccess) e = launch_kernel(k_join<D>, dim3((unsigned)(((int64_t)a.n_seq * a.n_kv * a.rows + rows - 1) / rows)), dim3(256), s, a);
     return e;

@@ -112,10 +112,12 @@ struct AttendPlan {
 };
 constexpr uint32_t kOwnWorkers = 2048, kPrefixWorkers = 256;  // waves, workgroups: what the GPU holds at once
 
+constexpr uint32_t prefix_waves(int d) { return d <= 192 ? 8 : 4; }  // of a workgroup
+
 inline AttendPlan plan_attend(int64_t n_seq, int64_t n_q, int64_t n_heads, int64_t n_kv, int d, int64_t n_prefix) {
     AttendPlan p;
     p.own_rows = n_heads / n_kv * n_q <= 16 || d > 192 ? 16 : 32;  // (32 rows of wider heads do not fit into the registers)
-    p.prefix_rows = d <= 128 ? 256 : 128;
+    p.prefix_rows = 32 * prefix_waves(d);
     p.own_workers = kOwnWorkers;
     p.prefix_workers = n_prefix ? kPrefixWorkers : 0;
     p.rows = (uint64_t)(n_seq * n_heads * n_q);

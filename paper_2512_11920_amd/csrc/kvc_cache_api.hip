@@ -76,7 +76,7 @@ int kvc_attend(kvc_ctx* ctx, const kvc_attend_t* p, void* stream) {
     const int64_t prefix_tiles = (rows * p->n_seq + plan.prefix_rows - 1) / plan.prefix_rows + p->n_prefix;
     const auto product = [](int64_t a, int64_t b, int64_t c) { return (__int128)a * b * c; };
     if (product(own_tiles * p->n_kv_heads, p->n_seq, own_tokens / 32 + 1) > INT32_MAX) return KVC_ERR_ARG;
-    if (p->n_prefix && product(prefix_tiles, p->n_kv_heads, prefix_tokens / 64 + 1) > INT32_MAX) return KVC_ERR_ARG;
+    if (p->n_prefix && product(prefix_tiles, p->n_kv_heads, prefix_tokens / 32 + 1) > INT32_MAX) return KVC_ERR_ARG;
     if (!p->d_work || !aligned(p->d_work, 256) || p->work_bytes < plan.bytes) return KVC_ERR_ARG;
     AttendArgs a;
     a.q = static_cast<const uint16_t*>(p->d_q);
