@@ -237,15 +237,13 @@ typedef float float16v __attribute__((ext_vector_type(16)));
 typedef short short4v __attribute__((ext_vector_type(4)));
 #define KVC_LDS(p) (__attribute__((address_space(3))) void*)(p)
 
-// How keys and values of 32 tokens lie in LDS, in chunks of 16 bytes, C to a row.  The lanes that read one chunk of 16 consecutive tokens shall meet in no
-// bank (16 chunks wide): the low bits of a chunk's number are turned by its token, and where whole rows would still begin in one
-// bank, every fourth row is followed by four chunks of padding.  (Only low bits are turned, so that addresses of other chunks are a constant away.)
+// How keys and values of 32 tokens lie in LDS, in chunks of 16 bytes, C to a row.  Two kinds of read shall meet in no bank (16 chunks wide): one chunk
+// of 16 consecutive tokens (keys), and four chunks of four consecutive tokens (values).  So the low bits of a chunk's number are turned by its
+// token: as many tokens as begin in one bank differ in them, the nearest ones by fours.
 template <int D>
 struct Layout {
-    static constexpr uint32_t C = D / 8, kMask = C % 16 == 0 || C % 8 != 0 ? 3 : 7, kPad = C % 16 == 0 ? 4 : 0;
-    static constexpr uint32_t kChunks = 32 * C + 8 * kPad;
-    __host__ __device__ static constexpr uint32_t turn(uint32_t t) { return C % 16 == 0 ? t & 3 : C % 8 == 0 ? t >> 1 & 7 : t >> 2 & 3; }
-    __host__ __device__ static constexpr uint32_t row(uint32_t t) { return t * C + t / 4 * kPad; }
+    static constexpr uint32_t C = D / 8, kMask = C % 16 == 0 ? 15 : C % 8 == 0 ? 7 : 3;
+    __host__ __device__ static constexpr uint32_t turn(uint32_t t) { return C % 16 == 0 ? (t & 3) << 2 | (t >> 2 & 3) : C % 8 == 0 ? (t >> 1 & 1) << 2 | (t >> 2 & 3) : t >> 2 & 3; }
 };
 
 // Waits until at most N of the wave's loads are on their way.
@@ -254,12 +252,17 @@ __device__ inline void wait_for_loads() {
     __builtin_amdgcn_s_waitcnt((N & 15) | N >> 4 << 14 | 7 << 4 | 15 << 8);
 }
 
-template <int D, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, WAVES / 4) void k_prefix(AttendArgs a) {
+template <uint32_t N>
+struct Constant {
+    static constexpr uint32_t value = N;
+};
+
+template <int D>
+__global__ __launch_bounds__(64 * kPrefixWaves, D <= 128 ? 2 : 1) void k_prefix(AttendArgs a) {
     using L = Layout<D>;
-    constexpr uint32_t C = L::C, kLoads = (C + WAVES - 1) / WAVES, kRows = 32 * WAVES, kVariants = (L::kMask + 1) / 2;
+    constexpr uint32_t C = L::C, kLoads = C / kPrefixWaves, kRows = 32 * kPrefixWaves, kKeys = (L::kMask + 1) / 2, kValues = (L::kMask + 1) / 4;
     __shared__ Sums sums;
-    __shared__ __align__(16) uint4v tile[kStages][2][L::kChunks];  // [stage][keys, values]
+    __shared__ __align__(16) uint4v tile[kStages][2][32 * C];  // [stage][keys, values]
     const auto row_tiles = [&](uint32_t g) {
         const Range r = group_of_prefix(a, g);
         return ((uint32_t)(r.end - r.begin) * a.rows + kRows - 1) / kRows;
@@ -270,34 +273,38 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void k_prefix(AttendArgs a) 
     if (blockIdx.x == 0) write_starts(sums, a.prefix_start, a.n_prefix, work_of);
     const uint32_t all = sums.all * a.n_kv, each = share(all, a.prefix_workers);
     // workgroups go to the XCDs in turn: an XCD's take neighbouring shares, which read the same tokens
-    const uint32_t worker = a.prefix_workers % 8 ? blockIdx.x : blockIdx.x % 8 * (a.prefix_workers / 8) + blockIdx.x / 8, begin = worker * each;
+    const uint32_t worker = blockIdx.x % 8 * (a.prefix_workers / 8) + blockIdx.x / 8, begin = worker * each;
     if (begin >= all) return;
     uint32_t left = min(each, all - begin);
 
     const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x / 64), n = lane & 31, h2 = lane >> 5;
-    // A tile comes in C loads of 64 chunks, the first half of them keys; a wave makes kLoads (where they are more than there are, some twice).  Of
-    // load j this lane's is chunk `from` of token `token`.
-    uint32_t token[kLoads], from[kLoads], number[kLoads];
+    // Waves 0 and 1 load keys, 2 and 3 values, half of a tile each: load j brings 64 chunks, of which this lane's is at byte `from` of the row of `token`.
+    const uint32_t kind = wave / 2, half = wave & 1;
+    uint32_t token[kLoads];
+    uint64_t from[kLoads];
 #pragma unroll
     for (uint32_t j = 0; j < kLoads; ++j) {
-        number[j] = (wave * kLoads + j) % C;
-        const uint32_t i = number[j] % (C / 2) * 64 + lane;
+        const uint32_t i = (half * kLoads + j) * 64 + lane;
         token[j] = i / C;
-        from[j] = 8 * (i % C ^ L::turn(token[j]));
+        from[j] = 16 * (i % C ^ L::turn(token[j]));
     }
     // What this lane reads of a tile of keys: row n, chunk 2c + h2; of values: a group of 16 lanes reads 16 channels of 4 tokens and gets
     // a channel's 4 tokens each, so rows 4 * h2 + l16 / 4 (+ 8, 16, 24), 8 bytes of chunk 4c + vc.
     const uint32_t l16 = lane & 15, vrow = 4 * h2 + l16 / 4, vc = (lane >> 4 & 1) * 2 + (l16 & 3) / 2;
-    uint32_t key_at[kVariants], value_at[2][kVariants == 2 ? 1 : 2];
+    uint32_t key_at[kKeys], value_at[2][kValues];
 #pragma unroll
-    for (uint32_t v = 0; v < kVariants; ++v) key_at[v] = 16 * (L::row(n) + ((2 * v + h2) ^ L::turn(n)));
+    for (uint32_t v = 0; v < kKeys; ++v) key_at[v] = 16 * (n * C + ((2 * v + h2) ^ L::turn(n)));
 #pragma unroll
     for (uint32_t e = 0; e < 2; ++e)
 #pragma unroll
-        for (uint32_t v = 0; v < (kVariants == 2 ? 1 : 2); ++v) value_at[e][v] = 16 * (L::row(8 * e + vrow) + ((4 * v + vc) ^ L::turn(8 * e + vrow))) + 8 * (l16 & 1);
+        for (uint32_t v = 0; v < kValues; ++v) value_at[e][v] = 16 * ((8 * e + vrow) * C + ((4 * v + vc) ^ L::turn(8 * e + vrow))) + 8 * (l16 & 1);
 
     const float scale = fabsf(a.scale_log2);
     const uint32_t flip = a.scale_log2 < 0.f ? 0x80008000u : 0u;  // a negative scale is the queries' sign
+    const uint32_t blocks = (uint32_t)min(a.n_cache_blocks, (int64_t)INT32_MAX);
+    // From tile to tile a token's place moves on by 32 tokens: so many blocks and so many rows (here in elements), and another block where that leaves the block.
+    const uint32_t step_blocks = fast_div(32, a.by_N), row_step = (32 - step_blocks * (uint32_t)a.g.N) * (uint32_t)a.g.row_stride, row_end = (uint32_t)(a.g.N * a.g.row_stride);
+    bool bad = false;
     uint32_t g, u, t, tiles, rts;
     {
         const Item it = find_item(sums, a.n_prefix, begin / a.n_kv, work_of);
@@ -309,11 +316,13 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void k_prefix(AttendArgs a) 
         t = rel - u * tiles;
     }
     for (;;) {
-        const uint32_t h = u / rts, rt = u - h * rts, len = uniform(prefix_length(a, g)), first_tile = t, n_tiles = min(tiles - t, left);
+        const uint32_t h = u / rts, rt = u - h * rts, first_tile = t, n_tiles = min(tiles - t, left);
+        // tokens that the piece may see, from its first on
+        const uint32_t len = min(uniform(prefix_length(a, g)) - t * kTile, n_tiles * kTile);
         const Range seqs = group_of_prefix(a, g);
         const uint32_t rows = (uint32_t)(seqs.end - seqs.begin) * a.rows;
         const int32_t* table = a.prefix_table + (int64_t)g * a.max_prefix_blocks;
-        const uint16_t *keys = a.k_cache + h * a.g.page_stride, *values = a.v_cache + h * a.g.page_stride;
+        const uint16_t* pages = (kind ? a.v_cache : a.k_cache) + h * a.g.page_stride;
         const uint32_t in_tile = wave * 32 + n, rr = rt * kRows + in_tile;  // the lane's row, of the tile and of the group
 
         uint4v q[D / 16];
@@ -329,53 +338,79 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void k_prefix(AttendArgs a) 
 #pragma unroll
                 for (int e = 0; e < 16; ++e) o[c][e] = 0.f;
         }
-        const auto look_up = [&](uint32_t i) { const uint32_t k = (t + i) * kTile + n; return i < n_tiles && k < len ? table[fast_div(k, a.by_N)] : -1; };
-        // loads tile i, whose token n lies in `block`; -> which of its tokens exist
-        const auto load = [&](uint32_t i, int32_t block) {
-            const bool there = in_cache(a, block);
-            const int64_t at = there ? place(a, block, (t + i) * kTile + n) : -1;
+        // token n of a tile: its entry of the table, and its row's place in the block
+        struct Where {
+            int32_t block;
+            uint32_t row;
+        };
+        uint32_t entry = fast_div(t * kTile + n, a.by_N), row = (t * kTile + n - entry * (uint32_t)a.g.N) * (uint32_t)a.g.row_stride;
+        const auto look_up = [&](uint32_t i) {  // (tiles in order)
+            Where w{table[i * kTile + n < len ? entry : 0], row};
+            entry += step_blocks;
+            row += row_step;
+            const bool next = row >= row_end;
+            entry += next ? 1 : 0;
+            row -= next ? row_end : 0;
+            return w;
+        };
+        // loads tile i; -> which of its tokens exist
+        const auto load = [&](uint32_t i, uint32_t stage, const Where& w) {
+            const bool seen = i * kTile + n < len, there = seen && (uint32_t)w.block < blocks;
+            bad = bad || (seen && w.block >= 0 && !there);
+            const uint64_t at = reinterpret_cast<uint64_t>(there ? pages + ((int64_t)w.block * a.g.block_stride + w.row) : kZeroRow);
             const int lo = (int)at, hi = (int)(at >> 32);
 #pragma unroll
             for (uint32_t j = 0; j < kLoads; ++j) {
-                const int64_t row = (uint32_t)__shfl(lo, token[j]) | (int64_t)__shfl(hi, token[j]) << 32;
-                const bool is_value = number[j] >= C / 2;
-                const uint32_t first = number[j] % (C / 2) * 64;
-                const uint16_t* p = row < 0 ? kZeroRow : (is_value ? values : keys) + row;
-                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(p + from[j]),
-                                                 KVC_LDS(&tile[i % kStages][is_value][first + first / C / 4 * L::kPad]), 16, 0, 0);
+                const uint64_t p = ((uint32_t)__shfl(lo, token[j]) | (uint64_t)(uint32_t)__shfl(hi, token[j]) << 32) + from[j];
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p, KVC_LDS(&tile[stage][kind][(half * kLoads + j) * 64]), 16, 0, 0);
             }
             return (uint32_t)__ballot(there);
         };
-
-        // Tiles 0..2 on their way, and the blocks of tiles 3 and 4; mask[k]: the tokens of tile i + k that exist.  What comes back comes in order: the
-        // present tile and the block number of the one to be loaded next are there when only what the last two steps asked for is missing.
-        uint32_t mask[3];
-        int32_t next[2], block[3];
+        uint4v k[D / 16];
+        const auto read_keys = [&](uint32_t stage) {
+            const char* p = reinterpret_cast<const char*>(&tile[stage][0][0]);
 #pragma unroll
-        for (uint32_t i = 0; i < 3; ++i) block[i] = look_up(i);
+            for (uint32_t c = 0; c < D / 16; ++c) k[c] = *reinterpret_cast<const uint4v*>(p + key_at[c % kKeys] + 32 * (c - c % kKeys));
+        };
+        half8 v[2][D / 32];
+        const auto read_values = [&](uint32_t stage) {
+            const char* p = reinterpret_cast<const char*>(&tile[stage][1][0]);
+#pragma unroll
+            for (uint32_t j = 0; j < 2; ++j)
+#pragma unroll
+                for (uint32_t c = 0; c < D / 32; ++c) {
+                    short4v part[2];
+#pragma unroll
+                    for (uint32_t e = 0; e < 2; ++e)
+                        part[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                            (__attribute__((address_space(3))) short4v*)KVC_LDS(p + value_at[e][c % kValues] + 16 * (16 * j * C) + 64 * (c - c % kValues)));
+                    v[j][c] = __builtin_bit_cast(half8, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
+                }
+        };
+
+        // Tiles 0..2 on their way, and the blocks of tiles 3 and 4 (of tile i in next[i % 2 ^ 1]); mask[k]: the tokens of tile i + k that exist.  What comes back
+        // comes in order: the next tile and the block number of the one to be loaded next are there when only what the last step asked for is missing.
+        uint32_t mask[3];
+        Where first[3], next[2];
+#pragma unroll
+        for (uint32_t i = 0; i < 3; ++i) first[i] = look_up(i);
         next[0] = look_up(3);
         __syncthreads();  // (the tiles of the last piece have been read)
-        mask[0] = load(0, block[0]);
-        mask[1] = load(1, block[1]);
+#pragma unroll
+        for (uint32_t i = 0; i < 3; ++i) mask[i] = load(i, i, first[i]);
         next[1] = look_up(4);
-        mask[2] = load(2, block[2]);
-        for (uint32_t i = 0; i < n_tiles; ++i) {
-            // tile i is there, and every wave is done with tile i - 1, whose place tile i + 3 takes
-            wait_for_loads<2 * kLoads + 1>();
-            __syncthreads();
-            const uint32_t coming = load(i + 3, next[0]);
-            next[0] = next[1];
-            next[1] = look_up(i + 5);
+        wait_for_loads<2 * kLoads + 1>();
+        __syncthreads();
+        read_keys(0);
+        const auto step = [&](auto stage_, uint32_t i) {
+            constexpr uint32_t stage = decltype(stage_)::value;
             float16v s;
 #pragma unroll
             for (int e = 0; e < 16; ++e) s[e] = 0.f;
-            const char* kt = reinterpret_cast<const char*>(&tile[i % kStages][0][0]);
-            const char* vt = reinterpret_cast<const char*>(&tile[i % kStages][1][0]);
 #pragma unroll
-            for (uint32_t c = 0; c < D / 16; ++c) {
-                const uint4v k = *reinterpret_cast<const uint4v*>(kt + key_at[c % kVariants] + 32 * (c - c % kVariants));
-                s = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, k), __builtin_bit_cast(half8, q[c]), s, 0, 0, 0);
-            }
+            for (uint32_t c = 0; c < D / 16; ++c) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, k[c]), __builtin_bit_cast(half8, q[c]), s, 0, 0, 0);
+            read_values(stage);
+            __builtin_amdgcn_sched_barrier(0);
             if (mask[0] != ~0u) {
                 const uint32_t here = mask[0] >> (4 * h2);
 #pragma unroll
@@ -400,27 +435,30 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void k_prefix(AttendArgs a) 
                 l += w;
                 p[e / 8][e % 8] = (_Float16)w;
             }
+            // tile i + 1 is there, and every wave is done with tile i - 1, whose place tile i + 3 takes
+            wait_for_loads<kLoads + 1>();
+            __syncthreads();
+            read_keys((stage + 1) % kStages);  // (behind the last tile, what lies there; it is not used)
 #pragma unroll
-            for (uint32_t k = 0; k < 2; ++k)
+            for (uint32_t j = 0; j < 2; ++j)
 #pragma unroll
-                for (uint32_t c = 0; c < D / 32; ++c) {
-                    short4v part[2];
-#pragma unroll
-                    for (uint32_t e = 0; e < 2; ++e)
-                        part[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)KVC_LDS(
-                            vt + value_at[e][kVariants == 2 ? 0 : c % 2] + 16 * L::row(16 * k) + 64 * (kVariants == 2 ? c : c - c % 2)));
-                    const half8 v = __builtin_bit_cast(half8, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
-                    o[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p[k], o[c], 0, 0, 0);
-                }
+                for (uint32_t c = 0; c < D / 32; ++c) o[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[j][c], p[j], o[c], 0, 0, 0);
             mask[0] = mask[1];
             mask[1] = mask[2];
-            mask[2] = coming;
+            mask[2] = load(i + 3, (stage + 3) % kStages, next[stage % 2]);
+            next[stage % 2] = look_up(i + 5);
+        };
+        for (uint32_t i = 0; i < n_tiles; i += 4) {
+            step(Constant<0>(), i);
+            if (i + 1 < n_tiles) step(Constant<1>(), i + 1);
+            if (i + 2 < n_tiles) step(Constant<2>(), i + 2);
+            if (i + 3 < n_tiles) step(Constant<3>(), i + 3);
         }
         const bool whole = first_tile == 0 && n_tiles == tiles;
         const float sum = both32(l, true);
         if (rr < rows) {
-            const uint32_t sq = fast_div(rr, a.by_rows), row = rr - sq * a.rows;
-            const int64_t slot = whole ? a.prefix_whole + ((int64_t)(seqs.begin + sq) * a.n_kv + h) * a.rows + row
+            const uint32_t sq = fast_div(rr, a.by_rows);
+            const int64_t slot = whole ? a.prefix_whole + ((int64_t)(seqs.begin + sq) * a.n_kv + h) * a.rows + (rr - sq * a.rows)
                                        : a.prefix_slots + (int64_t)(2 * worker + (first_tile == 0 ? 1 : 0)) * kRows + in_tile;
             float* out = a.sums + slot * D + 4 * h2;
 #pragma unroll
@@ -441,6 +479,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void k_prefix(AttendArgs a) 
             rts = uniform(row_tiles(g));
         }
     }
+    if (bad) atomicOr(&a.st->status, KVC_ST_BAD_INDEX);
 }
 
 // ---- joining pieces: D / 8 threads to a row, 8 channels each.  A row's pieces are read kAtOnce at a time: each read goes to memory, and takes as
@@ -545,11 +584,11 @@ static hipError_t launch_own(const AttendArgs& a, hipStream_t s) {
 
 template <>
 hipError_t launch_attend<KVC_HEAD_DIM>(const AttendArgs& a, hipStream_t s) {
-    constexpr int D = KVC_HEAD_DIM, W = prefix_waves(D);
+    constexpr int D = KVC_HEAD_DIM;
     hipError_t e;
     if constexpr (D <= 192) e = a.own_rows == 32 ? launch_own<D, 2>(a, s) : launch_own<D, 1>(a, s);
     else e = launch_own<D, 1>(a, s);
-    if (e == hipSuccess && a.n_prefix) e = launch_kernel(k_prefix<D, W>, dim3(a.prefix_workers), dim3(64 * W), s, a);
+    if (e == hipSuccess && a.n_prefix) e = launch_kernel(k_prefix<D>, dim3(a.prefix_workers), dim3(64 * kPrefixWaves), s, a);
     constexpr uint32_t rows = 256 / (D / 8);
     if (e == hipSuccess) e = launch_kernel(k_join<D>, dim3((unsigned)(((int64_t)a.n_seq * a.n_kv * a.rows + rows - 1) / rows)), dim3(256), s, a);
     return e;

@@ -112,14 +112,14 @@ struct AttendPlan {
 };
 constexpr uint32_t kOwnWorkers = 2048, kPrefixWorkers = 256;  // waves, workgroups: what the GPU holds at once
 
-constexpr uint32_t prefix_waves(int d) { return d <= 192 ? 8 : 4; }  // of a workgroup
+constexpr uint32_t kPrefixWaves = 4;  // of a workgroup
 
 inline AttendPlan plan_attend(int64_t n_seq, int64_t n_q, int64_t n_heads, int64_t n_kv, int d, int64_t n_prefix) {
     AttendPlan p;
     p.own_rows = n_heads / n_kv * n_q <= 16 || d > 192 ? 16 : 32;  // (32 rows of wider heads do not fit into the registers)
-    p.prefix_rows = 32 * prefix_waves(d);
+    p.prefix_rows = 32 * kPrefixWaves;
     p.own_workers = kOwnWorkers;
-    p.prefix_workers = n_prefix ? kPrefixWorkers : 0;
+    p.prefix_workers = n_prefix ? (d <= 128 ? 2 : 1) * kPrefixWorkers : 0;
     p.rows = (uint64_t)(n_seq * n_heads * n_q);
     p.slots = p.rows + 2ull * p.own_workers * p.own_rows + (n_prefix ? p.rows + 2ull * p.prefix_workers * p.prefix_rows : 0);
     p.starts = round_256((uint64_t)(n_seq + 1) * 4) + round_256((uint64_t)(n_prefix + 1) * 4);
