@@ -119,7 +119,7 @@ __global__ __launch_bounds__(256, D * R <= 128 ? 2 : 1) void k_own(AttendArgs a)
     const auto tiles_of = [&](uint32_t s) { return (own_length(a, s) + kTile - 1) / kTile; };
     add_up(sums, a.n_seq, tiles_of);
     if (blockIdx.x == 0) write_starts(sums, a.own_start, a.n_seq, tiles_of);
-    const uint32_t units = a.n_kv * a.own_tiles, all = sums.all * units, each = share(all, a.own_workers);
+    const uint32_t units = a.n_kv * a.own_tiles, all = uniform(sums.all) * units, each = share(all, a.own_workers);
     const uint32_t worker = uniform(blockIdx.x * 4 + threadIdx.x / 64), begin = worker * each;
     if (begin >= all) return;
     const uint32_t end = min(begin + each, all);
@@ -232,7 +232,7 @@ __global__ __launch_bounds__(256, D * R <= 128 ? 2 : 1) void k_own(AttendArgs a)
 }
 
 // ---- prefixes.  A worker is a workgroup: 32 rows of a group a wave share tiles of 32 tokens in LDS, of which four are there: the present one, two on their way ...
-constexpr int kStages = 4;
+constexpr uint32_t kStages = 4, kAhead = 8;
 typedef float float16v __attribute__((ext_vector_type(16)));
 typedef short short4v __attribute__((ext_vector_type(4)));
 #define KVC_LDS(p) (__attribute__((address_space(3))) void*)(p)
@@ -245,6 +245,15 @@ struct Layout {
     static constexpr uint32_t C = D / 8, kMask = C % 16 == 0 ? 15 : C % 8 == 0 ? 7 : 3;
     __host__ __device__ static constexpr uint32_t turn(uint32_t t) { return C % 16 == 0 ? (t & 3) << 2 | (t >> 2 & 3) : C % 8 == 0 ? (t >> 1 & 1) << 2 | (t >> 2 & 3) : t >> 2 & 3; }
 };
+
+// A load from memory to LDS, BYTES for each lane: to `to`, the same in all lanes, + BYTES * lane.  (The compiler's own form of it makes reads of any tile wait for
+// the loads of all of them.  The caller waits: wait_for_loads, then a barrier.)
+template <int BYTES>
+__device__ inline void load_to_lds(uint64_t from, void* to) {
+    const uint32_t at = uniform((uint32_t)reinterpret_cast<uintptr_t>(KVC_LDS(to)));
+    if constexpr (BYTES == 16) asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(at) : "memory");
+    else asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(at) : "memory");
+}
 
 // Waits until at most N of the wave's loads are on their way.
 template <uint32_t N>
@@ -263,6 +272,7 @@ __global__ __launch_bounds__(64 * kPrefixWaves, D <= 128 ? 2 : 1) void k_prefix(
     constexpr uint32_t C = L::C, kLoads = C / kPrefixWaves, kRows = 32 * kPrefixWaves, kKeys = (L::kMask + 1) / 2, kValues = (L::kMask + 1) / 4;
     __shared__ Sums sums;
     __shared__ __align__(16) uint4v tile[kStages][2][32 * C];  // [stage][keys, values]
+    __shared__ uint32_t ids[kPrefixWaves][kAhead][64];  // [wave][tile]: block of token n
     const auto row_tiles = [&](uint32_t g) {
         const Range r = group_of_prefix(a, g);
         return ((uint32_t)(r.end - r.begin) * a.rows + kRows - 1) / kRows;
@@ -271,7 +281,7 @@ __global__ __launch_bounds__(64 * kPrefixWaves, D <= 128 ? 2 : 1) void k_prefix(
     const auto work_of = [&](uint32_t g) { return row_tiles(g) * tiles_of(g); };
     add_up(sums, a.n_prefix, work_of);
     if (blockIdx.x == 0) write_starts(sums, a.prefix_start, a.n_prefix, work_of);
-    const uint32_t all = sums.all * a.n_kv, each = share(all, a.prefix_workers);
+    const uint32_t all = uniform(sums.all) * a.n_kv, each = share(all, a.prefix_workers);
     // workgroups go to the XCDs in turn: an XCD's take neighbouring shares, which read the same tokens
     const uint32_t worker = blockIdx.x % 8 * (a.prefix_workers / 8) + blockIdx.x / 8, begin = worker * each;
     if (begin >= all) return;
@@ -280,20 +290,24 @@ __global__ __launch_bounds__(64 * kPrefixWaves, D <= 128 ? 2 : 1) void k_prefix(
     const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x / 64), n = lane & 31, h2 = lane >> 5;
     // Waves 0 and 1 load keys, 2 and 3 values, half of a tile each: load j brings 64 chunks, of which this lane's is at byte `from` of the row of `token`.
     const uint32_t kind = wave / 2, half = wave & 1;
-    uint32_t token[kLoads];
-    uint64_t from[kLoads];
+    // (Where 64 chunks are whole rows, and where a row's length is a power of two, a lane's numbers differ by constants only.)
+    constexpr bool kRegular = 64 % C == 0, kSquare = C % 16 == 0;
+    uint32_t token_of[kRegular ? 1 : kLoads], from_of[kRegular ? 1 : kLoads];
 #pragma unroll
-    for (uint32_t j = 0; j < kLoads; ++j) {
+    for (uint32_t j = 0; j < (kRegular ? 1 : kLoads); ++j) {
         const uint32_t i = (half * kLoads + j) * 64 + lane;
-        token[j] = i / C;
-        from[j] = 16 * (i % C ^ L::turn(token[j]));
+        token_of[j] = i / C;
+        from_of[j] = 16 * (i % C ^ L::turn(token_of[j]));
     }
+    const auto token = [&](uint32_t j) { return kRegular ? token_of[0] + j * (64 / C) : token_of[j]; };
+    const auto from = [&](uint32_t j) { return kRegular ? from_of[0] ^ 16 * L::turn(j * (64 / C)) : from_of[j]; };
     // What this lane reads of a tile of keys: row n, chunk 2c + h2; of values: a group of 16 lanes reads 16 channels of 4 tokens and gets
     // a channel's 4 tokens each, so rows 4 * h2 + l16 / 4 (+ 8, 16, 24), 8 bytes of chunk 4c + vc.
     const uint32_t l16 = lane & 15, vrow = 4 * h2 + l16 / 4, vc = (lane >> 4 & 1) * 2 + (l16 & 3) / 2;
-    uint32_t key_at[kKeys], value_at[2][kValues];
+    uint32_t keys_at[kSquare ? 1 : kKeys], value_at[2][kValues];
 #pragma unroll
-    for (uint32_t v = 0; v < kKeys; ++v) key_at[v] = 16 * (n * C + ((2 * v + h2) ^ L::turn(n)));
+    for (uint32_t v = 0; v < (kSquare ? 1 : kKeys); ++v) keys_at[v] = 16 * (n * C + ((2 * v + h2) ^ L::turn(n)));
+    const auto key_at = [&](uint32_t c) { return (kSquare ? keys_at[0] ^ 32 * (c % kKeys) : keys_at[c % kKeys]) + 32 * (c - c % kKeys); };
 #pragma unroll
     for (uint32_t e = 0; e < 2; ++e)
 #pragma unroll
@@ -302,8 +316,10 @@ __global__ __launch_bounds__(64 * kPrefixWaves, D <= 128 ? 2 : 1) void k_prefix(
     const float scale = fabsf(a.scale_log2);
     const uint32_t flip = a.scale_log2 < 0.f ? 0x80008000u : 0u;  // a negative scale is the queries' sign
     const uint32_t blocks = (uint32_t)min(a.n_cache_blocks, (int64_t)INT32_MAX);
-    // From tile to tile a token's place moves on by 32 tokens: so many blocks and so many rows (here in elements), and another block where that leaves the block.
-    const uint32_t step_blocks = fast_div(32, a.by_N), row_step = (32 - step_blocks * (uint32_t)a.g.N) * (uint32_t)a.g.row_stride, row_end = (uint32_t)(a.g.N * a.g.row_stride);
+    // From tile to tile a token's place moves on by 32 tokens: so many blocks and so many rows, and another block where that leaves the block.
+    // (Strides are multiples of 8 elements, and counted in these.)
+    const uint32_t row_stride = (uint32_t)(a.g.row_stride / 8), block_stride = (uint32_t)(a.g.block_stride / 8);
+    const uint32_t step_blocks = fast_div(kTile, a.by_N), row_step = (kTile - step_blocks * (uint32_t)a.g.N) * row_stride, row_end = (uint32_t)a.g.N * row_stride;
     bool bad = false;
     uint32_t g, u, t, tiles, rts;
     {
@@ -338,95 +354,103 @@ __global__ __launch_bounds__(64 * kPrefixWaves, D <= 128 ? 2 : 1) void k_prefix(
 #pragma unroll
                 for (int e = 0; e < 16; ++e) o[c][e] = 0.f;
         }
-        // token n of a tile: its entry of the table, and its row's place in the block
-        struct Where {
-            int32_t block;
-            uint32_t row;
+        // token n of a tile: its entry of the table, and its row's place in the block; both for tiles in order
+        uint32_t entry = fast_div(t * kTile + n, a.by_N), row = (t * kTile + n - entry * (uint32_t)a.g.N) * row_stride, row_now = row;
+        const auto next_row = [&](uint32_t& r) {
+            r += row_step;
+            const bool next = r >= row_end;
+            r -= next ? row_end : 0;
+            return next;
         };
-        uint32_t entry = fast_div(t * kTile + n, a.by_N), row = (t * kTile + n - entry * (uint32_t)a.g.N) * (uint32_t)a.g.row_stride;
-        const auto look_up = [&](uint32_t i) {  // (tiles in order)
-            Where w{table[i * kTile + n < len ? entry : 0], row};
-            entry += step_blocks;
-            row += row_step;
-            const bool next = row >= row_end;
-            entry += next ? 1 : 0;
-            row -= next ? row_end : 0;
-            return w;
+        const auto look_up = [&](uint32_t i) {
+            load_to_lds<4>(reinterpret_cast<uint64_t>(table) + 4ull * (i * kTile + n < len ? entry : 0), &ids[wave][i % kAhead][0]);
+            entry += step_blocks + (next_row(row) ? 1 : 0);
         };
         // loads tile i; -> which of its tokens exist
-        const auto load = [&](uint32_t i, uint32_t stage, const Where& w) {
-            const bool seen = i * kTile + n < len, there = seen && (uint32_t)w.block < blocks;
-            bad = bad || (seen && w.block >= 0 && !there);
-            const uint64_t at = reinterpret_cast<uint64_t>(there ? pages + ((int64_t)w.block * a.g.block_stride + w.row) : kZeroRow);
-            const int lo = (int)at, hi = (int)(at >> 32);
+        const auto load = [&](uint32_t i, uint32_t stage) {
+            const uint32_t block = ids[wave][i % kAhead][lane];
+            const bool seen = i * kTile + n < len, there = seen && block < blocks;
+            bad = bad || (seen && (int32_t)block >= 0 && !there);
+            const uint64_t at = ((uint64_t)block * block_stride + row_now) * 16 + reinterpret_cast<uint64_t>(pages), zero = reinterpret_cast<uint64_t>(kZeroRow);
+            next_row(row_now);
+            const int lo = there ? (int)at : (int)zero, hi = there ? (int)(at >> 32) : (int)(zero >> 32);
 #pragma unroll
-            for (uint32_t j = 0; j < kLoads; ++j) {
-                const uint64_t p = ((uint32_t)__shfl(lo, token[j]) | (uint64_t)(uint32_t)__shfl(hi, token[j]) << 32) + from[j];
-                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p, KVC_LDS(&tile[stage][kind][(half * kLoads + j) * 64]), 16, 0, 0);
-            }
+            for (uint32_t j = 0; j < kLoads; ++j)
+                load_to_lds<16>(((uint32_t)__shfl(lo, token(j)) | (uint64_t)(uint32_t)__shfl(hi, token(j)) << 32) + from(j), &tile[stage][kind][(half * kLoads + j) * 64]);
             return (uint32_t)__ballot(there);
         };
-        uint4v k[D / 16];
-        const auto read_keys = [&](uint32_t stage) {
+        // scores of a tile, in powers of two but for `scale`
+        const auto make_scores = [&](float16v& x, uint32_t stage) {
             const char* p = reinterpret_cast<const char*>(&tile[stage][0][0]);
 #pragma unroll
-            for (uint32_t c = 0; c < D / 16; ++c) k[c] = *reinterpret_cast<const uint4v*>(p + key_at[c % kKeys] + 32 * (c - c % kKeys));
-        };
-        half8 v[2][D / 32];
-        const auto read_values = [&](uint32_t stage) {
-            const char* p = reinterpret_cast<const char*>(&tile[stage][1][0]);
+            for (int e = 0; e < 16; ++e) x[e] = 0.f;
 #pragma unroll
-            for (uint32_t j = 0; j < 2; ++j)
+            for (uint32_t c = 0; c < D / 16; ++c) {
+                const uint4v k = *reinterpret_cast<const uint4v*>(p + key_at(c));
+                x = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, k), __builtin_bit_cast(half8, q[c]), x, 0, 0, 0);
+            }
+        };
+        const auto hide = [&](float16v& x, uint32_t there) {  // scores of tokens that do not exist
+            const uint32_t here = there >> (4 * h2);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[e] = here >> (8 * (e / 4) + e % 4) & 1 ? x[e] : -INFINITY;
+        };
+        const auto largest = [&](const float16v& x) {
+            float top = fmaxf(x[0], x[1]);
+#pragma unroll
+            for (int e = 2; e < 16; ++e) top = fmaxf(top, x[e]);
+            return both32(top, false) * scale;
+        };
+        const auto follow = [&](float top) {
+            if (!__any(top > m + kLag)) return;
+            const float to = fmaxf(m, top), f = m == -INFINITY ? 0.f : power2(m - to);
+            m = to;
+            l *= f;
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c) o[c] *= f;
+        };
+
+        // Tiles 0..2 on their way, and the blocks of tiles 3 and 4; mask[k]: the tokens of tile i + 1 + k that exist.  What comes back comes in order: the next
+        // tile and the blocks of the one to be loaded next are there when only what the last step asked for is missing.
+        uint32_t mask[2];
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) look_up(i);
+        wait_for_loads<0>();
+        __syncthreads();  // (and the tiles of the last piece have been read)
+        float16v s;
+        {
+            const uint32_t there = load(0, 0);
+            mask[0] = load(1, 1);
+            mask[1] = load(2, 2);
+            look_up(4);
+            wait_for_loads<2 * kLoads + 1>();
+            __syncthreads();
+            make_scores(s, 0);
+            if (there != ~0u) hide(s, there);
+            follow(largest(s));
+        }
+        const auto step = [&](auto stage_, uint32_t i) {
+            constexpr uint32_t stage = decltype(stage_)::value;
+            // tile i + 1 is there, and every wave is done with tile i - 1, whose place tile i + 3 takes
+            wait_for_loads<kLoads + 1>();
+            __syncthreads();
+            // the next tile's scores, while this one's become weights
+            float16v next;
+            make_scores(next, (stage + 1) % kStages);  // (behind the last tile, of what lies there; it is not used)
+            half8 v[2][D / 32];
+            const auto read_values = [&](uint32_t j) {
+                const char* values = reinterpret_cast<const char*>(&tile[stage][1][0]);
 #pragma unroll
                 for (uint32_t c = 0; c < D / 32; ++c) {
                     short4v part[2];
 #pragma unroll
                     for (uint32_t e = 0; e < 2; ++e)
                         part[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                            (__attribute__((address_space(3))) short4v*)KVC_LDS(p + value_at[e][c % kValues] + 16 * (16 * j * C) + 64 * (c - c % kValues)));
+                            (__attribute__((address_space(3))) short4v*)KVC_LDS(values + value_at[e][c % kValues] + 16 * (16 * j * C) + 64 * (c - c % kValues)));
                     v[j][c] = __builtin_bit_cast(half8, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
                 }
-        };
-
-        // Tiles 0..2 on their way, and the blocks of tiles 3 and 4 (of tile i in next[i % 2 ^ 1]); mask[k]: the tokens of tile i + k that exist.  What comes back
-        // comes in order: the next tile and the block number of the one to be loaded next are there when only what the last step asked for is missing.
-        uint32_t mask[3];
-        Where first[3], next[2];
-#pragma unroll
-        for (uint32_t i = 0; i < 3; ++i) first[i] = look_up(i);
-        next[0] = look_up(3);
-        __syncthreads();  // (the tiles of the last piece have been read)
-#pragma unroll
-        for (uint32_t i = 0; i < 3; ++i) mask[i] = load(i, i, first[i]);
-        next[1] = look_up(4);
-        wait_for_loads<2 * kLoads + 1>();
-        __syncthreads();
-        read_keys(0);
-        const auto step = [&](auto stage_, uint32_t i) {
-            constexpr uint32_t stage = decltype(stage_)::value;
-            float16v s;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) s[e] = 0.f;
-#pragma unroll
-            for (uint32_t c = 0; c < D / 16; ++c) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, k[c]), __builtin_bit_cast(half8, q[c]), s, 0, 0, 0);
-            read_values(stage);
-            __builtin_amdgcn_sched_barrier(0);
-            if (mask[0] != ~0u) {
-                const uint32_t here = mask[0] >> (4 * h2);
-#pragma unroll
-                for (int e = 0; e < 16; ++e) s[e] = here >> (8 * (e / 4) + e % 4) & 1 ? s[e] : -INFINITY;
-            }
-            float top = fmaxf(s[0], s[1]);
-#pragma unroll
-            for (int e = 2; e < 16; ++e) top = fmaxf(top, s[e]);
-            top = both32(top, false) * scale;
-            if (__any(top > m + kLag)) {
-                const float to = fmaxf(m, top), f = m == -INFINITY ? 0.f : power2(m - to);
-                m = to;
-                l *= f;
-#pragma unroll
-                for (int c = 0; c < D / 32; ++c) o[c] *= f;
-            }
+            };
+            read_values(0);
             half8 p[2];
             const float low = kLift - (m == -INFINITY ? 0.f : m);
 #pragma unroll
@@ -435,18 +459,20 @@ __global__ __launch_bounds__(64 * kPrefixWaves, D <= 128 ? 2 : 1) void k_prefix(
                 l += w;
                 p[e / 8][e % 8] = (_Float16)w;
             }
-            // tile i + 1 is there, and every wave is done with tile i - 1, whose place tile i + 3 takes
-            wait_for_loads<kLoads + 1>();
-            __syncthreads();
-            read_keys((stage + 1) % kStages);  // (behind the last tile, what lies there; it is not used)
+            asm volatile("" : "+v"(p[0]), "+v"(p[1]), "+v"(l));  // (here, not behind the branches below, where the compiler would put them)
+            __builtin_amdgcn_sched_barrier(0);
+            if (mask[0] != ~0u) hide(next, mask[0]);
+            mask[0] = mask[1];
+            read_values(1);
 #pragma unroll
             for (uint32_t j = 0; j < 2; ++j)
 #pragma unroll
                 for (uint32_t c = 0; c < D / 32; ++c) o[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[j][c], p[j], o[c], 0, 0, 0);
-            mask[0] = mask[1];
-            mask[1] = mask[2];
-            mask[2] = load(i + 3, (stage + 3) % kStages, next[stage % 2]);
-            next[stage % 2] = look_up(i + 5);
+            const float top = largest(next);
+            mask[1] = load(i + 3, (stage + 3) % kStages);
+            look_up(i + 5);
+            if (i + 1 < n_tiles) follow(top);
+            s = next;
         };
         for (uint32_t i = 0; i < n_tiles; i += 4) {
             step(Constant<0>(), i);
@@ -454,6 +480,7 @@ __global__ __launch_bounds__(64 * kPrefixWaves, D <= 128 ? 2 : 1) void k_prefix(
             if (i + 2 < n_tiles) step(Constant<2>(), i + 2);
             if (i + 3 < n_tiles) step(Constant<3>(), i + 3);
         }
+        wait_for_loads<0>();  // (nothing may be on its way to this LDS when another workgroup has it)
         const bool whole = first_tile == 0 && n_tiles == tiles;
         const float sum = both32(l, true);
         if (rr < rows) {

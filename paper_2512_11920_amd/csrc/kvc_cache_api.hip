@@ -70,7 +70,7 @@ int kvc_attend(kvc_ctx* ctx, const kvc_attend_t* p, void* stream) {
     // rows are counted in 31 bits, and so are a row's tokens and the tiles of all units
     if ((int64_t)p->n_seq * p->n_heads > (int64_t)INT32_MAX / p->n_q) return KVC_ERR_ARG;
     const int64_t own_tokens = (int64_t)p->max_blocks * ctx->g.N, prefix_tokens = (int64_t)p->max_prefix_blocks * ctx->g.N;
-    if (own_tokens > INT32_MAX - 256 || prefix_tokens > INT32_MAX - 256) return KVC_ERR_ARG;
+    if (own_tokens > INT32_MAX - 256 || prefix_tokens > INT32_MAX - 256 || ctx->g.block_stride / 8 > UINT32_MAX) return KVC_ERR_ARG;
     const AttendPlan plan = plan_attend(p->n_seq, p->n_q, p->n_heads, p->n_kv_heads, ctx->g.d, p->n_prefix);
     const int64_t rows = (int64_t)(p->n_heads / p->n_kv_heads) * p->n_q, own_tiles = (rows + plan.own_rows - 1) / plan.own_rows;
     const int64_t prefix_tiles = (rows * p->n_seq + plan.prefix_rows - 1) / plan.prefix_rows + p->n_prefix;
