@@ -113,16 +113,15 @@ struct Place {
     uint32_t s, u, t, tiles, len;  // sequence; unit u of it (head and row tile); tile t of `tiles`
 };
 
+// The part of wave `worker`; called by all waves of a workgroup.
 template <int D, int R, bool EIGHT>
-__global__ __launch_bounds__(256, D * R <= 128 ? 2 : 1) void k_own(AttendArgs a) {
-    __shared__ Sums sums;
+__device__ inline void own_part(const AttendArgs& a, Sums& sums, uint32_t worker) {
     const auto tiles_of = [&](uint32_t s) { return (own_length(a, s) + kTile - 1) / kTile; };
     add_up(sums, a.n_seq, tiles_of);
-    if (blockIdx.x == 0) write_starts(sums, a.own_start, a.n_seq, tiles_of);
+    if (worker < 4) write_starts(sums, a.own_start, a.n_seq, tiles_of);
     const uint32_t units = a.n_kv * a.own_tiles, all = uniform(sums.all) * units, each = share(all, a.own_workers);
-    const uint32_t worker = uniform(blockIdx.x * 4 + threadIdx.x / 64), begin = worker * each;
-    if (begin >= all) return;
-    const uint32_t end = min(begin + each, all);
+    const uint32_t begin = worker * each, end = min(begin + each, all);
+    if (begin >= end) return;
 
     Place c;
     {
@@ -266,13 +265,20 @@ struct Constant {
     static constexpr uint32_t value = N;
 };
 
+// What prefix_part has in LDS.
 template <int D>
-__global__ __launch_bounds__(64 * kPrefixWaves, D <= 128 ? 2 : 1) void k_prefix(AttendArgs a) {
+struct PrefixTiles {
+    uint4v tile[kStages][2][32 * Layout<D>::C];   // [stage][keys, values]
+    uint32_t ids[kPrefixWaves][kAhead][64];       // [wave][tile]: block of token n
+};
+
+// The part of workgroup `worker`.
+template <int D>
+__device__ inline void prefix_part(const AttendArgs& a, Sums& sums, PrefixTiles<D>& lds, uint32_t worker) {
     using L = Layout<D>;
+    auto& tile = lds.tile;
+    auto& ids = lds.ids;
     constexpr uint32_t C = L::C, kLoads = C / kPrefixWaves, kRows = 32 * kPrefixWaves, kKeys = (L::kMask + 1) / 2, kValues = (L::kMask + 1) / 4;
-    __shared__ Sums sums;
-    __shared__ __align__(16) uint4v tile[kStages][2][32 * C];  // [stage][keys, values]
-    __shared__ uint32_t ids[kPrefixWaves][kAhead][64];  // [wave][tile]: block of token n
     const auto row_tiles = [&](uint32_t g) {
         const Range r = group_of_prefix(a, g);
         return ((uint32_t)(r.end - r.begin) * a.rows + kRows - 1) / kRows;
@@ -280,10 +286,9 @@ __global__ __launch_bounds__(64 * kPrefixWaves, D <= 128 ? 2 : 1) void k_prefix(
     const auto tiles_of = [&](uint32_t g) { return (prefix_length(a, g) + kTile - 1) / kTile; };
     const auto work_of = [&](uint32_t g) { return row_tiles(g) * tiles_of(g); };
     add_up(sums, a.n_prefix, work_of);
-    if (blockIdx.x == 0) write_starts(sums, a.prefix_start, a.n_prefix, work_of);
+    if (worker == 0) write_starts(sums, a.prefix_start, a.n_prefix, work_of);
     const uint32_t all = uniform(sums.all) * a.n_kv, each = share(all, a.prefix_workers);
-    // workgroups go to the XCDs in turn: an XCD's take neighbouring shares, which read the same tokens
-    const uint32_t worker = blockIdx.x % 8 * (a.prefix_workers / 8) + blockIdx.x / 8, begin = worker * each;
+    const uint32_t begin = worker * each;
     if (begin >= all) return;
     uint32_t left = min(each, all - begin);
 
@@ -460,6 +465,16 @@ __global__ __launch_bounds__(64 * kPrefixWaves, D <= 128 ? 2 : 1) void k_prefix(
                 p[e / 8][e % 8] = (_Float16)w;
             }
             asm volatile("" : "+v"(p[0]), "+v"(p[1]), "+v"(l));  // (here, not behind the branches below, where the compiler would put them)
+            // products with reads a few ahead of them and vector instructions between them (reads further ahead would not leave 256 registers enough)
+            constexpr int kProduct = 0x8, kRead = 0x100, kTrans = 0x400, kVector = 0x2;
+            __builtin_amdgcn_sched_group_barrier(kRead, 3, 0);
+#pragma unroll
+            for (uint32_t c = 0; c < D / 16; ++c) {
+                __builtin_amdgcn_sched_group_barrier(kProduct, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(kRead, 2, 0);
+                __builtin_amdgcn_sched_group_barrier(kTrans, 256 / D, 0);
+                __builtin_amdgcn_sched_group_barrier(kVector, 640 / D, 0);
+            }
             __builtin_amdgcn_sched_barrier(0);
             if (mask[0] != ~0u) hide(next, mask[0]);
             mask[0] = mask[1];
@@ -507,6 +522,40 @@ __global__ __launch_bounds__(64 * kPrefixWaves, D <= 128 ? 2 : 1) void k_prefix(
         }
     }
     if (bad) atomicOr(&a.st->status, KVC_ST_BAD_INDEX);
+}
+
+template <int D, int R, bool EIGHT>
+__global__ __launch_bounds__(256, D * R <= 128 ? 2 : 1) void k_own(AttendArgs a) {
+    __shared__ Sums sums;
+    own_part<D, R, EIGHT>(a, sums, uniform(blockIdx.x * 4 + threadIdx.x / 64));
+}
+
+// Workgroups go to the XCDs in turn: an XCD's take neighbouring parts of a prefix's work, which read the same tokens.
+__device__ inline uint32_t neighbour(uint32_t i, uint32_t n) { return i % 8 * (n / 8) + i / 8; }
+
+template <int D>
+__global__ __launch_bounds__(64 * kPrefixWaves, D <= 128 ? 2 : 1) void k_prefix(AttendArgs a) {
+    __shared__ Sums sums;
+    __shared__ PrefixTiles<D> lds;
+    prefix_part<D>(a, sums, lds, neighbour(blockIdx.x, a.prefix_workers));
+}
+
+// Both in one launch, two workgroups on each compute unit: the first half of them begins with prefixes, which keep the matrix units busy, the other with
+// the sequences' own tokens, which keep the memory busy; then they change.  Where there is little to do for prefixes (a.apart) each half does its own alone.
+template <int D, int R, bool EIGHT>
+__global__ __launch_bounds__(256, 2) void k_both(AttendArgs a) {
+    __shared__ Sums sums;
+    __shared__ PrefixTiles<D> lds;
+    const uint32_t half = gridDim.x / 2, i = blockIdx.x;
+#pragma nounroll
+    for (uint32_t turn = 0; turn < 2; ++turn) {
+        if (turn == (i < half ? 0 : 1)) {
+            if (!a.apart || i < half) prefix_part<D>(a, sums, lds, i < half ? neighbour(i, half) : half + neighbour(i - half, half));
+        } else if (!a.apart || i >= half) {
+            own_part<D, R, EIGHT>(a, sums, uniform((a.apart ? i - half : i) * 4 + threadIdx.x / 64));
+        }
+        __syncthreads();  // (the sums are used again)
+    }
 }
 
 // ---- joining pieces: D / 8 threads to a row, 8 channels each.  A row's pieces are read kAtOnce at a time: each read goes to memory, and takes as
@@ -604,18 +653,20 @@ __global__ __launch_bounds__(256) void k_join(AttendArgs a) {
 }
 
 template <int D, int R>
-static hipError_t launch_own(const AttendArgs& a, hipStream_t s) {
-    const dim3 grid(a.own_workers / 4);
-    return a.g.N % 8 == 0 ? launch_kernel(k_own<D, R, true>, grid, dim3(256), s, a) : launch_kernel(k_own<D, R, false>, grid, dim3(256), s, a);
+static hipError_t launch_parts(const AttendArgs& a, hipStream_t s) {
+    const bool eight = a.g.N % 8 == 0;
+    if constexpr (both_fit(D, R))
+        if (a.n_prefix) return launch_kernel(eight ? k_both<D, R, true> : k_both<D, R, false>, dim3(2 * kPrefixWorkers), dim3(256), s, a);
+    const hipError_t e = launch_kernel(eight ? k_own<D, R, true> : k_own<D, R, false>, dim3(a.own_workers / 4), dim3(256), s, a);
+    return e == hipSuccess && a.n_prefix ? launch_kernel(k_prefix<D>, dim3(a.prefix_workers), dim3(64 * kPrefixWaves), s, a) : e;
 }
 
 template <>
 hipError_t launch_attend<KVC_HEAD_DIM>(const AttendArgs& a, hipStream_t s) {
     constexpr int D = KVC_HEAD_DIM;
     hipError_t e;
-    if constexpr (D <= 192) e = a.own_rows == 32 ? launch_own<D, 2>(a, s) : launch_own<D, 1>(a, s);
-    else e = launch_own<D, 1>(a, s);
-    if (e == hipSuccess && a.n_prefix) e = launch_kernel(k_prefix<D>, dim3(a.prefix_workers), dim3(64 * kPrefixWaves), s, a);
+    if constexpr (D <= 192) e = a.own_rows == 32 ? launch_parts<D, 2>(a, s) : launch_parts<D, 1>(a, s);
+    else e = launch_parts<D, 1>(a, s);
     constexpr uint32_t rows = 256 / (D / 8);
     if (e == hipSuccess) e = launch_kernel(k_join<D>, dim3((unsigned)(((int64_t)a.n_seq * a.n_kv * a.rows + rows - 1) / rows)), dim3(256), s, a);
     return e;

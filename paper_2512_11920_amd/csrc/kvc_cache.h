@@ -95,6 +95,7 @@ struct AttendArgs {
     // the workspace, see AttendPlan
     uint32_t own_tiles;  // row tiles of one sequence and KV head
     uint32_t own_workers, prefix_workers, own_rows, prefix_rows;
+    bool apart;  // both parts in one launch, by workgroups of their own
     uint32_t* own_start;     // [n_seq + 1]
     uint32_t* prefix_start;  // [n_prefix + 1]
     float* sums;             // [slots][d]
@@ -110,9 +111,13 @@ struct AttendPlan {
     uint64_t rows, slots, starts;    // query rows; slots; bytes of the sums of tiles
     uint64_t bytes;
 };
-constexpr uint32_t kOwnWorkers = 2048, kPrefixWorkers = 256;  // waves, workgroups: what the GPU holds at once
+constexpr uint32_t kOwnWorkers = 2048, kPrefixWorkers = 256;  // waves, workgroups: with 2 of either, or 2 and 1, what the GPU holds at once
+constexpr uint32_t kPrefixWaves = 4;                          // of a workgroup
 
-constexpr uint32_t kPrefixWaves = 4;  // of a workgroup
+constexpr int64_t kApartTiles = 8192;
+
+// Whether the kernel that does both parts keeps two workgroups of its own on a compute unit (256 registers).
+constexpr bool both_fit(int d, int row_tiles) { return d * row_tiles <= 128; }
 
 inline AttendPlan plan_attend(int64_t n_seq, int64_t n_q, int64_t n_heads, int64_t n_kv, int d, int64_t n_prefix) {
     AttendPlan p;

@@ -109,6 +109,12 @@ int kvc_attend(kvc_ctx* ctx, const kvc_attend_t* p, void* stream) {
     a.own_tiles = (uint32_t)own_tiles;
     a.own_workers = plan.own_workers;
     a.prefix_workers = plan.prefix_workers;
+    // (tables may be longer than the prefixes in them)
+    a.apart = p->n_prefix && both_fit(ctx->g.d, plan.own_rows / 16) && product(prefix_tiles, p->n_kv_heads, prefix_tokens / 32 + 1) <= kApartTiles;
+    if (a.apart) {
+        a.own_workers = kOwnWorkers / 2;
+        a.prefix_workers = kPrefixWorkers;
+    }
     uint8_t* w = static_cast<uint8_t*>(p->d_work);
     a.own_start = reinterpret_cast<uint32_t*>(w);
     a.prefix_start = reinterpret_cast<uint32_t*>(w + round_256((uint64_t)(p->n_seq + 1) * 4));
