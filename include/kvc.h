@@ -346,7 +346,7 @@ int kvc_free_blocks(kvc_ctx* ctx, const int32_t* d_ids, int32_t n, int32_t n_lay
  * KVC_ST_POOL_FULL.  Pointers 16-byte aligned (d_used_out 8, d_work 256); the new buffers must not overlap the bound ones. */
 int kvc_compact_pool(kvc_ctx* ctx, void* d_pool_out, uint64_t pool_out_bytes, kvc_desc* d_desc_out, uint64_t* d_used_out, void* d_work,
                      uint64_t work_bytes, void* stream);
-/* Workspace of kvc_compact_pool on a bound pool of pool_bytes, in bytes: about a ninetieth of it. */
+/* Workspace of kvc_compact_pool on a bound pool of pool_bytes, in bytes: about a hundredth of it, and 10 KB. */
 uint64_t kvc_compact_workspace(uint64_t pool_bytes);
 
 /* kvc_bind_pool on buffers that kvc_compact_pool has filled: the cursor goes to *d_used (device memory, read on the

@@ -53,8 +53,9 @@ struct IdsArgs {  // fork and free
 };
 
 // Compaction works on a bitmap of the pool's 16-byte units: a set bit is a unit that a live payload holds.  A unit's new place is its
-// rank, the number of set bits before it.  A tile is 64 words of the bitmap, 4,096 units, 64 KB of pool.
-constexpr uint64_t kTileWords = 64, kTileUnits = kTileWords * 64;
+// rank, the number of set bits before it.  A group is 1,024 words of the bitmap, 65,536 units, 1 MB of pool.
+constexpr uint64_t kGroupWords = 1024;
+constexpr uint32_t kSmallWords = 256, kSmallPages = 4096;  // a pool that one workgroup compacts: 256 KB
 
 struct CompactArgs {
     const uint8_t* pool;
@@ -62,15 +63,15 @@ struct CompactArgs {
     uint8_t* pool_out;
     const kvc_desc* desc;
     kvc_desc* desc_out;
-    uint64_t n_desc, tiles;
-    unsigned long long* bits;  // [tiles * kTileWords]
-    uint16_t* before;          // [tiles * kTileWords]: set bits of the tile before the word
-    unsigned long long* base;  // [tiles]: set bits of a tile, then of all tiles before it
+    uint64_t n_desc, groups;
+    unsigned long long* bits;  // [groups * kGroupWords]
+    uint16_t* before;          // [groups * kGroupWords]: set bits of the group before the word
+    unsigned long long* base;  // [groups]: set bits of a group, then of all groups before it
     unsigned long long* used;  // out: bytes
     DevState* st;
 };
 
-inline uint64_t compact_tiles(uint64_t pool_bytes) { return (pool_bytes / 16 + kTileUnits - 1) / kTileUnits; }
+inline uint64_t compact_groups(uint64_t pool_bytes) { return (pool_bytes / 16 + 64 * kGroupWords - 1) / (64 * kGroupWords); }
 inline uint64_t round_256(uint64_t n) { return (n + 255) / 256 * 256; }
 
 struct AttendArgs {

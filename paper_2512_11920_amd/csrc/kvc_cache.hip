@@ -90,7 +90,7 @@ __global__ __launch_bounds__(256) void k_ids(IdsArgs a) {
 
 // ---- compaction.
 __global__ __launch_bounds__(256) void k_bits_zero(CompactArgs a) {
-    const uint64_t n = a.tiles * kTileWords / 2;
+    const uint64_t n = a.groups * kGroupWords / 2;
     for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (uint64_t)gridDim.x * 256) reinterpret_cast<uint4*>(a.bits)[i] = make_uint4(0, 0, 0, 0);
 }
 
@@ -108,13 +108,10 @@ __device__ inline Span span_of(const uint4& d, uint64_t units) {
     return s;
 }
 
-// Marks the units of a page's payload: whole words are stored (a store of all ones takes nothing from a shared or neighbouring
-// payload), the first and the last are or-ed.
-__global__ __launch_bounds__(256) void k_mark(CompactArgs a) {
-    const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= a.n_desc) return;
-    const Span s = span_of(reinterpret_cast<const uint4*>(a.desc)[i], a.units);
-    if (s.kind == 2) atomicOr(&a.st->status, KVC_ST_CORRUPT);
+// Marks the units of a page's payload: the first and the last word are or-ed, whole words between them are stored (a store of all ones takes nothing
+// from a shared or neighbouring payload).
+template <class Or, class Ones>
+__device__ inline void mark(const Span& s, Or or_word, Ones ones) {
     if (s.kind != 1 || s.n == 0) return;
     const uint64_t end = s.from + s.n, first = s.from / 64, last = (end - 1) / 64;
     const uint32_t lo = s.from & 63, hi = (uint32_t)(end - 1) & 63;
@@ -123,12 +120,20 @@ __global__ __launch_bounds__(256) void k_mark(CompactArgs a) {
     const uint32_t h0 = hi < 32 ? ~0u >> (31 - hi) : ~0u, h1 = hi < 32 ? 0 : ~0u >> (63 - hi);
     const unsigned long long low = l0 | (unsigned long long)l1 << 32, high = h0 | (unsigned long long)h1 << 32;
     if (first == last) {
-        atomicOr(a.bits + first, low & high);
+        or_word(first, low & high);
         return;
     }
-    atomicOr(a.bits + first, low);
-    for (uint64_t w = first + 1; w < last; ++w) a.bits[w] = ~0ull;
-    atomicOr(a.bits + last, high);
+    or_word(first, low);
+    for (uint64_t w = first + 1; w < last; ++w) ones(w);
+    or_word(last, high);
+}
+
+__global__ __launch_bounds__(256) void k_mark(CompactArgs a) {
+    const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= a.n_desc) return;
+    const Span s = span_of(reinterpret_cast<const uint4*>(a.desc)[i], a.units);
+    if (s.kind == 2) atomicOr(&a.st->status, KVC_ST_CORRUPT);
+    mark(s, [&](uint64_t w, unsigned long long v) { atomicOr(a.bits + w, v); }, [&](uint64_t w) { a.bits[w] = ~0ull; });
 }
 
 __device__ inline uint32_t scan_wave(uint32_t v) {  // inclusive
@@ -141,94 +146,153 @@ __device__ inline uint32_t scan_wave(uint32_t v) {  // inclusive
     return v;
 }
 
-__global__ __launch_bounds__(256) void k_count(CompactArgs a) {
-    const uint64_t tile = (uint64_t)blockIdx.x * 4 + threadIdx.x / 64;
-    if (tile >= a.tiles) return;
-    const uint32_t lane = threadIdx.x & 63;
-    const uint32_t n = __popcll(a.bits[tile * kTileWords + lane]), upto = scan_wave(n);
-    a.before[tile * kTileWords + lane] = (uint16_t)(upto - n);
-    if (lane == 63) a.base[tile] = upto;
+// Inclusive sums over a workgroup of 1,024, and their total.
+__device__ inline uint32_t scan_group(uint32_t v, uint32_t (&part)[16], uint32_t& all) {
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x / 64, upto = scan_wave(v);
+    if (lane == 63) part[wave] = upto;
+    __syncthreads();
+    uint32_t before = 0;
+    all = 0;
+#pragma unroll
+    for (uint32_t w = 0; w < 16; ++w) {
+        before += w < wave ? part[w] : 0;
+        all += part[w];
+    }
+    __syncthreads();
+    return before + upto;
 }
 
-// one workgroup: exclusive sums of all tiles' counts
+// a workgroup per group, a lane per word
+__global__ __launch_bounds__(1024) void k_count(CompactArgs a) {
+    __shared__ uint32_t part[16];
+    const uint64_t w = (uint64_t)blockIdx.x * kGroupWords + threadIdx.x;
+    const uint32_t n = __popcll(a.bits[w]);
+    uint32_t all;
+    const uint32_t upto = scan_group(n, part, all);
+    a.before[w] = (uint16_t)(upto - n);  // (at most 65,536 - 64)
+    if (threadIdx.x == 0) a.base[blockIdx.x] = all;
+}
+
+// one workgroup: sums of all groups before each
 __global__ __launch_bounds__(1024) void k_base(CompactArgs a) {
     __shared__ uint32_t part[16];
     unsigned long long sum = 0;
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x / 64;
-    for (uint64_t t0 = 0; t0 < a.tiles; t0 += 1024) {
-        const uint64_t t = t0 + threadIdx.x;
-        const uint32_t n = t < a.tiles ? (uint32_t)a.base[t] : 0, upto = scan_wave(n);
-        if (lane == 63) part[wave] = upto;
-        __syncthreads();
-        uint32_t before = 0, all = 0;
-        for (uint32_t w = 0; w < 16; ++w) {
-            before += w < wave ? part[w] : 0;
-            all += part[w];
-        }
-        if (t < a.tiles) a.base[t] = sum + before + upto - n;
+    for (uint64_t g0 = 0; g0 < a.groups; g0 += 1024) {
+        const uint64_t g = g0 + threadIdx.x;
+        const uint32_t n = g < a.groups ? (uint32_t)a.base[g] : 0;
+        uint32_t all;
+        const uint32_t upto = scan_group(n, part, all);
+        if (g < a.groups) a.base[g] = sum + upto - n;
         sum += all;
-        __syncthreads();
     }
     if (threadIdx.x == 0) *a.used = 16 * (sum < a.out_units ? sum : a.out_units);
 }
 
-__device__ inline uint64_t rank_of(const CompactArgs& a, uint64_t unit) {
-    const uint64_t w = unit / 64;
-    const uint32_t b = unit & 63;
-    const unsigned long long bits = a.bits[w];
+// set bits of a word below bit b
+__device__ inline uint32_t bits_below(unsigned long long bits, uint32_t b) {
     const uint32_t lo = (uint32_t)bits, hi = (uint32_t)(bits >> 32);
-    const uint32_t below = b < 32 ? __popc(lo & ~(~0u << b)) : __popc(lo) + __popc(hi & ~(~0u << (b - 32)));
-    return a.base[w / kTileWords] + a.before[w] + below;
+    return b < 32 ? __popc(lo & ~(~0u << b)) : __popc(lo) + __popc(hi & ~(~0u << (b - 32)));
 }
 
-// A wave moves a tile: 64 units at a time, the lanes whose unit is held load it and store it to its rank.
+// The descriptor of a page whose payload's first unit has the rank that `rank_of` gives.
+template <class F>
+__device__ inline uint4 rename(uint4 d, const CompactArgs& a, F rank_of) {
+    const Span s = span_of(d, a.units);
+    if (s.kind != 1) return no_page();
+    const uint64_t at = s.n ? rank_of(s.from) : 0;
+    if (at + s.n > a.out_units) {
+        atomicOr(&a.st->status, KVC_ST_POOL_FULL);
+        return no_page();
+    }
+    d.x = (uint32_t)(at * 16);
+    d.y = (uint32_t)(at >> 28);
+    return d;
+}
+
+// A wave moves a tile of 64 words, which its lanes read at once: then 64 units of a word at a time, the lanes whose unit is held load it and store it to
+// its rank.  Eight words are on their way while the eight before them are stored.
 constexpr int kMoveWords = 8;
 
-__global__ __launch_bounds__(256) void k_move(CompactArgs a) {
-    const uint64_t tile = (uint64_t)blockIdx.x * 4 + threadIdx.x / 64;
-    if (tile >= a.tiles) return;
+__device__ inline void move_tile(const CompactArgs& a, uint64_t tile) {
     const uint32_t lane = threadIdx.x & 63;
-    const uint64_t base = a.base[tile];
-    for (uint32_t w0 = 0; w0 < kTileWords; w0 += kMoveWords) {
-        uint4v r[kMoveWords];
-        uint64_t to[kMoveWords];
-#pragma unroll
-        for (int k = 0; k < kMoveWords; ++k) {
-            const uint64_t w = tile * kTileWords + w0 + k;
-            const unsigned long long bits = a.bits[w];
-            const uint32_t half = lane < 32 ? (uint32_t)bits : (uint32_t)(bits >> 32);
-            const uint32_t below = __popc(half & ~(~0u << (lane & 31))) + (lane < 32 ? 0 : __popc((uint32_t)bits));
-            to[k] = ~0ull;
-            r[k] = uint4v{0, 0, 0, 0};
-            if (half >> (lane & 31) & 1) {
-                to[k] = base + a.before[w] + below;
-                r[k] = reinterpret_cast<const uint4v*>(a.pool)[w * 64 + lane];
-            }
-        }
+    const uint64_t word = tile * 64 + lane, base = a.base[tile * 64 / kGroupWords];
+    const unsigned long long bits = a.bits[word];
+    const uint32_t lo = (uint32_t)bits, hi = (uint32_t)(bits >> 32), before = a.before[word];
+    const uint4v* from = reinterpret_cast<const uint4v*>(a.pool) + tile * 4096 + lane;
+    uint4v* to = reinterpret_cast<uint4v*>(a.pool_out) + base;
+    const uint64_t room = a.out_units > base ? a.out_units - base : 0;
+    uint4v r[2][kMoveWords];
+    const auto held = [&](uint32_t w) {  // whether the lane's unit of word w is
+        const uint32_t half = lane < 32 ? __builtin_amdgcn_readlane(lo, w) : __builtin_amdgcn_readlane(hi, w);
+        return (half >> (lane & 31) & 1) != 0;
+    };
+    const auto fetch = [&](uint4v (&x)[kMoveWords], uint32_t w0) {
 #pragma unroll
         for (int k = 0; k < kMoveWords; ++k)
-            if (to[k] < a.out_units) reinterpret_cast<uint4v*>(a.pool_out)[to[k]] = r[k];
+            if (held(w0 + k)) x[k] = from[(w0 + k) * 64];
+    };
+    const auto put = [&](const uint4v (&x)[kMoveWords], uint32_t w0) {
+#pragma unroll
+        for (int k = 0; k < kMoveWords; ++k) {
+            const uint32_t wl = __builtin_amdgcn_readlane(lo, w0 + k), wh = __builtin_amdgcn_readlane(hi, w0 + k);
+            const uint32_t at = __builtin_amdgcn_readlane(before, w0 + k) + __builtin_amdgcn_mbcnt_hi(wh, __builtin_amdgcn_mbcnt_lo(wl, 0));
+            if (held(w0 + k) && at < room) to[at] = x[k];
+        }
+    };
+    fetch(r[0], 0);
+#pragma nounroll
+    for (uint32_t w0 = 0; w0 < 64; w0 += 2 * kMoveWords) {
+        fetch(r[1], w0 + kMoveWords);
+        put(r[0], w0);
+        if (w0 + 2 * kMoveWords < 64) fetch(r[0], w0 + 2 * kMoveWords);
+        put(r[1], w0 + kMoveWords);
     }
 }
 
-__global__ __launch_bounds__(256) void k_rename(CompactArgs a) {
-    const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= a.n_desc) return;
-    uint4 d = reinterpret_cast<const uint4*>(a.desc)[i];
-    const Span s = span_of(d, a.units);
-    if (s.kind != 1) {
-        d = no_page();
-    } else {
-        const uint64_t at = s.n ? rank_of(a, s.from) : 0;
-        if (at + s.n > a.out_units) {
-            atomicOr(&a.st->status, KVC_ST_POOL_FULL);
-            d = no_page();
-        } else {
-            d.x = (uint32_t)(at * 16);
-            d.y = (uint32_t)(at >> 28);
-        }
+// the first `movers` workgroups move tiles, the others rename pages
+__global__ __launch_bounds__(256) void k_move(CompactArgs a, uint32_t movers) {
+    if (blockIdx.x < movers) {
+        const uint64_t tile = (uint64_t)blockIdx.x * 4 + threadIdx.x / 64;
+        if (tile < a.groups * (kGroupWords / 64)) move_tile(a, tile);
+        return;
     }
-    reinterpret_cast<uint4*>(a.desc_out)[i] = d;
+    const uint64_t i = (uint64_t)(blockIdx.x - movers) * 256 + threadIdx.x;
+    if (i >= a.n_desc) return;
+    reinterpret_cast<uint4*>(a.desc_out)[i] = rename(reinterpret_cast<const uint4*>(a.desc)[i], a, [&](uint64_t unit) {
+        const uint64_t w = unit / 64;
+        return a.base[w / kGroupWords] + a.before[w] + bits_below(a.bits[w], unit & 63);
+    });
+}
+
+// A pool that one workgroup compacts: everything but payloads and descriptors is in LDS, and there is one launch.
+__global__ __launch_bounds__(1024) void k_compact_small(CompactArgs a) {
+    __shared__ unsigned long long bits[kSmallWords];
+    __shared__ uint32_t before[kSmallWords];
+    __shared__ uint32_t part[16];
+    const uint32_t t = threadIdx.x;
+    if (t < kSmallWords) bits[t] = 0;
+    __syncthreads();
+    for (uint64_t i = t; i < a.n_desc; i += 1024) {
+        const Span s = span_of(reinterpret_cast<const uint4*>(a.desc)[i], a.units);
+        if (s.kind == 2) atomicOr(&a.st->status, KVC_ST_CORRUPT);
+        mark(s, [&](uint64_t w, unsigned long long v) { atomicOr(&bits[w], v); }, [&](uint64_t w) { atomicOr(&bits[w], ~0ull); });
+    }
+    __syncthreads();
+    const uint32_t n = t < kSmallWords ? __popcll(bits[t]) : 0;
+    uint32_t all;
+    const uint32_t upto = scan_group(n, part, all);
+    if (t < kSmallWords) before[t] = upto - n;
+    if (t == 0) *a.used = 16 * (all < a.out_units ? all : a.out_units);
+    __syncthreads();
+    for (uint32_t u = t; u < a.units; u += 1024) {
+        const uint32_t w = u / 64, b = u & 63;
+        const uint64_t at = before[w] + bits_below(bits[w], b);
+        const uint32_t half = b < 32 ? (uint32_t)bits[w] : (uint32_t)(bits[w] >> 32);
+        if ((half >> (b & 31) & 1) && at < a.out_units) reinterpret_cast<uint4*>(a.pool_out)[at] = reinterpret_cast<const uint4*>(a.pool)[u];
+    }
+    for (uint64_t i = t; i < a.n_desc; i += 1024)
+        reinterpret_cast<uint4*>(a.desc_out)[i] =
+            rename(reinterpret_cast<const uint4*>(a.desc)[i], a, [&](uint64_t unit) { return (uint64_t)before[unit / 64] + bits_below(bits[unit / 64], unit & 63); });
 }
 
 __global__ void k_adopt(DevState* st, const unsigned long long* used) {
@@ -251,12 +315,13 @@ hipError_t launch_fork(const IdsArgs& a, hipStream_t s) { return launch_kernel(k
 hipError_t launch_free(const IdsArgs& a, hipStream_t s) { return launch_kernel(k_ids<false>, dim3(groups(a.n_pages, 256), (unsigned)a.n_layers), dim3(256), s, a); }
 
 hipError_t launch_compact(const CompactArgs& a, hipStream_t s) {
-    hipError_t e = launch_kernel(k_bits_zero, dim3((unsigned)std::min<uint64_t>(groups(a.tiles * kTileWords / 2, 256), 2048)), dim3(256), s, a);
+    if (a.units <= 64 * kSmallWords && a.n_desc <= kSmallPages) return launch_kernel(k_compact_small, dim3(1), dim3(1024), s, a);
+    hipError_t e = launch_kernel(k_bits_zero, dim3((unsigned)std::min<uint64_t>(groups(a.groups * kGroupWords / 2, 256), 2048)), dim3(256), s, a);
     if (e == hipSuccess) e = launch_kernel(k_mark, dim3(groups(a.n_desc, 256)), dim3(256), s, a);
-    if (e == hipSuccess) e = launch_kernel(k_count, dim3(groups(a.tiles, 4)), dim3(256), s, a);
+    if (e == hipSuccess) e = launch_kernel(k_count, dim3((unsigned)a.groups), dim3(1024), s, a);
     if (e == hipSuccess) e = launch_kernel(k_base, dim3(1), dim3(1024), s, a);
-    if (e == hipSuccess) e = launch_kernel(k_move, dim3(groups(a.tiles, 4)), dim3(256), s, a);
-    if (e == hipSuccess) e = launch_kernel(k_rename, dim3(groups(a.n_desc, 256)), dim3(256), s, a);
+    const uint32_t movers = groups(a.units, 4 * 4096);
+    if (e == hipSuccess) e = launch_kernel(k_move, dim3(movers + groups(a.n_desc, 256)), dim3(256), s, a, movers);
     return e;
 }
 

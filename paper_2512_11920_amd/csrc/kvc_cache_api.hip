@@ -198,10 +198,10 @@ int kvc_free_blocks(kvc_ctx* ctx, const int32_t* d_ids, int32_t n, int32_t n_lay
     return ids_call(ctx, false, nullptr, d_ids, n, n_layers, pool_blocks_per_layer, stream);
 }
 
-// Workspace: the bitmap, the counts within tiles, the tiles' sums.
+// Workspace: the bitmap, the counts within groups, the groups' sums.
 uint64_t kvc_compact_workspace(uint64_t pool_bytes) {
-    const uint64_t tiles = compact_tiles(pool_bytes);
-    return tiles * kTileWords * 8 + round_256(tiles * kTileWords * 2) + round_256(tiles * 8);
+    const uint64_t groups = compact_groups(pool_bytes);
+    return groups * kGroupWords * 10 + round_256(groups * 8);
 }
 
 static bool apart(const void* a, uint64_t an, const void* b, uint64_t bn) {
@@ -225,13 +225,13 @@ int kvc_compact_pool(kvc_ctx* ctx, void* d_pool_out, uint64_t pool_out_bytes, kv
     a.desc = ctx->desc;
     a.desc_out = d_desc_out;
     a.n_desc = ctx->n_desc;
-    a.tiles = compact_tiles(ctx->pool_bytes);
-    if ((int64_t)(a.tiles / 4) > kMaxGroups - 1 || a.n_desc / 256 > (uint64_t)kMaxGroups - 1) return KVC_ERR_ARG;
+    a.groups = compact_groups(ctx->pool_bytes);
+    if (a.units / 16384 + a.n_desc / 256 > (uint64_t)kMaxGroups - 2 || a.groups * 4 > (uint64_t)kMaxGroups) return KVC_ERR_ARG;
     uint8_t* w = static_cast<uint8_t*>(d_work);
     a.bits = reinterpret_cast<unsigned long long*>(w);
-    w += a.tiles * kTileWords * 8;
+    w += a.groups * kGroupWords * 8;
     a.before = reinterpret_cast<uint16_t*>(w);
-    w += round_256(a.tiles * kTileWords * 2);
+    w += a.groups * kGroupWords * 2;
     a.base = reinterpret_cast<unsigned long long*>(w);
     a.used = reinterpret_cast<unsigned long long*>(d_used_out);
     a.st = ctx->st;
