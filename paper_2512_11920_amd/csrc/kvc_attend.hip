@@ -106,6 +106,20 @@ __device__ inline uint32_t uniform(uint32_t v) { return __builtin_amdgcn_readfir
 // tiles a worker takes
 __device__ inline uint32_t share(uint32_t tiles, uint32_t workers) { return max(1u, (tiles + workers - 1) / workers); }
 
+// Eight channels of the output, from their sums and the weights'.
+__device__ inline uint4v finished(const float4v (&o)[2], float l) {
+    const float f = l == 0.f ? 0.f : 1.f / l;
+    uint4v v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        half2 x;
+        x[0] = (_Float16)(o[e / 2][e % 2 * 2] * f);
+        x[1] = (_Float16)(o[e / 2][e % 2 * 2 + 1] * f);
+        v[e] = __builtin_bit_cast(uint32_t, x);
+    }
+    return v;
+}
+
 // ---- the sequences' own tokens.  A worker is a wave: tiles of 32 tokens go from memory to its registers, keys of the next tile while this
 // one's scores become weights, values while the next scores are made, so that a tile is always on its way; the block table is read one
 // tile further ahead.  R: tiles of 16 rows that share the tokens.
@@ -558,6 +572,86 @@ __global__ __launch_bounds__(256, 2) void k_both(AttendArgs a) {
     }
 }
 
+// ---- short sequences without a prefix.  A workgroup of kDirectWaves takes a unit, its waves the tiles in turn, and they join their sums in LDS: one launch, and the
+// lengths, the block table and the queries are asked for at once.
+template <int D, int R, bool EIGHT>
+__global__ __launch_bounds__(64 * kDirectWaves, D * R <= 128 ? 2 : 1) void k_direct(AttendArgs a) {
+    __shared__ float2v stats[kDirectWaves][16 * R];
+    __shared__ __align__(16) float sums[kDirectWaves][16 * R][D];
+    const uint32_t lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4, wave = uniform(threadIdx.x / 64);
+    const uint32_t units = a.n_kv * a.own_tiles, s = blockIdx.x / units, u = blockIdx.x - s * units, h = u / a.own_tiles, rt = u - h * a.own_tiles;
+    Source src{a.table + (int64_t)s * a.max_blocks, a.k_cache + h * a.g.page_stride, a.v_cache + h * a.g.page_stride, (uint32_t)a.max_blocks * (uint32_t)a.g.N};
+    Blocks<EIGHT> b = find_blocks<EIGHT>(a, src, wave * kTile);  // (as far as the table's row goes)
+    Rows<D> r[R];
+    uint32_t later[R];
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+        clear(r[j]);
+        const uint32_t row = min((rt * R + j) * 16 + n, (uint32_t)a.rows - 1);
+        const uint32_t in = fast_div(row, a.by_n_q), i = row - in * a.n_q;
+        const uint16_t* q = a.q + s * a.q_strides[0] + i * a.q_strides[1] + (h * a.group + in) * a.q_strides[2];
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k) r[j].q[k] = *reinterpret_cast<const uint4v*>(q + 32 * k + 8 * g);
+        later[j] = a.n_q - 1 - i;
+    }
+    const uint32_t len = uniform((uint32_t)max(a.lens[s], 0));
+    src.len = uniform(own_length(a, s));
+    const uint32_t tiles = (src.len + kTile - 1) / kTile;
+    for (uint32_t t = wave; t < tiles; t += kDirectWaves) {
+        if (t != wave) b = find_blocks<EIGHT>(a, src, t * kTile);
+        // (entries behind the last token are not block numbers)
+        if constexpr (EIGHT) {
+            b.k[0] = t * kTile + 8 * (n >> 2) < src.len ? b.k[0] : -1;
+            b.v[0] = t * kTile + 8 * g < src.len ? b.v[0] : -1;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) b.k[j] = t * kTile + 8 * (n >> 2) + 4 * j + (n & 3) < src.len ? b.k[j] : -1;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) b.v[j] = t * kTile + 8 * g + j < src.len ? b.v[j] : -1;
+        }
+        Tokens<D> x;
+        load_keys<D, EIGHT>(x, a, src, b, t * kTile);
+        const uint32_t there = load_values<D, EIGHT>(x, a, src, b, t * kTile);
+        half8 p[R];
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            float4v sc[2];
+            scores(sc, r[j], x);
+            p[j] = weights(r[j], sc, a.scale_log2, there, t * kTile, min(len > later[j] ? len - later[j] : 0, src.len));
+        }
+        add_values<D, R>(r, x, p);
+    }
+    const uint32_t workers = min(tiles, kDirectWaves);
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+        const float l = row_sum(r[j].l);
+        if (wave < workers) {
+            store_sums<D>(r[j], sums[wave][16 * j + n], g);
+            if (g == 0) stats[wave][16 * j + n] = float2v{r[j].m - kLift, l};
+        }
+    }
+    __syncthreads();
+    for (uint32_t k = threadIdx.x; k < 16 * R * (D / 8); k += 64 * kDirectWaves) {
+        const uint32_t in_tile = k / (D / 8), c = k % (D / 8), row = rt * R * 16 + in_tile;
+        if (row >= (uint32_t)a.rows) continue;
+        float m = -INFINITY, l = 0.f;
+        for (uint32_t w = 0; w < workers; ++w) m = fmaxf(m, stats[w][in_tile][0]);
+        float4v o[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+        for (uint32_t w = 0; w < workers; ++w) {
+            const float2v st = stats[w][in_tile];
+            if (st[0] == -INFINITY) continue;  // (a part in which the row saw no token)
+            const float f = power2(st[0] - m);
+            const float4v* x = reinterpret_cast<const float4v*>(&sums[w][in_tile][8 * c]);
+            l += st[1] * f;
+            o[0] += x[0] * f;
+            o[1] += x[1] * f;
+        }
+        const uint32_t in = fast_div(row, a.by_n_q), i = row - in * a.n_q, head = h * a.group + in;
+        *reinterpret_cast<uint4v*>(a.out + s * a.out_strides[0] + i * a.out_strides[1] + head * a.out_strides[2] + 8 * c) = finished(o, l);
+        if (a.lse && c == 0) a.lse[((int64_t)s * a.n_q + i) * a.n_heads + head] = lse_of(m, l);
+    }
+}
+
 // ---- joining pieces: D / 8 threads to a row, 8 channels each.  A row's pieces are read kAtOnce at a time: each read goes to memory, and takes as
 // long as all of them together.
 constexpr uint32_t kAtOnce = 8;
@@ -639,22 +733,15 @@ __global__ __launch_bounds__(256) void k_join(AttendArgs a) {
         }
     }
     const uint32_t in = fast_div(row, a.by_n_q), i = row - in * a.n_q, head = h * a.group + in;
-    const float f = l == 0.f ? 0.f : 1.f / l;
-    uint4v v;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        half2 x;
-        x[0] = (_Float16)(o[e / 2][e % 2 * 2] * f);
-        x[1] = (_Float16)(o[e / 2][e % 2 * 2 + 1] * f);
-        v[e] = __builtin_bit_cast(uint32_t, x);
-    }
-    *reinterpret_cast<uint4v*>(a.out + s * a.out_strides[0] + i * a.out_strides[1] + head * a.out_strides[2] + 8 * c) = v;
+    *reinterpret_cast<uint4v*>(a.out + s * a.out_strides[0] + i * a.out_strides[1] + head * a.out_strides[2] + 8 * c) = finished(o, l);
     if (a.lse && c == 0) a.lse[((int64_t)s * a.n_q + i) * a.n_heads + head] = lse_of(m, l);
 }
 
 template <int D, int R>
 static hipError_t launch_parts(const AttendArgs& a, hipStream_t s) {
     const bool eight = a.g.N % 8 == 0;
+    if constexpr (direct_fits(D, R))
+        if (a.direct) return launch_kernel(eight ? k_direct<D, R, true> : k_direct<D, R, false>, dim3((unsigned)a.n_seq * a.n_kv * a.own_tiles), dim3(64 * kDirectWaves), s, a);
     if constexpr (both_fit(D, R))
         if (a.n_prefix) return launch_kernel(eight ? k_both<D, R, true> : k_both<D, R, false>, dim3(2 * kPrefixWorkers), dim3(256), s, a);
     const hipError_t e = launch_kernel(eight ? k_own<D, R, true> : k_own<D, R, false>, dim3(a.own_workers / 4), dim3(256), s, a);
@@ -668,7 +755,7 @@ hipError_t launch_attend<KVC_HEAD_DIM>(const AttendArgs& a, hipStream_t s) {
     if constexpr (D <= 192) e = a.own_rows == 32 ? launch_parts<D, 2>(a, s) : launch_parts<D, 1>(a, s);
     else e = launch_parts<D, 1>(a, s);
     constexpr uint32_t rows = 256 / (D / 8);
-    if (e == hipSuccess) e = launch_kernel(k_join<D>, dim3((unsigned)(((int64_t)a.n_seq * a.n_kv * a.rows + rows - 1) / rows)), dim3(256), s, a);
+    if (e == hipSuccess && !a.direct) e = launch_kernel(k_join<D>, dim3((unsigned)(((int64_t)a.n_seq * a.n_kv * a.rows + rows - 1) / rows)), dim3(256), s, a);
     return e;
 }
 

@@ -96,7 +96,8 @@ struct AttendArgs {
     // the workspace, see AttendPlan
     uint32_t own_tiles;  // row tiles of one sequence and KV head
     uint32_t own_workers, prefix_workers, own_rows, prefix_rows;
-    bool apart;  // both parts in one launch, by workgroups of their own
+    bool direct;  // a workgroup for every unit, and nothing else
+    bool apart;   // both parts in one launch, by workgroups of their own
     uint32_t* own_start;     // [n_seq + 1]
     uint32_t* prefix_start;  // [n_prefix + 1]
     float* sums;             // [slots][d]
@@ -116,6 +117,8 @@ constexpr uint32_t kOwnWorkers = 2048, kPrefixWorkers = 256;  // waves, workgrou
 constexpr uint32_t kPrefixWaves = 4;                          // of a workgroup
 
 constexpr int64_t kApartTiles = 8192;
+constexpr uint32_t kDirectWaves = 8, kDirectTiles = 16;
+constexpr bool direct_fits(int d, int row_tiles) { return d * row_tiles <= 256; }  // into LDS
 
 // Whether the kernel that does both parts keeps two workgroups of its own on a compute unit (256 registers).
 constexpr bool both_fit(int d, int row_tiles) { return d * row_tiles <= 128; }

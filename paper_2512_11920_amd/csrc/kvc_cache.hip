@@ -67,7 +67,7 @@ __global__ __launch_bounds__(256) void k_copy_blocks(CopyArgs a) {
     }
 #pragma unroll
     for (int k = 0; k < kCopyChunks / 256; ++k)
-        if (at[k] >= 0) *reinterpret_cast<uint4v*>(y + at[k]) = r[k];
+        if (at[k] >= 0) __builtin_nontemporal_store(r[k], reinterpret_cast<uint4v*>(y + at[k]));
 }
 
 // ---- fork and free: a lane per descriptor.
@@ -85,7 +85,9 @@ __global__ __launch_bounds__(256) void k_ids(IdsArgs a) {
         return;
     }
     uint4* desc = reinterpret_cast<uint4*>(a.desc) + (int64_t)blockIdx.y * a.per_layer * a.ppb + page;
-    desc[(int64_t)dst * a.ppb] = FORK ? desc[(int64_t)src * a.ppb] : no_page();
+    uint4v* to = reinterpret_cast<uint4v*>(desc + (int64_t)dst * a.ppb);
+    if (FORK) __builtin_nontemporal_store(reinterpret_cast<const uint4v*>(desc)[(int64_t)src * a.ppb], to);
+    else *reinterpret_cast<uint4*>(to) = no_page();
 }
 
 // ---- compaction.

@@ -109,6 +109,7 @@ int kvc_attend(kvc_ctx* ctx, const kvc_attend_t* p, void* stream) {
     a.own_tiles = (uint32_t)own_tiles;
     a.own_workers = plan.own_workers;
     a.prefix_workers = plan.prefix_workers;
+    a.direct = p->n_prefix == 0 && direct_fits(ctx->g.d, plan.own_rows / 16) && own_tokens <= (int64_t)kDirectTiles * 32 && product(own_tiles, p->n_kv_heads, p->n_seq) <= kMaxGroups / 2;
     // (tables may be longer than the prefixes in them)
     a.apart = p->n_prefix && both_fit(ctx->g.d, plan.own_rows / 16) && product(prefix_tiles, p->n_kv_heads, prefix_tokens / 32 + 1) <= kApartTiles;
     if (a.apart) {
