@@ -298,6 +298,7 @@ int kvc_append(kvc_ctx* ctx, const kvc_append_t* a, void* stream);
  * Each prefix is read once for its group, not once for every sequence.  Lengths beyond their table's row set
  * KVC_ST_BAD_INDEX and are cut to it.  Sums, maxima and products are held in 32 bits; the weights e^(x_t - m)
  * are rounded to FP16 (11 bits, far from its smallest numbers) for the product with the values.
+ * Groups out of order set KVC_ST_BAD_INDEX, and no prefix is seen then.  d_out must not overlap what is read.
  * d_work: device memory of at least kvc_attend_workspace(...) bytes, 256-byte aligned, contents meaningless
  * between calls; calls that overlap in time need workspaces of their own. */
 typedef struct {

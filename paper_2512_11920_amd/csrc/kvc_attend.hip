@@ -299,7 +299,12 @@ __device__ inline void prefix_part(const AttendArgs& a, Sums& sums, PrefixTiles<
     };
     const auto tiles_of = [&](uint32_t g) { return (prefix_length(a, g) + kTile - 1) / kTile; };
     const auto work_of = [&](uint32_t g) { return row_tiles(g) * tiles_of(g); };
-    add_up(sums, a.n_prefix, work_of);
+    // groups out of order could hold a sequence twice, and more rows than there are: none is taken then
+    bool disorder = false;
+    for (uint32_t i = threadIdx.x; i < (uint32_t)a.n_prefix; i += 256) disorder = disorder || a.prefix_first[i] > a.prefix_first[i + 1];
+    const bool ordered = !__syncthreads_or(disorder);
+    if (disorder) atomicOr(&a.st->status, KVC_ST_BAD_INDEX);
+    add_up(sums, ordered ? a.n_prefix : 0, work_of);
     if (worker == 0) write_starts(sums, a.prefix_start, a.n_prefix, work_of);
     const uint32_t all = uniform(sums.all) * a.n_kv, each = share(all, a.prefix_workers);
     const uint32_t begin = worker * each;
@@ -689,7 +694,7 @@ __global__ __launch_bounds__(256) void k_join(AttendArgs a) {
     if (g >= 0) {
         const Range seqs = group_of_prefix(a, g);
         const uint32_t ptiles = (prefix_length(a, g) + kTile - 1) / kTile;
-        if (ptiles) {
+        if (ptiles && a.prefix_start[a.n_prefix]) {
             const uint32_t rts = ((uint32_t)(seqs.end - seqs.begin) * a.rows + a.prefix_rows - 1) / a.prefix_rows;
             const uint32_t rr = (s - seqs.begin) * a.rows + row, rt = rr / a.prefix_rows;
             shared.find(a.prefix_start[g] * a.n_kv + (h * rts + rt) * ptiles, ptiles, share(a.prefix_start[a.n_prefix] * a.n_kv, a.prefix_workers));

@@ -116,7 +116,13 @@ struct AttendPlan {
 constexpr uint32_t kOwnWorkers = 2048, kPrefixWorkers = 256;  // waves, workgroups: with 2 of either, or 2 and 1, what the GPU holds at once
 constexpr uint32_t kPrefixWaves = 4;                          // of a workgroup
 
-constexpr int64_t kApartTiles = 8192;
+// Up to so many tiles of prefixes (of 32 tokens, 128 rows and a KV head), half of the workgroups have the prefixes and half the sequences' own tokens; beyond
+// it every one has a part of both, which divides better but begins twice.  8 KV heads x 128, 8 query heads each, both parts by all / apart, us: prefix of 4,096 tokens
+// and 64 sequences of 1 to 512 (4,096 tiles) 51.7 / 38.2, 16,384 and 64 (16,384 tiles) 85.3 / 81.8, 8,192 and 256 (32,768 tiles) 160 / 154, with 512 to
+// 2,048 own tokens 331 / 294, 32,768 and 64 (32,768 tiles) 128 / 133; 32,768 and 256 (131,072 tiles) are divided.
+constexpr int64_t kApartTiles = 40960;
+// A call without prefixes whose tables hold at most so many tiles of 32 tokens is done by a workgroup of 8 waves for each unit, in one launch: one sequence of
+// 256 tokens, 4 heads x 64, 6.4 us instead of 9.7.
 constexpr uint32_t kDirectWaves = 8, kDirectTiles = 16;
 constexpr bool direct_fits(int d, int row_tiles) { return d * row_tiles <= 256; }  // into LDS
 

@@ -135,6 +135,41 @@ def test_lengths_and_groups(lens, prefix, first):
     _compare(c, out, lse)
 
 
+def _wider(table, width):
+    """The same table with room for longer rows: which kernels a call takes goes by the room, as lengths are on the device."""
+    return np.concatenate([table, np.full((len(table), width - table.shape[1]), -1, np.int32)], axis=1)
+
+
+@pytest.mark.parametrize("d,N", [(32, 16), (64, 5), (96, 24), (128, 16), (128, 31), (160, 8), (192, 16), (224, 3), (256, 16)])
+@pytest.mark.parametrize("rows", [(1, 1), (8, 4)])
+def test_short_sequences_in_wide_tables(d, N, rows):
+    """Without a prefix: in one launch, and divided over waves and joined."""
+    rng = np.random.default_rng(d + N)
+    group, q = rows
+    lens = EDGES + [200, 300]
+    c = _setup(rng, N, d, 2, group, q, lens, holes=0.05)
+    _, out, lse = _run(c)
+    _compare(c, out, lse)
+    c["table"] = _wider(c["table"], 40000 // N)
+    _, out, lse = _run(c)
+    _compare(c, out, lse)
+
+
+@pytest.mark.parametrize("d,N", [(32, 16), (64, 24), (96, 8), (128, 16), (128, 7), (160, 16), (256, 5)])
+@pytest.mark.parametrize("rows", [(3, 1), (8, 3)])
+def test_prefixes_in_wide_tables(d, N, rows):
+    """Where the tables have room for long prefixes, every workgroup has a part of both; rows of one tile and of several."""
+    rng = np.random.default_rng(d * 3 + N)
+    group, q = rows
+    lens = [0, 5, 31, 64, 100, 333, 7, 7, 7, 7, 12, 90]
+    c = _setup(rng, N, d, 2, group, q, lens, prefix=(500, 1, 64, 33), first=(0, 2, 7, 8, 12), holes=0.05)
+    _, out, lse = _run(c)
+    _compare(c, out, lse)
+    c["prefix_table"] = _wider(c["prefix_table"], 900000 // N)
+    _, out, lse = _run(c)
+    _compare(c, out, lse)
+
+
 def test_many_short_sequences():
     rng = np.random.default_rng(5)
     lens = rng.integers(0, 40, 700)
@@ -212,6 +247,22 @@ def test_bad_entries_are_passed_over_and_reported():
     c["lens"] = np.array([32, 32], np.int32)
     want, _, bound, _ = _want(c)
     assert (np.abs(out - want) <= bound).all()
+
+
+def test_groups_out_of_order_are_reported_and_not_seen():
+    rng = np.random.default_rng(16)
+    for first in ([0, 3, 1, 4], [4, 0, 4, 0], [2, 1, 0, -5]):
+        c = _setup(rng, 16, 64, 2, 2, 1, [50, 20, 0, 33], prefix=(40, 70, 10), first=first)
+        codec, out, _ = _run_with_pool(c)
+        assert codec.stats()["status"] == kvc.ST_BAD_INDEX, first
+        c["prefix_lens"] = np.zeros(0, np.int32)
+        want, _, bound, _ = _want(c)
+        assert (np.abs(out - want) <= bound).all(), first
+    # ends beyond the batch are cut to it
+    c = _setup(rng, 16, 64, 2, 2, 1, [50, 20, 0, 33], prefix=(40, 70), first=[-3, 2, 9])
+    codec, out, _ = _run_with_pool(c)
+    want, _, bound, _ = _want(c)
+    assert (np.abs(out - want) <= bound).all() and codec.stats()["status"] == 0
 
 
 def _run_with_pool(c):
