@@ -657,8 +657,8 @@ __global__ __launch_bounds__(64 * kDirectWaves, D * R <= 128 ? 2 : 1) void k_dir
     }
 }
 
-// ---- joining pieces: D / 8 threads to a row, 8 channels each.  A row's pieces are read kAtOnce at a time: each read goes to memory, and takes as
-// long as all of them together.
+// ---- joining pieces: D / 8 threads for 8 channels each, of a row and every a.join_lanes-th of its pieces.  A thread reads kAtOnce pieces at a time, as each read goes to memory
+// and takes as long as all of them together; where there are few rows, whose pieces are many, threads share them out and join their sums in LDS.
 constexpr uint32_t kAtOnce = 8;
 
 // Where the pieces of a unit are, for one of its rows: `n` workers from w0 on have one each, or one has it whole.
@@ -675,22 +675,25 @@ struct Pieces {
 
 template <int D>
 __global__ __launch_bounds__(256) void k_join(AttendArgs a) {
-    constexpr uint32_t kEach = D / 8, kRows = 256 / kEach;
-    const uint32_t in_group = threadIdx.x / kEach, c = threadIdx.x % kEach;
-    const int64_t id = (int64_t)blockIdx.x * kRows + in_group;
-    if (in_group >= kRows || id >= (int64_t)a.n_seq * a.n_kv * a.rows) return;
-    const uint32_t unit = fast_div((uint32_t)id, a.by_rows), row = (uint32_t)id - unit * a.rows, s = unit / a.n_kv, h = unit - s * a.n_kv;
+    constexpr uint32_t kEach = D / 8, kSlots = 256 / kEach;
+    __shared__ __align__(16) float4v sums[kSlots][kEach][2];
+    __shared__ float2v stats[kSlots];
+    const uint32_t place = threadIdx.x / kEach, c = threadIdx.x % kEach, lanes = a.join_lanes, in_group = place / lanes, first = place % lanes;
+    const uint32_t rows_here = kSlots / lanes;
+    const int64_t id = (int64_t)blockIdx.x * rows_here + in_group;
+    const bool have = in_group < rows_here && id < (int64_t)a.n_seq * a.n_kv * a.rows;
+    const uint32_t row_id = have ? (uint32_t)id : 0, unit = fast_div(row_id, a.by_rows), row = row_id - unit * a.rows, s = unit / a.n_kv, h = unit - s * a.n_kv;
     Pieces own, shared;
     const uint32_t before = a.own_start[s], tiles = a.own_start[s + 1] - before, all = a.own_start[a.n_seq];
     const int g = a.n_prefix ? prefix_of(a, s) : -1;
     if (tiles) {
         const uint32_t units = a.n_kv * a.own_tiles, rt = row / a.own_rows;
         own.find(before * units + (h * a.own_tiles + rt) * tiles, tiles, share(all * units, a.own_workers));
-        if (g < 0 && own.n == 1) return;  // finished by its worker
-        own.whole = id;
+        own.whole = row_id;
         own.rows = a.own_rows;
         own.slots = a.own_slots + (row - rt * a.own_rows);
     }
+    const bool finished_already = g < 0 && own.n == 1;  // by its worker
     if (g >= 0) {
         const Range seqs = group_of_prefix(a, g);
         const uint32_t ptiles = (prefix_length(a, g) + kTile - 1) / kTile;
@@ -698,45 +701,68 @@ __global__ __launch_bounds__(256) void k_join(AttendArgs a) {
             const uint32_t rts = ((uint32_t)(seqs.end - seqs.begin) * a.rows + a.prefix_rows - 1) / a.prefix_rows;
             const uint32_t rr = (s - seqs.begin) * a.rows + row, rt = rr / a.prefix_rows;
             shared.find(a.prefix_start[g] * a.n_kv + (h * rts + rt) * ptiles, ptiles, share(a.prefix_start[a.n_prefix] * a.n_kv, a.prefix_workers));
-            shared.whole = a.prefix_whole + id;
+            shared.whole = a.prefix_whole + row_id;
             shared.rows = a.prefix_rows;
             shared.slots = a.prefix_slots + (rr - rt * a.prefix_rows);
         }
     }
     float m = -INFINITY, l = 0.f;
     float4v o[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-    const uint32_t n = own.n + shared.n;
-    for (uint32_t k0 = 0; k0 < n; k0 += kAtOnce) {
+    const auto join = [&](float2v st, const float4v& x, const float4v& y, float top) {  // (of an empty piece, where the row saw no token, the sums are not looked at)
+        if (st[0] == -INFINITY) return;
+        const float w = power2(st[0] - top);
+        l += st[1] * w;
+        o[0] += x * w;
+        o[1] += y * w;
+    };
+    const uint32_t n = have && !finished_already ? own.n + shared.n : 0;
+    for (uint32_t k0 = first; k0 < n; k0 += kAtOnce * lanes) {
         float2v st[kAtOnce];
         float4v x[kAtOnce][2];
-#pragma unroll
-        for (uint32_t j = 0; j < kAtOnce; ++j) {
-            const uint32_t k = min(k0 + j, n - 1);
-            const int64_t slot = k < own.n ? own.slot(k) : shared.slot(k - own.n);
-            st[j] = a.stats[slot];
-            const float4v* p = reinterpret_cast<const float4v*>(a.sums + slot * D + 8 * c);
-            x[j][0] = p[0];
-            x[j][1] = p[1];
-            if (k0 + j >= n) st[j][0] = -INFINITY;
-        }
         float top = m;
 #pragma unroll
+        for (uint32_t j = 0; j < kAtOnce; ++j) {
+            const uint32_t k = k0 + j * lanes;
+            st[j] = float2v{-INFINITY, 0.f};
+            x[j][0] = x[j][1] = float4v{0.f, 0.f, 0.f, 0.f};
+            if (k < n) {
+                const int64_t slot = k < own.n ? own.slot(k) : shared.slot(k - own.n);
+                st[j] = a.stats[slot];
+                const float4v* p = reinterpret_cast<const float4v*>(a.sums + slot * D + 8 * c);
+                x[j][0] = p[0];
+                x[j][1] = p[1];
+            }
+        }
+#pragma unroll
         for (uint32_t j = 0; j < kAtOnce; ++j) top = fmaxf(top, st[j][0]);
-        if (top == -INFINITY) continue;  // pieces in which the row saw no token
+        if (top == -INFINITY) continue;
         const float f = power2(m - top);
         m = top;
         l *= f;
         o[0] *= f;
         o[1] *= f;
 #pragma unroll
-        for (uint32_t j = 0; j < kAtOnce; ++j) {
-            const float w = power2(st[j][0] - top);
-            if (st[j][0] == -INFINITY) continue;  // (their sums are zeros, or another piece's)
-            l += st[j][1] * w;
-            o[0] += x[j][0] * w;
-            o[1] += x[j][1] * w;
+        for (uint32_t j = 0; j < kAtOnce; ++j) join(st[j], x[j][0], x[j][1], top);
+    }
+    if (lanes > 1) {
+        if (place < kSlots) {
+            sums[place][c][0] = o[0];
+            sums[place][c][1] = o[1];
+            if (c == 0) stats[place] = float2v{m, l};
+        }
+        __syncthreads();
+        if (first == 0 && have) {
+            float top = m;
+            for (uint32_t j = 1; j < lanes; ++j) top = fmaxf(top, stats[place + j][0]);
+            const float f = top == -INFINITY ? 1.f : power2(m - top);
+            m = top;
+            l *= f;
+            o[0] *= f;
+            o[1] *= f;
+            for (uint32_t j = 1; j < lanes; ++j) join(stats[place + j], sums[place + j][c][0], sums[place + j][c][1], top);
         }
     }
+    if (!have || first != 0 || finished_already) return;
     const uint32_t in = fast_div(row, a.by_n_q), i = row - in * a.n_q, head = h * a.group + in;
     *reinterpret_cast<uint4v*>(a.out + s * a.out_strides[0] + i * a.out_strides[1] + head * a.out_strides[2] + 8 * c) = finished(o, l);
     if (a.lse && c == 0) a.lse[((int64_t)s * a.n_q + i) * a.n_heads + head] = lse_of(m, l);
@@ -759,9 +785,9 @@ hipError_t launch_attend<KVC_HEAD_DIM>(const AttendArgs& a, hipStream_t s) {
     hipError_t e;
     if constexpr (D <= 192) e = a.own_rows == 32 ? launch_parts<D, 2>(a, s) : launch_parts<D, 1>(a, s);
     else e = launch_parts<D, 1>(a, s);
-    constexpr uint32_t rows = 256 / (D / 8);
-    if (e == hipSuccess && !a.direct) e = launch_kernel(k_join<D>, dim3((unsigned)(((int64_t)a.n_seq * a.n_kv * a.rows + rows - 1) / rows)), dim3(256), s, a);
-    return e;
+    if (e != hipSuccess || a.direct) return e;
+    const uint32_t rows = 256 / (D / 8) / a.join_lanes;
+    return launch_kernel(k_join<D>, dim3((unsigned)(((int64_t)a.n_seq * a.n_kv * a.rows + rows - 1) / rows)), dim3(256), s, a);
 }
 
 }  // namespace kvc

@@ -94,6 +94,7 @@ struct AttendArgs {
     FastDiv by_N, by_rows, by_n_q;
     DevState* st;
     // the workspace, see AttendPlan
+    uint32_t join_lanes;  // threads that share the pieces of a row's eight channels
     uint32_t own_tiles;  // row tiles of one sequence and KV head
     uint32_t own_workers, prefix_workers, own_rows, prefix_rows;
     bool direct;  // a workgroup for every unit, and nothing else
@@ -113,7 +114,10 @@ struct AttendPlan {
     uint64_t rows, slots, starts;    // query rows; slots; bytes of the sums of tiles
     uint64_t bytes;
 };
-constexpr uint32_t kOwnWorkers = 2048, kPrefixWorkers = 256;  // waves, workgroups: with 2 of either, or 2 and 1, what the GPU holds at once
+// The sequences' own tokens: a wave on each SIMD.  (8 KB of keys and 8 KB of values on their way for each are enough; of 2,048 waves each has half as much, and as much to begin
+// with: 64 sequences of 512 to 8,192 tokens, 8 x 128, 217 us with 2,048, 211 with 1,024; 8 of 1,024 to 2,048, 32 x 128, 37.3 and 36.8; 4 of 1,000 to
+// 4,000 26.4 and 20.6.)  Prefixes: as many workgroups as the GPU holds at once, or half of them.
+constexpr uint32_t kOwnWorkers = 1024, kPrefixWorkers = 256;
 constexpr uint32_t kPrefixWaves = 4;                          // of a workgroup
 
 // Up to so many tiles of prefixes (of 32 tokens, 128 rows and a KV head), half of the workgroups have the prefixes and half the sequences' own tokens; beyond
@@ -133,7 +137,7 @@ inline AttendPlan plan_attend(int64_t n_seq, int64_t n_q, int64_t n_heads, int64
     AttendPlan p;
     p.own_rows = n_heads / n_kv * n_q <= 16 || d > 192 ? 16 : 32;  // (32 rows of wider heads do not fit into the registers)
     p.prefix_rows = 32 * kPrefixWaves;
-    p.own_workers = kOwnWorkers;
+    p.own_workers = (n_prefix && both_fit(d, (int)p.own_rows / 16) ? 2 : 1) * kOwnWorkers;
     p.prefix_workers = n_prefix ? (d <= 128 ? 2 : 1) * kPrefixWorkers : 0;
     p.rows = (uint64_t)(n_seq * n_heads * n_q);
     p.slots = p.rows + 2ull * p.own_workers * p.own_rows + (n_prefix ? p.rows + 2ull * p.prefix_workers * p.prefix_rows : 0);
