@@ -294,7 +294,8 @@ int kvc_append(kvc_ctx* ctx, const kvc_append_t* a, void* stream);
  * prefix_lens[g] tokens of row g of d_prefix_table where prefix_first[g] <= s < prefix_first[g+1].  With
  * x_t = scale * <q, k_t> and m = max x_t:  out = sum e^(x_t - m) v_t / sum e^(x_t - m), and, where asked for,
  * lse = m + ln sum e^(x_t - m).  Tokens without a block do not exist: what memory holds in their place, and
- * behind the last token, is never read into a sum.  A query that sees no token gets out = 0, lse = -inf.
+ * behind the last token, is never read into a sum, and an infinite or NaN value of one of the last tokens only into
+ * those of the queries that see it.  A query that sees no token gets out = 0, lse = -inf.
  * Each prefix is read once for its group, not once for every sequence.  Lengths beyond their table's row set
  * KVC_ST_BAD_INDEX and are cut to it.  Sums, maxima and products are held in 32 bits; the weights e^(x_t - m)
  * are rounded to FP16 (11 bits, far from its smallest numbers) for the product with the values.
@@ -315,7 +316,7 @@ typedef struct {
     const int32_t* d_prefix_lens;  /* [n_prefix] */
     const int32_t* d_prefix_first; /* [n_prefix + 1], non-decreasing, 0..n_seq; sequences outside all groups have no prefix */
     int32_t max_blocks, max_prefix_blocks, n_prefix, n_seq, n_q, n_heads, n_kv_heads;
-    float scale;
+    float scale;                   /* finite */
     void* d_work;
     uint64_t work_bytes;
 } kvc_attend_t;

@@ -48,26 +48,30 @@ struct Source {
     uint32_t len;       // tokens, at most the row's blocks hold
 };
 
-// Blocks of the 32 tokens from t on that a lane needs, as the table names them; -1: none, or the token is behind the end.
-// EIGHT: N is a multiple of 8, so that 8 tokens from a multiple of 8 on share a block.
+// Blocks of the 32 tokens from t on, as the table names them; -1: none, or the token is behind the end.  Where 8 tokens from a multiple of 8 on share a
+// block (EIGHT: N is a multiple of 8) a lane holds the two that it needs, of its keys and of its values; else that of token `lane` mod 32, and asks the others.
 template <bool EIGHT>
 struct Blocks {
-    int32_t k[EIGHT ? 1 : 2], v[EIGHT ? 1 : 8];
+    int32_t of[EIGHT ? 2 : 1];
+
+    __device__ int32_t key(int u) const { return EIGHT ? of[0] : __shfl(of[0], 8 * ((threadIdx.x & 15) >> 2) + 4 * u + (threadIdx.x & 3)); }
+    __device__ int32_t value(int j) const { return EIGHT ? of[EIGHT ? 1 : 0] : __shfl(of[0], 8 * ((threadIdx.x & 63) >> 4) + j); }
+    // token of t.. whose block of[i] is
+    __device__ static uint32_t token(int i) {
+        const uint32_t lane = threadIdx.x & 63;
+        return !EIGHT ? lane & 31 : i == 0 ? 8 * ((lane & 15) >> 2) : 8 * (lane >> 4);
+    }
+    __device__ void end_at(uint32_t t, uint32_t len) {  // no blocks from token len on
+#pragma unroll
+        for (int i = 0; i < (EIGHT ? 2 : 1); ++i) of[i] = t + token(i) < len ? of[i] : -1;
+    }
 };
 __device__ inline int32_t block_of(const AttendArgs& a, const Source& s, uint32_t t) { return t < s.len ? s.table[fast_div(t, a.by_N)] : -1; }
 template <bool EIGHT>
 __device__ inline Blocks<EIGHT> find_blocks(const AttendArgs& a, const Source& s, uint32_t t) {
-    const uint32_t lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     Blocks<EIGHT> b;
-    if constexpr (EIGHT) {
-        b.k[0] = block_of(a, s, t + 8 * (n >> 2));
-        b.v[0] = block_of(a, s, t + 8 * g);
-    } else {
 #pragma unroll
-        for (int u = 0; u < 2; ++u) b.k[u] = block_of(a, s, t + 8 * (n >> 2) + 4 * u + (n & 3));
-#pragma unroll
-        for (int j = 0; j < 8; ++j) b.v[j] = block_of(a, s, t + 8 * g + j);
-    }
+    for (int i = 0; i < (EIGHT ? 2 : 1); ++i) b.of[i] = block_of(a, s, t + b.token(i));
     return b;
 }
 __device__ inline bool in_cache(const AttendArgs& a, int32_t block) {
@@ -96,8 +100,9 @@ __device__ inline void load_keys(Tokens<D>& x, const AttendArgs& a, const Source
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
         if (u == 0 || !EIGHT) {
-            have = in_cache(a, b.k[EIGHT ? 0 : u]);
-            at = place(a, b.k[EIGHT ? 0 : u], first + 4 * u);
+            const int32_t block = b.key(u);
+            have = in_cache(a, block);
+            at = place(a, block, first + 4 * u);
         }
         const uint16_t* row = have && first + 4 * u < s.len ? s.k + at + (EIGHT ? 4 * u * a.g.row_stride : 0) : kZeroRow;
 #pragma unroll
@@ -135,8 +140,9 @@ __device__ inline uint32_t load_values(Tokens<D>& x, const AttendArgs& a, const 
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         if (j == 0 || !EIGHT) {
-            have = in_cache(a, b.v[EIGHT ? 0 : j]);
-            at = place(a, b.v[EIGHT ? 0 : j], first + j);
+            const int32_t block = b.value(j);
+            have = in_cache(a, block);
+            at = place(a, block, first + j);
         }
         const bool here = have && first + j < s.len;
         there |= here ? 1u << j : 0u;
@@ -217,22 +223,89 @@ __device__ inline half8 weights(Rows<D>& r, const float4v (&s)[2], float scale_l
     return p;
 }
 
+// Eight tokens' values of the lane's channel of output tile j of piece P.
+template <int D, int P>
+__device__ inline uint4v value_column(const Tokens<D>& x, int j) {
+    uint4v v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        v[e] = __builtin_amdgcn_perm(x.v[2 * e + 1][Piece<D, P>::regs + j / 2], x.v[2 * e][Piece<D, P>::regs + j / 2], j & 1 ? 0x07060302u : 0x05040100u);
+    return v;
+}
+
 template <int D, int R, int P = 0>
 __device__ inline void add_values(Rows<D> (&r)[R], const Tokens<D>& x, const half8 (&p)[R]) {
     if constexpr (P < piece_count(D)) {
         using Q = Piece<D, P>;
 #pragma unroll
         for (int j = 0; j < Q::w; ++j) {
-            uint4v v;
+            const half8 v = __builtin_bit_cast(half8, value_column<D, P>(x, j));
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                v[e] = __builtin_amdgcn_perm(x.v[2 * e + 1][Q::regs + j / 2], x.v[2 * e][Q::regs + j / 2], j & 1 ? 0x07060302u : 0x05040100u);
-#pragma unroll
-            for (int i = 0; i < R; ++i)
-                r[i].o[Q::before / 16 + j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, v), p[i], r[i].o[Q::before / 16 + j], 0, 0, 0);
+            for (int i = 0; i < R; ++i) r[i].o[Q::before / 16 + j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p[i], r[i].o[Q::before / 16 + j], 0, 0, 0);
         }
         add_values<D, R, P + 1>(r, x, p);
     }
+}
+
+// Where a tile holds tokens that some rows see and others do not, a value that is infinite or NaN must reach the former alone, and weight zero times it is
+// NaN.  In such a tile these values are counted (a product of ones), the rows that see any get the infinity, or both, and the values become zero.
+// 1.0 in each half that is an infinity of this sign, or NaN
+__device__ inline uint32_t ones_where(uint32_t v, uint32_t infinity) {
+    const uint32_t lo = v & 0xFFFFu, hi = v >> 16;
+    return (lo == infinity || (lo & 0x7FFFu) > 0x7C00u ? 0x3C00u : 0u) | (hi == infinity || (hi & 0x7FFFu) > 0x7C00u ? 0x3C000000u : 0u);
+}
+template <int D, int R, int P = 0>
+__device__ inline void add_infinite(Rows<D> (&r)[R], const Tokens<D>& x, const half8 (&seen)[R]) {
+    if constexpr (P < piece_count(D)) {
+        using Q = Piece<D, P>;
+#pragma unroll
+        for (int j = 0; j < Q::w; ++j) {
+            const uint4v v = value_column<D, P>(x, j);
+#pragma unroll
+            for (uint32_t sign = 0; sign < 2; ++sign) {
+                uint4v one;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) one[e] = ones_where(v[e], sign ? 0xFC00u : 0x7C00u);
+#pragma unroll
+                for (int i = 0; i < R; ++i) {
+                    const float4v n = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, one), seen[i], float4v{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) r[i].o[Q::before / 16 + j][e] += n[e] > 0.f ? (sign ? -INFINITY : INFINITY) : 0.f;
+                }
+                __builtin_amdgcn_sched_barrier(0);  // (one at a time: there are few registers)
+            }
+        }
+        add_infinite<D, R, P + 1>(r, x, seen);
+    }
+}
+
+// The tile from t on of a sequence of `len` tokens, of whose last n_q - 1 some rows see less than others.
+template <int D, int R>
+__device__ inline void add_tile(Rows<D> (&r)[R], Tokens<D>& x, const half8 (&p)[R], uint32_t t, uint32_t len, uint32_t n_q, const uint32_t (&limit)[R]) {
+    if (n_q > 1 && t + kTile + n_q - 1 > len) {
+        uint32_t carry = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int e = 0; e < D / 32; ++e) carry |= (x.v[j][e] & 0x7C007C00u) + 0x04000400u;  // an exponent of ones carries into the sign
+        if (__any(carry & 0x80008000u)) {
+            const uint32_t first = t + 8 * ((threadIdx.x & 63) >> 4);
+            half8 seen[R];
+#pragma unroll
+            for (int i = 0; i < R; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) seen[i][j] = first + j < limit[i] ? (_Float16)1.f : (_Float16)0.f;
+            add_infinite<D, R>(r, x, seen);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int e = 0; e < D / 32; ++e) {
+                    const uint32_t all = ((x.v[j][e] & 0x7C007C00u) + 0x04000400u) >> 15 & 0x00010001u;
+                    x.v[j][e] &= ~(all * 0xFFFFu);
+                }
+        }
+    }
+    add_values<D, R>(r, x, p);
 }
 
 template <int D, int P>

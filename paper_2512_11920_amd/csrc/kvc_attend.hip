@@ -229,7 +229,7 @@ __device__ inline void own_part(const AttendArgs& a, Sums& sums, uint32_t worker
         half8 p[R];
 #pragma unroll
         for (int j = 0; j < R; ++j) p[j] = weights(r[j], s[j], a.scale_log2, there, c.t * kTile, limit[j]);
-        add_values<D, R>(r, x, p);
+        add_tile<D, R>(r, x, p, c.t * kTile, c.len, a.n_q, limit);
         if (left > 1) there = load_values<D, EIGHT>(x, a, source(c1), b, c1.t * kTile);
         if (left == 1 || c1.t == 0) {
             close(c, first_tile);
@@ -337,7 +337,7 @@ __device__ inline void prefix_part(const AttendArgs& a, Sums& sums, PrefixTiles<
 #pragma unroll
         for (uint32_t v = 0; v < kValues; ++v) value_at[e][v] = 16 * ((8 * e + vrow) * C + ((4 * v + vc) ^ L::turn(8 * e + vrow))) + 8 * (l16 & 1);
 
-    const float scale = fabsf(a.scale_log2);
+    const float scale = fmaxf(fabsf(a.scale_log2), 1e-38f);  // (of zero too, so that times the -infinity of a token that does not exist it is no NaN)
     const uint32_t flip = a.scale_log2 < 0.f ? 0x80008000u : 0u;  // a negative scale is the queries' sign
     const uint32_t blocks = (uint32_t)min(a.n_cache_blocks, (int64_t)INT32_MAX);
     // From tile to tile a token's place moves on by 32 tokens: so many blocks and so many rows, and another block where that leaves the block.
@@ -604,27 +604,20 @@ __global__ __launch_bounds__(64 * kDirectWaves, D * R <= 128 ? 2 : 1) void k_dir
     const uint32_t tiles = (src.len + kTile - 1) / kTile;
     for (uint32_t t = wave; t < tiles; t += kDirectWaves) {
         if (t != wave) b = find_blocks<EIGHT>(a, src, t * kTile);
-        // (entries behind the last token are not block numbers)
-        if constexpr (EIGHT) {
-            b.k[0] = t * kTile + 8 * (n >> 2) < src.len ? b.k[0] : -1;
-            b.v[0] = t * kTile + 8 * g < src.len ? b.v[0] : -1;
-        } else {
-#pragma unroll
-            for (int j = 0; j < 2; ++j) b.k[j] = t * kTile + 8 * (n >> 2) + 4 * j + (n & 3) < src.len ? b.k[j] : -1;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) b.v[j] = t * kTile + 8 * g + j < src.len ? b.v[j] : -1;
-        }
+        b.end_at(t * kTile, src.len);  // (entries behind the last token are not block numbers)
         Tokens<D> x;
         load_keys<D, EIGHT>(x, a, src, b, t * kTile);
         const uint32_t there = load_values<D, EIGHT>(x, a, src, b, t * kTile);
         half8 p[R];
+        uint32_t limit[R];
 #pragma unroll
         for (int j = 0; j < R; ++j) {
             float4v sc[2];
             scores(sc, r[j], x);
-            p[j] = weights(r[j], sc, a.scale_log2, there, t * kTile, min(len > later[j] ? len - later[j] : 0, src.len));
+            limit[j] = min(len > later[j] ? len - later[j] : 0, src.len);
+            p[j] = weights(r[j], sc, a.scale_log2, there, t * kTile, limit[j]);
         }
-        add_values<D, R>(r, x, p);
+        add_tile<D, R>(r, x, p, t * kTile, src.len, a.n_q, limit);
     }
     const uint32_t workers = min(tiles, kDirectWaves);
 #pragma unroll

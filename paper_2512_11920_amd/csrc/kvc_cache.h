@@ -128,7 +128,7 @@ constexpr int64_t kApartTiles = 40960;
 // A call without prefixes whose tables hold at most so many tiles of 32 tokens is done by a workgroup of 8 waves for each unit, in one launch: one sequence of
 // 256 tokens, 4 heads x 64, 6.4 us instead of 9.7.
 constexpr uint32_t kDirectWaves = 8, kDirectTiles = 16;
-constexpr bool direct_fits(int d, int row_tiles) { return d * row_tiles <= 256; }  // into LDS
+constexpr bool direct_fits(int d, int row_tiles) { return d <= 224 && d * row_tiles <= 256; }  // into LDS and 256 registers
 
 // Whether the kernel that does both parts keeps two workgroups of its own on a compute unit (256 registers).
 constexpr bool both_fit(int d, int row_tiles) { return d * row_tiles <= 128; }

@@ -1,4 +1,6 @@
 // Entry points of the decode-step operators (see include/kvc.h): argument checks and kernel launches only.
+#include <cmath>
+
 #include "kvc_cache.h"
 #include "kvc_ctx.h"
 
@@ -78,6 +80,7 @@ int kvc_attend(kvc_ctx* ctx, const kvc_attend_t* p, void* stream) {
     if (product(own_tiles * p->n_kv_heads, p->n_seq, own_tokens / 32 + 1) > INT32_MAX) return KVC_ERR_ARG;
     if (p->n_prefix && product(prefix_tiles, p->n_kv_heads, prefix_tokens / 32 + 1) > INT32_MAX) return KVC_ERR_ARG;
     if (!p->d_work || !aligned(p->d_work, 256) || p->work_bytes < plan.bytes) return KVC_ERR_ARG;
+    if (!std::isfinite(p->scale * 1.44269504088896341f)) return KVC_ERR_ARG;
     AttendArgs a;
     a.q = static_cast<const uint16_t*>(p->d_q);
     a.out = static_cast<uint16_t*>(p->d_out);

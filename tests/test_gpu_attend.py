@@ -55,7 +55,7 @@ def _dev_cache(x, c):
     return t.transpose(1, 2).contiguous() if c["token_major"] else t
 
 
-def _run(c, lse=True, stream=None):
+def _run(c, lse=True, scale=None):
     """-> codec, out, lse of a call, with the queries as a slice of a wider tensor."""
     N, d, kv, ppb = c["N"], c["d"], c["kv"], c["ppb"]
     codec = kvc.Codec(N, d, ppb)
@@ -71,7 +71,7 @@ def _run(c, lse=True, stream=None):
     kw = {}
     if n_prefix:
         kw = {k_: torch.from_numpy(c[k_]).to(DEV) for k_ in ("prefix_table", "prefix_lens", "prefix_first")}
-    codec.attend(out, q, k, torch.from_numpy(c["table"]).to(DEV), torch.from_numpy(c["lens"]).to(DEV), work, v_cache=v, lse=sums, **kw)
+    codec.attend(out, q, k, torch.from_numpy(c["table"]).to(DEV), torch.from_numpy(c["lens"]).to(DEV), work, v_cache=v, lse=sums, scale=scale, **kw)
     torch.cuda.synchronize()
     return codec, out.cpu().numpy().astype(np.float64), None if sums is None else sums.cpu().numpy().astype(np.float64)
 
@@ -83,8 +83,8 @@ def _want(c, scale=None):
                       c["prefix_table"], c["prefix_lens"], c["prefix_first"])
 
 
-def _compare(c, out, lse):
-    want, wl, bound, lb = _want(c)
+def _compare(c, out, lse, scale=None):
+    want, wl, bound, lb = _want(c, scale)
     off = np.abs(out - want)
     assert np.isfinite(out).all()
     assert (off <= bound).all(), (np.argwhere(off > bound)[:5], off.max(), (off / bound).max())
@@ -227,6 +227,38 @@ def test_infinities_in_seen_tokens_come_through():
     assert np.isfinite(out[0]).all()
     assert np.isinf(out[2, 0, :, 7]).all() and np.isfinite(np.delete(out[2, 0], 7, axis=1)).all()
     assert (np.isnan(out[1, 0]) == np.isnan(want[1, 0])).all()
+
+
+@pytest.mark.parametrize("d,kv,group,q,N,prefix", [(64, 2, 2, 3, 16, ()), (128, 1, 8, 1, 16, (70,)), (128, 1, 4, 4, 6, (70,)), (96, 2, 4, 9, 8, ()), (192, 1, 8, 4, 16, (33,)), (256, 1, 2, 2, 8, ())])
+def test_infinite_values_reach_only_the_queries_that_see_them(d, kv, group, q, N, prefix):
+    """Of the last tokens, the earlier queries see fewer; and where the sequence is shorter than the queries are many, the first see none."""
+    rng = np.random.default_rng([17, d, q])
+    lens = [1, 2, 31, 32, 33, 64, 65, 100, 700]
+    c = _setup(rng, N, d, kv, group, q, lens, prefix=prefix, first=(0, 5) if prefix else (0,))
+    for s, n in enumerate(lens):
+        for back in range(1, min(q, n) + 1):
+            t = n - back
+            at = c["table"][s, t // N], slice(kv, 2 * kv), t % N
+            bad = rng.integers(0, d, 3)
+            c["k"][at][:, bad] = np.array([np.inf, -np.inf, np.nan], np.float16)
+    _, out, lse = _run(c)
+    with np.errstate(invalid="ignore"):
+        want, wl, bound, lb = _want(c)
+    fine = np.isfinite(want)
+    assert (np.isnan(out) == np.isnan(want)).all()
+    assert (out[~fine & ~np.isnan(want)] == want[~fine & ~np.isnan(want)]).all()
+    assert (np.abs(out - want)[fine] <= bound[fine]).all()
+    none = np.isneginf(wl)
+    assert np.isneginf(lse[none]).all() and (np.abs(lse[~none] - wl[~none]) <= lb[~none]).all()
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.2, 1e-30])
+@pytest.mark.parametrize("d,q,N", [(64, 1, 16), (128, 3, 6), (192, 2, 16)])
+def test_scales_of_zero_and_below(scale, d, q, N):
+    rng = np.random.default_rng([18, d])
+    c = _setup(rng, N, d, 2, 4, q, [50, 20, 0, 333, 1], prefix=(40, 97, 600), first=(0, 2, 4, 5), holes=0.3)
+    _, out, lse = _run(c, scale=scale)
+    _compare(c, out, lse, scale)
 
 
 def test_bad_entries_are_passed_over_and_reported():
@@ -391,6 +423,9 @@ def test_refusals():
             continue
         with pytest.raises(kvc.KvcError):
             codec.attend(**{**good, **bad})
+    for scale in (float("nan"), float("inf"), 3e38):
+        with pytest.raises(kvc.KvcError):
+            codec.attend(**{**good, "scale": scale})
     for sizes in ((1, 1, 5, 2, 64), (1, 0, 4, 2, 64), (1, 1, 4, 2, 60), (-1, 1, 4, 2, 64), (1, 1, 4, 0, 64)):
         with pytest.raises(kvc.KvcError):
             kvc.attend_workspace(*sizes)
