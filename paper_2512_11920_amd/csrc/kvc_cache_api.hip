@@ -235,7 +235,7 @@ int kvc_compact_pool(kvc_ctx* ctx, void* d_pool_out, uint64_t pool_out_bytes, kv
     a.desc_out = d_desc_out;
     a.n_desc = ctx->n_desc;
     a.groups = compact_groups(ctx->pool_bytes);
-    if (a.units / 16384 + a.n_desc / 256 > (uint64_t)kMaxGroups - 2 || a.groups * 4 > (uint64_t)kMaxGroups) return KVC_ERR_ARG;
+    if (a.groups * 64 + a.n_desc / 256 > (uint64_t)kMaxGroups - 1) return KVC_ERR_ARG;
     uint8_t* w = static_cast<uint8_t*>(d_work);
     a.bits = reinterpret_cast<unsigned long long*>(w);
     w += a.groups * kGroupWords * 8;
