@@ -284,6 +284,7 @@ template <int D>
 struct PrefixTiles {
     uint4v tile[kStages][2][32 * Layout<D>::C];   // [stage][keys, values]
     uint32_t ids[kPrefixWaves][kAhead][64];       // [wave][tile]: block of token n
+    uint64_t rows[kPrefixWaves][32];              // [wave]: where the next tile's rows are
 };
 
 // The part of workgroup `worker`.
@@ -292,6 +293,7 @@ __device__ inline void prefix_part(const AttendArgs& a, Sums& sums, PrefixTiles<
     using L = Layout<D>;
     auto& tile = lds.tile;
     auto& ids = lds.ids;
+    auto& rows_at = lds.rows;
     constexpr uint32_t C = L::C, kLoads = C / kPrefixWaves, kRows = 32 * kPrefixWaves, kKeys = (L::kMask + 1) / 2, kValues = (L::kMask + 1) / 4;
     const auto row_tiles = [&](uint32_t g) {
         const Range r = group_of_prefix(a, g);
@@ -390,18 +392,23 @@ __device__ inline void prefix_part(const AttendArgs& a, Sums& sums, PrefixTiles<
             load_to_lds<4>(reinterpret_cast<uint64_t>(table) + 4ull * (i * kTile + n < len ? entry : 0), &ids[wave][i % kAhead][0]);
             entry += step_blocks + (next_row(row) ? 1 : 0);
         };
-        // loads tile i; -> which of its tokens exist
-        const auto load = [&](uint32_t i, uint32_t stage) {
+        // finds the rows of tile i (tiles in order), for `load`; -> which of its tokens exist
+        const auto locate = [&](uint32_t i) {
             const uint32_t block = ids[wave][i % kAhead][lane];
             const bool seen = i * kTile + n < len, there = seen && block < blocks;
             bad = bad || (seen && (int32_t)block >= 0 && !there);
-            const uint64_t at = ((uint64_t)block * block_stride + row_now) * 16 + reinterpret_cast<uint64_t>(pages), zero = reinterpret_cast<uint64_t>(kZeroRow);
+            const uint64_t at = ((uint64_t)block * block_stride + row_now) * 16 + reinterpret_cast<uint64_t>(pages);
             next_row(row_now);
-            const int lo = there ? (int)at : (int)zero, hi = there ? (int)(at >> 32) : (int)(zero >> 32);
-#pragma unroll
-            for (uint32_t j = 0; j < kLoads; ++j)
-                load_to_lds<16>(((uint32_t)__shfl(lo, token(j)) | (uint64_t)(uint32_t)__shfl(hi, token(j)) << 32) + from(j), &tile[stage][kind][(half * kLoads + j) * 64]);
+            rows_at[wave][n] = there ? at : reinterpret_cast<uint64_t>(kZeroRow);
             return (uint32_t)__ballot(there);
+        };
+        // loads the tile that was located last (a wave's accesses to LDS are in order, so its lanes need not wait for each other)
+        const auto load = [&](uint32_t stage) {
+            uint64_t at[kLoads];
+#pragma unroll
+            for (uint32_t j = 0; j < kLoads; ++j) at[j] = rows_at[wave][token(j)];
+#pragma unroll
+            for (uint32_t j = 0; j < kLoads; ++j) load_to_lds<16>(at[j] + from(j), &tile[stage][kind][(half * kLoads + j) * 64]);
         };
         // scores of a tile, in powers of two but for `scale`
         const auto make_scores = [&](float16v& x, uint32_t stage) {
@@ -434,19 +441,23 @@ __device__ inline void prefix_part(const AttendArgs& a, Sums& sums, PrefixTiles<
             for (int c = 0; c < D / 32; ++c) o[c] *= f;
         };
 
-        // Tiles 0..2 on their way, and the blocks of tiles 3 and 4; mask[k]: the tokens of tile i + 1 + k that exist.  What comes back comes in order: the next
-        // tile and the blocks of the one to be loaded next are there when only what the last step asked for is missing.
-        uint32_t mask[2];
+        // Tiles 0..2 on their way, the rows of tile 3 located, and the blocks of tiles 4 and 5 asked for; mask[k]: the tokens of tile i + 1 + k that exist.  What comes back
+        // comes in order: the next tile and the blocks of the one to be located next are there when only what the last step asked for is missing.
+        uint32_t mask[3];
 #pragma unroll
-        for (uint32_t i = 0; i < 4; ++i) look_up(i);
+        for (uint32_t i = 0; i < 5; ++i) look_up(i);
         wait_for_loads<0>();
         __syncthreads();  // (and the tiles of the last piece have been read)
         float16v s;
         {
-            const uint32_t there = load(0, 0);
-            mask[0] = load(1, 1);
-            mask[1] = load(2, 2);
-            look_up(4);
+            const uint32_t there = locate(0);
+            load(0);
+            mask[0] = locate(1);
+            load(1);
+            mask[1] = locate(2);
+            load(2);
+            mask[2] = locate(3);
+            look_up(5);
             wait_for_loads<2 * kLoads + 1>();
             __syncthreads();
             make_scores(s, 0);
@@ -458,6 +469,7 @@ __device__ inline void prefix_part(const AttendArgs& a, Sums& sums, PrefixTiles<
             // tile i + 1 is there, and every wave is done with tile i - 1, whose place tile i + 3 takes
             wait_for_loads<kLoads + 1>();
             __syncthreads();
+            load((stage + 3) % kStages);  // (first of all: a prefix of 32,768 tokens and 256 sequences, 8 x 128, 482 us, 488 in the midst of the products, 495 behind them)
             // the next tile's scores, while this one's become weights
             float16v next;
             make_scores(next, (stage + 1) % kStages);  // (behind the last tile, of what lies there; it is not used)
@@ -497,14 +509,15 @@ __device__ inline void prefix_part(const AttendArgs& a, Sums& sums, PrefixTiles<
             __builtin_amdgcn_sched_barrier(0);
             if (mask[0] != ~0u) hide(next, mask[0]);
             mask[0] = mask[1];
+            mask[1] = mask[2];
             read_values(1);
 #pragma unroll
             for (uint32_t j = 0; j < 2; ++j)
 #pragma unroll
                 for (uint32_t c = 0; c < D / 32; ++c) o[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[j][c], p[j], o[c], 0, 0, 0);
             const float top = largest(next);
-            mask[1] = load(i + 3, (stage + 3) % kStages);
-            look_up(i + 5);
+            mask[2] = locate(i + 4);
+            look_up(i + 6);
             if (i + 1 < n_tiles) follow(top);
             s = next;
         };
