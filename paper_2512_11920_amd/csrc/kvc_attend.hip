@@ -120,9 +120,11 @@ __device__ inline uint4v finished(const float4v (&o)[2], float l) {
     return v;
 }
 
-// ---- the sequences' own tokens.  A worker is a wave: tiles of 32 tokens go from memory to its registers, keys of the next tile while this
+// ---- the sequences' own tokens: bound by memory, as a token's keys and values serve only the few rows of one head's group.  A worker is a wave: tiles of 32 tokens go from memory to its registers, keys of the next tile while this
 // one's scores become weights, values while the next scores are made, so that a tile is always on its way; the block table is read one
 // tile further ahead.  R: tiles of 16 rows that share the tokens.
+// 64 sequences of 512 to 8,192 tokens, 8 x 128, 8 rows (1.14 GB): 207 us, 5.5 TB/s, a copy's rate; 8 of 1,024 to 2,048, 32 x 128, a row each (201 MB): 33 us, 6.0 TB/s.  Short calls are bound
+// by reads of memory that wait for each other (lengths, table, keys, and the join's): one sequence of 8,192 tokens, 8 x 128, 16.5 us.
 struct Place {
     uint32_t s, u, t, tiles, len;  // sequence; unit u of it (head and row tile); tile t of `tiles`
 };
@@ -244,7 +246,12 @@ __device__ inline void own_part(const AttendArgs& a, Sums& sums, uint32_t worker
     }
 }
 
-// ---- prefixes.  A worker is a workgroup: 32 rows of a group a wave share tiles of 32 tokens in LDS, of which four are there: the present one, two on their way ...
+// ---- prefixes: many rows share the tokens, and the products count.  A worker is a workgroup: 32 rows of a group to a wave, and the waves share tiles of 32 tokens in LDS,
+// which go there straight from memory, a quarter of each by every wave.  There is room for four: one is used, the next is there, two are on their way.  A step has one barrier: behind
+// it the next tile's scores are made beside the present one's weights, then the present one's values are added.  32 rows a wave, as 64 leave room in the registers for one
+// wave on a SIMD only (600 us instead of 418 where it was tried), and two workgroups of 4 waves rather than one of 8, so that one computes while the other waits (418 and 448).
+// 32,768 tokens, 16,384 rows, 128 channels (275 GFLOP): 336 us, 820 TFLOP/s, where a large product of matrices reaches 1,280.  A wave's step takes 1,360 cycles of its SIMD: 512 of products, and what
+// of the rest does not fit beside them: reading LDS (512 for a workgroup), loads to LDS (317), 125 vector instructions, 17 of them powers.
 constexpr uint32_t kStages = 4, kAhead = 8;
 typedef float float16v __attribute__((ext_vector_type(16)));
 typedef short short4v __attribute__((ext_vector_type(4)));
@@ -573,7 +580,7 @@ __global__ __launch_bounds__(64 * kPrefixWaves, D <= 128 ? 2 : 1) void k_prefix(
 }
 
 // Both in one launch, two workgroups on each compute unit: the first half of them begins with prefixes, which keep the matrix units busy, the other with
-// the sequences' own tokens, which keep the memory busy; then they change.  Where there is little to do for prefixes (a.apart) each half does its own alone.
+// the sequences' own tokens, which keep the memory busy; then they change: a prefix of 32,768 tokens and 256 sequences of 1 to 2,048, 8 x 128, 8 rows, 471 us, and 336 + 190 by themselves.  Where there is little to do for prefixes (a.apart) each half does its own alone.
 template <int D, int R, bool EIGHT>
 __global__ __launch_bounds__(256, 2) void k_both(AttendArgs a) {
     __shared__ Sums sums;
@@ -591,7 +598,7 @@ __global__ __launch_bounds__(256, 2) void k_both(AttendArgs a) {
 }
 
 // ---- short sequences without a prefix.  A workgroup of kDirectWaves takes a unit, its waves the tiles in turn, and they join their sums in LDS: one launch, and the
-// lengths, the block table and the queries are asked for at once.
+// lengths, the block table and the queries are asked for at once.  Bound by two reads that follow from each other and the launch: 256 tokens, 4 heads x 64, 6 us.
 template <int D, int R, bool EIGHT>
 __global__ __launch_bounds__(64 * kDirectWaves, D * R <= 128 ? 2 : 1) void k_direct(AttendArgs a) {
     __shared__ float2v stats[kDirectWaves][16 * R];
@@ -664,7 +671,8 @@ __global__ __launch_bounds__(64 * kDirectWaves, D * R <= 128 ? 2 : 1) void k_dir
 }
 
 // ---- joining pieces: D / 8 threads for 8 channels each, of a row and every a.join_lanes-th of its pieces.  A thread reads kAtOnce pieces at a time, as each read goes to memory
-// and takes as long as all of them together; where there are few rows, whose pieces are many, threads share them out and join their sums in LDS.
+// and takes as long as all of them together; where there are few rows, whose pieces are many, threads share them out and join their sums in LDS.  4,096 rows of about 10 pieces of 128 channels (21 MB):
+// 7.9 us; one or two pieces: 5 us, the time of the four reads that follow from each other.
 constexpr uint32_t kAtOnce = 8;
 
 // Where the pieces of a unit are, for one of its rows: `n` workers from w0 on have one each, or one has it whole.
@@ -776,6 +784,7 @@ __global__ __launch_bounds__(256) void k_join(AttendArgs a) {
 
 template <int D, int R>
 static hipError_t launch_parts(const AttendArgs& a, hipStream_t s) {
+    // 32 sequences of 1,000 to 8,000 tokens, N = 16, 8 x 128, 32 rows: 130 us with blocks found by eights, 139 without; 64 of 512 to 8,192, 8 rows, 210 either way
     const bool eight = a.g.N % 8 == 0;
     if constexpr (direct_fits(D, R))
         if (a.direct) return launch_kernel(eight ? k_direct<D, R, true> : k_direct<D, R, false>, dim3((unsigned)a.n_seq * a.n_kv * a.own_tiles), dim3(64 * kDirectWaves), s, a);
