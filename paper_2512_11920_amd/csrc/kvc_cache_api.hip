@@ -29,7 +29,7 @@ int kvc_append(kvc_ctx* ctx, const kvc_append_t* p, void* stream) {
     if (!heads_ok(ctx, p->d_v_cache, p->n_kv_heads)) return KVC_ERR_ARG;
     if (p->n_seq == 0 || p->n_new == 0) return KVC_OK;
     if (!on_ctx_device(ctx)) return KVC_ERR_ARG;
-    if (!p->d_k_cache || !p->d_block_table || !p->d_lens || !p->d_k_new || !p->d_v_new) return KVC_ERR_ARG;
+    if (!p->d_k_cache || (!p->d_block_table && p->max_blocks) || !p->d_lens || !p->d_k_new || !p->d_v_new) return KVC_ERR_ARG;
     if (!aligned(p->d_k_cache, 16) || !aligned(p->d_v_cache, 16) || !aligned(p->d_k_new, 16) || !aligned(p->d_v_new, 16)) return KVC_ERR_ARG;
     if (!strides_ok(p->k_strides) || !strides_ok(p->v_strides)) return KVC_ERR_ARG;
     if ((int64_t)p->n_seq * p->n_new > kMaxGroups) return KVC_ERR_ARG;
@@ -65,10 +65,10 @@ int kvc_attend(kvc_ctx* ctx, const kvc_attend_t* p, void* stream) {
     if (!heads_ok(ctx, p->d_v_cache, p->n_kv_heads) || p->n_heads < p->n_kv_heads || p->n_heads % p->n_kv_heads) return KVC_ERR_ARG;
     if (p->n_seq == 0) return KVC_OK;
     if (!on_ctx_device(ctx)) return KVC_ERR_ARG;
-    if (!p->d_q || !p->d_out || !p->d_k_cache || !p->d_block_table || !p->d_lens) return KVC_ERR_ARG;
+    if (!p->d_q || !p->d_out || !p->d_k_cache || (!p->d_block_table && p->max_blocks) || !p->d_lens) return KVC_ERR_ARG;
     if (!aligned(p->d_q, 16) || !aligned(p->d_out, 16) || !aligned(p->d_k_cache, 16) || !aligned(p->d_v_cache, 16)) return KVC_ERR_ARG;
     if (!strides_ok(p->q_strides) || !strides_ok(p->out_strides)) return KVC_ERR_ARG;
-    if (p->n_prefix > 0 && (!p->d_prefix_table || !p->d_prefix_lens || !p->d_prefix_first)) return KVC_ERR_ARG;
+    if (p->n_prefix > 0 && ((!p->d_prefix_table && p->max_prefix_blocks) || !p->d_prefix_lens || !p->d_prefix_first)) return KVC_ERR_ARG;
     // rows are counted in 31 bits, and so are a row's tokens and the tiles of all units
     if ((int64_t)p->n_seq * p->n_heads > (int64_t)INT32_MAX / p->n_q) return KVC_ERR_ARG;
     const int64_t own_tokens = (int64_t)p->max_blocks * ctx->g.N, prefix_tokens = (int64_t)p->max_prefix_blocks * ctx->g.N;
@@ -81,6 +81,7 @@ int kvc_attend(kvc_ctx* ctx, const kvc_attend_t* p, void* stream) {
     if (p->n_prefix && product(prefix_tiles, p->n_kv_heads, prefix_tokens / 32 + 1) > INT32_MAX) return KVC_ERR_ARG;
     if (!p->d_work || !aligned(p->d_work, 256) || p->work_bytes < plan.bytes) return KVC_ERR_ARG;
     if (!std::isfinite(p->scale * 1.44269504088896341f)) return KVC_ERR_ARG;
+    if ((int64_t)plan.rows > kMaxGroups * (2048 / ctx->g.d)) return KVC_ERR_ARG;  // what one launch joins, d / 8 threads a row
     AttendArgs a;
     a.q = static_cast<const uint16_t*>(p->d_q);
     a.out = static_cast<uint16_t*>(p->d_out);

@@ -198,6 +198,17 @@ def test_blocks_that_are_not_there():
     assert (out[0] == 0).all() and np.isneginf(lse[0]).all() and np.isneginf(lse[3]).all()
 
 
+@pytest.mark.parametrize("own,prefix", [(0, 3), (3, 0), (0, 0)])
+def test_tables_of_no_blocks(own, prefix):
+    """Sequences without tokens of their own behind a prefix, a prefix of no blocks, and both: tables of width zero."""
+    rng = np.random.default_rng(19)
+    c = _setup(rng, 16, 64, 2, 2, 1, [16 * own] * 3, prefix=(16 * prefix,), first=(0, 2), room=0)
+    c["table"], c["prefix_table"] = c["table"][:, :own], c["prefix_table"][:, :prefix]
+    _, out, lse = _run(c)
+    _compare(c, out, lse)
+    assert (out[2] == 0).all() == (own == 0)
+
+
 def test_large_scores_leave_one_token():
     """Scores far apart: weights underflow to one token's, running maxima rise late."""
     rng = np.random.default_rng(8)
