@@ -44,9 +44,18 @@ __device__ inline int prefix_of(const AttendArgs& a, int s) {
     return lo > 0 && s < a.prefix_first[lo] ? lo - 1 : -1;
 }
 
+// How the tiles of prefixes are divided: `each` to a worker, or, if `apart`, so many of one unit to a worker, as if units were multiples of it.
+struct Division {
+    uint32_t each, apart;
+    __device__ uint32_t room(uint32_t tiles) const { return apart ? (tiles + each - 1) / each * each : tiles; }
+};
+constexpr uint32_t kPieceCost = 7;
+
 // ---- dividing the work: sums of f(0..n-1), with the items dealt to the 256 threads of a workgroup in runs of `each`.
 struct Sums {
     uint32_t before[256], wave[4], all, each;
+    uint32_t workers[8];
+    Division division;
 };
 template <class F>
 __device__ inline void add_up(Sums& s, uint32_t n, F f) {
@@ -307,15 +316,44 @@ __device__ inline void prefix_part(const AttendArgs& a, Sums& sums, PrefixTiles<
         return ((uint32_t)(r.end - r.begin) * a.rows + kRows - 1) / kRows;
     };
     const auto tiles_of = [&](uint32_t g) { return (prefix_length(a, g) + kTile - 1) / kTile; };
-    const auto work_of = [&](uint32_t g) { return row_tiles(g) * tiles_of(g); };
+    Division div{1, 0};
+    const auto work_of = [&](uint32_t g) { return row_tiles(g) * div.room(tiles_of(g)); };
     // groups out of order could hold a sequence twice, and more rows than there are: none is taken then
     bool disorder = false;
     for (uint32_t i = threadIdx.x; i < (uint32_t)a.n_prefix; i += 256) disorder = disorder || a.prefix_first[i] > a.prefix_first[i + 1];
     const bool ordered = !__syncthreads_or(disorder);
     if (disorder) atomicOr(&a.st->status, KVC_ST_BAD_INDEX);
-    add_up(sums, ordered ? a.n_prefix : 0, work_of);
-    if (worker == 0) write_starts(sums, a.prefix_start, a.n_prefix, work_of);
-    const uint32_t all = uniform(sums.all) * a.n_kv, each = share(all, a.prefix_workers);
+    // A piece takes as long to begin and to end as kPieceCost tiles, so a worker rather has up to so many tiles more than two pieces.  Lanes 32c + g find out how many
+    // workers it would take if each had c tiles more than an even share, but of one unit.  45 sequences in 5 groups, 6 x 96, N = 24, prefixes of a few hundred: 30 us, 33 by even shares;
+    // 151 sequences in 6 groups, 8 x 160: 58 and 73; a prefix of 4,096 for 64 sequences, whose even shares are parts of one unit each, 38.2 and 37.6.
+    if (a.n_prefix <= 32 && (uint32_t)(a.n_prefix * a.n_kv) <= a.prefix_workers) {
+        const uint32_t g = threadIdx.x % 32, c = threadIdx.x / 32;
+        const bool have = ordered && g < (uint32_t)a.n_prefix;
+        const uint32_t rts = have ? row_tiles(g) : 0, tiles = have ? tiles_of(g) : 0;
+        uint32_t total = rts * tiles;
+        for (int k = 1; k < a.n_prefix; k *= 2) total += __shfl_xor(total, k);
+        div.each = share(uniform(total) * a.n_kv, a.prefix_workers);
+        uint32_t n = min(rts * ((tiles + div.each + c - 1) / (div.each + c)), a.prefix_workers + 1);
+        for (int k = 1; k < a.n_prefix; k *= 2) n += __shfl_xor(n, k);
+        if (g == 0) sums.workers[c] = n * a.n_kv;
+        __syncthreads();
+        uint32_t more = kPieceCost + 1;
+#pragma unroll
+        for (uint32_t k = kPieceCost + 1; k-- > 0;) more = uniform(sums.workers[k]) <= a.prefix_workers ? k : more;
+        div.apart = more <= kPieceCost;
+        div.each += div.apart ? more : 0;
+        add_up(sums, ordered ? a.n_prefix : 0, work_of);
+    } else {
+        add_up(sums, ordered ? a.n_prefix : 0, work_of);
+        div.each = share(uniform(sums.all) * a.n_kv, a.prefix_workers);
+    }
+    if (worker == 0) {
+        write_starts(sums, a.prefix_start, a.n_prefix, work_of);
+        if (threadIdx.x == 0) a.prefix_start[a.n_prefix + 1] = div.each << 1 | (div.apart ? 1 : 0);
+    }
+    if (threadIdx.x == 0) sums.division = div;  // (kept here: there are few registers)
+    __syncthreads();
+    const uint32_t all = uniform(sums.all) * a.n_kv, each = div.each;
     const uint32_t begin = worker * each;
     if (begin >= all) return;
     uint32_t left = min(each, all - begin);
@@ -337,14 +375,16 @@ __device__ inline void prefix_part(const AttendArgs& a, Sums& sums, PrefixTiles<
     // What this lane reads of a tile of keys: row n, chunk 2c + h2; of values: a group of 16 lanes reads 16 channels of 4 tokens and gets
     // a channel's 4 tokens each, so rows 4 * h2 + l16 / 4 (+ 8, 16, 24), 8 bytes of chunk 4c + vc.
     const uint32_t l16 = lane & 15, vrow = 4 * h2 + l16 / 4, vc = (lane >> 4 & 1) * 2 + (l16 & 3) / 2;
-    uint32_t keys_at[kSquare ? 1 : kKeys], value_at[2][kValues];
+    uint32_t keys_at[kSquare ? 1 : kKeys], values_at[2][kSquare ? 1 : kValues];
 #pragma unroll
     for (uint32_t v = 0; v < (kSquare ? 1 : kKeys); ++v) keys_at[v] = 16 * (n * C + ((2 * v + h2) ^ L::turn(n)));
     const auto key_at = [&](uint32_t c) { return (kSquare ? keys_at[0] ^ 32 * (c % kKeys) : keys_at[c % kKeys]) + 32 * (c - c % kKeys); };
 #pragma unroll
     for (uint32_t e = 0; e < 2; ++e)
 #pragma unroll
-        for (uint32_t v = 0; v < kValues; ++v) value_at[e][v] = 16 * ((8 * e + vrow) * C + ((4 * v + vc) ^ L::turn(8 * e + vrow))) + 8 * (l16 & 1);
+        for (uint32_t v = 0; v < (kSquare ? 1 : kValues); ++v) values_at[e][v] = 16 * ((8 * e + vrow) * C + ((4 * v + vc) ^ L::turn(8 * e + vrow))) + 8 * (l16 & 1);
+
+    const auto value_at = [&](uint32_t e, uint32_t v) { return kSquare ? values_at[e][0] ^ 64 * v : values_at[e][v]; };
 
     const float scale = fmaxf(fabsf(a.scale_log2), 1e-38f);  // (of zero too, so that times the -infinity of a token that does not exist it is no NaN)
     const uint32_t flip = a.scale_log2 < 0.f ? 0x80008000u : 0u;  // a negative scale is the queries' sign
@@ -360,9 +400,9 @@ __device__ inline void prefix_part(const AttendArgs& a, Sums& sums, PrefixTiles<
         g = uniform(it.i);
         tiles = uniform(tiles_of(g));
         rts = uniform(row_tiles(g));
-        const uint32_t rel = begin - uniform(it.start) * a.n_kv;
-        u = rel / tiles;
-        t = rel - u * tiles;
+        const uint32_t rel = begin - uniform(it.start) * a.n_kv, room = uniform(div.room(tiles));
+        u = rel / room;
+        t = rel - u * room;
     }
     for (;;) {
         const uint32_t h = u / rts, rt = u - h * rts, first_tile = t, n_tiles = min(tiles - t, left);
@@ -489,7 +529,7 @@ __device__ inline void prefix_part(const AttendArgs& a, Sums& sums, PrefixTiles<
 #pragma unroll
                     for (uint32_t e = 0; e < 2; ++e)
                         part[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                            (__attribute__((address_space(3))) short4v*)KVC_LDS(values + value_at[e][c % kValues] + 16 * (16 * j * C) + 64 * (c - c % kValues)));
+                            (__attribute__((address_space(3))) short4v*)KVC_LDS(values + value_at(e, c % kValues) + 16 * (16 * j * C) + 64 * (c - c % kValues)));
                     v[j][c] = __builtin_bit_cast(half8, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
                 }
             };
@@ -549,13 +589,13 @@ __device__ inline void prefix_part(const AttendArgs& a, Sums& sums, PrefixTiles<
                     *reinterpret_cast<float4v*>(out + 32 * c + 8 * e) = float4v{o[c][4 * e], o[c][4 * e + 1], o[c][4 * e + 2], o[c][4 * e + 3]};
             if (h2 == 0) a.stats[slot] = float2v{m - kLift, sum};
         }
-        left -= n_tiles;
+        left -= min(left, uniform(sums.division.room(tiles)) - first_tile);
         if (left == 0) break;
         t = 0;
         if (++u == rts * a.n_kv) {
             u = 0;
             do ++g;
-            while (uniform(work_of(g)) == 0);
+            while (uniform(row_tiles(g) * tiles_of(g)) == 0);
             tiles = uniform(tiles_of(g));
             rts = uniform(row_tiles(g));
         }
@@ -714,7 +754,9 @@ __global__ __launch_bounds__(256) void k_join(AttendArgs a) {
         if (ptiles && a.prefix_start[a.n_prefix]) {
             const uint32_t rts = ((uint32_t)(seqs.end - seqs.begin) * a.rows + a.prefix_rows - 1) / a.prefix_rows;
             const uint32_t rr = (s - seqs.begin) * a.rows + row, rt = rr / a.prefix_rows;
-            shared.find(a.prefix_start[g] * a.n_kv + (h * rts + rt) * ptiles, ptiles, share(a.prefix_start[a.n_prefix] * a.n_kv, a.prefix_workers));
+            const uint32_t code = a.prefix_start[a.n_prefix + 1];
+            const Division div{code >> 1, code & 1};
+            shared.find(a.prefix_start[g] * a.n_kv + (h * rts + rt) * div.room(ptiles), ptiles, div.each);
             shared.whole = a.prefix_whole + row_id;
             shared.rows = a.prefix_rows;
             shared.slots = a.prefix_slots + (rr - rt * a.prefix_rows);

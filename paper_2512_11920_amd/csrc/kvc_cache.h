@@ -1,6 +1,8 @@
 // Shared declarations of the decode-step operators: their entry points (kvc_cache_api.hip), the kernels that move
 // blocks, tokens and payloads (kvc_cache.hip) and attention (kvc_attend.hip).
 #pragma once
+#include <algorithm>
+
 #include "kvc_common.h"
 
 namespace kvc {
@@ -100,7 +102,7 @@ struct AttendArgs {
     bool direct;  // a workgroup for every unit, and nothing else
     bool apart;   // both parts in one launch, by workgroups of their own
     uint32_t* own_start;     // [n_seq + 1]
-    uint32_t* prefix_start;  // [n_prefix + 1]
+    uint32_t* prefix_start;  // [n_prefix + 2]: and how they are divided
     float* sums;             // [slots][d]
     float2v* stats;          // [slots]: reference and sum of the weights
     int64_t own_slots, prefix_whole, prefix_slots;   // first slots of what the own part shares, and of the prefix part's
@@ -116,7 +118,8 @@ struct AttendPlan {
 };
 // The sequences' own tokens: a wave on each SIMD.  (8 KB of keys and 8 KB of values on their way for each are enough; of 2,048 waves each has half as much, and as much to begin
 // with: 64 sequences of 512 to 8,192 tokens, 8 x 128, 217 us with 2,048, 211 with 1,024; 8 of 1,024 to 2,048, 32 x 128, 37.3 and 36.8; 4 of 1,000 to
-// 4,000 26.4 and 20.6.)  Prefixes: as many workgroups as the GPU holds at once, or half of them.
+// 4,000 26.4 and 20.6.  Narrower heads have less in a tile, and more waves: 64 of 4,096 to 16,384, 8 x 32, 227 us with 1,024, 135 with 4,096; 1,024 to 16,384, 8 x 64, 226 and, with
+// 2,048, 207.)  Prefixes: as many workgroups as the GPU holds at once, or half of them.
 constexpr uint32_t kOwnWorkers = 1024, kPrefixWorkers = 256;
 constexpr uint32_t kPrefixWaves = 4;                          // of a workgroup
 
@@ -139,11 +142,11 @@ inline AttendPlan plan_attend(int64_t n_seq, int64_t n_q, int64_t n_heads, int64
     // (32 rows of heads beyond 192 do not fit into the registers.)
     p.own_rows = n_heads / n_kv * n_q <= 16 || d > 192 ? 16 : 32;
     p.prefix_rows = 32 * kPrefixWaves;
-    p.own_workers = (n_prefix && both_fit(d, (int)p.own_rows / 16) ? 2 : 1) * kOwnWorkers;
+    p.own_workers = n_prefix ? (both_fit(d, (int)p.own_rows / 16) ? 2 : 1) * kOwnWorkers : std::max(1u, 128u / (d * p.own_rows / 16)) * kOwnWorkers;
     p.prefix_workers = n_prefix ? (d <= 128 ? 2 : 1) * kPrefixWorkers : 0;
     p.rows = (uint64_t)(n_seq * n_heads * n_q);
     p.slots = p.rows + 2ull * p.own_workers * p.own_rows + (n_prefix ? p.rows + 2ull * p.prefix_workers * p.prefix_rows : 0);
-    p.starts = round_256((uint64_t)(n_seq + 1) * 4) + round_256((uint64_t)(n_prefix + 1) * 4);
+    p.starts = round_256((uint64_t)(n_seq + 1) * 4) + round_256((uint64_t)(n_prefix + 2) * 4);
     p.bytes = p.starts + round_256(p.slots * 8) + p.slots * (uint64_t)d * 4;
     return p;
 }

@@ -219,7 +219,7 @@ __device__ inline uint4 rename(uint4 d, const CompactArgs& a, F rank_of) {
 
 // A wave moves what is held of kMoveWords words, 4 KB of pool: lane i has unit i of each word, loads it if it is held and stores it to its rank.
 // The workgroups of a megabyte are dealt to the XCDs so that each has a run of them, as neighbours write to the same lines.  1.09 GB, 16 x 128 pages, half of them
-// live and in random order, 1.04 GB of traffic: 64 words a wave 241 us, 16 words 224, 4 words 212, and 205 us with runs (5.1 TB/s).
+// live and in random order, 1.16 GB of traffic: 64 words a wave 241 us, 16 words 224, 4 words 212, and 204 us with runs (5.7 TB/s).
 constexpr uint32_t kMoveWords = 4, kMoveGroups = (uint32_t)kGroupWords / (4 * kMoveWords);  // words of a wave; workgroups of 1,024 words
 
 __device__ inline void move_words(const CompactArgs& a, uint64_t first) {
