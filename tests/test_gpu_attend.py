@@ -170,6 +170,19 @@ def test_prefixes_in_wide_tables(d, N, rows):
     _compare(c, out, lse)
 
 
+@pytest.mark.parametrize("d,seqs,group,q,prefix,first", [
+    (160, 400, 8, 4, (160,), (0, 400)),             # 100 tiles of rows: even shares of one unit each would take 300 workers, longer ones 200
+    (64, 400, 8, 4, (160,), (0, 400)),
+    (160, 280, 16, 8, (70,), (0, 280)),             # more units than workers
+    (32, 90, 4, 1, (300, 31, 0, 500), (0, 20, 21, 40, 88)),
+    (64, 40, 2, 1, tuple(range(20, 56)), tuple(range(37)))])  # more prefixes than lanes look at
+def test_division_of_prefixes(d, seqs, group, q, prefix, first):
+    rng = np.random.default_rng([20, d, seqs])
+    c = _setup(rng, 16, d, 1, group, q, rng.integers(0, 9, seqs), prefix=prefix, first=first)
+    _, out, lse = _run(c)
+    _compare(c, out, lse)
+
+
 def test_many_short_sequences():
     rng = np.random.default_rng(5)
     lens = rng.integers(0, 40, 700)
