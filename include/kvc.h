@@ -295,7 +295,9 @@ int kvc_append(kvc_ctx* ctx, const kvc_append_t* a, void* stream);
  * x_t = scale * <q, k_t> and m = max x_t:  out = sum e^(x_t - m) v_t / sum e^(x_t - m), and, where asked for,
  * lse = m + ln sum e^(x_t - m).  Tokens without a block do not exist: what memory holds in their place, and
  * behind the last token, is never read into a sum, and an infinite or NaN value of one of the last tokens only into
- * those of the queries that see it.  A query that sees no token gets out = 0, lse = -inf.
+ * those of the queries that see it.  A query that sees no token gets out = 0, lse = -inf, and so does one all of whose scores are -infinity (its weights
+ * are taken as zero, which 0 / 0 leaves open).  A NaN score that a query sees makes its out and lse NaN.  An infinite value that it sees with a weight of zero (the score is
+ * -infinity, or the weight was rounded, below 2^-34 of the largest) makes its channel of out NaN, or infinite where it is of one of the last tokens.
  * Each prefix is read once for its group, not once for every sequence.  Lengths beyond their table's row set
  * KVC_ST_BAD_INDEX and are cut to it.  Sums, maxima and products are held in 32 bits; the weights e^(x_t - m)
  * are rounded to FP16 (11 bits, far from its smallest numbers) for the product with the values.

@@ -193,7 +193,8 @@ __device__ inline void scores(float4v (&s)[2], const Rows<D>& r, const Tokens<D>
             s[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, x.k[u][c]), __builtin_bit_cast(half8, r.q[c]), s[u], 0, 0, 0);
 }
 
-// Scores of tokens t + 8g.. become weights, of those below the row's limit that exist; the row's reference follows their maximum.
+// Scores of tokens t + 8g.. become weights, of those below the row's limit that exist; the row's reference follows their maximum.  (Maxima pass
+// NaN over, so a reference is never NaN; the weights' sum keeps it.)
 template <int D>
 __device__ inline half8 weights(Rows<D>& r, const float4v (&s)[2], float scale_log2, uint32_t there, uint32_t t, uint32_t limit) {
     const uint32_t first = t + 8 * ((threadIdx.x & 63) >> 4), n = limit > first ? limit - first : 0;

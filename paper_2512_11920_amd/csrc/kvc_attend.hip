@@ -129,6 +129,11 @@ __device__ inline uint4v finished(const float4v (&o)[2], float l) {
     return v;
 }
 
+// What joins pieces: the weight that a piece with reference m has relative to `top`, the largest of the row's.  A piece may have the reference -infinity, which is
+// smaller than any other and equal to itself, and yet hold NaN in its sums (all its scores are NaN, or -infinity and a value infinite), so that none is passed over:
+// one in which the row saw no token adds zeros.
+__device__ inline float join_weight(float m, float top) { return m == top ? 1.f : power2(m - top); }
+
 // ---- the sequences' own tokens: bound by memory, as a token's keys and values serve only the few rows of one head's group.  A worker is a wave: tiles of 32 tokens go from memory to its registers, keys of the next tile while this
 // one's scores become weights, values while the next scores are made, so that a tile is always on its way; the block table is read one
 // tile further ahead.  R: tiles of 16 rows that share the tokens.
@@ -697,8 +702,7 @@ __global__ __launch_bounds__(64 * kDirectWaves, D * R <= 128 ? 2 : 1) void k_dir
         float4v o[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
         for (uint32_t w = 0; w < workers; ++w) {
             const float2v st = stats[w][in_tile];
-            if (st[0] == -INFINITY) continue;  // (a part in which the row saw no token)
-            const float f = power2(st[0] - m);
+            const float f = join_weight(st[0], m);
             const float4v* x = reinterpret_cast<const float4v*>(&sums[w][in_tile][8 * c]);
             l += st[1] * f;
             o[0] += x[0] * f;
@@ -764,9 +768,8 @@ __global__ __launch_bounds__(256) void k_join(AttendArgs a) {
     }
     float m = -INFINITY, l = 0.f;
     float4v o[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-    const auto join = [&](float2v st, const float4v& x, const float4v& y, float top) {  // (of an empty piece, where the row saw no token, the sums are not looked at)
-        if (st[0] == -INFINITY) return;
-        const float w = power2(st[0] - top);
+    const auto join = [&](float2v st, const float4v& x, const float4v& y, float top) {
+        const float w = join_weight(st[0], top);
         l += st[1] * w;
         o[0] += x * w;
         o[1] += y * w;
@@ -791,8 +794,7 @@ __global__ __launch_bounds__(256) void k_join(AttendArgs a) {
         }
 #pragma unroll
         for (uint32_t j = 0; j < kAtOnce; ++j) top = fmaxf(top, st[j][0]);
-        if (top == -INFINITY) continue;
-        const float f = power2(m - top);
+        const float f = join_weight(m, top);
         m = top;
         l *= f;
         o[0] *= f;
@@ -810,7 +812,7 @@ __global__ __launch_bounds__(256) void k_join(AttendArgs a) {
         if (first == 0 && have) {
             float top = m;
             for (uint32_t j = 1; j < lanes; ++j) top = fmaxf(top, stats[place + j][0]);
-            const float f = top == -INFINITY ? 1.f : power2(m - top);
+            const float f = join_weight(m, top);
             m = top;
             l *= f;
             o[0] *= f;
