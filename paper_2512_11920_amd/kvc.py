@@ -206,6 +206,7 @@ class Codec:
         _check(self._L.kvc_create(C.byref(self._ctx), C.byref(self.cfg)), "kvc_create")
         self.pool = None
         self.desc = None
+        self._leaving = []  # (event, tensor): see _let_go
         self._block_stride = self._span = self.block_elems  # of the contiguous layout
 
     # -- geometry
@@ -218,6 +219,10 @@ class Codec:
         return self.page_elems * self.cfg.pages_per_block
 
     def close(self):
+        while self._leaving:
+            event, _ = self._leaving.pop()
+            if event is not None:
+                event.synchronize()
         if self._ctx:
             self._L.kvc_destroy(self._ctx)
             self._ctx = C.c_void_p()
@@ -401,12 +406,29 @@ class Codec:
             _check(rc, "kvc_compact_pool")
 
     def adopt_pool(self, pool, desc, used, stream=None):
-        """Go on with the buffers that compact_pool has filled."""
+        """Go on with the buffers that compact_pool has filled.  stream comes after the compaction, and after calls on other streams that read the old ones: those are the
+        allocator's again once it has passed this call (hold codec.pool and codec.desc for longer where that is not so)."""
         assert (pool.is_cuda or pool.is_pinned()) and desc.is_cuda and pool.is_contiguous() and desc.is_contiguous()
         assert pool.element_size() == 1 and desc.element_size() == 1 and desc.numel() % 16 == 0
         assert used.is_cuda and used.element_size() == 8 and used.numel() == 1
         _check(self._L.kvc_adopt_pool(self._ctx, pool.data_ptr(), pool.numel(), desc.data_ptr(), desc.numel() // 16, used.data_ptr(), _stream(stream)), "kvc_adopt_pool")
+        self._let_go((self.pool, self.desc), stream)
         self.pool, self.desc = pool, desc
+
+    def _let_go(self, tensors, stream):
+        """The codec may hold the last references, and work that reads their memory is still on its way: it is not handed out again before the stream has passed here.
+        The allocator sees to that for device memory; pinned memory is held here until an event has passed (or, of a call that is captured, until the codec is closed)."""
+        import torch
+
+        stream = torch.cuda.current_stream() if stream is None else stream
+        self._leaving = [(e, t) for e, t in self._leaving if e is None or not e.query()]
+        for t in tensors:
+            if t is None:
+                continue
+            if t.is_cuda:
+                t.record_stream(stream)
+            else:
+                self._leaving.append((None if torch.cuda.is_current_stream_capturing() else stream.record_event(), t))
 
     def stats(self, stream=None, check: bool = False) -> dict:
         st = Stats()
