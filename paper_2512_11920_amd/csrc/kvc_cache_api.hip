@@ -214,9 +214,13 @@ uint64_t kvc_compact_workspace(uint64_t pool_bytes) {
     return groups * kGroupWords * 10 + round_256(groups * 8);
 }
 
-static bool apart(const void* a, uint64_t an, const void* b, uint64_t bn) {
-    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-    return x + an <= y || y + bn <= x;
+struct Buffer {
+    const void* at;
+    uint64_t n;
+};
+static bool apart(const Buffer& a, const Buffer& b) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a.at), y = reinterpret_cast<uintptr_t>(b.at);
+    return x <= y ? y - x >= a.n : x - y >= b.n;
 }
 
 int kvc_compact_pool(kvc_ctx* ctx, void* d_pool_out, uint64_t pool_out_bytes, kvc_desc* d_desc_out, uint64_t* d_used_out, void* d_work, uint64_t work_bytes, void* stream) {
@@ -226,7 +230,12 @@ int kvc_compact_pool(kvc_ctx* ctx, void* d_pool_out, uint64_t pool_out_bytes, kv
     if (!d_pool_out || !d_desc_out || !d_used_out || !d_work || pool_out_bytes == 0 || (pool_out_bytes & 15)) return KVC_ERR_ARG;
     if (!aligned(d_pool_out, 16) || !aligned(d_desc_out, 16) || !aligned(d_used_out, 8) || !aligned(d_work, 256)) return KVC_ERR_ARG;
     if (work_bytes < kvc_compact_workspace(ctx->pool_bytes)) return KVC_ERR_ARG;
-    if (!apart(d_pool_out, pool_out_bytes, ctx->pool, ctx->pool_bytes) || !apart(d_desc_out, ctx->n_desc * 16, ctx->desc, ctx->n_desc * 16)) return KVC_ERR_ARG;
+    const Buffer written[] = {{d_pool_out, pool_out_bytes}, {d_desc_out, ctx->n_desc * 16}, {d_used_out, 8}, {d_work, kvc_compact_workspace(ctx->pool_bytes)}};
+    for (const Buffer& w : written) {
+        if (!apart(w, {ctx->pool, ctx->pool_bytes}) || !apart(w, {ctx->desc, ctx->n_desc * 16})) return KVC_ERR_ARG;
+        for (const Buffer* o = written; o != &w; ++o)
+            if (!apart(w, *o)) return KVC_ERR_ARG;
+    }
     CompactArgs a;
     a.pool = ctx->pool;
     a.units = ctx->pool_bytes / 16;

@@ -1,0 +1,35 @@
+"""What the decode-step calls refuse before they launch anything, found without a GPU (tests/cache_calls.py)."""
+import pytest
+
+from cache_calls import answers
+from paper_2512_11920_amd import kvc
+
+MB = 1 << 20
+#: buffers of a compaction, and their bytes: a pool that one workgroup compacts, and a larger one
+SIZES = [dict(pool=64 * 1024, desc=16 * 100, pool_out=32 * 1024, desc_out=16 * 100, used=8), dict(pool=8 * MB, desc=16 * 5000, pool_out=8 * MB, desc_out=16 * 5000, used=8)]
+
+
+def _compaction(sizes, **at):
+    sizes = dict(sizes, work=kvc.compact_workspace(sizes["pool"]))
+    where = {name: (i + 1) << 30 for i, name in enumerate(sizes)}
+    return sizes, dict(where, op="compact", pool_bytes=sizes["pool"], out_bytes=sizes["pool_out"], pages=sizes["desc"] // 16, **at)
+
+
+@pytest.mark.parametrize("sizes", SIZES)
+def test_compaction_refuses_buffers_that_overlap(sizes):
+    """None of what it writes may lie in what it reads, or in something else that it writes."""
+    sizes, good = _compaction(sizes)
+    written = ("pool_out", "desc_out", "used", "work")
+    pairs = [(a, b) for a in written for b in sizes if a != b and not (b in written and b < a)]
+    calls, want = [good], [kvc.OK]
+    for a, b in pairs:
+        align = 256 if "work" in (a, b) else 16
+        for at, code in ((good[b], kvc.ERR_ARG), (good[b] + (sizes[b] - 1) // align * align, kvc.ERR_ARG), (good[b] - (sizes[a] - 1) // align * align, kvc.ERR_ARG),
+                         (good[b] + -(-sizes[b] // align) * align, kvc.OK), (good[b] - -(-sizes[a] // align) * align, kvc.OK)):
+            calls.append(dict(good, **{a: at}))
+            want.append(code)
+    calls.append(dict(good, out_bytes=(1 << 64) - 16, pool_out=good["pool"] - 256))  # (its end has no address)
+    want.append(kvc.ERR_ARG)
+    got = answers(calls)
+    assert [g[0] for g in got] == want, [(c, g, w) for c, g, w in zip(calls, got, want) if g[0] != w]
+    assert all((n > 0) == (code == kvc.OK) for code, n, _, _ in got)
