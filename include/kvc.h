@@ -347,7 +347,7 @@ int kvc_free_blocks(kvc_ctx* ctx, const int32_t* d_ids, int32_t n, int32_t n_lay
  * their new places and *d_used_out the bytes they take.  The bound pool and table are only read: decodes may go on,
  * until kvc_adopt_pool puts the context on the new ones.  A descriptor whose payload leaves the bound pool
  * becomes INVALID and sets KVC_ST_CORRUPT; one whose payload does not fit into pool_out_bytes becomes INVALID and sets
- * KVC_ST_POOL_FULL.  Pointers 16-byte aligned (d_used_out 8, d_work 256); none of the new
+ * KVC_ST_POOL_FULL.  d_pool_out and d_desc_out may be in pinned, device-mapped host memory, as the bound ones may.  Pointers 16-byte aligned (d_used_out 8, d_work 256); none of the new
  * buffers may overlap another, or a bound one. */
 int kvc_compact_pool(kvc_ctx* ctx, void* d_pool_out, uint64_t pool_out_bytes, kvc_desc* d_desc_out, uint64_t* d_used_out, void* d_work,
                      uint64_t work_bytes, void* stream);

@@ -54,6 +54,17 @@ bool hip_ok(hipError_t e) {
     return e == hipSuccess;
 }
 
+bool seen_by_device(void** p, hipPointerAttribute_t* attr) {
+    if (!hip_ok(hipPointerGetAttributes(attr, *p))) {
+        (void)hipGetLastError();  // the failed query is ours: leave no error behind for the caller's next check
+        return false;
+    }
+    if (attr->type != hipMemoryTypeHost) return attr->type == hipMemoryTypeDevice || attr->type == hipMemoryTypeManaged;
+    if (!attr->devicePointer) return false;
+    *p = attr->devicePointer;
+    return true;
+}
+
 bool on_ctx_device(const kvc_ctx* ctx) {
     int dev = -1;
     return hip_ok(hipGetDevice(&dev)) && dev == ctx->device;
@@ -160,16 +171,7 @@ int kvc_bind_pool(kvc_ctx* ctx, void* d_pool, uint64_t pool_bytes, kvc_desc* d_d
     // The pool may also live in pinned, device-mapped host memory (a slow-link tier): take the address
     // the device sees.  Pageable host memory is rejected here rather than faulting in a kernel.
     hipPointerAttribute_t attr;
-    if (!hip_ok(hipPointerGetAttributes(&attr, d_pool))) {
-        (void)hipGetLastError();  // the failed query is ours: leave no error behind for the caller's next check
-        return KVC_ERR_ARG;
-    }
-    if (attr.type == hipMemoryTypeHost) {
-        if (!attr.devicePointer) return KVC_ERR_ARG;
-        d_pool = attr.devicePointer;
-    } else if (attr.type != hipMemoryTypeDevice && attr.type != hipMemoryTypeManaged) {
-        return KVC_ERR_ARG;
-    }
+    if (!kvc::seen_by_device(&d_pool, &attr)) return KVC_ERR_ARG;
     hipPointerAttribute_t dattr;
     if (!hip_ok(hipPointerGetAttributes(&dattr, d_desc))) {
         (void)hipGetLastError();

@@ -230,6 +230,11 @@ int kvc_compact_pool(kvc_ctx* ctx, void* d_pool_out, uint64_t pool_out_bytes, kv
     if (!d_pool_out || !d_desc_out || !d_used_out || !d_work || pool_out_bytes == 0 || (pool_out_bytes & 15)) return KVC_ERR_ARG;
     if (!aligned(d_pool_out, 16) || !aligned(d_desc_out, 16) || !aligned(d_used_out, 8) || !aligned(d_work, 256)) return KVC_ERR_ARG;
     if (work_bytes < kvc_compact_workspace(ctx->pool_bytes)) return KVC_ERR_ARG;
+    // (where the bound ones may be, these may be: see kvc_bind_pool)
+    hipPointerAttribute_t attr;
+    void* desc_at = d_desc_out;
+    if (!seen_by_device(&d_pool_out, &attr) || !seen_by_device(&desc_at, &attr)) return KVC_ERR_ARG;
+    d_desc_out = static_cast<kvc_desc*>(desc_at);
     const Buffer written[] = {{d_pool_out, pool_out_bytes}, {d_desc_out, ctx->n_desc * 16}, {d_used_out, 8}, {d_work, kvc_compact_workspace(ctx->pool_bytes)}};
     for (const Buffer& w : written) {
         if (!apart(w, {ctx->pool, ctx->pool_bytes}) || !apart(w, {ctx->desc, ctx->n_desc * 16})) return KVC_ERR_ARG;

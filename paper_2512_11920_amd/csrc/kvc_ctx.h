@@ -26,6 +26,9 @@ namespace kvc {
 // Notes a failure for kvc_strerror(KVC_ERR_HIP).
 bool hip_ok(hipError_t e);
 
+// The address by which the device sees memory that it can reach: its own, or pinned and mapped host memory.  False: other memory, which a kernel would fault on.
+bool seen_by_device(void** p, hipPointerAttribute_t* attr);
+
 // Every call must be made with the context's device current: buffers and streams belong to it.
 bool on_ctx_device(const kvc_ctx* ctx);
 

@@ -105,6 +105,7 @@ public:
         }
     }
     bool is_cuda() const { return t ? t->is_cuda() : truth(get("is_cuda")); }
+    bool is_pinned() const { return truth(call("is_pinned")); }
     bool is_contiguous() const { return t ? t->is_contiguous() : truth(call("is_contiguous")); }
     bool holds(at::ScalarType type) const {
         if (t) return t->scalar_type() == type;
@@ -315,14 +316,14 @@ int32_t* table_of(PyObject* o, long long n, int32_t* each) {
     *each = narrow(r.each);
     return static_cast<int32_t*>(t.data_ptr());
 }
-// whole bytes, at least so many, of memory on the GPU
+// whole bytes of memory on the GPU, or in pinned memory too
 struct Bytes {
     void* at;
     long long n;
 };
-Bytes bytes(PyObject* o, const char* what) {
+Bytes bytes(PyObject* o, const char* what, bool pinned_too = false) {
     const Tensor t(o);
-    require(t.is_cuda() && t.is_contiguous() && t.holds(at::kByte), what);
+    require((t.is_cuda() || (pinned_too && t.is_pinned())) && t.is_contiguous() && t.holds(at::kByte), what);
     return {t.data_ptr(), t.numel()};
 }
 
@@ -444,7 +445,7 @@ PyObject* py_fork(PyObject*, PyObject* const* a, Py_ssize_t given) {
 PyObject* py_compact(PyObject*, PyObject* const* a, Py_ssize_t given) {
     return guarded(given, 7, [&] {
         kvc_ctx* ctx = address<kvc_ctx*>(a[0]);
-        const Bytes pool = bytes(a[2], "pool_out: contiguous uint8 CUDA tensor"), desc = bytes(a[3], "desc_out: contiguous uint8 CUDA tensor"),
+        const Bytes pool = bytes(a[2], "pool_out: contiguous uint8 tensor, CUDA or pinned", true), desc = bytes(a[3], "desc_out: contiguous uint8 CUDA tensor"),
                     work = bytes(a[5], "work: contiguous uint8 CUDA tensor");
         require(desc.n == 16 * (wide)integer(a[1]), "desc_out: as many descriptors as are bound");
         const Tensor used(a[4]);

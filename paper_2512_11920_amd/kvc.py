@@ -399,7 +399,8 @@ class Codec:
 
     def compact_pool(self, pool_out, desc_out, used_out, work, stream=None):
         """The live payloads of the bound pool, moved together to the beginning of pool_out, with their descriptors in desc_out
-        and the bytes they take in used_out (int64, one element).  work: uint8 of compact_workspace(pool bytes)."""
+        and the bytes they take in used_out (int64, one element).  pool_out: uint8 tensor, CUDA or pinned host memory; work: uint8 of
+        compact_workspace(pool bytes)."""
         rc = _call.compact(self._ctx.value, 0 if self.desc is None else self.desc.numel() // 16, pool_out, desc_out, used_out, work,
                            _stream_now() if stream is None else stream.cuda_stream)
         if rc:

@@ -1,7 +1,7 @@
 """What the decode-step calls refuse before they launch anything, found without a GPU (tests/cache_calls.py)."""
 import pytest
 
-from cache_calls import answers
+from cache_calls import HOST, SEEN_LOWER, UNREACHABLE, answers
 from paper_2512_11920_amd import kvc
 
 MB = 1 << 20
@@ -33,3 +33,16 @@ def test_compaction_refuses_buffers_that_overlap(sizes):
     got = answers(calls)
     assert [g[0] for g in got] == want, [(c, g, w) for c, g, w in zip(calls, got, want) if g[0] != w]
     assert all((n > 0) == (code == kvc.OK) for code, n, _, _ in got)
+
+
+@pytest.mark.parametrize("sizes", SIZES)
+def test_compaction_writes_where_the_device_sees_pinned_memory(sizes):
+    """As kvc_bind_pool takes pools: pinned memory by the device's address, other host memory not at all."""
+    _, good = _compaction(sizes)
+    pinned = dict(good, pool_out=HOST + (7 << 30), desc_out=HOST + (8 << 30))
+    both = dict(pinned, pool=HOST + (9 << 30), desc=HOST + (10 << 30))
+    got = answers([good, pinned, both])
+    assert [(g[0], g[2], g[3]) for g in got] == [(kvc.OK, good["pool_out"], good["desc_out"])] + [(kvc.OK, pinned["pool_out"] - SEEN_LOWER, pinned["desc_out"] - SEEN_LOWER)] * 2
+    refused = [dict(good, pool_out=UNREACHABLE), dict(good, desc_out=UNREACHABLE),
+               dict(both, pool_out=both["pool"] - SEEN_LOWER), dict(pinned, used=pinned["pool_out"] - SEEN_LOWER)]  # (the device sees them in one place)
+    assert [g[:2] for g in answers(refused)] == [(kvc.ERR_ARG, 0)] * len(refused)
