@@ -302,6 +302,8 @@ int kvc_append(kvc_ctx* ctx, const kvc_append_t* a, void* stream);
  * KVC_ST_BAD_INDEX and are cut to it.  Sums, maxima and products are held in 32 bits; the weights e^(x_t - m)
  * are rounded to FP16 (11 bits, far from its smallest numbers) for the product with the values.
  * Groups out of order set KVC_ST_BAD_INDEX, and no prefix is seen then.  d_out must not overlap what is read.
+ * Lengths are on the device, so the width of a table stands for the longest: a call is refused if n_seq * n_kv_heads * (a KV head's rows of a sequence, by 16 or 32) *
+ * (max_blocks * N / 32 + 1) passes 2^31 - 1, or the like of the prefixes (rows of all groups by 128); and which kernels it takes goes by the widths.
  * d_work: device memory of at least kvc_attend_workspace(...) bytes, 256-byte aligned, contents meaningless
  * between calls; calls that overlap in time need workspaces of their own. */
 typedef struct {
@@ -323,7 +325,7 @@ typedef struct {
     uint64_t work_bytes;
 } kvc_attend_t;
 int kvc_attend(kvc_ctx* ctx, const kvc_attend_t* a, void* stream);
-/* Workspace of a call of these sizes, in bytes (0: sizes that kvc_attend refuses). */
+/* Workspace of a call of these sizes, in bytes (0: sizes that kvc_attend refuses, with whatever tables). */
 uint64_t kvc_attend_workspace(int32_t n_seq, int32_t n_q, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t n_prefix);
 
 /* Copy of cache blocks: in every layer l < n_layers, block l*blocks_per_layer + src[i] is copied to block

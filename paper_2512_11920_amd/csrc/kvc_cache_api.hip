@@ -20,6 +20,10 @@ static const uint16_t* values_of(const kvc_ctx* ctx, const void* k, const void* 
     return v ? static_cast<const uint16_t*>(v) : static_cast<const uint16_t*>(k) + n_kv * ctx->g.page_stride;
 }
 static bool heads_ok(const kvc_ctx* ctx, const void* v, int32_t n_kv) { return n_kv >= 1 && (int64_t)n_kv * (v ? 1 : 2) == ctx->g.ppb; }
+// Query rows are counted in 31 bits, and joined by one launch, d / 8 threads a row.
+static bool rows_ok(int64_t n_seq, int64_t n_q, int64_t n_heads, int d) {
+    return n_seq * n_heads <= INT32_MAX / n_q && n_seq * n_heads * n_q <= kMaxGroups * (2048 / d);
+}
 static int launched(hipError_t e) { return hip_ok(e) ? KVC_OK : KVC_ERR_HIP; }
 
 extern "C" {
@@ -56,7 +60,7 @@ int kvc_append(kvc_ctx* ctx, const kvc_append_t* p, void* stream) {
 
 uint64_t kvc_attend_workspace(int32_t n_seq, int32_t n_q, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t n_prefix) {
     if (n_seq < 0 || n_q < 1 || n_kv_heads < 1 || n_heads < n_kv_heads || n_heads % n_kv_heads || head_dim < 32 || head_dim > 256 || head_dim % 32 || n_prefix < 0) return 0;
-    if ((int64_t)n_seq * n_heads > (int64_t)INT32_MAX / n_q) return 0;
+    if (!rows_ok(n_seq, n_q, n_heads, head_dim)) return 0;
     return plan_attend(n_seq, n_q, n_heads, n_kv_heads, head_dim, n_prefix).bytes;
 }
 
@@ -69,8 +73,8 @@ int kvc_attend(kvc_ctx* ctx, const kvc_attend_t* p, void* stream) {
     if (!aligned(p->d_q, 16) || !aligned(p->d_out, 16) || !aligned(p->d_k_cache, 16) || !aligned(p->d_v_cache, 16)) return KVC_ERR_ARG;
     if (!strides_ok(p->q_strides) || !strides_ok(p->out_strides)) return KVC_ERR_ARG;
     if (p->n_prefix > 0 && ((!p->d_prefix_table && p->max_prefix_blocks) || !p->d_prefix_lens || !p->d_prefix_first)) return KVC_ERR_ARG;
-    // rows are counted in 31 bits, and so are a row's tokens and the tiles of all units
-    if ((int64_t)p->n_seq * p->n_heads > (int64_t)INT32_MAX / p->n_q) return KVC_ERR_ARG;
+    if (!rows_ok(p->n_seq, p->n_q, p->n_heads, ctx->g.d)) return KVC_ERR_ARG;
+    // a row's tokens are counted in 31 bits, and so are the tiles of all units
     const int64_t own_tokens = (int64_t)p->max_blocks * ctx->g.N, prefix_tokens = (int64_t)p->max_prefix_blocks * ctx->g.N;
     if (own_tokens > INT32_MAX - 256 || prefix_tokens > INT32_MAX - 256 || ctx->g.block_stride / 8 > UINT32_MAX) return KVC_ERR_ARG;
     const AttendPlan plan = plan_attend(p->n_seq, p->n_q, p->n_heads, p->n_kv_heads, ctx->g.d, p->n_prefix);
@@ -81,7 +85,6 @@ int kvc_attend(kvc_ctx* ctx, const kvc_attend_t* p, void* stream) {
     if (p->n_prefix && product(prefix_tiles, p->n_kv_heads, prefix_tokens / 32 + 1) > INT32_MAX) return KVC_ERR_ARG;
     if (!p->d_work || !aligned(p->d_work, 256) || p->work_bytes < plan.bytes) return KVC_ERR_ARG;
     if (!std::isfinite(p->scale * 1.44269504088896341f)) return KVC_ERR_ARG;
-    if ((int64_t)plan.rows > kMaxGroups * (2048 / ctx->g.d)) return KVC_ERR_ARG;  // what one launch joins, d / 8 threads a row
     AttendArgs a;
     a.q = static_cast<const uint16_t*>(p->d_q);
     a.out = static_cast<uint16_t*>(p->d_out);

@@ -46,3 +46,18 @@ def test_compaction_writes_where_the_device_sees_pinned_memory(sizes):
     refused = [dict(good, pool_out=UNREACHABLE), dict(good, desc_out=UNREACHABLE),
                dict(both, pool_out=both["pool"] - SEEN_LOWER), dict(pinned, used=pinned["pool_out"] - SEEN_LOWER)]  # (the device sees them in one place)
     assert [g[:2] for g in answers(refused)] == [(kvc.ERR_ARG, 0)] * len(refused)
+
+
+@pytest.mark.parametrize("d", [32, 96, 128, 256])
+@pytest.mark.parametrize("n_q,group", [(1, 1), (3, 8)])
+def test_attention_has_a_workspace_for_the_sizes_that_it_takes(d, n_q, group):
+    """Query rows up to what one launch joins: 2^24 - 1 workgroups of 2048 / d (rounded down) rows.  Beyond it the call is refused, and has no workspace."""
+    most = ((1 << 24) - 1) * (2048 // d) // (n_q * group)
+    calls, works = [], []
+    for n_seq in (most, most + 1):
+        work = kvc.load().kvc_attend_workspace(n_seq, n_q, group, 1, d, 0)
+        works.append(work > 0)
+        calls.append(dict(op="attend", N=16, d=d, ppb=2, n_seq=n_seq, n_q=n_q, n_heads=group, n_kv_heads=1, max_blocks=1, n_cache_blocks=1, scale=1.0, d_q=MB, d_out=MB, d_k_cache=MB,
+                          d_block_table=MB, d_lens=MB, d_work=MB, work_bytes=work or 1 << 60))
+    assert works == [True, False]
+    assert [g[0] for g in answers(calls)] == [kvc.OK, kvc.ERR_ARG]
