@@ -384,7 +384,8 @@ class Codec:
 
     def fork_blocks(self, src_ids, dst_ids, n_layers: int = 1, pool_blocks_per_layer: int | None = None, stream=None):
         """In every layer, pool block dst_ids[i] becomes a second name of what pool block src_ids[i] holds."""
-        assert src_ids is not None
+        if src_ids is None:  # (no assert statement: without it the call below would free dst_ids)
+            raise AssertionError("src_ids: contiguous int32 CUDA tensor")
         rc = _call.fork(self._ctx.value, src_ids, dst_ids, n_layers, self._pool_blocks(n_layers) if pool_blocks_per_layer is None else pool_blocks_per_layer,
                         _stream_now() if stream is None else stream.cuda_stream)
         if rc:
