@@ -414,15 +414,19 @@ class Codec:
         assert pool.element_size() == 1 and desc.element_size() == 1 and desc.numel() % 16 == 0
         assert used.is_cuda and used.element_size() == 8 and used.numel() == 1
         _check(self._L.kvc_adopt_pool(self._ctx, pool.data_ptr(), pool.numel(), desc.data_ptr(), desc.numel() // 16, used.data_ptr(), _stream(stream)), "kvc_adopt_pool")
-        self._let_go((self.pool, self.desc), stream)
-        self.pool, self.desc = pool, desc
+        old, self.pool, self.desc = (self.pool, self.desc), pool, desc
+        self._let_go(old, stream)
 
     def _let_go(self, tensors, stream):
         """The codec may hold the last references, and work that reads their memory is still on its way: it is not handed out again before the stream has passed here.
         The allocator sees to that for device memory; pinned memory is held here until an event has passed (or, of a call that is captured, until the codec is closed)."""
         import torch
 
-        stream = torch.cuda.current_stream() if stream is None else stream
+        if stream is None:
+            stream = torch.cuda.current_stream()
+        elif not hasattr(stream, "record_event"):  # no stream of torch's, but something that names one
+            at = C.cast(stream.cuda_stream, C.c_void_p).value
+            stream = torch.cuda.ExternalStream(at) if at else torch.cuda.default_stream()
         self._leaving = [(e, t) for e, t in self._leaving if e is None or not e.query()]
         for t in tensors:
             if t is None:
