@@ -357,7 +357,8 @@ int kvc_compact_pool(kvc_ctx* ctx, void* d_pool_out, uint64_t pool_out_bytes, kv
 uint64_t kvc_compact_workspace(uint64_t pool_bytes);
 
 /* kvc_bind_pool on buffers that kvc_compact_pool has filled: the cursor goes to *d_used (device memory, read on the
- * stream), the status stays.  The old buffers may be released when the compaction, and whatever else was enqueued on them, has run. */
+ * stream), the status stays.  The old buffers may be released when the compaction, and whatever else was enqueued on them, has run.
+ * Graphs that were captured before go on with the old ones. */
 int kvc_adopt_pool(kvc_ctx* ctx, void* d_pool, uint64_t pool_bytes, kvc_desc* d_desc, uint64_t n_desc_pages, const uint64_t* d_used, void* stream);
 
 /* Reduce the descriptor table and read the device state.  The only call that synchronises

@@ -25,7 +25,7 @@ UNITS = [("kvc_kernels.hip", (), "kvc_kernels.o"), ("kvc_api.hip", (), "kvc_api.
 SOURCES = [os.path.join(_CSRC, f) for f in ("kvc_kernels.hip", "kvc_codec.hip", "kvc_api.hip", "kvc_cache.hip", "kvc_attend.hip", "kvc_cache_api.hip")]
 HEADERS = [os.path.join(_CSRC, f) for f in ("kvc_common.h", "kvc_fastdiv.h", "kvc_device.h", "kvc_codec.h", "kvc_ctx.h", "kvc_cache.h", "kvc_attend.h")] + [os.path.join(_ROOT, "include", "kvc.h")]
 LIB = os.path.join(_PKG, "libkvc.so")
-#: the same library with every LDS index and pool span the kernels compute checked against its bounds
+#: the same library with every LDS index and pool span the codec's kernels compute checked against its bounds
 #: (a violation sets status bit 8); a GPU test runs the parity cases through it
 LIB_DEBUG = os.path.join(_PKG, "libkvc_dbg.so")
 OBJ_DIR = os.path.join(_PKG, "_build")

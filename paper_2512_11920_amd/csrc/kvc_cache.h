@@ -123,13 +123,15 @@ struct AttendPlan {
 constexpr uint32_t kOwnWorkers = 1024, kPrefixWorkers = 256;
 constexpr uint32_t kPrefixWaves = 4;                          // of a workgroup
 
-// Up to so many tiles of prefixes (of 32 tokens, 128 rows and a KV head), half of the workgroups have the prefixes and half the sequences' own tokens; beyond
-// it every one has a part of both, which divides better but begins twice.  8 KV heads x 128, 8 query heads each, both parts by all / apart, us: prefix of 4,096 tokens
-// and 64 sequences of 1 to 512 (4,096 tiles) 51.7 / 38.2, 16,384 and 64 (16,384 tiles) 85.3 / 81.8, 8,192 and 256 (32,768 tiles) 160 / 154, with 512 to
-// 2,048 own tokens 331 / 294, 32,768 and 64 (32,768 tiles) 128 / 133; 32,768 and 256 (131,072 tiles) are divided.
+// Up to so many tiles of prefixes (of 32 tokens, 128 rows and a KV head; as the tables are wide, which may be more than there are), half of the workgroups have the prefixes and
+// half the sequences' own tokens; beyond it every one has a part of both, which divides better but begins twice.  8 KV heads x 128, 8 query heads each, both parts by all / apart, us; own tokens few (1 to
+// 512) and many (512 to 2,048; for 128 sequences 512 to 4,096): prefix of 4,096 for 64 sequences (4,096 tiles) 51.4 / 39.4; 16,384 and 64 (16,384 tiles) 79 / 78; 8,192 and 256
+// (32,768 tiles) 159 / 152 and 333 / 296; 32,768 and 64 (32,768 tiles, 41,000 as they are counted here) 119 / 121 and 156 / 144; 12,288 and 256 (49,152 tiles) 186 / 188 and 342 / 305; 32,768 and 128
+// (65,536 tiles) 202 / 217 and 330 / 289; 16,384 and 256 (65,536 tiles) 226 / 235 and 359 / 319; 32,768 and 192 (98,304 tiles) 296 / 336; 24,576 and 256 with 1 to 2,048 (98,304 tiles) 399 / 394; 32,768 and
+// 256 with 1 to 2,048 (131,072 tiles) 481 / 483.  So calls of many own tokens would rather be apart beyond it too, but these are counted on the device.
 constexpr int64_t kApartTiles = 40960;
 // A call without prefixes whose tables hold at most so many tiles of 32 tokens is done by a workgroup of 8 waves for each unit, in one launch: one sequence of
-// 256 tokens, 4 heads x 64, 6.4 us instead of 9.7.
+// 256 tokens, 4 heads x 64, 6.4 us instead of 9.7.  (Wider tables take the other way, however short the sequences are.)
 constexpr uint32_t kDirectWaves = 8, kDirectTiles = 16;
 constexpr bool direct_fits(int d, int row_tiles) { return d <= 224 && d * row_tiles <= 256; }  // into LDS and 256 registers
 

@@ -5,8 +5,8 @@
 
 namespace kvc {
 
-// Debug build (-DKVC_DEBUG_BOUNDS=1): every LDS slot index and pool span the kernels compute is checked
-// against its bounds; a violation sets status bit 8 instead of being executed silently.  Off by default.
+// Debug build (-DKVC_DEBUG_BOUNDS=1): every LDS slot index and pool span the codec's kernels compute is checked
+// against its bounds (the decode steps' kernels have no such checks); a violation sets status bit 8 instead of being executed silently.  Off by default.
 #ifndef KVC_DEBUG_BOUNDS
 #define KVC_DEBUG_BOUNDS 0
 #endif
