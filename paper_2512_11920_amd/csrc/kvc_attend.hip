@@ -265,8 +265,8 @@ __device__ inline void own_part(const AttendArgs& a, Sums& sums, uint32_t worker
 // it the next tile's scores are made beside the present one's weights, then the present one's values are added.  32 rows a wave, as 64 leave room in the registers for one
 // wave on a SIMD only (600 us instead of 418 where it was tried: with results in accumulation registers, from which each score was moved first, and weights that waited for their scores;
 // the present step was not measured with 64), and two workgroups of 4 waves rather than one of 8, so that one computes while the other waits (418 and 448).
-// 32,768 tokens, 16,384 rows, 128 channels (275 GFLOP): 343 us, 800 TFLOP/s, where a large product of matrices reaches 1,280.  (In calls that follow each other the clock falls for the first
-// milliseconds: 337 to 430 us.)  A wave's step takes 1,360 cycles of its SIMD: 512 of products, and what
+// 32,768 tokens, 16,384 rows, 128 channels (275 GFLOP): 336 to 343 us on two cards, 800 to 820 TFLOP/s, where a large product of matrices reaches 1,280.  (In calls that follow each other the clock
+// falls for the first milliseconds: 334 to 430 us.)  A wave's step takes 1,360 cycles of its SIMD: 512 of products, and what
 // of the rest does not fit beside them: reading LDS (512 for a workgroup), loads to LDS (317), 125 vector instructions, 17 of them powers.
 constexpr uint32_t kStages = 4, kAhead = 8;
 typedef float float16v __attribute__((ext_vector_type(16)));
@@ -628,7 +628,7 @@ __global__ __launch_bounds__(64 * kPrefixWaves, D <= 128 ? 2 : 1) void k_prefix(
 }
 
 // Both in one launch, two workgroups on each compute unit: the first half of them begins with prefixes, which keep the matrix units busy, the other with
-// the sequences' own tokens, which keep the memory busy; then they change: a prefix of 32,768 tokens and 256 sequences of 1 to 2,048, 8 x 128, 8 rows, 474 us, and 343 + 205 by themselves.  Where there is little to do for prefixes (a.apart) each half does its own alone.
+// the sequences' own tokens, which keep the memory busy; then they change: a prefix of 32,768 tokens and 256 sequences of 1 to 2,048, 8 x 128, 8 rows, 465 to 474 us (calls in a row 460 to 635), and 336 to 343 + 205 by themselves.  Where there is little to do for prefixes (a.apart) each half does its own alone.
 template <int D, int R, bool EIGHT>
 __global__ __launch_bounds__(256, 2) void k_both(AttendArgs a) {
     __shared__ Sums sums;
