@@ -430,6 +430,12 @@ __device__ inline void prefix_part(const AttendArgs& a, Sums& sums, PrefixTiles<
             const uint16_t* p = a.q + (seqs.begin + sq) * a.q_strides[0] + i * a.q_strides[1] + (h * a.group + in) * a.q_strides[2];
 #pragma unroll
             for (int c = 0; c < D / 16; ++c) q[c] = *reinterpret_cast<const uint4v*>(p + 16 * c + 8 * h2) ^ flip;
+            if (a.scale_log2 == 0.f) {  // (zero times each product: zero queries where they are finite, NaN where they are not, as zero times infinity)
+#pragma unroll
+                for (int c = 0; c < D / 16; ++c)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) q[c][e] = (((q[c][e] & 0x7C007C00u) + 0x04000400u) >> 15 & 0x00010001u) * 0x7E00u;
+            }
 #pragma unroll
             for (int c = 0; c < D / 32; ++c)
 #pragma unroll
