@@ -12,8 +12,8 @@ evict    evict: the tokens with the least weight leave, but for the last ones, a
 In 4 bits, 32 neighbouring channels of a token share a power of two 2^e, and each is one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 of
 it, with a sign.  e is the smallest whole number for which the largest magnitude is at most 7 * 2^e, and at most 13; a
 magnitude becomes the nearest of the eight, halfway the one of even number.  A group with a value that is not finite
-is NaN.  A page of N tokens of a head is N * d/2 bytes of codes (channel 2i in the low half of byte i), N * d/32 bytes of
-e + 127, and as many more as make a multiple of 16.
+is NaN.  A page of N tokens of a head is N * d/2 bytes of codes (channel 2i of a token in the low half of its byte i), N
+bytes of e + 127 for each 32 channels, and as many more as make a multiple of 16.
 
 Inputs have the distribution of LLaMA-shaped K/V caches: per (K|V, head, channel) a scale exp(N(0, 0.5)), for keys
 2 % of the channels ten times larger.  Blocks of a sequence lie anywhere in the cache.  Lengths are spread evenly over a
@@ -186,7 +186,7 @@ def _parts(case, cache):
     """Codes [block][page][token][d/2] and exponents [block][page][token][d/32] of a cache in 4 bits, as views."""
     N, d = case["N"], case["d"]
     pages = cache.view(len(cache), -1, _page_bytes(case))
-    return pages[:, :, :N * d // 2].unflatten(-1, (N, d // 2)), pages[:, :, N * d // 2:N * d // 2 + N * d // 32].unflatten(-1, (N, d // 32))
+    return pages[:, :, :N * d // 2].unflatten(-1, (N, d // 2)), pages[:, :, N * d // 2:N * d // 2 + N * d // 32].unflatten(-1, (d // 32, N)).transpose(-1, -2)
 
 
 # ------------------------------------------------------------------------------------------------ inputs
@@ -487,11 +487,11 @@ def _exact_blocks(case, cache):
     N, d = case["N"], case["d"]
     raw = cache.cpu().numpy().reshape(len(cache), -1, _page_bytes(case))
     code = raw[:, :, :N * d // 2].reshape(len(raw), -1, N, d // 2)
-    exp = raw[:, :, N * d // 2:N * d // 2 + N * d // 32].reshape(len(raw), -1, N, d // 32)
+    exp = raw[:, :, N * d // 2:N * d // 2 + N * d // 32].reshape(len(raw), -1, d // 32, N)
     table = _exact_value(np.arange(16)[None, :], np.arange(256)[:, None])
     out = np.empty((*code.shape[:3], d))
     for c in range(d):
-        out[..., c] = table[exp[..., c // 32], code[..., c // 2] >> (4 * (c & 1)) & 15]
+        out[..., c] = table[exp[:, :, c // 32], code[..., c // 2] >> (4 * (c & 1)) & 15]
     return out
 
 
