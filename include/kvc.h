@@ -328,6 +328,82 @@ int kvc_attend(kvc_ctx* ctx, const kvc_attend_t* a, void* stream);
 /* Workspace of a call of these sizes, in bytes (0: sizes that kvc_attend refuses, with whatever tables). */
 uint64_t kvc_attend_workspace(int32_t n_seq, int32_t n_q, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t n_prefix);
 
+/* A cache in 4 bits: the values of the same pages, in about a quarter of the memory.  32 neighbouring channels of a token share a power of two 2^e, and each is one of
+ * 0, 0.5, 1, 1.5, 2, 3, 4, 6 of it, with a sign.  e is the smallest whole number with max |x| <= 7 * 2^e, and at most 13; a magnitude becomes the nearest of the eight,
+ * halfway the one of even number, beyond 6 * 2^e that.  (So nothing is off by more than 2^e, but for magnitudes beyond 57,344 = 7 * 2^13, which become 49,152.)  32
+ * channels of which one is infinite or NaN are all NaN.  What a code stands for is an FP16 number.
+ * A page is N * d/2 bytes of codes (token by token, channel 2i in the low half of byte i; the sign is the code's highest bit, the rest the
+ * number of the magnitude), N bytes of e + 127 for every 32 channels in turn (0 where all are zero, 255 for NaN), and 0 to 15 bytes that make a multiple of 16.  A block is
+ * pages_per_block pages in a row, a cache blocks in a row, whatever kvc_set_cache_layout says; 16-byte aligned. */
+uint64_t kvc_fp4_block_bytes(int32_t tokens_per_block, int32_t head_dim, int32_t pages_per_block); /* 0: a shape that kvc_create refuses */
+
+/* kvc_append into a cache in 4 bits: the caches of *a are in 4 bits, the new rows are FP16. */
+int kvc_append_fp4(kvc_ctx* ctx, const kvc_append_t* a, void* stream);
+
+/* Blocks of a cache in 4 bits, in FP16: block src[i] of d_cache goes to block dst[i] of d_out (NULL: i), i < n.  d_out has the context's geometry and layout; no block
+ * may be destination twice, and the two may not overlap.  A pair with an id < 0 is skipped, one with an id beyond its buffer too, and sets KVC_ST_BAD_INDEX. */
+int kvc_unpack_fp4(kvc_ctx* ctx, void* d_out, int64_t n_out_blocks, const void* d_cache, int64_t n_cache_blocks, const int32_t* d_src_ids, const int32_t* d_dst_ids, int32_t n, void* stream);
+
+/* kvc_attend over a cache in 4 bits, as if its values were in FP16: the same numbers, rounded the same way.  There are no prefixes (n_prefix = 0; d_prefix_* are not looked at):
+ * parts can be joined by their lse. */
+int kvc_attend_fp4(kvc_ctx* ctx, const kvc_attend_t* a, void* stream);
+/* Workspace of a call of these sizes, in bytes (0: sizes that it refuses, with whatever tables). */
+uint64_t kvc_attend_fp4_workspace(int32_t n_seq, int32_t n_q, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim);
+
+/* The attention weight that tokens get.  For every sequence s, KV head h and token t < lens[s]
+ *     weights_out[s][h][t] = w + sum over queries i and heads of h's group of e^(scale * <q, k_t> - lse),
+ * over the queries that see t, which are those of kvc_attend (query i sees the tokens t < lens[s] - (n_q - 1 - i)), with w = weights[s][h][t], or 0 for the last n_q tokens,
+ * which are new; those also get their position, positions[s][h][t] = seen[s] - (lens[s] - t).  lse is what attention over the same tokens gave (of all tokens that the weights shall
+ * sum to one over: with a prefix, of both parts); a query with lse = -infinity gives nothing.  Where a NaN score or lse is seen, the weight is NaN.  Tokens without a block get
+ * nothing, and what lies behind lens[s] in the arrays is not touched.  Scores, weights and sums are held in 32 bits, added in a fixed order.  weights_out may be weights.
+ * Lengths beyond the table's row or `width` set KVC_ST_BAD_INDEX and are cut. */
+typedef struct {
+    const void* d_q;         /* FP16, with q_strides as in kvc_attend_t */
+    int64_t q_strides[3];
+    const void* d_k_cache;   /* pages h < n_kv_heads of a block are keys; pages_per_block is n_kv_heads or twice that */
+    int64_t n_cache_blocks;
+    const int32_t* d_block_table; /* [n_seq][max_blocks] */
+    const int32_t* d_lens;        /* [n_seq] */
+    const float* d_lse;           /* [n_seq][n_q][n_heads] */
+    const float* d_weights;       /* [n_seq][n_kv_heads][width] */
+    float* d_weights_out;
+    int32_t* d_positions;         /* [n_seq][n_kv_heads][width] */
+    const int32_t* d_seen;        /* [n_seq]: tokens that the sequence has had, evicted and new ones included */
+    int32_t max_blocks, n_seq, n_q, n_heads, n_kv_heads, width;
+    int32_t fp4;                  /* the cache is in 4 bits */
+    float scale;                  /* finite */
+} kvc_weigh_t;
+int kvc_weigh(kvc_ctx* ctx, const kvc_weigh_t* a, void* stream);
+
+/* Eviction.  Of every sequence and KV head keep[s] of the lens[s] tokens stay (all, if there are no more): those at positions >= seen[s] - min(recent, keep[s]), and of the
+ * others the ones with the largest weights; of equal weights the lowest slots leave first, and NaN is larger than all.  (If more than keep[s] are at such positions, the highest slots of them stay.)  The slots t < keep[s] hold what stays: a token that stays below
+ * keep[s] keeps its slot, and those from there on go, in order, to the slots that were left, in order.  Keys, values, weights and positions go with the token, each head for itself; new_lens[s]
+ * is what stays.  Attention does not look at the order, and positions say which token is where.  What lies from new_lens[s] on is not touched.
+ * Blocks are written in place: those that hold slots below keep[s] must be the sequence's alone.  A sequence with a token that has no block, or lies beyond its table's row or `width`,
+ * stays as it is, and sets KVC_ST_BAD_INDEX.  weights_out may be weights, positions_out positions, new_lens lens. */
+typedef struct {
+    void* d_k_cache;
+    void* d_v_cache;        /* NULL: values are in d_k_cache */
+    int64_t n_cache_blocks; /* of either */
+    const int32_t* d_block_table; /* [n_seq][max_blocks] */
+    const int32_t* d_lens;        /* [n_seq] */
+    const int32_t* d_keep;        /* [n_seq]; below 0: 0 */
+    const int32_t* d_seen;        /* [n_seq] */
+    int32_t* d_new_lens;          /* [n_seq] */
+    const float* d_weights;       /* [n_seq][n_kv_heads][width] */
+    float* d_weights_out;
+    const int32_t* d_positions;   /* [n_seq][n_kv_heads][width] */
+    int32_t* d_positions_out;
+    int32_t max_blocks, n_seq, n_kv_heads, width;
+    int32_t recent;               /* >= 0 */
+    int32_t fp4;                  /* the caches are in 4 bits */
+    void* d_work;                 /* kvc_evict_workspace bytes, 256-byte aligned, contents meaningless between calls; calls that overlap in time need their own */
+    uint64_t work_bytes;
+} kvc_evict_t;
+int kvc_evict(kvc_ctx* ctx, const kvc_evict_t* a, void* stream);
+/* (0: sizes that kvc_evict refuses) */
+uint64_t kvc_evict_workspace(int32_t n_seq, int32_t n_kv_heads, int32_t width);
+
 /* Copy of cache blocks: in every layer l < n_layers, block l*blocks_per_layer + src[i] is copied to block
  * l*blocks_per_layer + dst[i] of the same cache, i < n.  One block may be copied to several; no block may be
  * both source and destination, nor destination twice. */

@@ -1,7 +1,8 @@
 """Build libkvc.so (HIP, gfx950) in-tree with hipcc.  No GPU is needed to compile.
 
 The codec kernels (csrc/kvc_codec.hip) are compiled once per group of page shapes
-(-DKVC_SHAPE_GROUP=k), attention (csrc/kvc_attend.hip) once per head dimension, side by side with the other sources; the
+(-DKVC_SHAPE_GROUP=k), attention (csrc/kvc_attend.hip, csrc/kvc_attend_fp4.hip) and
+the weighing of tokens (csrc/kvc_weigh.hip) once per head dimension, side by side with the other sources; the
 objects are then linked."""
 from __future__ import annotations
 
@@ -19,11 +20,15 @@ HEAD_DIMS = range(32, 257, 32)  # see csrc/kvc_attend.hip
 #: from an accumulation register first, two instructions a score
 VECTOR_RESULTS = ("-mllvm", "-amdgpu-mfma-vgpr-form")
 #: (source, extra defines, object name)
-UNITS = [("kvc_kernels.hip", (), "kvc_kernels.o"), ("kvc_api.hip", (), "kvc_api.o"), ("kvc_cache.hip", (), "kvc_cache.o"), ("kvc_cache_api.hip", (), "kvc_cache_api.o")] + \
+UNITS = [("kvc_kernels.hip", (), "kvc_kernels.o"), ("kvc_api.hip", (), "kvc_api.o"), ("kvc_cache.hip", (), "kvc_cache.o"), ("kvc_cache_api.hip", (), "kvc_cache_api.o"),
+         ("kvc_fp4.hip", (), "kvc_fp4.o"), ("kvc_evict.hip", (), "kvc_evict.o"), ("kvc_fp4_api.hip", (), "kvc_fp4_api.o")] + \
+        [(f"kvc_{name}.hip", (f"-DKVC_HEAD_DIM={d}", *VECTOR_RESULTS), f"kvc_{name}_{d}.o") for name in ("attend_fp4", "weigh") for d in HEAD_DIMS] + \
         [("kvc_attend.hip", (f"-DKVC_HEAD_DIM={d}", *VECTOR_RESULTS), f"kvc_attend_{d}.o") for d in HEAD_DIMS] + \
         [("kvc_codec.hip", (f"-DKVC_SHAPE_GROUP={g}",), f"kvc_codec_{g}.o") for g in range(SHAPE_GROUPS)]
-SOURCES = [os.path.join(_CSRC, f) for f in ("kvc_kernels.hip", "kvc_codec.hip", "kvc_api.hip", "kvc_cache.hip", "kvc_attend.hip", "kvc_cache_api.hip")]
-HEADERS = [os.path.join(_CSRC, f) for f in ("kvc_common.h", "kvc_fastdiv.h", "kvc_device.h", "kvc_codec.h", "kvc_ctx.h", "kvc_cache.h", "kvc_attend.h")] + [os.path.join(_ROOT, "include", "kvc.h")]
+SOURCES = [os.path.join(_CSRC, f) for f in ("kvc_kernels.hip", "kvc_codec.hip", "kvc_api.hip", "kvc_cache.hip", "kvc_attend.hip", "kvc_cache_api.hip", "kvc_fp4.hip", "kvc_attend_fp4.hip", "kvc_weigh.hip",
+                                               "kvc_evict.hip", "kvc_fp4_api.hip")]
+HEADERS = [os.path.join(_CSRC, f) for f in ("kvc_common.h", "kvc_fastdiv.h", "kvc_device.h", "kvc_codec.h", "kvc_ctx.h", "kvc_cache.h", "kvc_attend.h",
+                                               "kvc_divide.h", "kvc_checks.h", "kvc_fp4.h", "kvc_attend_fp4.h")] + [os.path.join(_ROOT, "include", "kvc.h")]
 LIB = os.path.join(_PKG, "libkvc.so")
 #: the same library with every LDS index and pool span the codec's kernels compute checked against its bounds
 #: (a violation sets status bit 8); a GPU test runs the parity cases through it

@@ -4,7 +4,7 @@
 // its query rows; or a prefix, a KV head and some rows of its group), each of so many tiles of tokens, and worker w of W takes the tiles from w * T / W to
 // (w + 1) * T / W of all T.  A unit that one worker has alone is finished there; the pieces of others are left as sums and joined
 // by k_join.  Lengths are on the device, so each workgroup adds them up for itself.
-#include "kvc_attend.h"
+#include "kvc_divide.h"
 
 #ifndef KVC_HEAD_DIM
 #error "KVC_HEAD_DIM: the head dimension to compile"
@@ -12,15 +12,6 @@
 
 namespace kvc {
 
-__device__ inline uint32_t length_of(const AttendArgs& a, int32_t len, int32_t blocks) {
-    const int64_t most = (int64_t)blocks * a.g.N;
-    if (len > most) {
-        atomicOr(&a.st->status, KVC_ST_BAD_INDEX);
-        return (uint32_t)most;
-    }
-    return len < 0 ? 0 : (uint32_t)len;
-}
-__device__ inline uint32_t own_length(const AttendArgs& a, int s) { return length_of(a, a.lens[s], a.max_blocks); }
 __device__ inline uint32_t prefix_length(const AttendArgs& a, int g) { return length_of(a, a.prefix_lens[g], a.max_prefix_blocks); }
 
 // Sequences of prefix g.
@@ -44,105 +35,13 @@ __device__ inline int prefix_of(const AttendArgs& a, int s) {
     return lo > 0 && s < a.prefix_first[lo] ? lo - 1 : -1;
 }
 
-// How the tiles of prefixes are divided: `each` to a worker, or, if `apart`, so many of one unit to a worker, as if units were multiples of it.
-struct Division {
-    uint32_t each, apart;
-    __device__ uint32_t room(uint32_t tiles) const { return apart ? (tiles + each - 1) / each * each : tiles; }
-};
 constexpr uint32_t kPieceCost = 7;
-
-// ---- dividing the work: sums of f(0..n-1), with the items dealt to the 256 threads of a workgroup in runs of `each`.
-struct Sums {
-    uint32_t before[256], wave[4], all, each;
-    uint32_t workers[8];
-    Division division;
-};
-template <class F>
-__device__ inline void add_up(Sums& s, uint32_t n, F f) {
-    const uint32_t t = threadIdx.x, lane = t & 63, each = (n + 255) / 256;
-    uint32_t sum = 0;
-    if (t < 256)
-        for (uint32_t i = t * each; i < n && i < (t + 1) * each; ++i) sum += f(i);
-    uint32_t upto = sum;
-#pragma unroll
-    for (int k = 1; k < 64; k *= 2) {
-        const uint32_t o = __shfl_up(upto, k);
-        if (lane >= (uint32_t)k) upto += o;
-    }
-    if (lane == 63 && t < 256) s.wave[t / 64] = upto;
-    __syncthreads();
-    if (t < 256) {
-        uint32_t base = 0;
-        for (uint32_t w = 0; w < t / 64; ++w) base += s.wave[w];
-        s.before[t] = base + upto - sum;
-        if (t == 255) s.all = base + upto, s.each = each;
-    }
-    __syncthreads();
-}
-// The sum before every item, and of all, for k_join.
-template <class F>
-__device__ inline void write_starts(const Sums& s, uint32_t* start, uint32_t n, F f) {
-    const uint32_t t = threadIdx.x;
-    if (t >= 256) return;
-    uint32_t at = s.before[t];
-    for (uint32_t i = t * s.each; i < n && i < (t + 1) * s.each; ++i) {
-        start[i] = at;
-        at += f(i);
-    }
-    if (t == 0) start[n] = s.all;
-}
-// The item that holds position p < s.all, and the sum before it.
-struct Item {
-    uint32_t i, start;
-};
-template <class F>
-__device__ inline Item find_item(const Sums& s, uint32_t n, uint32_t p, F f) {
-    uint32_t lo = 0;  // the last run that begins at or before p (runs of no work begin where the next does)
-#pragma unroll
-    for (uint32_t k = 128; k; k /= 2)
-        if (s.before[lo + k] <= p) lo += k;
-    Item r{lo * s.each, s.before[lo]};
-    while (r.i + 1 < n) {
-        const uint32_t v = f(r.i);
-        if (p - r.start < v) break;
-        r.start += v;
-        ++r.i;
-    }
-    return r;
-}
-__device__ inline uint32_t uniform(uint32_t v) { return __builtin_amdgcn_readfirstlane(v); }
-
-// tiles a worker takes
-__device__ inline uint32_t share(uint32_t tiles, uint32_t workers) { return max(1u, (tiles + workers - 1) / workers); }
-
-// Eight channels of the output, from their sums and the weights'.
-__device__ inline uint4v finished(const float4v (&o)[2], float l) {
-    const float f = l == 0.f ? 0.f : 1.f / l;
-    uint4v v;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        half2 x;
-        x[0] = (_Float16)(o[e / 2][e % 2 * 2] * f);
-        x[1] = (_Float16)(o[e / 2][e % 2 * 2 + 1] * f);
-        v[e] = __builtin_bit_cast(uint32_t, x);
-    }
-    return v;
-}
-
-// What joins pieces: the weight that a piece with reference m has relative to `top`, the largest of the row's.  A piece may have the reference -infinity, which is
-// smaller than any other and equal to itself, and yet hold NaN in its sums (all its scores are NaN, or -infinity and a value infinite), so that none is passed over:
-// one in which the row saw no token adds zeros.
-__device__ inline float join_weight(float m, float top) { return m == top ? 1.f : power2(m - top); }
 
 // ---- the sequences' own tokens: bound by memory, as a token's keys and values serve only the few rows of one head's group.  A worker is a wave: tiles of 32 tokens go from memory to its registers, keys of the next tile while this
 // one's scores become weights, values while the next scores are made, so that a tile is always on its way; the block table is read one
 // tile further ahead.  R: tiles of 16 rows that share the tokens.
 // 64 sequences of 512 to 8,192 tokens, 8 x 128, 8 rows (1.14 GB): 207 us, 5.5 TB/s, a copy's rate; 8 of 1,024 to 2,048, 32 x 128, a row each (201 MB): 33 us, 6.0 TB/s.  Short calls are bound
 // by reads of memory that wait for each other (lengths, table, keys, and the join's): one sequence of 8,192 tokens, 8 x 128, 16.5 us.
-struct Place {
-    uint32_t s, u, t, tiles, len;  // sequence; unit u of it (head and row tile); tile t of `tiles`
-};
-
 // The part of wave `worker`; called by all waves of a workgroup.
 template <int D, int R, bool EIGHT>
 __device__ inline void own_part(const AttendArgs& a, Sums& sums, uint32_t worker) {
@@ -848,14 +747,18 @@ static hipError_t launch_parts(const AttendArgs& a, hipStream_t s) {
 }
 
 template <>
+hipError_t launch_join<KVC_HEAD_DIM>(const AttendArgs& a, hipStream_t s) {
+    const uint32_t rows = 256 / (KVC_HEAD_DIM / 8) / a.join_lanes;
+    return launch_kernel(k_join<KVC_HEAD_DIM>, dim3((unsigned)(((int64_t)a.n_seq * a.n_kv * a.rows + rows - 1) / rows)), dim3(256), s, a);
+}
+
+template <>
 hipError_t launch_attend<KVC_HEAD_DIM>(const AttendArgs& a, hipStream_t s) {
     constexpr int D = KVC_HEAD_DIM;
     hipError_t e;
     if constexpr (D <= 192) e = a.own_rows == 32 ? launch_parts<D, 2>(a, s) : launch_parts<D, 1>(a, s);
     else e = launch_parts<D, 1>(a, s);
-    if (e != hipSuccess || a.direct) return e;
-    const uint32_t rows = 256 / (D / 8) / a.join_lanes;
-    return launch_kernel(k_join<D>, dim3((unsigned)(((int64_t)a.n_seq * a.n_kv * a.rows + rows - 1) / rows)), dim3(256), s, a);
+    return e != hipSuccess || a.direct ? e : launch_join<D>(a, s);
 }
 
 }  // namespace kvc

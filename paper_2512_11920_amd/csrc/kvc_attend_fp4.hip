@@ -1,0 +1,233 @@
+// Attention over a paged cache in 4 bits, compiled once per head dimension (-DKVC_HEAD_DIM=d).  The work is divided as attention over FP16 divides a call without prefixes
+// (kvc_attend.hip), pieces are joined by its k_join, and a tile becomes FP16 in registers (kvc_attend_fp4.h).
+#include "kvc_attend_fp4.h"
+
+#ifndef KVC_HEAD_DIM
+#error "KVC_HEAD_DIM: the head dimension to compile"
+#endif
+
+namespace kvc {
+
+template <int D, bool EIGHT>
+struct TileFp4 {
+    KeysFp4<D> k;
+    ValuesFp4<D, EIGHT> v;
+    uint32_t there;
+
+    __device__ void load(const AttendFp4Args& x, const SourceFp4& s, const Blocks<EIGHT>& b, uint32_t t) {
+        load_keys<D, EIGHT>(k, x.a, x.f, s, b, t);
+        there = load_values<D, EIGHT>(v, x.a, x.f, s, b, t);
+    }
+};
+
+// What a wave does with a tile.
+template <int D, int R, bool EIGHT>
+__device__ inline void add_tile_fp4(Rows<D> (&r)[R], const AttendFp4Args& x, const TileFp4<D, EIGHT>& tile, uint32_t t, uint32_t len, const uint32_t (&limit)[R]) {
+    Tokens<D> tokens;
+    expand_keys<D, EIGHT>(tokens, tile.k);
+    half8 p[R];
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+        float4v s[2];
+        scores(s, r[j], tokens);
+        p[j] = weights(r[j], s, x.a.scale_log2, tile.there, t, limit[j]);
+    }
+    expand_values<D, EIGHT>(tokens, tile.v, tile.there);
+    add_tile<D, R>(r, tokens, p, t, len, x.a.n_q, limit);
+}
+
+// ---- any lengths: a worker is a wave, the next tile is on its way while this one is computed, its block numbers a tile further ahead.
+template <int D, int R, bool EIGHT>
+__device__ inline void own_part_fp4(const AttendFp4Args& x, Sums& sums, uint32_t worker) {
+    const AttendArgs& a = x.a;
+    const auto tiles_of = [&](uint32_t s) { return (own_length(a, s) + kTile - 1) / kTile; };
+    add_up(sums, a.n_seq, tiles_of);
+    if (worker < 4) write_starts(sums, a.own_start, a.n_seq, tiles_of);
+    const uint32_t units = a.n_kv * a.own_tiles, all = uniform(sums.all) * units, each = share(all, a.own_workers);
+    const uint32_t begin = worker * each, end = min(begin + each, all);
+    if (begin >= end) return;
+
+    Place c;
+    {
+        const Item it = find_item(sums, a.n_seq, begin / units, tiles_of);
+        c.s = uniform(it.i);
+        c.len = uniform(own_length(a, c.s));
+        c.tiles = (c.len + kTile - 1) / kTile;
+        const uint32_t rel = begin - uniform(it.start) * units;
+        c.u = rel / c.tiles;
+        c.t = rel - c.u * c.tiles;
+    }
+    const auto advance = [&](Place& p) {  // (there is a next tile)
+        if (++p.t < p.tiles) return;
+        p.t = 0;
+        if (++p.u < units) return;
+        p.u = 0;
+        do {
+            ++p.s;
+            p.len = uniform(own_length(a, p.s));
+        } while (p.len == 0);
+        p.tiles = (p.len + kTile - 1) / kTile;
+    };
+    const auto source = [&](const Place& p) {
+        const uint32_t h = p.u / a.own_tiles;
+        return SourceFp4{Source{a.table + (int64_t)p.s * a.max_blocks, nullptr, nullptr, p.len}, x.k + (int64_t)h * x.f.page, x.v + (int64_t)h * x.f.page};
+    };
+
+    const uint32_t lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    Rows<D> r[R];
+    uint32_t limit[R];
+    const auto open = [&](const Place& p) {
+        const uint32_t h = p.u / a.own_tiles, rt = p.u - h * a.own_tiles;
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            clear(r[j]);
+            const uint32_t row = min((rt * R + j) * 16 + n, (uint32_t)a.rows - 1);  // (rows beyond the last are computed with it, and not stored)
+            const uint32_t in = fast_div(row, a.by_n_q), i = row - in * a.n_q;
+            load_query<D>(r[j].q, a.q + p.s * a.q_strides[0] + i * a.q_strides[1] + (h * a.group + in) * a.q_strides[2], g);
+            const uint32_t later = a.n_q - 1 - i, len = (uint32_t)a.lens[p.s];
+            limit[j] = min(len > later ? len - later : 0, p.len);
+        }
+    };
+    const auto close = [&](const Place& p, uint32_t first_tile) {
+        const uint32_t h = p.u / a.own_tiles, rt = p.u - h * a.own_tiles;
+        const bool whole = first_tile == 0 && p.t + 1 == p.tiles;
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            const float l = row_sum(r[j].l);
+            const uint32_t row = (rt * R + j) * 16 + n;
+            if (row >= (uint32_t)a.rows) continue;
+            const uint32_t in = fast_div(row, a.by_n_q), i = row - in * a.n_q, head = h * a.group + in;
+            if (whole) {
+                store_pieces<D, 0>(r[j], a.out + p.s * a.out_strides[0] + i * a.out_strides[1] + head * a.out_strides[2], l == 0.f ? 0.f : 1.f / l, g);
+                if (a.lse && g == 0) a.lse[((int64_t)p.s * a.n_q + i) * a.n_heads + head] = lse_of(r[j].m - kLift, l);
+            } else {
+                const int64_t slot = a.own_slots + (int64_t)(2 * worker + (first_tile == 0 ? 1 : 0)) * (16 * R) + 16 * j + n;
+                store_sums<D>(r[j], a.sums + slot * D, g);
+                if (g == 0) a.stats[slot] = float2v{r[j].m - kLift, l};
+            }
+        }
+    };
+
+    // c: the tile computed; c1: the one loaded; c2: the one whose blocks are looked up
+    Place c1 = c, c2 = c;
+    uint32_t left = end - begin, first_tile = c.t;
+    TileFp4<D, EIGHT> here, next;
+    Blocks<EIGHT> b = find_blocks<EIGHT>(a, source(c).at, c.t * kTile);
+    open(c);
+    here.load(x, source(c), b, c.t * kTile);
+    if (left > 1) {
+        advance(c1);
+        b = find_blocks<EIGHT>(a, source(c1).at, c1.t * kTile);
+        c2 = c1;
+    }
+    const auto step = [&](TileFp4<D, EIGHT>& now, TileFp4<D, EIGHT>& then) {  // -> whether it was the last one
+        if (left > 1) {
+            then.load(x, source(c1), b, c1.t * kTile);
+            if (left > 2) {
+                advance(c2);
+                b = find_blocks<EIGHT>(a, source(c2).at, c2.t * kTile);
+            }
+        }
+        add_tile_fp4<D, R, EIGHT>(r, x, now, c.t * kTile, c.len, limit);
+        if (left == 1 || c1.t == 0) {
+            close(c, first_tile);
+            if (left == 1) return true;
+            open(c1);
+            first_tile = 0;
+        }
+        c = c1;
+        c1 = c2;
+        --left;
+        return false;
+    };
+    while (!step(here, next) && !step(next, here)) {
+    }
+}
+
+template <int D, int R, bool EIGHT>
+__global__ __launch_bounds__(256, D * R <= 128 ? 2 : 1) void k_own_fp4(AttendFp4Args x) {
+    __shared__ Sums sums;
+    own_part_fp4<D, R, EIGHT>(x, sums, uniform(blockIdx.x * 4 + threadIdx.x / 64));
+}
+
+// ---- short sequences: a workgroup of kDirectWaves takes a unit, its waves the tiles in turn, and they join their sums in LDS: one launch.
+template <int D, int R, bool EIGHT>
+__global__ __launch_bounds__(64 * kDirectWaves, D * R <= 128 ? 2 : 1) void k_direct_fp4(AttendFp4Args x) {
+    const AttendArgs& a = x.a;
+    __shared__ float2v stats[kDirectWaves][16 * R];
+    __shared__ __align__(16) float sums[kDirectWaves][16 * R][D];
+    const uint32_t lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4, wave = uniform(threadIdx.x / 64);
+    const uint32_t units = a.n_kv * a.own_tiles, s = blockIdx.x / units, u = blockIdx.x - s * units, h = u / a.own_tiles, rt = u - h * a.own_tiles;
+    SourceFp4 src{Source{a.table + (int64_t)s * a.max_blocks, nullptr, nullptr, (uint32_t)a.max_blocks * (uint32_t)a.g.N}, x.k + (int64_t)h * x.f.page, x.v + (int64_t)h * x.f.page};
+    Blocks<EIGHT> b = find_blocks<EIGHT>(a, src.at, wave * kTile);  // (as far as the table's row goes)
+    Rows<D> r[R];
+    uint32_t later[R];
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+        clear(r[j]);
+        const uint32_t row = min((rt * R + j) * 16 + n, (uint32_t)a.rows - 1);
+        const uint32_t in = fast_div(row, a.by_n_q), i = row - in * a.n_q;
+        load_query<D>(r[j].q, a.q + s * a.q_strides[0] + i * a.q_strides[1] + (h * a.group + in) * a.q_strides[2], g);
+        later[j] = a.n_q - 1 - i;
+    }
+    const uint32_t len = uniform((uint32_t)max(a.lens[s], 0));
+    src.at.len = uniform(own_length(a, s));
+    const uint32_t tiles = (src.at.len + kTile - 1) / kTile;
+    for (uint32_t t = wave; t < tiles; t += kDirectWaves) {
+        if (t != wave) b = find_blocks<EIGHT>(a, src.at, t * kTile);
+        b.end_at(t * kTile, src.at.len);  // (entries behind the last token are not block numbers)
+        TileFp4<D, EIGHT> tile;
+        tile.load(x, src, b, t * kTile);
+        uint32_t limit[R];
+#pragma unroll
+        for (int j = 0; j < R; ++j) limit[j] = min(len > later[j] ? len - later[j] : 0, src.at.len);
+        add_tile_fp4<D, R, EIGHT>(r, x, tile, t * kTile, src.at.len, limit);
+    }
+    const uint32_t workers = min(tiles, kDirectWaves);
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+        const float l = row_sum(r[j].l);
+        if (wave < workers) {
+            store_sums<D>(r[j], sums[wave][16 * j + n], g);
+            if (g == 0) stats[wave][16 * j + n] = float2v{r[j].m - kLift, l};
+        }
+    }
+    __syncthreads();
+    for (uint32_t k = threadIdx.x; k < 16 * R * (D / 8); k += 64 * kDirectWaves) {
+        const uint32_t in_tile = k / (D / 8), c = k % (D / 8), row = rt * R * 16 + in_tile;
+        if (row >= (uint32_t)a.rows) continue;
+        float m = -INFINITY, l = 0.f;
+        for (uint32_t w = 0; w < workers; ++w) m = fmaxf(m, stats[w][in_tile][0]);
+        float4v o[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+        for (uint32_t w = 0; w < workers; ++w) {
+            const float2v st = stats[w][in_tile];
+            const float f = join_weight(st[0], m);
+            const float4v* v = reinterpret_cast<const float4v*>(&sums[w][in_tile][8 * c]);
+            l += st[1] * f;
+            o[0] += v[0] * f;
+            o[1] += v[1] * f;
+        }
+        const uint32_t in = fast_div(row, a.by_n_q), i = row - in * a.n_q, head = h * a.group + in;
+        *reinterpret_cast<uint4v*>(a.out + s * a.out_strides[0] + i * a.out_strides[1] + head * a.out_strides[2] + 8 * c) = finished(o, l);
+        if (a.lse && c == 0) a.lse[((int64_t)s * a.n_q + i) * a.n_heads + head] = lse_of(m, l);
+    }
+}
+
+template <int D, int R>
+static hipError_t launch_parts_fp4(const AttendFp4Args& x, hipStream_t s) {
+    const bool eight = x.a.g.N % 8 == 0;
+    if constexpr (direct_fits(D, R))
+        if (x.a.direct) return launch_kernel(eight ? k_direct_fp4<D, R, true> : k_direct_fp4<D, R, false>, dim3((unsigned)x.a.n_seq * x.a.n_kv * x.a.own_tiles), dim3(64 * kDirectWaves), s, x);
+    return launch_kernel(eight ? k_own_fp4<D, R, true> : k_own_fp4<D, R, false>, dim3(x.a.own_workers / 4), dim3(256), s, x);
+}
+
+template <>
+hipError_t launch_attend_fp4<KVC_HEAD_DIM>(const AttendFp4Args& x, hipStream_t s) {
+    constexpr int D = KVC_HEAD_DIM;
+    hipError_t e;
+    if constexpr (D <= 192) e = x.a.own_rows == 32 ? launch_parts_fp4<D, 2>(x, s) : launch_parts_fp4<D, 1>(x, s);
+    else e = launch_parts_fp4<D, 1>(x, s);
+    return e != hipSuccess || x.a.direct ? e : launch_join<D>(x.a, s);
+}
+
+}  // namespace kvc

@@ -163,5 +163,8 @@ hipError_t launch_adopt(DevState* st, const unsigned long long* used, hipStream_
 // attention, one source per head dimension
 template <int D>
 hipError_t launch_attend(const AttendArgs& a, hipStream_t s);
+// its second launch, which joins the pieces that the first left in the workspace
+template <int D>
+hipError_t launch_join(const AttendArgs& a, hipStream_t s);
 
 }  // namespace kvc

@@ -1,0 +1,231 @@
+// Eviction: of every sequence and KV head, `keep` tokens stay, the last `recent` positions and the heaviest of the others.  Tokens of a head may lie in any order, as attention does not
+// look at it, so what stays is not moved together from the beginning on: tokens at slots from `keep` on that stay go to the slots below it whose tokens leave, of which there are as many.
+// Sources and destinations are then apart, and no more is moved than has to be.
+#include "kvc_divide.h"
+#include "kvc_fp4.h"
+
+namespace kvc {
+
+constexpr uint32_t kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
+constexpr uint32_t kKeysKept = 16384;  // in LDS, 64 KB, so that two workgroups are on a compute unit
+
+// Weights in the order of whole numbers: -infinity..., zeros of either sign alike, ...infinity, NaN, and tokens that are safe.
+__device__ inline uint32_t order_of(float w) {
+    if (w != w) return 0xFFFFFFFEu;
+    const uint32_t b = __float_as_uint(w == 0.f ? 0.f : w);
+    return b >> 31 ? ~b : b | 0x80000000u;
+}
+
+struct SelectLds {
+    uint32_t keys[kKeysKept];
+    uint32_t bins[256];
+    uint32_t ties[kSelectWaves], holes[kSelectWaves], fillers[kSelectWaves];
+    uint32_t digit, rank;
+};
+
+// ---- which tokens leave: a workgroup per sequence and head.  The weight of the heaviest that leaves is found 8 bits at a time, of equal ones the lowest slots leave; then the lists of slots are
+// written in order.
+__global__ __launch_bounds__(kSelectThreads) void k_select(EvictArgs a) {
+    __shared__ SelectLds lds;
+    const uint32_t unit = blockIdx.x, s = fast_div(unit, a.by_n_kv), tid = threadIdx.x, lane = tid & 63, wave = uniform(tid / 64);
+    const int32_t given = a.lens[s], keep = max(a.keep[s], 0);
+    const uint32_t len = (uint32_t)max(given, 0);
+    const float* weights = a.weights + (int64_t)unit * a.width;
+    const int32_t* positions = a.positions + (int64_t)unit * a.width;
+    float* weights_out = a.weights_out + (int64_t)unit * a.width;
+    int32_t* positions_out = a.positions_out + (int64_t)unit * a.width;
+    // a sequence with a token that has no block, or no weight, is left as it is
+    bool bad = given > a.width || (int64_t)given > (int64_t)a.max_blocks * a.g.N;
+    if (!bad)
+        for (uint32_t i = tid; (int64_t)i * a.g.N < len; i += kSelectThreads) {
+            const int32_t block = a.table[(int64_t)s * a.max_blocks + i];
+            bad = bad || block < 0 || block >= a.n_cache_blocks;
+        }
+    bad = __syncthreads_or(bad);
+    if (bad && tid == 0) atomicOr(&a.st->status, KVC_ST_BAD_INDEX);
+    const bool stays_all = bad || len <= (uint32_t)keep;
+    if (tid == 0) {
+        if (stays_all) a.counts[unit] = 0;
+        if (unit == s * a.n_kv) a.left[s] = bad ? given : min((int32_t)len, keep);
+    }
+    if (stays_all) {
+        const uint32_t n = min(len, (uint32_t)a.width);
+        if (weights_out != weights)
+            for (uint32_t t = tid; t < n; t += kSelectThreads) weights_out[t] = weights[t];
+        if (positions_out != positions)
+            for (uint32_t t = tid; t < n; t += kSelectThreads) positions_out[t] = positions[t];
+        return;
+    }
+    const int64_t safe_from = (int64_t)a.seen[s] - min(a.recent, keep);
+    const auto make_key = [&](uint32_t t) { return (int64_t)positions[t] >= safe_from ? 0xFFFFFFFFu : order_of(weights[t]); };
+    const bool kept = len <= kKeysKept;
+    const auto key = [&](uint32_t t) { return kept ? lds.keys[t] : make_key(t); };
+    if (kept)
+        for (uint32_t t = tid; t < len; t += kSelectThreads) lds.keys[t] = make_key(t);
+    uint32_t prefix = 0, rank = len - (uint32_t)keep;  // the rank-th smallest (from 1) of the keys that begin as prefix does
+    for (int shift = 24; shift >= 0; shift -= 8) {
+        if (tid < 256) lds.bins[tid] = 0;
+        __syncthreads();
+        for (uint32_t t = tid; t < len; t += kSelectThreads) {
+            const uint32_t k = key(t);
+            if (shift == 24 || (k ^ prefix) >> (shift + 8) == 0) atomicAdd(&lds.bins[k >> shift & 255], 1u);
+        }
+        __syncthreads();
+        if (wave == 0) {
+            uint32_t n[4], mine = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) mine += n[j] = lds.bins[4 * lane + j];
+            uint32_t upto = mine;
+#pragma unroll
+            for (int k = 1; k < 64; k *= 2) {
+                const uint32_t o = __shfl_up(upto, k);
+                if (lane >= (uint32_t)k) upto += o;
+            }
+            uint32_t before = upto - mine;
+            if (before < rank && rank <= upto) {  // (one lane)
+                uint32_t j = 0;
+                while (before + n[j] < rank) before += n[j++];
+                lds.digit = 4 * lane + j;
+                lds.rank = rank - before;
+            }
+        }
+        __syncthreads();
+        prefix |= lds.digit << shift;
+        rank = lds.rank;
+    }
+    // keys below `prefix` leave, and the first `rank` that equal it.  Each wave goes through slots in a row, 64 at a time.
+    const uint32_t part = (len + kSelectThreads - 1) / kSelectThreads * 64, from = min(wave * part, len), to = min(from + part, len);
+    uint32_t ties = 0;
+    for (uint32_t t = from + lane; t - lane < to; t += 64) ties += __popcll(__ballot(t < to && key(t) == prefix));
+    if (lane == 0) lds.ties[wave] = ties;
+    __syncthreads();
+    uint32_t ties_before = 0;
+    for (uint32_t w = 0; w < wave; ++w) ties_before += lds.ties[w];
+    const uint64_t below = (1ull << lane) - 1;
+    const auto walk = [&](auto each) {  // each(t, hole, filler, which lanes have holes, which have fillers)
+        uint32_t seen = ties_before;
+        for (uint32_t t = from + lane; t - lane < to; t += 64) {
+            const uint32_t k = t < to ? key(t) : 0xFFFFFFFFu;
+            const uint64_t equal = __ballot(t < to && k == prefix);
+            const bool leaves = t < to && (k < prefix || (k == prefix && seen + __popcll(equal & below) < rank));
+            seen += __popcll(equal);
+            const bool hole = leaves && t < (uint32_t)keep, filler = t < to && !leaves && t >= (uint32_t)keep;
+            each(t, hole, filler, __ballot(hole), __ballot(filler));
+        }
+    };
+    uint32_t holes = 0, fillers = 0;
+    walk([&](uint32_t, bool, bool, uint64_t h, uint64_t f) { holes += __popcll(h), fillers += __popcll(f); });
+    if (lane == 0) lds.holes[wave] = holes, lds.fillers[wave] = fillers;
+    __syncthreads();
+    uint32_t hole_at = 0, filler_at = 0, count = 0;
+    for (uint32_t w = 0; w < kSelectWaves; ++w) {
+        if (w < wave) hole_at += lds.holes[w], filler_at += lds.fillers[w];
+        count += lds.holes[w];
+    }
+    int32_t* hole_list = a.holes + (int64_t)unit * a.most;
+    int32_t* filler_list = a.fillers + (int64_t)unit * a.most;
+    walk([&](uint32_t t, bool hole, bool filler, uint64_t h, uint64_t f) {
+        if (hole) hole_list[hole_at + __popcll(h & below)] = (int32_t)t;
+        if (filler) filler_list[filler_at + __popcll(f & below)] = (int32_t)t;
+        hole_at += __popcll(h);
+        filler_at += __popcll(f);
+        if (!hole && t < to && t < (uint32_t)keep) {
+            if (weights_out != weights) weights_out[t] = weights[t];
+            if (positions_out != positions) positions_out[t] = positions[t];
+        }
+    });
+    if (tid == 0) a.counts[unit] = (int32_t)count;
+    __syncthreads();
+    for (uint32_t j = tid; j < count; j += kSelectThreads) {
+        const int32_t hole = hole_list[j], filler = filler_list[j];
+        weights_out[hole] = weights[filler];
+        positions_out[hole] = positions[filler];
+    }
+}
+
+// ---- the rows move: the moves of all sequences and heads, in equal shares to the workgroups, 64 at a time: a thread each finds where they go from and to, then the workgroup moves them, a lane per 16 bytes
+// of keys or values (and the exponent that belongs to them).
+constexpr uint32_t kMoveGroups = 2048, kMoves = 64;
+
+template <bool FP4>
+__global__ __launch_bounds__(256) void k_move_rows(EvictArgs a) {
+    __shared__ Sums sums;
+    struct Move {
+        int64_t from, to;        // bytes from the beginning of a cache to a row's page, and FP16: to the row
+        uint32_t row_from, row_to;
+    };
+    __shared__ Move moves[kMoves];
+    const uint32_t units = (uint32_t)a.n_seq * a.n_kv, tid = threadIdx.x;
+    if (blockIdx.x == 0)
+        for (uint32_t s = tid; s < (uint32_t)a.n_seq; s += 256) a.new_lens[s] = a.left[s];
+    const auto count_of = [&](uint32_t u) { return (uint32_t)a.counts[u]; };
+    add_up(sums, units, count_of);
+    const uint32_t all = sums.all, each = share(all, gridDim.x);
+    uint32_t begin = blockIdx.x * each;
+    if (begin >= all) return;
+    const uint32_t end = min(begin + each, all), lanes = (uint32_t)(FP4 ? a.g.d / 32 : a.g.lpr);  // of a row
+    for (; begin < end; begin += kMoves) {
+        const uint32_t n = min(kMoves, end - begin);
+        __syncthreads();
+        if (tid < n) {
+            const Item it = find_item(sums, units, begin + tid, count_of);
+            const int64_t at = (int64_t)it.i * a.most + (begin + tid - it.start);
+            const uint32_t s = fast_div(it.i, a.by_n_kv), h = it.i - s * a.n_kv, from = (uint32_t)a.fillers[at], to = (uint32_t)a.holes[at];
+            const uint32_t in_from = fast_div(from, a.by_N), in_to = fast_div(to, a.by_N);
+            const int64_t b_from = a.table[(int64_t)s * a.max_blocks + in_from], b_to = a.table[(int64_t)s * a.max_blocks + in_to];
+            Move m;
+            m.row_from = from - in_from * (uint32_t)a.g.N;
+            m.row_to = to - in_to * (uint32_t)a.g.N;
+            if (FP4) {
+                m.from = b_from * a.f.block + (int64_t)h * a.f.page;
+                m.to = b_to * a.f.block + (int64_t)h * a.f.page;
+            } else {
+                m.from = 2 * (b_from * a.g.block_stride + h * a.g.page_stride + m.row_from * a.g.row_stride);
+                m.to = 2 * (b_to * a.g.block_stride + h * a.g.page_stride + m.row_to * a.g.row_stride);
+            }
+            moves[tid] = m;
+        }
+        __syncthreads();
+        const uint32_t items = n * 2 * lanes;
+        constexpr uint32_t kAtOnce = 4;
+        for (uint32_t i0 = tid; i0 < items; i0 += 256 * kAtOnce) {
+            uint4v r[kAtOnce];
+            uint8_t e[kAtOnce];
+            uint8_t* to[kAtOnce];
+            uint8_t* exp_to[kAtOnce];
+#pragma unroll
+            for (uint32_t j = 0; j < kAtOnce; ++j) {
+                const uint32_t i = i0 + 256 * j;
+                to[j] = nullptr;
+                if (i < items) {
+                    const uint32_t row = fast_div(i, a.by_lanes), c = i - row * lanes;
+                    const Move& m = moves[row >> 1];
+                    uint8_t* base = row & 1 ? a.v : a.k;
+                    if (FP4) {
+                        const uint8_t* from = base + m.from;
+                        r[j] = *reinterpret_cast<const uint4v*>(from + m.row_from * (uint32_t)(a.g.d / 2) + 16 * c);
+                        e[j] = from[a.f.exps + c * (uint32_t)a.g.N + m.row_from];
+                        to[j] = base + m.to + m.row_to * (uint32_t)(a.g.d / 2) + 16 * c;
+                        exp_to[j] = base + m.to + a.f.exps + c * (uint32_t)a.g.N + m.row_to;
+                    } else {
+                        r[j] = *reinterpret_cast<const uint4v*>(base + m.from + 16 * c);
+                        to[j] = base + m.to + 16 * c;
+                    }
+                }
+            }
+#pragma unroll
+            for (uint32_t j = 0; j < kAtOnce; ++j)
+                if (to[j]) {
+                    *reinterpret_cast<uint4v*>(to[j]) = r[j];
+                    if (FP4) *exp_to[j] = e[j];
+                }
+        }
+    }
+}
+
+hipError_t launch_evict(const EvictArgs& a, hipStream_t s) {
+    const hipError_t e = launch_kernel(k_select, dim3((unsigned)a.n_seq * (unsigned)a.n_kv), dim3(kSelectThreads), s, a);
+    return e != hipSuccess ? e : launch_kernel(a.fp4 ? k_move_rows<true> : k_move_rows<false>, dim3(kMoveGroups), dim3(256), s, a);
+}
+
+}  // namespace kvc

@@ -1,0 +1,108 @@
+// Shared declarations of the operators that keep the paged cache small: a cache held in 4 bits (kvc_fp4.hip, kvc_attend_fp4.hip), the attention weight that
+// tokens get (kvc_weigh.hip), eviction (kvc_evict.hip), and their entry points (kvc_fp4_api.hip).
+#pragma once
+#include "kvc_cache.h"
+
+namespace kvc {
+
+// A page in 4 bits: N rows of d/2 bytes of codes, then for every 32 channels the N tokens' exponent bytes, then what makes it a multiple of 16 bytes.  The
+// exponents of 8 tokens are 8 bytes in a row, as one lane needs them of a group of channels.
+struct Fp4Pages {
+    uint32_t page, exps;  // bytes of a page; where its exponents begin
+    int64_t block;        // bytes of a block
+};
+inline Fp4Pages fp4_pages(int N, int d, int64_t ppb) {
+    Fp4Pages f;
+    f.exps = (uint32_t)(N * d / 2);
+    f.page = (uint32_t)((N * 17 * d / 32 + 15) / 16 * 16);
+    f.block = ppb * f.page;
+    return f;
+}
+
+struct AppendFp4Args {
+    uint8_t* k_cache;
+    uint8_t* v_cache;  // already at the first value page
+    Fp4Pages f;
+    AppendArgs a;      // (its caches are not looked at)
+};
+
+struct UnpackFp4Args {
+    const uint8_t* cache;
+    uint16_t* out;
+    int64_t n_cache_blocks, n_out_blocks;
+    const int32_t* src;  // NULL: block i
+    const int32_t* dst;
+    Fp4Pages f;
+    Geometry g;
+    int32_t n, chunks, pieces;  // as in CopyArgs
+    FastDiv by_lpr, by_N, by_pieces;
+    DevState* st;
+};
+
+struct AttendFp4Args {
+    AttendArgs a;  // (its caches are not looked at)
+    const uint8_t* k;
+    const uint8_t* v;  // already at the first value page
+    Fp4Pages f;
+};
+
+struct WeighArgs {
+    AttendArgs a;           // out, v_cache and the workspace are not looked at; lse is read
+    const uint8_t* k;       // a cache in 4 bits, or NULL
+    Fp4Pages f;
+    const float* before;    // [n_seq][n_kv][width]
+    float* after;
+    int32_t* positions;     // [n_seq][n_kv][width]
+    const int32_t* seen;    // [n_seq]
+    int32_t width;
+    uint32_t workers;       // waves
+};
+
+struct EvictArgs {
+    uint8_t* k;
+    uint8_t* v;  // already at the first value page
+    bool fp4;
+    Fp4Pages f;
+    Geometry g;
+    int64_t n_cache_blocks;
+    const int32_t* table;
+    const int32_t* lens;
+    const int32_t* keep;
+    const float* weights;
+    float* weights_out;
+    const int32_t* positions;
+    int32_t* positions_out;
+    const int32_t* seen;
+    int32_t* new_lens;
+    int32_t recent, width, max_blocks, n_seq, n_kv;
+    int32_t most;  // moves of a sequence and head, at most
+    FastDiv by_N, by_n_kv, by_lanes;  // (lanes that move a row)
+    DevState* st;
+    // the workspace
+    int32_t* counts;   // [n_seq * n_kv]: moves
+    int32_t* left;     // [n_seq]: tokens that stay
+    int32_t* holes;    // [n_seq * n_kv][most]
+    int32_t* fillers;  // [n_seq * n_kv][most]
+};
+
+// Workers of attention over a cache in 4 bits: a tile is a quarter of FP16's bytes, so more waves are needed for as many bytes on their way, and they fit.
+inline AttendPlan plan_attend_fp4(int64_t n_seq, int64_t n_q, int64_t n_heads, int64_t n_kv, int d) {
+    AttendPlan p = plan_attend(n_seq, n_q, n_heads, n_kv, d, 0);
+    p.own_workers = (d * p.own_rows / 16 <= 128 ? 2 : 1) * kOwnWorkers;
+    p.slots = p.rows + 2ull * p.own_workers * p.own_rows;
+    p.bytes = p.starts + round_256(p.slots * 8) + p.slots * (uint64_t)d * 4;
+    return p;
+}
+constexpr uint32_t kWeighWorkers = 2048;
+
+hipError_t launch_append_fp4(const AppendFp4Args& a, hipStream_t s);
+hipError_t launch_unpack_fp4(const UnpackFp4Args& a, hipStream_t s);
+hipError_t launch_evict(const EvictArgs& a, hipStream_t s);
+
+// one source per head dimension
+template <int D>
+hipError_t launch_attend_fp4(const AttendFp4Args& a, hipStream_t s);
+template <int D>
+hipError_t launch_weigh(const WeighArgs& a, hipStream_t s);
+
+}  // namespace kvc

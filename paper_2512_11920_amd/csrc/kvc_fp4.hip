@@ -1,0 +1,110 @@
+// Rows into a cache held in 4 bits, and its blocks back to FP16.
+//
+// A magnitude is one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 times 2^e, e of 32 channels of a token.  gfx950 converts pairs both ways in one instruction, to the nearest (halfway to the even
+// code), beyond 6 to 6; a test compares them with the definition for every FP16 value.  2^e times a code is an FP16 number, as e is 13 at most and FP16 values are multiples of 2^-24.
+#include "kvc_fp4.h"
+
+namespace kvc {
+
+typedef _Float16 half2f __attribute__((ext_vector_type(2)));
+
+// (a value of its own: of a vector's element the compiler takes the first one's bits)
+__device__ inline half2f pair(uint32_t v) { return __builtin_bit_cast(half2f, v); }
+
+// Exponent byte of a group whose largest magnitude has the FP16 bits m: the smallest e with m <= 7 * 2^e, so that nothing is off by more than 2^e; 13 at most, so that 4 * 2^e is an FP16 number.
+__device__ inline uint32_t exponent_byte(uint32_t m) {
+    const uint32_t bits = __float_as_uint((float)__builtin_bit_cast(_Float16, (uint16_t)m));
+    const uint32_t e = ((bits + 0x1FFFFF) >> 23) - 2;  // (7 * 2^e is 1.75 * 2^(e+2): a larger mantissa goes on to the next power)
+    return m == 0 ? 0 : min(e, 140u);
+}
+
+// ---- append: a workgroup per new token, a lane per 16 bytes of its K and V rows, four lanes to a group of 32 channels.
+__global__ __launch_bounds__(256) void k_append_fp4(AppendFp4Args x) {
+    const AppendArgs& a = x.a;
+    const uint32_t s = fast_div(blockIdx.x, a.by_n_new), i = blockIdx.x - s * (uint32_t)a.n_new;
+    const int64_t t = (int64_t)a.lens[s] - a.n_new + i;
+    if (t < 0) return;
+    const uint32_t at = fast_div((uint32_t)t, a.by_N), row = (uint32_t)t - at * (uint32_t)a.g.N;
+    if (at >= (uint32_t)a.max_blocks) {
+        if (threadIdx.x == 0) atomicOr(&a.st->status, KVC_ST_BAD_INDEX);
+        return;
+    }
+    const int32_t block = a.table[(int64_t)s * a.max_blocks + at];
+    if (block < 0) return;
+    if (block >= a.n_cache_blocks) {
+        if (threadIdx.x == 0) atomicOr(&a.st->status, KVC_ST_BAD_INDEX);
+        return;
+    }
+    const uint32_t each = (uint32_t)(a.n_kv * a.g.lpr);  // (a multiple of 4, so a group's lanes are there together)
+    for (uint32_t c = threadIdx.x; c < 2 * each; c += blockDim.x) {
+        const bool v = c >= each;
+        const uint32_t e = v ? c - each : c, h = fast_div(e, a.by_lpr), k = e - h * (uint32_t)a.g.lpr;
+        const uint16_t* from = v ? a.v_new + s * a.v_strides[0] + i * a.v_strides[1] + h * a.v_strides[2]
+                                 : a.k_new + s * a.k_strides[0] + i * a.k_strides[1] + h * a.k_strides[2];
+        const uint4v r = reinterpret_cast<const uint4v*>(from)[k];
+        uint32_t m = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) m = max(m, max(r[j] & 0x7FFFu, r[j] >> 16 & 0x7FFFu));
+        m = max(m, (uint32_t)__shfl_xor((int)m, 1));
+        m = max(m, (uint32_t)__shfl_xor((int)m, 2));
+        const bool finite = m < 0x7C00;
+        const uint32_t exp = finite ? exponent_byte(m) : 255;
+        const float scale = __uint_as_float(finite && m ? exp << 23 : 127u << 23);
+        uint32_t codes = 0;
+        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(codes, pair(r[0]), scale, 0);
+        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(codes, pair(r[1]), scale, 1);
+        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(codes, pair(r[2]), scale, 2);
+        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(codes, pair(r[3]), scale, 3);
+        uint8_t* page = (v ? x.v_cache : x.k_cache) + block * x.f.block + (int64_t)h * x.f.page;
+        reinterpret_cast<uint32_t*>(page + row * (uint32_t)(a.g.d / 2))[k] = finite ? codes : 0;
+        if ((k & 3) == 0) page[x.f.exps + (k / 4) * (uint32_t)a.g.N + row] = (uint8_t)exp;
+    }
+}
+
+// ---- unpack: a workgroup per 16 KB of FP16, a lane per 8 channels, four of them on their way before the first store.
+__global__ __launch_bounds__(256) void k_unpack_fp4(UnpackFp4Args a) {
+    const uint32_t i = fast_div(blockIdx.x, a.by_pieces), piece = blockIdx.x - i * (uint32_t)a.pieces;
+    const int32_t src = a.src ? a.src[i] : (int32_t)i, dst = a.dst ? a.dst[i] : (int32_t)i;
+    if (src < 0 || dst < 0) return;
+    if (src >= a.n_cache_blocks || dst >= a.n_out_blocks) {
+        if (threadIdx.x == 0) atomicOr(&a.st->status, KVC_ST_BAD_INDEX);
+        return;
+    }
+    const uint8_t* x = a.cache + src * a.f.block;
+    uint16_t* y = a.out + dst * a.g.block_stride;
+    uint32_t codes[kCopyChunks / 256], exps[kCopyChunks / 256];
+    int64_t at[kCopyChunks / 256];
+#pragma unroll
+    for (int k = 0; k < kCopyChunks / 256; ++k) {
+        const uint32_t c = piece * kCopyChunks + k * 256 + threadIdx.x;
+        at[k] = -1;
+        codes[k] = exps[k] = 0;
+        if (c < (uint32_t)a.chunks) {
+            const uint32_t line = fast_div(c, a.by_lpr), in_row = c - line * (uint32_t)a.g.lpr, page = fast_div(line, a.by_N), row = line - page * (uint32_t)a.g.N;
+            const uint8_t* p = x + (int64_t)page * a.f.page;
+            codes[k] = reinterpret_cast<const uint32_t*>(p + row * (uint32_t)(a.g.d / 2))[in_row];
+            exps[k] = p[a.f.exps + in_row / 4 * (uint32_t)a.g.N + row];
+            at[k] = page * a.g.page_stride + row * a.g.row_stride + 8 * in_row;
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kCopyChunks / 256; ++k) {
+        const float scale = __uint_as_float(exps[k] << 23);
+        uint4v r;
+        r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes[k], scale, 0));
+        r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes[k], scale, 1));
+        r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes[k], scale, 2));
+        r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes[k], scale, 3));
+        if (at[k] >= 0) *reinterpret_cast<uint4v*>(y + at[k]) = r;
+    }
+}
+
+hipError_t launch_append_fp4(const AppendFp4Args& a, hipStream_t s) {
+    const unsigned threads = (unsigned)std::min<int64_t>(256, (2ll * a.a.n_kv * a.a.g.lpr + 63) / 64 * 64);
+    return launch_kernel(k_append_fp4, dim3((unsigned)(a.a.n_seq * a.a.n_new)), dim3(threads), s, a);
+}
+hipError_t launch_unpack_fp4(const UnpackFp4Args& a, hipStream_t s) {
+    return launch_kernel(k_unpack_fp4, dim3((unsigned)a.pieces * (unsigned)a.n), dim3(256), s, a);
+}
+
+}  // namespace kvc

@@ -26,6 +26,11 @@ struct Entries {
     decltype(&kvc_fork_blocks) fork;
     decltype(&kvc_free_blocks) free;
     decltype(&kvc_compact_pool) compact;
+    decltype(&kvc_append_fp4) append_fp4;
+    decltype(&kvc_unpack_fp4) unpack_fp4;
+    decltype(&kvc_attend_fp4) attend_fp4;
+    decltype(&kvc_weigh) weigh;
+    decltype(&kvc_evict) evict;
 } e;
 
 // a Python error has been set
@@ -150,9 +155,9 @@ struct Blocks {
     void* at;
     long long n;
 };
-Blocks blocks(PyObject* o, PyObject* stride, PyObject* span) {
+Blocks blocks(PyObject* o, PyObject* stride, PyObject* span, at::ScalarType type = at::kHalf) {
     const Tensor t(o);
-    require(t.is_cuda() && t.is_contiguous() && t.holds(at::kHalf));
+    require(t.is_cuda() && t.is_contiguous() && t.holds(type));
     const long long have = t.numel(), need = integer(span);
     return {t.data_ptr(), have < need ? 0 : (have - need) / integer(stride) + 1};
 }
@@ -207,11 +212,13 @@ int unlocked(F f) {
 
 // init(addresses of the entry points, in the order of Entries)
 PyObject* py_init(PyObject*, PyObject* const* a, Py_ssize_t given) {
-    return guarded(given, 11, [&] {
+    return guarded(given, 16, [&] {
         e = Entries{address<decltype(e.compress)>(a[0]), address<decltype(e.compress_mixed)>(a[1]), address<decltype(e.decompress)>(a[2]),
                     address<decltype(e.gather)>(a[3]),   address<decltype(e.prefetch)>(a[4]),       address<decltype(e.append)>(a[5]),
                     address<decltype(e.attend)>(a[6]),   address<decltype(e.copy)>(a[7]),           address<decltype(e.fork)>(a[8]),
-                    address<decltype(e.free)>(a[9]),     address<decltype(e.compact)>(a[10])};
+                    address<decltype(e.free)>(a[9]),     address<decltype(e.compact)>(a[10]),        address<decltype(e.append_fp4)>(a[11]),
+                    address<decltype(e.unpack_fp4)>(a[12]), address<decltype(e.attend_fp4)>(a[13]), address<decltype(e.weigh)>(a[14]),
+                    address<decltype(e.evict)>(a[15])};
         return 0;
     });
 }
@@ -327,13 +334,15 @@ Bytes bytes(PyObject* o, const char* what, bool pinned_too = false) {
     return {t.data_ptr(), t.numel()};
 }
 
-// append(ctx, stride, span, pages, cache, v_cache, block_table, lens, k_new, v_new, d, stream)
+// append(ctx, stride, span, pages, cache, v_cache, block_table, lens, k_new, v_new, d, stream); a cache in 4 bits has bytes for elements
+template <bool FP4>
 PyObject* py_append(PyObject*, PyObject* const* a, Py_ssize_t given) {
     return guarded(given, 12, [&] {
         kvc_ctx* ctx = address<kvc_ctx*>(a[0]);
-        const Blocks b = blocks(a[4], a[1], a[2]);
+        const at::ScalarType type = FP4 ? at::kByte : at::kHalf;
+        const Blocks b = blocks(a[4], a[1], a[2], type);
         const bool apart = a[5] != Py_None;
-        const Blocks vb = apart ? blocks(a[5], a[1], a[2]) : Blocks{nullptr, b.n};
+        const Blocks vb = apart ? blocks(a[5], a[1], a[2], type) : Blocks{nullptr, b.n};
         require(vb.n == b.n, "key and value caches of as many blocks");
         const long long pages = integer(a[3]);
         const Rows4 k = rows4(a[8], "k_new: float16 CUDA tensor [sequence][token][head][channel]"), v = rows4(a[9], "v_new: float16 CUDA tensor [sequence][token][head][channel]");
@@ -353,17 +362,19 @@ PyObject* py_append(PyObject*, PyObject* const* a, Py_ssize_t given) {
         p.d_v_new = v.at;
         for (int i = 0; i < 3; ++i) p.k_strides[i] = k.strides[i], p.v_strides[i] = v.strides[i];
         void* stream = address<void*>(a[11]);
-        return unlocked([&] { return e.append(ctx, &p, stream); });
+        return unlocked([&] { return (FP4 ? e.append_fp4 : e.append)(ctx, &p, stream); });
     });
 }
 
 // attend(ctx, stride, span, pages, d, out, q, cache, v_cache, block_table, lens, work, scale, prefix_table, prefix_lens, prefix_first, lse, stream)
+template <bool FP4>
 PyObject* py_attend(PyObject*, PyObject* const* a, Py_ssize_t given) {
     return guarded(given, 18, [&] {
         kvc_ctx* ctx = address<kvc_ctx*>(a[0]);
-        const Blocks b = blocks(a[7], a[1], a[2]);
+        const at::ScalarType type = FP4 ? at::kByte : at::kHalf;
+        const Blocks b = blocks(a[7], a[1], a[2], type);
         const bool apart = a[8] != Py_None;
-        const Blocks vb = apart ? blocks(a[8], a[1], a[2]) : Blocks{nullptr, b.n};
+        const Blocks vb = apart ? blocks(a[8], a[1], a[2], type) : Blocks{nullptr, b.n};
         require(vb.n == b.n, "key and value caches of as many blocks");
         const long long pages = integer(a[3]);
         const Rows4 out = rows4(a[5], "out: float16 CUDA tensor [sequence][token][head][channel]"), q = rows4(a[6], "q: float16 CUDA tensor [sequence][token][head][channel]");
@@ -411,7 +422,7 @@ PyObject* py_attend(PyObject*, PyObject* const* a, Py_ssize_t given) {
             p.d_lse = static_cast<float*>(lse.data_ptr());
         }
         void* stream = address<void*>(a[17]);
-        return unlocked([&] { return e.attend(ctx, &p, stream); });
+        return unlocked([&] { return (FP4 ? e.attend_fp4 : e.attend)(ctx, &p, stream); });
     });
 }
 
@@ -456,10 +467,126 @@ PyObject* py_compact(PyObject*, PyObject* const* a, Py_ssize_t given) {
     });
 }
 
+// unpack_fp4(ctx, stride, span, block_bytes, out, cache, src_ids, dst_ids, stream)
+PyObject* py_unpack_fp4(PyObject*, PyObject* const* a, Py_ssize_t given) {
+    return guarded(given, 9, [&] {
+        kvc_ctx* ctx = address<kvc_ctx*>(a[0]);
+        const Blocks out = blocks(a[4], a[1], a[2]), cache = blocks(a[5], a[3], a[3], at::kByte);
+        const int32_t n = narrow(a[6] != Py_None ? Tensor(a[6]).numel() : a[7] != Py_None ? Tensor(a[7]).numel() : cache.n);
+        const int32_t *src = a[6] == Py_None ? nullptr : ids_of(a[6], n), *dst = a[7] == Py_None ? nullptr : ids_of(a[7], n);
+        require(src || n <= cache.n, "cache: a block for every destination");
+        require(dst || n <= out.n, "out: room for every block");
+        void* stream = address<void*>(a[8]);
+        return unlocked([&] { return e.unpack_fp4(ctx, out.at, out.n, cache.at, cache.n, src, dst, n, stream); });
+    });
+}
+
+// a cache of either kind
+Blocks any_blocks(PyObject* o, PyObject* stride, PyObject* span, PyObject* block_bytes, bool fp4) {
+    return fp4 ? blocks(o, block_bytes, block_bytes, at::kByte) : blocks(o, stride, span);
+}
+// [sequence][KV head][slot], contiguous
+struct Slots {
+    void* at;
+    long long n[3];
+};
+Slots slots(PyObject* o, at::ScalarType type, const char* what) {
+    const Tensor t(o);
+    require(t.is_cuda() && t.is_contiguous() && t.holds(type) && t.dim() == 3, what);
+    return {t.data_ptr(), {t.size(0), t.size(1), t.size(2)}};
+}
+void same_slots(const Slots& a, const Slots& b) {
+    for (int i = 0; i < 3; ++i) require(a.n[i] == b.n[i], "weights and positions of one shape");
+}
+const char kWeights[] = "weights: contiguous float32 CUDA tensor [sequence][KV head][slot]", kPositions[] = "positions: contiguous int32 CUDA tensor [sequence][KV head][slot]";
+
+// weigh(ctx, stride, span, block_bytes, pages, d, weights, positions, seen, q, cache, block_table, lens, lse, weights_out, scale, stream)
+PyObject* py_weigh(PyObject*, PyObject* const* a, Py_ssize_t given) {
+    return guarded(given, 17, [&] {
+        kvc_ctx* ctx = address<kvc_ctx*>(a[0]);
+        const bool fp4 = Tensor(a[10]).holds(at::kByte);
+        const Blocks b = any_blocks(a[10], a[1], a[2], a[3], fp4);
+        const long long pages = integer(a[4]);
+        const Slots before = slots(a[6], at::kFloat, kWeights), after = a[14] == Py_None ? before : slots(a[14], at::kFloat, kWeights), positions = slots(a[7], at::kInt, kPositions);
+        same_slots(before, after);
+        same_slots(before, positions);
+        const Rows4 q = rows4(a[9], "q: float16 CUDA tensor [sequence][token][head][channel]");
+        require(q.n[3] == integer(a[5]), "head_dim channels");
+        require(q.n[0] == before.n[0], "weights: of as many sequences as there are queries of");
+        require(before.n[1] == pages || 2 * before.n[1] == pages, "a page of the block for every head of K, and of V where they share blocks");
+        kvc_weigh_t p;
+        p.d_q = q.at;
+        for (int i = 0; i < 3; ++i) p.q_strides[i] = q.strides[i];
+        p.d_k_cache = b.at;
+        p.n_cache_blocks = b.n;
+        p.n_seq = narrow(q.n[0]);
+        p.n_q = narrow(q.n[1]);
+        p.n_heads = narrow(q.n[2]);
+        p.n_kv_heads = narrow(before.n[1]);
+        p.width = narrow(before.n[2]);
+        p.d_block_table = table_of(a[11], q.n[0], &p.max_blocks);
+        p.d_lens = ids_of(a[12], q.n[0]);
+        const Tensor lse(a[13]);
+        require(lse.is_cuda() && lse.is_contiguous() && lse.holds(at::kFloat) && lse.numel() == (wide)q.n[0] * q.n[1] * q.n[2], "lse: contiguous float32 CUDA tensor [sequence][token][head]");
+        p.d_lse = static_cast<const float*>(lse.data_ptr());
+        p.d_weights = static_cast<const float*>(before.at);
+        p.d_weights_out = static_cast<float*>(after.at);
+        p.d_positions = static_cast<int32_t*>(positions.at);
+        p.d_seen = ids_of(a[8], q.n[0]);
+        p.fp4 = fp4;
+        const double scale = PyFloat_AsDouble(a[15]);
+        if (scale == -1.0 && PyErr_Occurred()) throw Raised();
+        p.scale = (float)scale;
+        void* stream = address<void*>(a[16]);
+        return unlocked([&] { return e.weigh(ctx, &p, stream); });
+    });
+}
+
+// evict(ctx, stride, span, block_bytes, pages, cache, v_cache, block_table, lens, keep, recent, weights, positions, seen, new_lens, work, weights_out, positions_out, stream)
+PyObject* py_evict(PyObject*, PyObject* const* a, Py_ssize_t given) {
+    return guarded(given, 19, [&] {
+        kvc_ctx* ctx = address<kvc_ctx*>(a[0]);
+        const bool fp4 = Tensor(a[5]).holds(at::kByte), apart = a[6] != Py_None;
+        const Blocks b = any_blocks(a[5], a[1], a[2], a[3], fp4), vb = apart ? any_blocks(a[6], a[1], a[2], a[3], fp4) : Blocks{nullptr, b.n};
+        require(vb.n == b.n, "key and value caches of as many blocks");
+        const long long pages = integer(a[4]);
+        const Slots weights = slots(a[11], at::kFloat, kWeights), weights_out = a[16] == Py_None ? weights : slots(a[16], at::kFloat, kWeights);
+        const Slots positions = slots(a[12], at::kInt, kPositions), positions_out = a[17] == Py_None ? positions : slots(a[17], at::kInt, kPositions);
+        same_slots(weights, weights_out);
+        same_slots(weights, positions);
+        same_slots(weights, positions_out);
+        require(weights.n[1] * (apart ? 1 : 2) == pages, "a page of the block for every head of K, and of V where they share blocks");
+        kvc_evict_t p;
+        p.d_k_cache = b.at;
+        p.d_v_cache = vb.at;
+        p.n_cache_blocks = b.n;
+        p.n_seq = narrow(weights.n[0]);
+        p.n_kv_heads = narrow(weights.n[1]);
+        p.width = narrow(weights.n[2]);
+        p.d_block_table = table_of(a[7], weights.n[0], &p.max_blocks);
+        p.d_lens = ids_of(a[8], weights.n[0]);
+        p.d_keep = ids_of(a[9], weights.n[0]);
+        p.recent = narrow(integer(a[10]));
+        p.d_seen = ids_of(a[13], weights.n[0]);
+        p.d_new_lens = ids_of(a[14], weights.n[0]);
+        p.d_weights = static_cast<const float*>(weights.at);
+        p.d_weights_out = static_cast<float*>(weights_out.at);
+        p.d_positions = static_cast<const int32_t*>(positions.at);
+        p.d_positions_out = static_cast<int32_t*>(positions_out.at);
+        p.fp4 = fp4;
+        const Bytes work = bytes(a[15], "work: contiguous uint8 CUDA tensor");
+        p.d_work = work.at;
+        p.work_bytes = (uint64_t)work.n;
+        void* stream = address<void*>(a[18]);
+        return unlocked([&] { return e.evict(ctx, &p, stream); });
+    });
+}
+
 #define KVC_METHOD(name, f) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {KVC_METHOD("init", py_init), KVC_METHOD("compress", py_compress), KVC_METHOD("decompress", py_decompress), KVC_METHOD("gather", py_gather),
-                         KVC_METHOD("prefetch", py_prefetch), KVC_METHOD("append", py_append), KVC_METHOD("attend", py_attend), KVC_METHOD("copy", py_copy),
-                         KVC_METHOD("fork", py_fork),         KVC_METHOD("compact", py_compact), {nullptr, nullptr, 0, nullptr}};
+                         KVC_METHOD("prefetch", py_prefetch), KVC_METHOD("append", py_append<false>), KVC_METHOD("attend", py_attend<false>), KVC_METHOD("copy", py_copy),
+                         KVC_METHOD("fork", py_fork),         KVC_METHOD("compact", py_compact), KVC_METHOD("append_fp4", py_append<true>), KVC_METHOD("unpack_fp4", py_unpack_fp4),
+                         KVC_METHOD("attend_fp4", py_attend<true>), KVC_METHOD("weigh", py_weigh), KVC_METHOD("evict", py_evict), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_kvc_py", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -27,7 +27,8 @@ EXPORTS = ("kvc_create", "kvc_destroy", "kvc_set_scheme", "kvc_set_cache_layout"
            "kvc_compress_blocks_mixed", "kvc_decompress_blocks", "kvc_gather_decompress", "kvc_set_prefetch_policy", "kvc_prefetch_reset", "kvc_prefetch_layers", "kvc_prefetch_window_workspace",
            "kvc_prefetch_layers_window", "kvc_prefetch_layers_window_static", "kvc_append", "kvc_attend", "kvc_attend_workspace", "kvc_copy_blocks", "kvc_fork_blocks",
            "kvc_free_blocks", "kvc_compact_pool", "kvc_compact_workspace", "kvc_adopt_pool", "kvc_wall_clock_khz", "kvc_device_clocks", "kvc_stats", "kvc_page_scales",
-           "kvc_copy_bytes", "kvc_strerror")
+           "kvc_copy_bytes", "kvc_strerror", "kvc_fp4_block_bytes", "kvc_append_fp4", "kvc_unpack_fp4", "kvc_attend_fp4", "kvc_attend_fp4_workspace", "kvc_weigh", "kvc_evict",
+           "kvc_evict_workspace")
 
 
 class Config(C.Structure):
@@ -52,6 +53,19 @@ class Attend(C.Structure):
                 ("d_prefix_table", C.c_void_p), ("d_prefix_lens", C.c_void_p), ("d_prefix_first", C.c_void_p), ("max_blocks", C.c_int32),
                 ("max_prefix_blocks", C.c_int32), ("n_prefix", C.c_int32), ("n_seq", C.c_int32), ("n_q", C.c_int32), ("n_heads", C.c_int32),
                 ("n_kv_heads", C.c_int32), ("scale", C.c_float), ("d_work", C.c_void_p), ("work_bytes", C.c_uint64)]
+
+
+class Weigh(C.Structure):
+    _fields_ = [("d_q", C.c_void_p), ("q_strides", C.c_int64 * 3), ("d_k_cache", C.c_void_p), ("n_cache_blocks", C.c_int64), ("d_block_table", C.c_void_p), ("d_lens", C.c_void_p),
+                ("d_lse", C.c_void_p), ("d_weights", C.c_void_p), ("d_weights_out", C.c_void_p), ("d_positions", C.c_void_p), ("d_seen", C.c_void_p), ("max_blocks", C.c_int32),
+                ("n_seq", C.c_int32), ("n_q", C.c_int32), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("width", C.c_int32), ("fp4", C.c_int32), ("scale", C.c_float)]
+
+
+class Evict(C.Structure):
+    _fields_ = [("d_k_cache", C.c_void_p), ("d_v_cache", C.c_void_p), ("n_cache_blocks", C.c_int64), ("d_block_table", C.c_void_p), ("d_lens", C.c_void_p), ("d_keep", C.c_void_p),
+                ("d_seen", C.c_void_p), ("d_new_lens", C.c_void_p), ("d_weights", C.c_void_p), ("d_weights_out", C.c_void_p), ("d_positions", C.c_void_p), ("d_positions_out", C.c_void_p),
+                ("max_blocks", C.c_int32), ("n_seq", C.c_int32), ("n_kv_heads", C.c_int32), ("width", C.c_int32), ("recent", C.c_int32), ("fp4", C.c_int32), ("d_work", C.c_void_p),
+                ("work_bytes", C.c_uint64)]
 
 
 class KvcError(RuntimeError):
@@ -141,6 +155,22 @@ def load():
     L.kvc_compact_workspace.argtypes = [C.c_uint64]
     L.kvc_adopt_pool.restype = C.c_int
     L.kvc_adopt_pool.argtypes = [vp, vp, C.c_uint64, vp, C.c_uint64, vp, vp]
+    L.kvc_fp4_block_bytes.restype = C.c_uint64
+    L.kvc_fp4_block_bytes.argtypes = [C.c_int32] * 3
+    L.kvc_append_fp4.restype = C.c_int
+    L.kvc_append_fp4.argtypes = [vp, C.POINTER(Append), vp]
+    L.kvc_unpack_fp4.restype = C.c_int
+    L.kvc_unpack_fp4.argtypes = [vp, vp, C.c_int64, vp, C.c_int64, i32p, i32p, C.c_int32, vp]
+    L.kvc_attend_fp4.restype = C.c_int
+    L.kvc_attend_fp4.argtypes = [vp, C.POINTER(Attend), vp]
+    L.kvc_attend_fp4_workspace.restype = C.c_uint64
+    L.kvc_attend_fp4_workspace.argtypes = [C.c_int32] * 5
+    L.kvc_weigh.restype = C.c_int
+    L.kvc_weigh.argtypes = [vp, C.POINTER(Weigh), vp]
+    L.kvc_evict.restype = C.c_int
+    L.kvc_evict.argtypes = [vp, C.POINTER(Evict), vp]
+    L.kvc_evict_workspace.restype = C.c_uint64
+    L.kvc_evict_workspace.argtypes = [C.c_int32] * 3
     L.kvc_wall_clock_khz.restype = C.c_int
     L.kvc_wall_clock_khz.argtypes = [C.POINTER(C.c_int32)]
     L.kvc_device_clocks.restype = C.c_int
@@ -156,7 +186,8 @@ def load():
     from . import _kvc_py
 
     _kvc_py.init(*(C.cast(f, vp).value for f in (L.kvc_compress_blocks, L.kvc_compress_blocks_mixed, L.kvc_decompress_blocks, L.kvc_gather_decompress, L.kvc_prefetch_layers,
-                                                  L.kvc_append, L.kvc_attend, L.kvc_copy_blocks, L.kvc_fork_blocks, L.kvc_free_blocks, L.kvc_compact_pool)))
+                                                  L.kvc_append, L.kvc_attend, L.kvc_copy_blocks, L.kvc_fork_blocks, L.kvc_free_blocks, L.kvc_compact_pool,
+                                                  L.kvc_append_fp4, L.kvc_unpack_fp4, L.kvc_attend_fp4, L.kvc_weigh, L.kvc_evict)))
     _call = _kvc_py
     _lib = L
     return L
@@ -208,6 +239,8 @@ class Codec:
         self.desc = None
         self._leaving = []  # (event, tensor): see _let_go
         self._block_stride = self._span = self.block_elems  # of the contiguous layout
+        #: bytes of a block of a cache in 4 bits
+        self.fp4_block_bytes = int(self._L.kvc_fp4_block_bytes(tokens_per_block, head_dim, pages_per_block))
 
     # -- geometry
     @property
@@ -370,6 +403,50 @@ class Codec:
         if rc:
             _check(rc, "kvc_attend")
 
+    # -- a cache in 4 bits: uint8, contiguous, fp4_block_bytes for every block, whatever set_cache_layout says
+    def append_fp4(self, cache, block_table, lens, k_new, v_new, v_cache=None, stream=None):
+        """append into a cache in 4 bits: k_new and v_new are float16."""
+        c, size = self.cfg, self.fp4_block_bytes
+        rc = _call.append_fp4(self._ctx.value, size, size, c.pages_per_block, cache, v_cache, block_table, lens, k_new, v_new, c.head_dim,
+                              _stream_now() if stream is None else stream.cuda_stream)
+        if rc:
+            _check(rc, "kvc_append_fp4")
+
+    def unpack_fp4(self, out, cache, src_ids=None, dst_ids=None, stream=None):
+        """Block src_ids[i] of a cache in 4 bits, in FP16, to block dst_ids[i] of out (default: i): for compress_blocks, or for attend."""
+        rc = _call.unpack_fp4(self._ctx.value, self._block_stride, self._span, self.fp4_block_bytes, out, cache, src_ids, dst_ids,
+                              _stream_now() if stream is None else stream.cuda_stream)
+        if rc:
+            _check(rc, "kvc_unpack_fp4")
+
+    def attend_fp4(self, out, q, cache, block_table, lens, work, v_cache=None, scale=None, lse=None, stream=None):
+        """attend, without prefixes, over a cache in 4 bits; work: uint8 of attend_fp4_workspace(...) bytes."""
+        c, size = self.cfg, self.fp4_block_bytes
+        rc = _call.attend_fp4(self._ctx.value, size, size, c.pages_per_block, c.head_dim, out, q, cache, v_cache, block_table, lens, work,
+                              c.head_dim ** -0.5 if scale is None else scale, None, None, None, lse, _stream_now() if stream is None else stream.cuda_stream)
+        if rc:
+            _check(rc, "kvc_attend_fp4")
+
+    # -- what tokens are looked at, and which of them stay
+    def weigh(self, weights, positions, seen, q, cache, block_table, lens, lse, weights_out=None, scale=None, stream=None):
+        """weights[s][h][t] (float32 [n_seq][n_kv_heads][slots]) += what the queries of head h's group that see token t gave it of their attention, e^(scale * <q, k_t> - lse); the n_q
+        last tokens are new, and begin at zero.  q, lse as attend had them, and got them; cache: float16, or in 4 bits (uint8), keys first.  positions (int32, as
+        weights): of the new tokens, from seen (int32 [n_seq]), the tokens that a sequence has had so far.  weights_out: default weights."""
+        c = self.cfg
+        rc = _call.weigh(self._ctx.value, self._block_stride, self._span, self.fp4_block_bytes, c.pages_per_block, c.head_dim, weights, positions, seen, q, cache, block_table, lens, lse,
+                         weights_out, c.head_dim ** -0.5 if scale is None else scale, _stream_now() if stream is None else stream.cuda_stream)
+        if rc:
+            _check(rc, "kvc_weigh")
+
+    def evict(self, cache, block_table, lens, keep, recent: int, weights, positions, seen, new_lens, work, v_cache=None, weights_out=None, positions_out=None, stream=None):
+        """Of every sequence and KV head keep[s] tokens stay: the last `recent` positions, and of the others the heaviest.  Their rows move into the slots below keep[s], in place, with their weights
+        and positions (weights_out, positions_out: default in place); new_lens[s] (may be lens) is how many stay.  keep, seen, new_lens: int32 [n_seq]; cache: float16, or in 4 bits
+        (uint8); work: uint8 of evict_workspace(...) bytes."""
+        rc = _call.evict(self._ctx.value, self._block_stride, self._span, self.fp4_block_bytes, self.cfg.pages_per_block, cache, v_cache, block_table, lens, keep, recent, weights, positions, seen,
+                         new_lens, work, weights_out, positions_out, _stream_now() if stream is None else stream.cuda_stream)
+        if rc:
+            _check(rc, "kvc_evict")
+
     def copy_blocks(self, cache, src_ids, dst_ids, n_layers: int = 1, blocks_per_layer: int | None = None, stream=None):
         """In every layer, cache block src_ids[i] is copied to block dst_ids[i].  blocks_per_layer: default all there are."""
         rc = _call.copy(self._ctx.value, self._block_stride, self._span, cache, src_ids, dst_ids, n_layers, blocks_per_layer,
@@ -465,6 +542,22 @@ def attend_workspace(n_seq: int, n_q: int, n_heads: int, n_kv_heads: int, head_d
     n = int(load().kvc_attend_workspace(int(n_seq), int(n_q), int(n_heads), int(n_kv_heads), int(head_dim), int(n_prefix)))
     if not n:
         raise KvcError(ERR_ARG, "kvc_attend_workspace")
+    return n
+
+
+def attend_fp4_workspace(n_seq: int, n_q: int, n_heads: int, n_kv_heads: int, head_dim: int) -> int:
+    """Bytes of device workspace attend_fp4 needs for a call of these sizes."""
+    n = int(load().kvc_attend_fp4_workspace(int(n_seq), int(n_q), int(n_heads), int(n_kv_heads), int(head_dim)))
+    if not n:
+        raise KvcError(ERR_ARG, "kvc_attend_fp4_workspace")
+    return n
+
+
+def evict_workspace(n_seq: int, n_kv_heads: int, slots: int) -> int:
+    """Bytes of device workspace evict needs for weights [n_seq][n_kv_heads][slots]."""
+    n = int(load().kvc_evict_workspace(int(n_seq), int(n_kv_heads), int(slots)))
+    if not n:
+        raise KvcError(ERR_ARG, "kvc_evict_workspace")
     return n
 
 
