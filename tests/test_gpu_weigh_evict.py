@@ -1,0 +1,375 @@
+"""weigh and evict against plain statements in 64 bits: weights within a bound that is derived term by term (fp4_reference.weigh), everything that moves bit for bit."""
+import numpy as np
+import pytest
+import torch
+
+import fp4_reference as ref
+from gpu_util import DEV
+from paper_2512_11920_amd import kvc
+
+pytestmark = pytest.mark.gpu
+
+
+def _dev(x):
+    return torch.from_numpy(np.ascontiguousarray(x)).to(DEV)
+
+
+def _codec(N, d, ppb, token_major=False):
+    c = kvc.Codec(N, d, ppb)
+    c.alloc_pool(1, 4096, DEV)
+    if token_major:
+        c.set_cache_layout(N * ppb * d, d, ppb * d)
+    return c
+
+
+def _table(rng, lens, N, width, spare=3):
+    each = [-(-max(0, int(n)) // N) for n in lens]
+    perm = rng.permutation(sum(each) + spare).astype(np.int32)
+    table, at = np.full((len(lens), width), -1, np.int32), 0
+    for s, n in enumerate(each):
+        table[s, :n] = perm[at:at + n]
+        at += n
+    return table, sum(each) + spare
+
+
+def _weigh_case(seed, N, d, kv, group, nq, lens, fp4, separate=False, token_major=False, room=0, holes=False):
+    rng = np.random.default_rng(seed)
+    lens = np.array(lens, np.int32)
+    width = max(1, -(-int(lens.max(initial=0)) // N)) + 1
+    table, blocks = _table(rng, lens, N, width)
+    ppb = kv if separate else 2 * kv
+    pages = (rng.standard_normal((blocks, ppb, N, d)) * np.exp(0.5 * rng.standard_normal((ppb, 1, d)))).astype(np.float16)
+    owned = np.zeros((blocks, N), bool)
+    for s, n in enumerate(lens):
+        for t in range(n):
+            owned[table[s, t // N], t % N] = True
+    c = dict(N=N, d=d, kv=kv, ppb=ppb, lens=lens, fp4=fp4, token_major=token_major)
+    if fp4:
+        cache = rng.integers(0, 256, (blocks, ppb * ref.page_bytes(N, d))).astype(np.uint8)
+        codes, exps = ref.parts(cache, N, d, ppb)
+        x, e = ref.pack(pages)
+        own = owned[:, None, :, None]
+        codes[:] = np.where(own, x, codes)
+        exps[:] = np.where(own, e, 255)
+        with np.errstate(over="ignore", invalid="ignore"):
+            pages = ref.values(codes, exps).astype(np.float16)
+    else:
+        pages = np.where(owned[:, None, :, None], pages, np.float16(np.nan))
+        cache = pages.transpose(0, 2, 1, 3) if token_major else pages
+    if holes:
+        table[rng.random(table.shape) < 0.2] = -1
+    S, H = len(lens), kv * group
+    q = rng.standard_normal((S, nq, H, d)).astype(np.float16)
+    # sums of a plausible size: about what attention would give
+    lse = np.log(np.maximum(lens, 1))[:, None, None] + rng.uniform(0, 3, (S, nq, H))
+    c.update(table=table, cache=np.ascontiguousarray(cache), pages=pages, q=q, lse=lse.astype(np.float32))
+    slots = width * N + room
+    c["weights"] = np.exp(2 * rng.standard_normal((S, kv, slots))).astype(np.float32)
+    c["positions"] = rng.integers(-5, 1000, (S, kv, slots)).astype(np.int32)
+    c["seen"] = (lens + rng.integers(0, 500, S)).astype(np.int32)
+    return c
+
+
+def _weigh(c, scale=None, apart=True, stream=None):
+    codec = _codec(c["N"], c["d"], c["ppb"], c["token_major"] and not c["fp4"])
+    S, nq, H, d = c["q"].shape
+    q = _dev(np.concatenate([c["q"], np.full((S, nq, 2, d), np.nan, np.float16)], 2))[:, :, :H]
+    weights, positions = _dev(c["weights"]), _dev(c["positions"])
+    out = torch.full_like(weights, -3.0) if apart else None
+    args = (weights, positions, _dev(c["seen"]), q, _dev(c["cache"]), _dev(c["table"]), _dev(c["lens"]), _dev(c["lse"]))
+    torch.cuda.synchronize()
+    codec.weigh(*args, weights_out=out, scale=scale, stream=stream)
+    torch.cuda.synchronize()
+    if apart:
+        assert np.array_equal(weights.cpu().numpy(), c["weights"])
+    return (out if apart else weights).cpu().numpy(), positions.cpu().numpy(), codec.stats()["status"]
+
+
+def _check_weigh(c, scale=None, apart=True, status=0, **kw):
+    got, positions, st = _weigh(c, scale, apart, **kw)
+    want, want_positions, bound = ref.weigh(c["weights"], c["positions"], c["seen"], c["q"], c["pages"], c["kv"], c["N"], c["table"], c["lens"], c["lse"], c["d"] ** -0.5 if scale is None else scale)
+    slot = np.arange(got.shape[2])
+    inside = slot[None, None] < np.minimum(np.maximum(c["lens"], 0), c["table"].shape[1] * c["N"])[:, None, None]
+    inside = np.broadcast_to(inside, got.shape)
+    assert (np.abs(got - want)[inside] <= bound[inside]).all(), float((np.abs(got - want)[inside] / np.maximum(bound[inside], 1e-38)).max())
+    assert np.array_equal(got[~inside], np.full_like(got, -3.0)[~inside] if apart else c["weights"][~inside])
+    assert np.array_equal(positions, want_positions)
+    assert st == status
+    return got
+
+
+@pytest.mark.parametrize("d", range(32, 257, 32))
+@pytest.mark.parametrize("N", [16, 8, 5, 1])
+@pytest.mark.parametrize("fp4", [False, True])
+def test_weights_of_every_head_dimension(d, N, fp4):
+    if N * d > 4096:
+        N = 4096 // d
+    for kv, group, nq in ((2, 1, 1), (1, 5, 3), (2, 7, 4)):
+        _check_weigh(_weigh_case(d + N, N, d, kv, group, nq, [0, 1, 2, 31, 32, 33, 70], fp4, separate=kv == 1, token_major=nq == 3, room=nq, holes=nq == 4), apart=nq != 3)
+
+
+@pytest.mark.parametrize("fp4", [False, True])
+def test_weights_of_chunks(fp4):
+    """More queries than a tile has rows, and than some sequences have tokens."""
+    _check_weigh(_weigh_case(1, 16, 64, 2, 2, 40, [100, 40, 7, 0, 39], fp4))
+    _check_weigh(_weigh_case(2, 7, 128, 1, 1, 17, [60, 17, 16], fp4))
+
+
+@pytest.mark.parametrize("fp4", [False, True])
+@pytest.mark.parametrize("scale", [0.0, -0.2, 1.5])
+def test_scales(fp4, scale):
+    c = _weigh_case(3, 16, 64, 2, 3, 2, [77, 40, 3], fp4)
+    c["lse"] += 20 * abs(scale)
+    _check_weigh(c, scale=scale)
+
+
+@pytest.mark.parametrize("fp4", [False, True])
+@pytest.mark.parametrize("nq", [2, 20])
+def test_queries_that_see_nothing_and_sums_that_are_not_finite(fp4, nq):
+    c = _weigh_case(4, 16, 64, 2, 1, nq, [77, 40, 30], fp4)
+    c["lse"][0, 0] = -np.inf           # gives nothing
+    c["lse"][1, 1, 0] = np.inf         # e^-inf
+    c["lse"][2, 1, 1] = np.nan         # every token that it sees
+    got, _, _ = _weigh(c)
+    want, _, bound = ref.weigh(c["weights"], c["positions"], c["seen"], c["q"], c["pages"], 2, 16, c["table"], c["lens"], c["lse"], 64 ** -0.5)
+    for s, n in enumerate(c["lens"]):
+        w, g, b = want[s, :, :n], got[s, :, :n], bound[s, :, :n]
+        assert np.array_equal(np.isnan(w), np.isnan(g)) and np.isnan(w).any() == (s == 2)
+        ok = ~np.isnan(w) & ~np.isnan(b)
+        assert (np.abs(w - g)[ok] <= b[ok]).all()
+
+
+def test_lengths_beyond_the_table_or_the_weights_are_cut():
+    c = _weigh_case(5, 16, 32, 1, 2, 1, [40, 90, 64], False)
+    c["table"] = np.ascontiguousarray(c["table"][:, :5])
+    c["weights"], c["positions"] = (np.ascontiguousarray(c[k][:, :, :100]) for k in ("weights", "positions"))
+    _check_weigh(c, status=kvc.ST_BAD_INDEX)  # (90 tokens, a table of 80)
+    c = _weigh_case(5, 16, 32, 1, 2, 1, [40, 90, 64], False)
+    c["weights"], c["positions"] = (np.ascontiguousarray(c[k][:, :, :70]) for k in ("weights", "positions"))
+    want, pos, bound = ref.weigh(c["weights"], c["positions"], c["seen"], c["q"], c["pages"], 1, 16, c["table"], c["lens"], c["lse"], 32 ** -0.5)
+    got, positions, status = _weigh(c)
+    assert status == kvc.ST_BAD_INDEX and np.array_equal(pos, positions)
+    for s, n in enumerate((40, 70, 64)):
+        assert (np.abs(got - want)[s, :, :n] <= bound[s, :, :n]).all() and (got[s, :, n:] == -3).all()
+    c = _weigh_case(6, 16, 32, 1, 2, 1, [40, 90, 64], False)
+    c["table"][1, 3] = len(c["pages"])
+    _check_weigh(c, status=kvc.ST_BAD_INDEX)
+
+
+def test_weights_of_many_sequences_and_of_one_long_one():
+    rng = np.random.default_rng(0)
+    _check_weigh(_weigh_case(7, 16, 32, 1, 1, 1, rng.integers(0, 40, 700), True))
+    c = _weigh_case(8, 16, 128, 2, 4, 1, [9001], False)
+    got = _check_weigh(c)
+    assert np.array_equal(_weigh(c)[0], got)
+
+
+def test_weights_sum_to_the_number_of_queries():
+    """With the sums that attention gives, every query hands out a weight of one, over all tokens: new sequences, so nothing was there before."""
+    for fp4 in (False, True):
+        c = _weigh_case(9, 16, 128, 2, 4, 30, [30, 30, 30], fp4)
+        codec = _codec(16, 128, 4)
+        S, nq, H, d = c["q"].shape
+        out, lse = torch.empty(c["q"].shape, dtype=torch.float16, device=DEV), torch.empty((S, nq, H), device=DEV)
+        attend, size = (codec.attend_fp4, kvc.attend_fp4_workspace) if fp4 else (codec.attend, kvc.attend_workspace)
+        attend(out, _dev(c["q"]), _dev(c["cache"]), _dev(c["table"]), _dev(c["lens"]), torch.empty(size(S, nq, H, 2, d), dtype=torch.uint8, device=DEV), lse=lse)
+        c["lse"] = lse.cpu().numpy()
+        got = _weigh(c, apart=False)[0][:, :, :30]
+        # every weight is off by what its score and its query's sum are, in attention and here: 128 u * sum |q k| * scale (|q k| summed is below 128 * 40) and a few u beside
+        assert (np.abs(got.astype(np.float64).sum(2) - nq * 4) <= nq * 4 * (128 * 2.0 ** -24 * 128 * 40 * 128 ** -0.5 + 2.0 ** -18)).all()
+
+
+# ------------------------------------------------------------------------------------------------ eviction
+
+
+def _evict_case(seed, N, d, kv, lens, keep, fp4=False, separate=False, token_major=False, kind="heavy", room=3):
+    rng = np.random.default_rng(seed)
+    lens = np.array(lens, np.int32)
+    width = max(1, -(-int(lens.max(initial=0)) // N)) + 1
+    table, blocks = _table(rng, lens, N, width)
+    ppb = kv if separate else 2 * kv
+    n = 1 + separate
+    if fp4:
+        caches = [rng.integers(0, 256, (blocks, ppb * ref.page_bytes(N, d))).astype(np.uint8) for _ in range(n)]
+    else:
+        caches = [rng.integers(0, 1 << 16, (blocks, N, ppb, d) if token_major else (blocks, ppb, N, d)).astype(np.uint16) for _ in range(n)]
+    S, slots = len(lens), width * N + room
+    w = {"heavy": np.exp(4 * rng.standard_normal((S, kv, slots))), "ties": rng.integers(0, 3, (S, kv, slots)) * 0.25, "zeros": np.zeros((S, kv, slots)),
+         "any": rng.integers(0, 1 << 32, (S, kv, slots), dtype=np.uint32).view(np.float32)}[kind].astype(np.float32)
+    if kind == "ties":
+        w[rng.random(w.shape) < 0.1] = -0.0
+    if kind == "any":
+        w[rng.random(w.shape) < 0.1] = np.nan
+        w[rng.random(w.shape) < 0.1] = np.inf
+        w[rng.random(w.shape) < 0.05] = -np.inf
+    seen = (lens + rng.integers(0, 50, S)).astype(np.int32)
+    positions = np.zeros((S, kv, slots), np.int32)
+    for s in range(S):
+        for h in range(kv):
+            positions[s, h] = seen[s] - lens[s] + rng.permutation(slots)
+            at = positions[s, h, :max(0, lens[s])]
+            at[:] = rng.permutation(np.arange(len(at))) + seen[s] - lens[s]
+    return dict(N=N, d=d, kv=kv, ppb=ppb, lens=lens, keep=np.broadcast_to(np.array(keep, np.int32), lens.shape).copy(), table=table, caches=caches, fp4=fp4, separate=separate, token_major=token_major,
+                weights=w, positions=positions, seen=seen)
+
+
+def _check_evict(c, recent, apart=True, status=0, stream=None, same_lens=False):
+    N, d, kv = c["N"], c["d"], c["kv"]
+    codec = _codec(N, d, c["ppb"], c["token_major"])
+    S, _, slots = c["weights"].shape
+    caches = [_dev(x if c["fp4"] else x.view(np.float16)) for x in c["caches"]]
+    weights, positions, lens = _dev(c["weights"]), _dev(c["positions"]), _dev(c["lens"])
+    w_out, p_out = (torch.full_like(weights, -3.0), torch.full_like(positions, -77)) if apart else (None, None)
+    new_lens = lens if same_lens else torch.full_like(lens, -9)
+    work = torch.full((kvc.evict_workspace(S, kv, slots),), 0xCC, dtype=torch.uint8, device=DEV)
+    args = (caches[0], _dev(c["table"]), lens, _dev(c["keep"]), recent, weights, positions, _dev(c["seen"]), new_lens, work)
+    torch.cuda.synchronize()
+    codec.evict(*args, v_cache=caches[1] if c["separate"] else None, weights_out=w_out, positions_out=p_out, stream=stream)
+    torch.cuda.synchronize()
+    want = [x.copy() for x in c["caches"]]
+    if c["fp4"]:
+        rows = [p for x in want for p in ref.parts(x, N, d, c["ppb"])]
+        if not c["separate"]:
+            rows = [r[:, a:a + kv] for r in rows for a in (0, kv)]
+    else:
+        rows = [x.transpose(0, 2, 1, 3) if c["token_major"] else x for x in want]
+        if not c["separate"]:
+            rows = [r[:, a:a + kv] for r in rows for a in (0, kv)]
+    w, p = c["weights"].copy(), c["positions"].copy()
+    want_lens, want_status = ref.evict(rows, N, c["table"], c["lens"], c["keep"], recent, w, p, c["seen"])
+    for got, x in zip(caches, want):
+        assert np.array_equal(got.cpu().numpy().view(x.dtype), x)
+    assert np.array_equal(new_lens.cpu().numpy(), np.maximum(want_lens, 0) if not want_status else want_lens)
+    inside = np.arange(slots)[None, None] < want_lens[:, None, None]
+    inside = np.broadcast_to(inside, w.shape)
+    got_w, got_p = (w_out if apart else weights).cpu().numpy(), (p_out if apart else positions).cpu().numpy()
+    assert np.array_equal(got_w[inside].view(np.uint32), w[inside].view(np.uint32)) and np.array_equal(got_p[inside], p[inside])
+    if apart:
+        assert (got_w[~inside] == -3).all() and (got_p[~inside] == -77).all()
+        assert np.array_equal(weights.cpu().numpy().view(np.uint32), c["weights"].view(np.uint32)) and np.array_equal(positions.cpu().numpy(), c["positions"])
+    else:
+        assert np.array_equal(got_w[~inside].view(np.uint32), c["weights"][~inside].view(np.uint32)) and np.array_equal(got_p[~inside], c["positions"][~inside])
+    assert codec.stats()["status"] == (kvc.ST_BAD_INDEX if want_status else 0)
+    assert (want_status == 4) == (status != 0)
+
+
+LENS = [0, 1, 2, 33, 64, 100, 257]
+
+
+@pytest.mark.parametrize("N,d,kv", [(16, 64, 4), (16, 128, 2), (5, 32, 1), (24, 96, 3), (1, 256, 2), (7, 160, 2), (8, 192, 1), (16, 224, 1)])
+@pytest.mark.parametrize("fp4,separate,token_major", [(False, False, False), (False, True, True), (True, False, False), (True, True, False)])
+def test_eviction_moves_rows(N, d, kv, fp4, separate, token_major):
+    for keep, recent in ((40, 8), (1, 0), (256, 256)):
+        _check_evict(_evict_case(N + d, N, d, kv, LENS, keep, fp4, separate, token_major), recent, apart=keep != 1)
+
+
+@pytest.mark.parametrize("kind", ["heavy", "ties", "zeros", "any"])
+@pytest.mark.parametrize("keep,recent", [(0, 0), (1, 1), (32, 0), (50, 10), (50, 1000), (99, 3), (256, 0), (1000, 5)])
+def test_eviction_of_weights_of_every_kind(kind, keep, recent):
+    _check_evict(_evict_case(1, 16, 32, 3, LENS, keep, kind=kind), recent, apart=False)
+
+
+@pytest.mark.parametrize("n", [1023, 1024, 1025, 5000, 16384, 16385, 20001])
+def test_eviction_of_long_sequences(n):
+    for kind, keep in (("heavy", n - 1), ("ties", n // 3), ("heavy", n // 2)):
+        _check_evict(_evict_case(n, 16, 32, 1, [n, 7], keep, kind=kind), 100)
+
+
+def test_a_budget_for_each_sequence():
+    _check_evict(_evict_case(2, 16, 64, 2, [100, 100, 100, 100, 30, 0], [0, 50, 99, 200, -4, 5]), 20, same_lens=True)
+
+
+def test_positions_that_are_no_positions():
+    """More tokens claim to be recent than stay: the highest slots do; and positions at the ends of 32 bits."""
+    c = _evict_case(3, 16, 32, 2, [100, 64, 40], 30)
+    c["positions"][:] = 10**6
+    _check_evict(c, 10)
+    c["positions"][:, :, ::2] = -2**31
+    c["positions"][:, :, 1::3] = 2**31 - 1
+    c["seen"][:] = [-2**31, 2**31 - 1, 5]
+    _check_evict(c, 2**31 - 1)
+
+
+def test_sequences_that_cannot_be_evicted_are_left():
+    for what in ("missing", "beyond", "table", "slots"):
+        c = _evict_case(4, 16, 64, 2, [100, 90, 70, 64], 40)
+        if what == "missing":
+            c["table"][1, 2] = -1
+        elif what == "beyond":
+            c["table"][1, 5] = len(c["caches"][0])
+        elif what == "table":
+            c["lens"][1] = 16 * c["table"].shape[1] + 1
+            c["weights"], c["positions"] = (np.concatenate([x, x], 2) for x in (c["weights"], c["positions"]))
+        else:
+            c["lens"][1] = c["weights"].shape[2] + 1
+            c["table"][1] = c["table"][0]  # (not read: nothing of either is moved twice)
+            c["keep"][0] = 1000
+            continue
+        _check_evict(c, 5, apart=False, status=4)
+    c = _evict_case(5, 16, 64, 2, [20, 30], 10)
+    c["lens"] = np.array([-2, 30], np.int32)
+    _check_evict(c, 5, apart=False)
+
+
+def test_a_block_behind_the_last_token_is_not_looked_at():
+    c = _evict_case(6, 16, 64, 2, [96, 90], 40)
+    c["table"][0, 6] = 10**6
+    _check_evict(c, 5)
+
+
+def test_offsets_past_32_bits():
+    """Rows that move to and from the end of caches of 5 GB, in FP16 and in 4 bits."""
+    N, d, kv = 16, 128, 4
+    for fp4 in (False, True):
+        c = _evict_case(7, N, d, kv, [100, 64], 40, fp4)
+        codec = _codec(N, d, 2 * kv)
+        size = codec.fp4_block_bytes if fp4 else 2 * kv * N * d
+        blocks, n = 5 * 10**9 // (size * (1 if fp4 else 2)), len(c["caches"][0])
+        big = torch.zeros((blocks, size), dtype=torch.uint8 if fp4 else torch.float16, device=DEV)
+        small = _dev(c["caches"][0] if fp4 else c["caches"][0].view(np.float16))
+        big[blocks - n:] = small.view(n, -1)
+        table = np.where(c["table"] >= 0, c["table"] + blocks - n, -1).astype(np.int32)
+        results = []
+        for cache, t in ((small, c["table"]), (big, table)):
+            weights, positions, lens = _dev(c["weights"]), _dev(c["positions"]), _dev(c["lens"])
+            work = torch.empty(kvc.evict_workspace(2, kv, weights.shape[2]), dtype=torch.uint8, device=DEV)
+            codec.evict(cache, _dev(t), lens, _dev(c["keep"]), 4, weights, positions, _dev(c["seen"]), lens, work)
+            results.append(cache.view(-1, size)[-n:].view(torch.uint8).clone())
+        assert torch.equal(results[0], results[1]) and not torch.equal(results[0], _dev(c["caches"][0].view(np.uint8)).view(n, -1))
+        del big
+
+
+@pytest.mark.parametrize("what", ["dtype", "positions", "weights", "table", "keep", "work", "recent", "pages", "overlap"])
+def test_the_binding_refuses(what):
+    codec = _codec(16, 64, 4)
+    cache = torch.zeros((3, 4, 16, 64), dtype=torch.float16, device=DEV)
+    ids = torch.zeros(2, dtype=torch.int32, device=DEV)
+    a = dict(cache=cache, block_table=torch.zeros((2, 2), dtype=torch.int32, device=DEV), lens=ids, keep=ids.clone(), recent=1, weights=torch.zeros((2, 2, 8), device=DEV),
+             positions=torch.zeros((2, 2, 8), dtype=torch.int32, device=DEV), seen=ids.clone(), new_lens=ids.clone(), work=torch.empty(kvc.evict_workspace(2, 2, 8), dtype=torch.uint8, device=DEV))
+    codec.evict(**a)
+    long = torch.zeros(100, device=DEV)
+    bad = {"dtype": dict(cache=cache.float()), "positions": dict(positions=a["positions"][:, :, :7].contiguous()), "weights": dict(weights=a["weights"].double()), "table": dict(block_table=a["block_table"][:1]),
+           "keep": dict(keep=ids[:1]), "work": dict(work=a["work"][:256]), "recent": dict(recent=-1), "pages": dict(v_cache=cache),
+           "overlap": dict(weights=long[:32].view(2, 2, 8), weights_out=long[4:36].view(2, 2, 8))}[what]
+    with pytest.raises((AssertionError, kvc.KvcError)):
+        codec.evict(**dict(a, **bad))
+    # weigh takes the same kind of records
+    q = torch.zeros((2, 1, 4, 64), dtype=torch.float16, device=DEV)
+    w = dict(weights=a["weights"], positions=a["positions"], seen=ids, q=q, cache=cache, block_table=a["block_table"], lens=ids, lse=torch.zeros((2, 1, 4), device=DEV))
+    codec.weigh(**w)
+    bad = {"dtype": dict(cache=cache.float()), "positions": dict(positions=a["positions"].long()), "weights": dict(weights=a["weights"][:1]), "table": dict(block_table=a["block_table"][:1]),
+           "keep": dict(seen=ids[:1]), "work": dict(lse=w["lse"][:, :, :3]), "recent": dict(q=q[:, :, :3]), "pages": dict(weights=torch.zeros((2, 3, 8), device=DEV)),
+           "overlap": dict(weights=long[:32].view(2, 2, 8), weights_out=long[4:36].view(2, 2, 8))}[what]
+    with pytest.raises((AssertionError, kvc.KvcError)):
+        codec.weigh(**dict(w, **bad))
+
+
+def test_another_stream_and_nothing_to_do():
+    s = torch.cuda.Stream()
+    _check_evict(_evict_case(8, 16, 64, 2, [100, 3], 40), 5, stream=s)
+    _check_weigh(_weigh_case(10, 16, 64, 2, 2, 1, [100, 3], False), stream=s)
+    codec = _codec(16, 64, 4)
+    cache = torch.zeros((1, 4, 16, 64), dtype=torch.float16, device=DEV)
+    ids, none = torch.empty(0, dtype=torch.int32, device=DEV), torch.empty((0, 2, 8), device=DEV)
+    codec.evict(cache, ids.view(0, 1), ids, ids, 0, none, none.int(), ids, ids, torch.empty(kvc.evict_workspace(0, 2, 8), dtype=torch.uint8, device=DEV))
+    codec.weigh(none, none.int(), ids, torch.empty((0, 1, 4, 64), dtype=torch.float16, device=DEV), cache, ids.view(0, 1), ids, torch.empty((0, 1, 4), device=DEV))
