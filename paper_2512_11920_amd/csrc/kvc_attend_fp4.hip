@@ -14,13 +14,49 @@ struct TileFp4 {
     ValuesFp4<D, EIGHT> v;
     uint32_t there;
 
-    __device__ void load(const AttendFp4Args& x, const SourceFp4& s, const Blocks<EIGHT>& b, uint32_t t) {
-        load_keys<D, EIGHT>(k, x.a, x.f, s, b, t);
-        there = load_values<D, EIGHT>(v, x.a, x.f, s, b, t);
+    __device__ void load(const AttendFp4Args& x, const SourceFp4& s, const Blocks<EIGHT>& b, uint32_t t, bool live, bool& bad) {
+        load_keys<D, EIGHT>(k, x.a, x.f, s, b, t, live, bad);
+        there = load_values<D, EIGHT>(v, x.a, x.f, s, b, t, live, bad);
     }
 };
 
-// What a wave does with a tile.
+// Whether a value of the tile may not be finite: exponents from 141 on, of which append writes NaN's.
+template <int D, bool EIGHT>
+__device__ inline bool may_be_infinite(const TileFp4<D, EIGHT>& x) {
+    bool any = false;
+#pragma unroll
+    for (int p = 0; p < piece_count(D); ++p)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t byte = EIGHT ? x.v.e[p][EIGHT ? j / 4 : j] >> (EIGHT ? 8 * (j % 4) : 0) & 255 : x.v.e[p][j];
+            any = any || (x.there >> j & 1 && byte > 140);
+        }
+    return __any(any);
+}
+
+// One piece's values of 8 tokens times the rows' weights; `mine`: rows for which the result is taken.
+template <int D, int R, int P = 0>
+__device__ inline void add_values_of(Rows<D> (&r)[R], const Tokens<D>& x, const half8 (&p)[R], const bool (&mine)[R]) {
+    if constexpr (P < piece_count(D)) {
+        using Q = Piece<D, P>;
+#pragma unroll
+        for (int j = 0; j < Q::w; ++j) {
+            const half8 v = __builtin_bit_cast(half8, value_column<D, P>(x, j));
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                float4v& o = r[i].o[Q::before / 16 + j];
+                const float4v n = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p[i], o, 0, 0, 0);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] = mine[i] ? n[e] : o[e];
+            }
+            __builtin_amdgcn_sched_barrier(0);  // (one at a time: there are few registers)
+        }
+        add_values_of<D, R, P + 1>(r, x, p, mine);
+    }
+}
+
+// What a wave does with a tile.  Among the last n_q tokens some rows see values that others do not, and weight zero times one that is not finite is NaN: there, rows that see so many
+// of the tile's tokens are done by themselves, the other tokens' values being zero.
 template <int D, int R, bool EIGHT>
 __device__ inline void add_tile_fp4(Rows<D> (&r)[R], const AttendFp4Args& x, const TileFp4<D, EIGHT>& tile, uint32_t t, uint32_t len, const uint32_t (&limit)[R]) {
     Tokens<D> tokens;
@@ -32,8 +68,25 @@ __device__ inline void add_tile_fp4(Rows<D> (&r)[R], const AttendFp4Args& x, con
         scores(s, r[j], tokens);
         p[j] = weights(r[j], s, x.a.scale_log2, tile.there, t, limit[j]);
     }
+    if (x.a.n_q > 1 && t + kTile + x.a.n_q - 1 > len && may_be_infinite<D, EIGHT>(tile)) {
+        const uint32_t first = t + 8 * ((threadIdx.x & 63) >> 4);
+#pragma nounroll
+        for (uint32_t cut = 1; cut <= kTile; ++cut) {  // rows that see the tile's first `cut` tokens, and no more
+            bool mine[R], any = false;
+#pragma unroll
+            for (int j = 0; j < R; ++j) {
+                mine[j] = min(limit[j] > t ? limit[j] - t : 0, (uint32_t)kTile) == cut;
+                any = any || mine[j];
+            }
+            if (!__any(any)) continue;
+            const uint32_t n = t + cut > first ? t + cut - first : 0;
+            expand_values<D, EIGHT>(tokens, tile.v, tile.there & (n >= 8 ? 0xFFu : ~(~0u << n)));
+            add_values_of<D, R>(r, tokens, p, mine);
+        }
+        return;
+    }
     expand_values<D, EIGHT>(tokens, tile.v, tile.there);
-    add_tile<D, R>(r, tokens, p, t, len, x.a.n_q, limit);
+    add_values<D, R>(r, tokens, p);
 }
 
 // ---- any lengths: a worker is a wave, the next tile is on its way while this one is computed, its block numbers a tile further ahead.
@@ -70,7 +123,7 @@ __device__ inline void own_part_fp4(const AttendFp4Args& x, Sums& sums, uint32_t
     };
     const auto source = [&](const Place& p) {
         const uint32_t h = p.u / a.own_tiles;
-        return SourceFp4{Source{a.table + (int64_t)p.s * a.max_blocks, nullptr, nullptr, p.len}, x.k + (int64_t)h * x.f.page, x.v + (int64_t)h * x.f.page};
+        return SourceFp4{a.table + (int64_t)p.s * a.max_blocks, p.len, x.k + (int64_t)h * x.f.page, x.v + (int64_t)h * x.f.page};
     };
 
     const uint32_t lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
@@ -86,6 +139,8 @@ __device__ inline void own_part_fp4(const AttendFp4Args& x, Sums& sums, uint32_t
             load_query<D>(r[j].q, a.q + p.s * a.q_strides[0] + i * a.q_strides[1] + (h * a.group + in) * a.q_strides[2], g);
             const uint32_t later = a.n_q - 1 - i, len = (uint32_t)a.lens[p.s];
             limit[j] = min(len > later ? len - later : 0, p.len);
+#pragma unroll
+            for (int k = 0; k < D / 32; ++k) asm volatile("" : "+v"(r[j].q[k]));  // (waited for here, not in every step)
         }
     };
     const auto close = [&](const Place& p, uint32_t first_tile) {
@@ -108,26 +163,28 @@ __device__ inline void own_part_fp4(const AttendFp4Args& x, Sums& sums, uint32_t
         }
     };
 
-    // c: the tile computed; c1: the one loaded; c2: the one whose blocks are looked up
-    Place c1 = c, c2 = c;
+    // c: the tile computed; c1 and c2: those on their way; c3: the one whose blocks are looked up, before c2 is asked for, so that waiting for them is not waiting for it.
+    // All loads are made in any case (behind the last tile, of zeros): the compiler then knows how many come after those that it waits for.
     uint32_t left = end - begin, first_tile = c.t;
-    TileFp4<D, EIGHT> here, next;
-    Blocks<EIGHT> b = find_blocks<EIGHT>(a, source(c).at, c.t * kTile);
+    const auto next = [&](const Place& p, uint32_t ahead) {
+        Place n = p;
+        if (left > ahead) advance(n);
+        return n;
+    };
+    const auto find = [&](const Place& p) { return look_up<EIGHT>(a, a.table + (int64_t)p.s * a.max_blocks, p.len, p.t * kTile); };
+    bool bad = false;
+    TileFp4<D, EIGHT> tiles[3];
+    Place c1 = next(c, 1), c2 = next(c1, 2);
+    Blocks<EIGHT> b = find(c), b1 = find(c1), b2 = find(c2);
     open(c);
-    here.load(x, source(c), b, c.t * kTile);
-    if (left > 1) {
-        advance(c1);
-        b = find_blocks<EIGHT>(a, source(c1).at, c1.t * kTile);
-        c2 = c1;
-    }
+    tiles[0].load(x, source(c), b, c.t * kTile, true, bad);
+    tiles[1].load(x, source(c1), b1, c1.t * kTile, left > 1, bad);
     const auto step = [&](TileFp4<D, EIGHT>& now, TileFp4<D, EIGHT>& then) {  // -> whether it was the last one
-        if (left > 1) {
-            then.load(x, source(c1), b, c1.t * kTile);
-            if (left > 2) {
-                advance(c2);
-                b = find_blocks<EIGHT>(a, source(c2).at, c2.t * kTile);
-            }
-        }
+        const Place c3 = next(c2, 3);
+        const Blocks<EIGHT> b3 = find(c3);
+        __builtin_amdgcn_sched_barrier(0);
+        then.load(x, source(c2), b2, c2.t * kTile, left > 2, bad);
+        __builtin_amdgcn_sched_barrier(0);
         add_tile_fp4<D, R, EIGHT>(r, x, now, c.t * kTile, c.len, limit);
         if (left == 1 || c1.t == 0) {
             close(c, first_tile);
@@ -137,11 +194,14 @@ __device__ inline void own_part_fp4(const AttendFp4Args& x, Sums& sums, uint32_t
         }
         c = c1;
         c1 = c2;
+        c2 = c3;
+        b2 = b3;
         --left;
         return false;
     };
-    while (!step(here, next) && !step(next, here)) {
+    while (!step(tiles[0], tiles[2]) && !step(tiles[1], tiles[0]) && !step(tiles[2], tiles[1])) {
     }
+    if (bad) atomicOr(&a.st->status, KVC_ST_BAD_INDEX);
 }
 
 template <int D, int R, bool EIGHT>
@@ -158,8 +218,9 @@ __global__ __launch_bounds__(64 * kDirectWaves, D * R <= 128 ? 2 : 1) void k_dir
     __shared__ __align__(16) float sums[kDirectWaves][16 * R][D];
     const uint32_t lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4, wave = uniform(threadIdx.x / 64);
     const uint32_t units = a.n_kv * a.own_tiles, s = blockIdx.x / units, u = blockIdx.x - s * units, h = u / a.own_tiles, rt = u - h * a.own_tiles;
-    SourceFp4 src{Source{a.table + (int64_t)s * a.max_blocks, nullptr, nullptr, (uint32_t)a.max_blocks * (uint32_t)a.g.N}, x.k + (int64_t)h * x.f.page, x.v + (int64_t)h * x.f.page};
-    Blocks<EIGHT> b = find_blocks<EIGHT>(a, src.at, wave * kTile);  // (as far as the table's row goes)
+    SourceFp4 src{a.table + (int64_t)s * a.max_blocks, (uint32_t)a.max_blocks * (uint32_t)a.g.N, x.k + (int64_t)h * x.f.page, x.v + (int64_t)h * x.f.page};
+    Blocks<EIGHT> b;
+    if (wave * kTile < src.len) b = look_up<EIGHT>(a, src.table, src.len, wave * kTile);  // (as far as the table's row goes)
     Rows<D> r[R];
     uint32_t later[R];
 #pragma unroll
@@ -171,18 +232,19 @@ __global__ __launch_bounds__(64 * kDirectWaves, D * R <= 128 ? 2 : 1) void k_dir
         later[j] = a.n_q - 1 - i;
     }
     const uint32_t len = uniform((uint32_t)max(a.lens[s], 0));
-    src.at.len = uniform(own_length(a, s));
-    const uint32_t tiles = (src.at.len + kTile - 1) / kTile;
+    src.len = uniform(own_length(a, s));
+    const uint32_t tiles = (src.len + kTile - 1) / kTile;
+    bool bad = false;
     for (uint32_t t = wave; t < tiles; t += kDirectWaves) {
-        if (t != wave) b = find_blocks<EIGHT>(a, src.at, t * kTile);
-        b.end_at(t * kTile, src.at.len);  // (entries behind the last token are not block numbers)
+        if (t != wave) b = look_up<EIGHT>(a, src.table, src.len, t * kTile);
         TileFp4<D, EIGHT> tile;
-        tile.load(x, src, b, t * kTile);
+        tile.load(x, src, b, t * kTile, true, bad);
         uint32_t limit[R];
 #pragma unroll
-        for (int j = 0; j < R; ++j) limit[j] = min(len > later[j] ? len - later[j] : 0, src.at.len);
-        add_tile_fp4<D, R, EIGHT>(r, x, tile, t * kTile, src.at.len, limit);
+        for (int j = 0; j < R; ++j) limit[j] = min(len > later[j] ? len - later[j] : 0, src.len);
+        add_tile_fp4<D, R, EIGHT>(r, x, tile, t * kTile, src.len, limit);
     }
+    if (bad) atomicOr(&a.st->status, KVC_ST_BAD_INDEX);
     const uint32_t workers = min(tiles, kDirectWaves);
 #pragma unroll
     for (int j = 0; j < R; ++j) {

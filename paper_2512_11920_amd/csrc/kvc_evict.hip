@@ -16,6 +16,9 @@ __device__ inline uint32_t order_of(float w) {
     return b >> 31 ? ~b : b | 0x80000000u;
 }
 
+// set bits of lanes before this one
+__device__ inline uint32_t before_lane(uint64_t lanes) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(lanes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)lanes, 0)); }
+
 struct SelectLds {
     uint32_t keys[kKeysKept];
     uint32_t bins[256];
@@ -101,13 +104,12 @@ __global__ __launch_bounds__(kSelectThreads) void k_select(EvictArgs a) {
     __syncthreads();
     uint32_t ties_before = 0;
     for (uint32_t w = 0; w < wave; ++w) ties_before += lds.ties[w];
-    const uint64_t below = (1ull << lane) - 1;
     const auto walk = [&](auto each) {  // each(t, hole, filler, which lanes have holes, which have fillers)
         uint32_t seen = ties_before;
         for (uint32_t t = from + lane; t - lane < to; t += 64) {
             const uint32_t k = t < to ? key(t) : 0xFFFFFFFFu;
             const uint64_t equal = __ballot(t < to && k == prefix);
-            const bool leaves = t < to && (k < prefix || (k == prefix && seen + __popcll(equal & below) < rank));
+            const bool leaves = t < to && (k < prefix || (k == prefix && seen + before_lane(equal) < rank));
             seen += __popcll(equal);
             const bool hole = leaves && t < (uint32_t)keep, filler = t < to && !leaves && t >= (uint32_t)keep;
             each(t, hole, filler, __ballot(hole), __ballot(filler));
@@ -125,8 +127,8 @@ __global__ __launch_bounds__(kSelectThreads) void k_select(EvictArgs a) {
     int32_t* hole_list = a.holes + (int64_t)unit * a.most;
     int32_t* filler_list = a.fillers + (int64_t)unit * a.most;
     walk([&](uint32_t t, bool hole, bool filler, uint64_t h, uint64_t f) {
-        if (hole) hole_list[hole_at + __popcll(h & below)] = (int32_t)t;
-        if (filler) filler_list[filler_at + __popcll(f & below)] = (int32_t)t;
+        if (hole) hole_list[hole_at + before_lane(h)] = (int32_t)t;
+        if (filler) filler_list[filler_at + before_lane(f)] = (int32_t)t;
         hole_at += __popcll(h);
         filler_at += __popcll(f);
         if (!hole && t < to && t < (uint32_t)keep) {

@@ -55,7 +55,8 @@ struct WeighArgs {
     int32_t* positions;     // [n_seq][n_kv][width]
     const int32_t* seen;    // [n_seq]
     int32_t width;
-    uint32_t workers;       // waves
+    bool many;              // queries
+    uint32_t workers;       // waves, or workgroups of many queries
 };
 
 struct EvictArgs {
@@ -93,7 +94,7 @@ inline AttendPlan plan_attend_fp4(int64_t n_seq, int64_t n_q, int64_t n_heads, i
     p.bytes = p.starts + round_256(p.slots * 8) + p.slots * (uint64_t)d * 4;
     return p;
 }
-constexpr uint32_t kWeighWorkers = 2048;
+constexpr uint32_t kWeighWorkers = 2048, kWeighGroups = 768, kManyRows = 64;
 
 hipError_t launch_append_fp4(const AppendFp4Args& a, hipStream_t s);
 hipError_t launch_unpack_fp4(const UnpackFp4Args& a, hipStream_t s);

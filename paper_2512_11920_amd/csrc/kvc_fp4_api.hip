@@ -188,7 +188,8 @@ int kvc_weigh(kvc_ctx* ctx, const kvc_weigh_t* p, void* stream) {
     x.positions = p->d_positions;
     x.seen = p->d_seen;
     x.width = p->width;
-    x.workers = kWeighWorkers;
+    x.many = x.a.rows > (int32_t)kManyRows;
+    x.workers = x.many ? kWeighGroups : kWeighWorkers;
     hipStream_t s = static_cast<hipStream_t>(stream);
     switch (ctx->g.d) {
         case 32: return launched(launch_weigh<32>(x, s));

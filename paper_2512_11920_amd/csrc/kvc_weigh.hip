@@ -1,6 +1,6 @@
 // The attention weight that tokens get, compiled once per head dimension (-DKVC_HEAD_DIM=d): W[s][h][t] += sum over the queries of head h's group that see t of e^(scale <q, k_t> - lse).
 //
-// Scores are made with queries as rows and tokens as columns, S = Q K^T, so that a lane of group g has four queries' scores of one token: they are added in the lane, then over the four
+// Scores are made with queries as rows and tokens as columns, S = Q K^T, so that a lane of group g = lane / 16 has four queries' scores of one token: they are added in the lane, then over the four
 // groups.  A token's weight is written by one lane in one order: the same call gives the same bits.
 #include "kvc_attend_fp4.h"
 
@@ -17,40 +17,72 @@ __device__ inline uint32_t weighed_length(const WeighArgs& x, int s) {
     atomicOr(&x.a.st->status, KVC_ST_BAD_INDEX);
     return (uint32_t)x.width;
 }
+__device__ inline SourceFp4 keys_of(const WeighArgs& x, uint32_t s, uint32_t h, uint32_t len) {
+    return SourceFp4{x.a.table + (int64_t)s * x.a.max_blocks, len, x.k ? x.k + (int64_t)h * x.f.page : reinterpret_cast<const uint8_t*>(x.a.k_cache + h * x.a.g.page_stride), nullptr};
+}
 
-// Keys of 32 tokens on their way, and what their tokens had.
+// Keys of 32 tokens on their way: token 8 * (n / 4) + 4u + n % 4 of them is column n of score tile u.
 template <int D, bool FP4, bool EIGHT>
 struct KeyTile {
     KeysFp4<D> packed;
-    Tokens<D> keys;
-    float had;
-    bool there[2];  // the lane's tokens
+    uint4v keys[2][D / 32];
+    uint32_t there;  // bit u
 
-    __device__ void load(const WeighArgs& x, const SourceFp4& s, const Blocks<EIGHT>& b, const Place& p) {
-        const uint32_t t = p.t * kTile;
-        if constexpr (FP4) load_keys<D, EIGHT>(packed, x.a, x.f, s, b, t);
-        else load_keys<D, EIGHT>(keys, x.a, s.at, b, t);
+    __device__ void load(const WeighArgs& x, const SourceFp4& s, const Blocks<EIGHT>& b, uint32_t t, bool live, bool& bad) {
+        const uint32_t lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4, first = t + 8 * (n >> 2) + (n & 3);
+        there = 0;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             const int32_t block = b.key(u);
-            there[u] = block >= 0 && block < x.a.n_cache_blocks;
+            const bool have = is_there(x.a, block, live && first + 4 * u < s.len, bad);
+            there |= have ? 1u << u : 0u;
+            if constexpr (!FP4) {
+                bytes_at row = have ? (bytes_at)s.k + 2 * place(x.a, block, first + 4 * u) : (bytes_at)kZeroRow;
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) keys[u][c] = load_from<uint4v>(row + 64 * c + 16 * g);
+            }
         }
-        const uint32_t lane = threadIdx.x & 63, token = token_of(t);
-        had = 0.f;
-        if (lane < 32 && token < p.len && (int64_t)token < (int64_t)x.a.lens[p.s] - x.a.n_q) had = x.before[((int64_t)p.s * x.a.n_kv + p.u) * x.width + token];
+        if constexpr (FP4) load_keys<D, EIGHT>(packed, x.a, x.f, s, b, t, live, bad);
     }
-    __device__ const Tokens<D>& expand() {
-        if constexpr (FP4) expand_keys<D, EIGHT>(keys, packed);
-        return keys;
-    }
-    // token whose weight lanes 0 to 31 write
-    __device__ static uint32_t token_of(uint32_t t) {
-        const uint32_t lane = threadIdx.x & 63;
-        return t + 8 * ((lane & 15) >> 2) + 4 * (lane >> 4 & 1) + (lane & 3);
+    __device__ void expand(uint4v (&to)[2][D / 32]) const {
+        if constexpr (FP4) {
+            Tokens<D> tokens;
+            expand_keys<D, EIGHT>(tokens, packed);
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) to[u][c] = tokens.k[u][c];
+        } else {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) to[u][c] = keys[u][c];
+        }
     }
 };
 
-// 16 queries, and of the lane's four (4g..4g+3): -lse in powers of two, and the tokens they see.
+// Query row `row` of a sequence and KV head: its token, and where it and its sum are.
+struct Row {
+    uint32_t i, head;
+    __device__ Row(const AttendArgs& a, uint32_t h, uint32_t row) {
+        const uint32_t in = fast_div(row, a.by_n_q);
+        i = row - in * a.n_q;
+        head = h * a.group + in;
+    }
+    __device__ const uint16_t* query(const AttendArgs& a, uint32_t s) const { return a.q + s * a.q_strides[0] + i * a.q_strides[1] + head * a.q_strides[2]; }
+    // -lse in powers of two; a query that sees nothing gives weights of zero
+    __device__ float low(const AttendArgs& a, uint32_t s) const {
+        const float lse = a.lse[((int64_t)s * a.n_q + i) * a.n_heads + head];
+        return lse == -INFINITY ? -INFINITY : -lse * 1.44269504088896341f;
+    }
+    // tokens it sees
+    __device__ uint32_t limit(const AttendArgs& a, uint32_t full, uint32_t len) const {
+        const uint32_t later = a.n_q - 1 - i;
+        return min(full > later ? full - later : 0, len);
+    }
+};
+
+// 16 queries, and of the lane's four (4g..4g+3): -lse, and the tokens they see.
 template <int D>
 struct Queries {
     uint4v q[D / 32];
@@ -58,48 +90,80 @@ struct Queries {
     uint32_t limit[4];
 
     template <bool FP4>
-    __device__ void load(const WeighArgs& x, const Place& p, uint32_t rt) {
+    __device__ void load(const WeighArgs& x, uint32_t s, uint32_t h, uint32_t full, uint32_t len, uint32_t rt) {
         const AttendArgs& a = x.a;
-        const uint32_t lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4, len = (uint32_t)a.lens[p.s];
+        const uint32_t lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4, last = (uint32_t)a.rows - 1;
         {
-            const uint32_t row = min(rt * 16 + n, (uint32_t)a.rows - 1), in = fast_div(row, a.by_n_q), i = row - in * a.n_q;
-            const uint16_t* from = a.q + p.s * a.q_strides[0] + i * a.q_strides[1] + (p.u * a.group + in) * a.q_strides[2];
-            if constexpr (FP4) load_query<D>(q, from, g);
-            else
+            const uint16_t* from = Row(a, h, min(rt * 16 + n, last)).query(a, s);
+            if constexpr (FP4) {
+                load_query<D>(q, from, g);
+            } else {
 #pragma unroll
                 for (int k = 0; k < D / 32; ++k) q[k] = *reinterpret_cast<const uint4v*>(from + 32 * k + 8 * g);
+            }
         }
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const uint32_t row = rt * 16 + 4 * g + r, in = fast_div(min(row, (uint32_t)a.rows - 1), a.by_n_q), i = min(row, (uint32_t)a.rows - 1) - in * a.n_q, later = a.n_q - 1 - i;
-            const float lse = a.lse[((int64_t)p.s * a.n_q + i) * a.n_heads + p.u * a.group + in];
-            low[r] = lse == -INFINITY ? -INFINITY : -lse * 1.44269504088896341f;  // (a query that sees nothing: weights of zero)
-            limit[r] = row < (uint32_t)a.rows ? min(len > later ? len - later : 0, p.len) : 0;
+            const uint32_t row = rt * 16 + 4 * g + r;
+            const Row of(a, h, min(row, last));
+            low[r] = of.low(a, s);
+            limit[r] = row <= last ? of.limit(a, full, len) : 0;
         }
     }
 };
 
 template <int D>
-__device__ inline void add_weights(float (&sum)[2], const WeighArgs& x, const Queries<D>& q, const Tokens<D>& k, uint32_t t) {
-    float4v s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+__device__ inline void score(float4v (&s)[2], const uint4v (&q)[D / 32], const uint4v (&k)[2][D / 32]) {
+    s[0] = s[1] = float4v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int c = 0; c < D / 32; ++c)
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
-            s[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, q.q[c]), __builtin_bit_cast(half8, k.k[u][c]), s[u], 0, 0, 0);
-    const uint32_t lane = threadIdx.x & 63, token = t + 8 * ((lane & 15) >> 2) + (lane & 3);
+        for (int u = 0; u < 2; ++u) s[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, q[c]), __builtin_bit_cast(half8, k[u][c]), s[u], 0, 0, 0);
+}
+// ALL: every query sees every token.
+template <bool ALL>
+__device__ inline void add_weights(float (&sum)[2], const float4v (&s)[2], float scale_log2, const float (&low)[4], const uint32_t (&limit)[4], uint32_t token) {
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const float w = power2(fmaf(s[u][r], x.a.scale_log2, q.low[r]));
-            sum[u] += token + 4 * u < q.limit[r] ? w : 0.f;
+            const float w = power2(fmaf(s[u][r], scale_log2, low[r]));
+            sum[u] += ALL || token + 4 * u < limit[r] ? w : 0.f;
         }
 }
 
-// Work is divided as attention divides it, a unit being a sequence and a KV head.  FEW: a head has 16 queries or fewer, which stay in registers.
-template <int D, bool FP4, bool EIGHT, bool FEW>
-__global__ __launch_bounds__(256, 2) void k_weigh(WeighArgs x) {
+// What a lane's tokens got, added to what they had, and positions of those that are new.
+struct Result {
+    float* after;
+    int32_t* positions;
+
+    // lanes 0 to 31 write a token each, this one
+    __device__ static uint32_t token(uint32_t t) {
+        const uint32_t lane = threadIdx.x & 63;
+        return t + 8 * ((lane & 15) >> 2) + 4 * (lane >> 4 & 1) + (lane & 3);
+    }
+    __device__ void store(float (&sum)[2], uint32_t there, float had, const WeighArgs& x, uint32_t t, uint32_t full, uint32_t len, int32_t seen) const {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            sum[u] = row_sum(sum[u]);
+            if (!(there >> u & 1)) sum[u] = 0.f;
+        }
+        const uint32_t lane = threadIdx.x & 63, at = token(t), from_end = full - at;
+        if (lane >= 32 || at >= len) return;
+        const bool is_new = from_end <= (uint32_t)x.a.n_q;
+        after[at] = (is_new ? 0.f : had) + (lane < 16 ? sum[0] : sum[1]);
+        if (is_new) positions[at] = (int32_t)((uint32_t)seen - from_end);
+    }
+};
+__device__ inline Result result_of(const WeighArgs& x, uint32_t s, uint32_t h) {
+    const int64_t at = ((int64_t)s * x.a.n_kv + h) * x.width;
+    return Result{x.after + at, x.positions + at};
+}
+
+// ---- few queries: bound by memory.  Work is divided as attention divides it, a unit being a sequence and a KV head, and tiles are on their way as in k_own_fp4.  ONE: a head has 16 queries
+// or fewer, which stay in registers.
+template <int D, bool FP4, bool EIGHT, bool ONE>
+__global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_weigh(WeighArgs x) {
     __shared__ Sums sums;
     const AttendArgs& a = x.a;
     const uint32_t worker = uniform(blockIdx.x * 4 + threadIdx.x / 64);
@@ -119,86 +183,184 @@ __global__ __launch_bounds__(256, 2) void k_weigh(WeighArgs x) {
         c.u = rel / c.tiles;
         c.t = rel - c.u * c.tiles;
     }
-    const auto advance = [&](Place& p) {  // (there is a next tile)
-        if (++p.t < p.tiles) return;
-        p.t = 0;
-        if (++p.u < units) return;
-        p.u = 0;
+    uint32_t left = end - begin;
+    const auto next = [&](const Place& p, uint32_t ahead) {
+        Place n = p;
+        if (left <= ahead || ++n.t < n.tiles) return n;
+        n.t = 0;
+        if (++n.u < units) return n;
+        n.u = 0;
         do {
-            ++p.s;
-            p.len = uniform(weighed_length(x, p.s));
-        } while (p.len == 0);
-        p.tiles = (p.len + kTile - 1) / kTile;
+            ++n.s;
+            n.len = uniform(weighed_length(x, n.s));
+        } while (n.len == 0);
+        n.tiles = (n.len + kTile - 1) / kTile;
+        return n;
     };
-    const auto source = [&](const Place& p) {
-        return SourceFp4{Source{a.table + (int64_t)p.s * a.max_blocks, FP4 ? nullptr : a.k_cache + p.u * a.g.page_stride, nullptr, p.len}, FP4 ? x.k + (int64_t)p.u * x.f.page : nullptr, nullptr};
+    struct Ahead {
+        KeyTile<D, FP4, EIGHT> keys;
+        float had;
+    };
+    bool bad = false;
+    const auto find = [&](const Place& p) { return look_up<EIGHT>(a, a.table + (int64_t)p.s * a.max_blocks, p.len, p.t * kTile); };
+    const auto load = [&](Ahead& to, const Place& p, const Blocks<EIGHT>& b, bool live) {
+        to.keys.load(x, keys_of(x, p.s, p.u, p.len), b, p.t * kTile, live, bad);
+        to.had = load_from<float>((bytes_at)(x.before + ((int64_t)p.s * a.n_kv + p.u) * x.width + min(Result::token(p.t * kTile), p.len - 1)));
     };
 
     const uint32_t lane = threadIdx.x & 63, row_tiles = (a.rows + 15) / 16;
     Queries<D> q;
-    // c: the tile computed; c1: the one loaded; c2: the one whose blocks are looked up
-    Place c1 = c, c2 = c;
-    uint32_t left = end - begin;
-    KeyTile<D, FP4, EIGHT> here, next;
-    Blocks<EIGHT> b = find_blocks<EIGHT>(a, source(c).at, c.t * kTile);
-    if (FEW) q.template load<FP4>(x, c, 0);
-    here.load(x, source(c), b, c);
-    if (left > 1) {
-        advance(c1);
-        b = find_blocks<EIGHT>(a, source(c1).at, c1.t * kTile);
-        c2 = c1;
-    }
-    const auto step = [&](KeyTile<D, FP4, EIGHT>& now, KeyTile<D, FP4, EIGHT>& then) {  // -> whether it was the last one
-        if (left > 1) {
-            then.load(x, source(c1), b, c1);
-            if (left > 2) {
-                advance(c2);
-                b = find_blocks<EIGHT>(a, source(c2).at, c2.t * kTile);
-            }
-        }
-        const uint32_t t = c.t * kTile;
-        const Tokens<D>& keys = now.expand();
+    uint32_t full;
+    int32_t seen;
+    const auto open = [&](const Place& p) {
+        full = uniform((uint32_t)a.lens[p.s]);
+        seen = x.seen[p.s];
+        if (ONE) q.template load<FP4>(x, p.s, p.u, full, p.len, 0);
+        asm volatile("" : "+v"(seen));  // (waited for here, not in every step)
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k) asm volatile("" : "+v"(q.q[k]));
+    };
+    // c: the tile computed; c1 and c2: those on their way; c3: the one whose blocks are looked up
+    Ahead tiles[3];
+    Place c1 = next(c, 1), c2 = next(c1, 2);
+    Blocks<EIGHT> b = find(c), b1 = find(c1), b2 = find(c2);
+    open(c);
+    load(tiles[0], c, b, true);
+    load(tiles[1], c1, b1, left > 1);
+    const auto step = [&](Ahead& now, Ahead& then) {  // -> whether it was the last one
+        const Place c3 = next(c2, 3);
+        const Blocks<EIGHT> b3 = find(c3);
+        __builtin_amdgcn_sched_barrier(0);
+        load(then, c2, b2, left > 2);
+        __builtin_amdgcn_sched_barrier(0);
+        const uint32_t t = c.t * kTile, token = t + 8 * ((lane & 15) >> 2) + (lane & 3);
+        uint4v keys[2][D / 32];
+        now.keys.expand(keys);
         float sum[2] = {0.f, 0.f};
-        if (FEW) {
-            add_weights(sum, x, q, keys, t);
+        float4v s[2];
+        if (ONE) {
+            score<D>(s, q.q, keys);
+            add_weights<false>(sum, s, a.scale_log2, q.low, q.limit, token);
         } else {
             for (uint32_t rt = 0; rt < row_tiles; ++rt) {
-                q.template load<FP4>(x, c, rt);
-                add_weights(sum, x, q, keys, t);
+                q.template load<FP4>(x, c.s, c.u, full, c.len, rt);
+                score<D>(s, q.q, keys);
+                add_weights<false>(sum, s, a.scale_log2, q.low, q.limit, token);
             }
         }
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            sum[u] = row_sum(sum[u]);
-            if (!now.there[u]) sum[u] = 0.f;
-        }
-        const uint32_t token = now.token_of(t);
-        if (lane < 32 && token < c.len) {
-            const int64_t at = ((int64_t)c.s * a.n_kv + c.u) * x.width + token;
-            const int64_t from_end = (int64_t)a.lens[c.s] - token;
-            x.after[at] = now.had + (lane < 16 ? sum[0] : sum[1]);
-            if (from_end <= a.n_q) x.positions[at] = (int32_t)(x.seen[c.s] - from_end);
-        }
+        result_of(x, c.s, c.u).store(sum, now.keys.there, now.had, x, t, full, c.len, seen);
         if (left == 1) return true;
-        if (FEW && c1.t == 0) q.template load<FP4>(x, c1, 0);
+        if (c1.t == 0) open(c1);
         c = c1;
         c1 = c2;
+        c2 = c3;
+        b2 = b3;
         --left;
         return false;
     };
-    while (!step(here, next) && !step(next, here)) {
+    while (!step(tiles[0], tiles[2]) && !step(tiles[1], tiles[0]) && !step(tiles[2], tiles[1])) {
     }
+    if (bad) atomicOr(&a.st->status, KVC_ST_BAD_INDEX);
 }
 
-template <int D, bool FP4>
+// ---- many queries: bound by the products and the powers.  A workgroup takes 128 tokens of a sequence and head, 32 to a wave, whose keys stay in registers; 16 queries at a time come to LDS for all waves, the
+// next ones on their way meanwhile, with their -lse and the tokens they see.
+constexpr uint32_t kChunk = 4 * kTile;
+template <int D, bool FP4, bool EIGHT>
+__global__ __launch_bounds__(256, 2) void k_weigh_many(WeighArgs x) {
+    constexpr uint32_t kStride = 2 * D + 16;  // bytes of a query in LDS: 16 lanes that read the same channels of 16 queries meet in no bank
+    constexpr uint32_t kPieces = (16 * D / 8 + 255) / 256;  // of 16 bytes, of a thread
+    __shared__ Sums sums;
+    __shared__ __align__(16) uint8_t queries[2][16 * kStride];
+    __shared__ __align__(16) float lows[2][16];
+    __shared__ __align__(16) uint32_t limits[2][16];
+    const AttendArgs& a = x.a;
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform(tid / 64), n = lane & 15, g = lane >> 4, row_tiles = (a.rows + 15) / 16;
+    const auto chunks_of = [&](uint32_t s) { return (weighed_length(x, s) + kChunk - 1) / kChunk; };
+    add_up(sums, a.n_seq, chunks_of);
+    const uint32_t all = uniform(sums.all) * a.n_kv;
+    bool bad = false;
+    for (uint32_t chunk = blockIdx.x; chunk < all; chunk += gridDim.x) {
+        const Item it = find_item(sums, a.n_seq, chunk / a.n_kv, chunks_of);
+        const uint32_t s = uniform(it.i), len = uniform(weighed_length(x, s)), chunks = (len + kChunk - 1) / kChunk, rel = chunk - uniform(it.start) * a.n_kv, h = rel / chunks;
+        const uint32_t begin = (rel - h * chunks) * kChunk, t = begin + wave * kTile, full = uniform((uint32_t)a.lens[s]);
+        const bool live = t < len;
+        uint4v ahead[kPieces];
+        float low_ahead = 0.f;
+        uint32_t limit_ahead = 0;
+        const auto ask = [&](uint32_t rt) {
+#pragma unroll
+            for (uint32_t k = 0; k < kPieces; ++k) {
+                const uint32_t i = min(tid + 256 * k, 16u * D / 8 - 1), row = min(rt * 16 + i / (D / 8), (uint32_t)a.rows - 1);
+                ahead[k] = load_from<uint4v>((bytes_at)(Row(a, h, row).query(a, s) + 8 * (i % (D / 8))));
+            }
+            if (tid < 16) {
+                const uint32_t row = rt * 16 + tid;
+                const Row of(a, h, min(row, (uint32_t)a.rows - 1));
+                low_ahead = of.low(a, s);
+                limit_ahead = row < (uint32_t)a.rows ? of.limit(a, full, len) : 0;
+            }
+        };
+        const auto put = [&](uint32_t buffer) {
+#pragma unroll
+            for (uint32_t k = 0; k < kPieces; ++k) {
+                const uint32_t i = tid + 256 * k;
+                if (i < 16 * D / 8) *reinterpret_cast<uint4v*>(&queries[buffer][i / (D / 8) * kStride + i % (D / 8) * 16]) = ahead[k];
+            }
+            if (tid < 16) lows[buffer][tid] = low_ahead, limits[buffer][tid] = limit_ahead;
+        };
+        const SourceFp4 src = keys_of(x, s, h, len);
+        const Blocks<EIGHT> b = look_up<EIGHT>(a, src.table, len, t);
+        KeyTile<D, FP4, EIGHT> tile;
+        tile.load(x, src, b, t, live, bad);
+        ask(0);
+        uint4v keys[2][D / 32];
+        tile.expand(keys);
+        const uint32_t token = t + 8 * (n >> 2) + (n & 3);
+        const float had = load_from<float>((bytes_at)(x.before + ((int64_t)s * a.n_kv + h) * x.width + min(Result::token(t), len - 1)));
+        // (queries that see all of the chunk, and exist, need no comparison)
+        const bool all_seen = begin + kChunk + a.n_q <= full + 1 && begin + kChunk <= len;
+        float sum[2] = {0.f, 0.f};
+        for (uint32_t rt = 0; rt < row_tiles; ++rt) {
+            const uint32_t buffer = rt & 1;
+            put(buffer);  // (the waves that read this buffer are past the last barrier)
+            __syncthreads();
+            if (rt + 1 < row_tiles) ask(rt + 1);
+            uint4v q[D / 32];
+            if constexpr (FP4) {
+                const uint8_t* row = &queries[buffer][n * kStride];
+                load_query<D>(q, reinterpret_cast<const uint16_t*>(row), g);
+            } else {
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) q[c] = *reinterpret_cast<const uint4v*>(&queries[buffer][n * kStride + 64 * c + 16 * g]);
+            }
+            const float4v l = *reinterpret_cast<const float4v*>(&lows[buffer][4 * g]);
+            const uint4v m = *reinterpret_cast<const uint4v*>(&limits[buffer][4 * g]);
+            const float low[4] = {l[0], l[1], l[2], l[3]};
+            const uint32_t limit[4] = {m[0], m[1], m[2], m[3]};
+            float4v sc[2];
+            score<D>(sc, q, keys);
+            if (all_seen && 16 * rt + 16 <= (uint32_t)a.rows) add_weights<true>(sum, sc, a.scale_log2, low, limit, token);
+            else add_weights<false>(sum, sc, a.scale_log2, low, limit, token);
+        }
+        __syncthreads();  // (the buffers are used again)
+        result_of(x, s, h).store(sum, tile.there, had, x, t, full, len, x.seen[s]);
+    }
+    if (bad) atomicOr(&a.st->status, KVC_ST_BAD_INDEX);
+}
+
+template <int D, bool FP4, bool EIGHT>
 static hipError_t launch_weigh_of(const WeighArgs& x, hipStream_t s) {
-    const bool eight = x.a.g.N % 8 == 0, few = x.a.rows <= 16;
-    return launch_kernel(eight ? (few ? k_weigh<D, FP4, true, true> : k_weigh<D, FP4, true, false>) : (few ? k_weigh<D, FP4, false, true> : k_weigh<D, FP4, false, false>), dim3(x.workers / 4), dim3(256), s, x);
+    if (x.many) return launch_kernel(k_weigh_many<D, FP4, EIGHT>, dim3(x.workers), dim3(256), s, x);
+    return launch_kernel(x.a.rows <= 16 ? k_weigh<D, FP4, EIGHT, true> : k_weigh<D, FP4, EIGHT, false>, dim3(x.workers / 4), dim3(256), s, x);
 }
 
 template <>
 hipError_t launch_weigh<KVC_HEAD_DIM>(const WeighArgs& x, hipStream_t s) {
-    return x.k ? launch_weigh_of<KVC_HEAD_DIM, true>(x, s) : launch_weigh_of<KVC_HEAD_DIM, false>(x, s);
+    constexpr int D = KVC_HEAD_DIM;
+    const bool eight = x.a.g.N % 8 == 0;
+    if (x.k) return eight ? launch_weigh_of<D, true, true>(x, s) : launch_weigh_of<D, true, false>(x, s);
+    return eight ? launch_weigh_of<D, false, true>(x, s) : launch_weigh_of<D, false, false>(x, s);
 }
 
 }  // namespace kvc

@@ -115,6 +115,15 @@ def test_weights_of_chunks(fp4):
     _check_weigh(_weigh_case(2, 7, 128, 1, 1, 17, [60, 17, 16], fp4))
 
 
+@pytest.mark.parametrize("d", range(32, 257, 32))
+@pytest.mark.parametrize("N", [16, 3])
+@pytest.mark.parametrize("fp4", [False, True])
+def test_many_queries_of_every_head_dimension(d, N, fp4):
+    """80 and 66 rows: the last tile of rows full and not, chunks of tokens that all queries see and that some do."""
+    _check_weigh(_weigh_case(d, N, d, 1, 2, 40, [150, 40, 7, 0, 39], fp4, holes=N == 3))
+    _check_weigh(_weigh_case(d + 1, N, d, 2, 3, 22, [290, 22], fp4, separate=True, token_major=True), apart=False)
+
+
 @pytest.mark.parametrize("fp4", [False, True])
 @pytest.mark.parametrize("scale", [0.0, -0.2, 1.5])
 def test_scales(fp4, scale):
