@@ -630,16 +630,17 @@ constexpr uint32_t kAtOnce = 8;
 // Where the pieces of a unit are, for one of its rows: `n` workers from w0 on have one each, or one has it whole.
 struct Pieces {
     int64_t whole, slots;
-    uint32_t n = 0, w0 = 0, rows = 0;
+    uint32_t n = 0, w0 = 0, rows = 0, stride = 1;  // stride: from a piece's worker to the next one's
 
     __device__ void find(uint32_t start, uint32_t tiles, uint32_t each) {
         w0 = start / each;
         n = (start + tiles - 1) / each - w0 + 1;
     }
-    __device__ int64_t slot(uint32_t k) const { return n == 1 ? whole : slots + (int64_t)(2 * (w0 + k) + (k == 0 ? 1 : 0)) * rows; }
+    __device__ int64_t slot(uint32_t k) const { return n == 1 ? whole : slots + (int64_t)(2 * (w0 + k) * stride + (k == 0 ? 1 : 0)) * rows; }
 };
 
-template <int D>
+// BY_UNIT: workers are dealt ranges of the sequences' tiles, the units of each range in turn (kvc_attend_fp4.hip); else ranges of the tiles of all units.
+template <int D, bool BY_UNIT>
 __global__ __launch_bounds__(256) void k_join(AttendArgs a) {
     constexpr uint32_t kEach = D / 8, kSlots = 256 / kEach;
     __shared__ __align__(16) float4v sums[kSlots][kEach][2];
@@ -653,11 +654,13 @@ __global__ __launch_bounds__(256) void k_join(AttendArgs a) {
     const uint32_t before = a.own_start[s], tiles = a.own_start[s + 1] - before, all = a.own_start[a.n_seq];
     const int g = a.n_prefix ? prefix_of(a, s) : -1;
     if (tiles) {
-        const uint32_t units = a.n_kv * a.own_tiles, rt = row / a.own_rows;
-        own.find(before * units + (h * a.own_tiles + rt) * tiles, tiles, share(all * units, a.own_workers));
+        const uint32_t units = a.n_kv * a.own_tiles, rt = row / a.own_rows, u = h * a.own_tiles + rt;
+        if (BY_UNIT) own.find(before, tiles, share(all, a.own_workers / units));
+        else own.find(before * units + u * tiles, tiles, share(all * units, a.own_workers));
         own.whole = row_id;
         own.rows = a.own_rows;
-        own.slots = a.own_slots + (row - rt * a.own_rows);
+        own.slots = a.own_slots + (row - rt * a.own_rows) + (BY_UNIT ? (int64_t)2 * u * a.own_rows : 0);
+        if (BY_UNIT) own.stride = units;
     }
     const bool finished_already = g < 0 && own.n == 1;  // by its worker
     if (g >= 0) {
@@ -747,9 +750,9 @@ static hipError_t launch_parts(const AttendArgs& a, hipStream_t s) {
 }
 
 template <>
-hipError_t launch_join<KVC_HEAD_DIM>(const AttendArgs& a, hipStream_t s) {
+hipError_t launch_join<KVC_HEAD_DIM>(const AttendArgs& a, bool by_unit, hipStream_t s) {
     const uint32_t rows = 256 / (KVC_HEAD_DIM / 8) / a.join_lanes;
-    return launch_kernel(k_join<KVC_HEAD_DIM>, dim3((unsigned)(((int64_t)a.n_seq * a.n_kv * a.rows + rows - 1) / rows)), dim3(256), s, a);
+    return launch_kernel(by_unit ? k_join<KVC_HEAD_DIM, true> : k_join<KVC_HEAD_DIM, false>, dim3((unsigned)(((int64_t)a.n_seq * a.n_kv * a.rows + rows - 1) / rows)), dim3(256), s, a);
 }
 
 template <>
@@ -758,7 +761,7 @@ hipError_t launch_attend<KVC_HEAD_DIM>(const AttendArgs& a, hipStream_t s) {
     hipError_t e;
     if constexpr (D <= 192) e = a.own_rows == 32 ? launch_parts<D, 2>(a, s) : launch_parts<D, 1>(a, s);
     else e = launch_parts<D, 1>(a, s);
-    return e != hipSuccess || a.direct ? e : launch_join<D>(a, s);
+    return e != hipSuccess || a.direct ? e : launch_join<D>(a, false, s);
 }
 
 }  // namespace kvc

@@ -25,15 +25,78 @@ struct SourceFp4 {
     const uint8_t* v;
 };
 
-// Entries of the block table for the 32 tokens from t on, as Blocks has them (kvc_attend.h), looked up whether the tokens are there or not: loads that are always made can be waited for
-// one by one.  (There is a token.)
+// Where 32 tokens are: blocks as the table names them, and rows in the blocks.  Where 8 tokens from a multiple of 8 on share a block (EIGHT: N is a multiple of 8) a lane holds those of the first
+// of its 8 keys and of its 8 values; else of token `lane` mod 32, and asks the others.
 template <bool EIGHT>
-__device__ inline Blocks<EIGHT> look_up(const AttendArgs& a, const int32_t* table, uint32_t len, uint32_t t) {
-    Blocks<EIGHT> b;
+struct Spots {
+    int32_t block[EIGHT ? 2 : 1];
+    uint32_t row[EIGHT ? 2 : 1];
+};
+// Looks up tile after tile.  From one to the next of a sequence a token's place moves on by 32 tokens: so many blocks and so many rows, and another block where that leaves the block.  What the
+// table says is asked for whether the tokens are there or not: loads that are always made can be waited for one by one.
+template <bool EIGHT>
+struct Finder {
+    static constexpr int kSpots = EIGHT ? 2 : 1;
+    uint32_t entry[kSpots], row[kSpots];
+
+    // token of a tile that spot i is of
+    __device__ static uint32_t token(int i) {
+        const uint32_t lane = threadIdx.x & 63;
+        return !EIGHT ? lane & 31 : i == 0 ? 8 * ((lane & 15) >> 2) : 8 * (lane >> 4);
+    }
+    // first: tile t is not the one behind the last that was looked up.  len: tokens of the sequence, not 0
+    __device__ Spots<EIGHT> find(const AttendArgs& a, const int32_t* table, uint32_t len, uint32_t t, bool first) {
+        const uint32_t N = (uint32_t)a.g.N, last = fast_div(len - 1, a.by_N);
+        Spots<EIGHT> s;
+        if (first) {
 #pragma unroll
-    for (int i = 0; i < (EIGHT ? 2 : 1); ++i) b.of[i] = load_from<int32_t>((bytes_at)(table + fast_div(min(t + b.token(i), len - 1), a.by_N)));
-    return b;
+            for (int i = 0; i < kSpots; ++i) {
+                entry[i] = fast_div(t * kTile + token(i), a.by_N);
+                row[i] = t * kTile + token(i) - entry[i] * N;
+            }
+        } else {
+            const uint32_t blocks = fast_div(kTile, a.by_N), rows = kTile - blocks * N;
+#pragma unroll
+            for (int i = 0; i < kSpots; ++i) {
+                row[i] += rows;
+                const bool leaves = row[i] >= N;
+                row[i] -= leaves ? N : 0;
+                entry[i] += blocks + (leaves ? 1 : 0);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kSpots; ++i) {
+            s.block[i] = load_from<int32_t>((bytes_at)(table + min(entry[i], last)));
+            s.row[i] = row[i];
+        }
+        return s;
+    }
+};
+// A block and a row: of the lane's keys (score tile u) or values (token j).
+struct Spot {
+    int32_t block;
+    uint32_t row;
+};
+template <bool EIGHT>
+__device__ inline Spot key_spot(const Spots<EIGHT>& s, int u) {
+    if constexpr (EIGHT) return {s.block[0], s.row[0] + 4 * u + (threadIdx.x & 3)};
+    const int lane = 8 * ((threadIdx.x & 15) >> 2) + 4 * u + (threadIdx.x & 3);
+    return {__shfl(s.block[0], lane), (uint32_t)__shfl((int)s.row[0], lane)};
 }
+template <bool EIGHT>
+__device__ inline Spot value_spot(const Spots<EIGHT>& s, int j) {
+    if constexpr (EIGHT) return {s.block[EIGHT ? 1 : 0], s.row[EIGHT ? 1 : 0] + j};
+    const int lane = 8 * ((threadIdx.x & 63) >> 4) + j;
+    return {__shfl(s.block[0], lane), (uint32_t)__shfl((int)s.row[0], lane)};
+}
+// Whether a token that exists has a block; `bad` notes entries beyond the cache.
+__device__ inline bool is_there(const AttendArgs& a, int32_t block, bool exists, bool& bad) {
+    const bool in = (uint32_t)block < (uint32_t)min(a.n_cache_blocks, (int64_t)INT32_MAX + 1);  // (not what is below zero)
+    bad = bad || (exists && !in && block >= 0);
+    return exists && in;
+}
+// The page of a block (its bytes are counted in 32 bits), from the head's page of block 0 on.
+__device__ inline bytes_at page_of(const uint8_t* pages, const Fp4Pages& f, int32_t block) { return (bytes_at)pages + (uint64_t)(uint32_t)block * (uint32_t)f.block; }
 
 template <int D>
 struct KeysFp4 {
@@ -79,51 +142,35 @@ __device__ inline uint32_t key_group(uint32_t g) { return Piece<D, P>::before / 
 template <int D, int P>
 __device__ inline uint32_t value_group(uint32_t n) { return Piece<D, P>::before / 32 + Piece<D, P>::w * n / 32; }
 
-// exps: the exponents of a token's first group, `step` bytes before those of the next group
 template <int D, bool EIGHT, int P = 0>
-__device__ inline void load_key_exps(KeysFp4<D>& x, int u, bytes_at exps, uint32_t step, uint32_t g) {
+__device__ inline void load_key_exps(KeysFp4<D>& x, int u, bytes_at exps, bool have, uint32_t N, uint32_t g) {
     if constexpr (P < piece_count(D)) {
-        bytes_at p = exps + key_group<D, P>(g) * step;
+        const bytes_at p = have ? exps + key_group<D, P>(g) * N : (bytes_at)kZeroCodes;
         if constexpr (EIGHT) load_codes<8>(x.e[P], p);
         else load_codes<1>(&x.e[P][u], p);
-        load_key_exps<D, EIGHT, P + 1>(x, u, exps, step, g);
+        load_key_exps<D, EIGHT, P + 1>(x, u, exps, have, N, g);
     }
-}
-
-// Row of token t in its block.
-__device__ inline uint32_t row_of(const AttendArgs& a, uint32_t t) { return t - fast_div(t, a.by_N) * (uint32_t)a.g.N; }
-
-// Whether a block is there: an entry of a token that exists, and within the cache.  `bad` notes entries beyond it.
-__device__ inline bool is_there(const AttendArgs& a, int32_t block, bool exists, bool& bad) {
-    const bool beyond = block >= a.n_cache_blocks;
-    bad = bad || (exists && beyond);
-    return exists && block >= 0 && !beyond;
 }
 
 // live: whether there is such a tile at all.
 template <int D, bool EIGHT>
-__device__ inline void load_keys(KeysFp4<D>& x, const AttendArgs& a, const Fp4Pages& f, const SourceFp4& s, const Blocks<EIGHT>& b, uint32_t t, bool live, bool& bad) {
-    const uint32_t lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4, octet = t + 8 * (n >> 2);
-    const bytes_at zero = (bytes_at)kZeroCodes, pages = (bytes_at)s.k;
+__device__ inline void load_keys(KeysFp4<D>& x, const AttendArgs& a, const Fp4Pages& f, const SourceFp4& s, const Spots<EIGHT>& spots, uint32_t t, bool live, bool& bad) {
+    const uint32_t lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4, octet = t + 8 * (n >> 2), N = (uint32_t)a.g.N;
     if constexpr (EIGHT) {
-        const int32_t block = b.key(0);
-        const bool have = is_there(a, block, live && octet < s.len, bad);
-        const uint32_t row = row_of(a, octet);
-        bytes_at page = pages + block * f.block;
-        bytes_at codes = have ? page + (row + (n & 3)) * (D / 2) : zero;  // (rows behind the last token are the page's all the same, and not seen)
+        const Spot at = key_spot<EIGHT>(spots, 0);
+        const bool have = is_there(a, at.block, live && octet < s.len, bad);
+        const bytes_at page = page_of(s.k, f, at.block), codes = have ? page + at.row * (D / 2) : (bytes_at)kZeroCodes;  // (rows behind the last token are the page's all the same, and not seen)
         load_key_codes<D>(x, 0, codes, g);
         load_key_codes<D>(x, 1, codes + 4 * (D / 2), g);
-        load_key_exps<D, true>(x, 0, have ? page + f.exps + row : zero, have ? (uint32_t)a.g.N : 0, g);
+        load_key_exps<D, true>(x, 0, page + f.exps + spots.row[0], have, N, g);
     } else {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const uint32_t at = octet + 4 * u + (n & 3);
-            const int32_t block = b.key(u);
-            const bool have = is_there(a, block, live && at < s.len, bad);
-            const uint32_t row = row_of(a, at);
-            bytes_at page = pages + block * f.block;
-            load_key_codes<D>(x, u, have ? page + row * (D / 2) : zero, g);
-            load_key_exps<D, false>(x, u, have ? page + f.exps + row : zero, have ? (uint32_t)a.g.N : 0, g);
+            const Spot at = key_spot<EIGHT>(spots, u);
+            const bool have = is_there(a, at.block, live && octet + 4 * u + (n & 3) < s.len, bad);
+            const bytes_at page = page_of(s.k, f, at.block);
+            load_key_codes<D>(x, u, have ? page + at.row * (D / 2) : (bytes_at)kZeroCodes, g);
+            load_key_exps<D, false>(x, u, page + f.exps + at.row, have, N, g);
         }
     }
 }
@@ -137,49 +184,46 @@ __device__ inline void load_value_codes(ValuesFp4<D, EIGHT>& x, int j, bytes_at 
     }
 }
 template <int D, bool EIGHT, int P = 0>
-__device__ inline void load_value_exps(ValuesFp4<D, EIGHT>& x, int j, bytes_at exps, uint32_t step, uint32_t n) {
+__device__ inline void load_value_exps(ValuesFp4<D, EIGHT>& x, int j, bytes_at exps, bool have, uint32_t N, uint32_t n) {
     if constexpr (P < piece_count(D)) {
-        bytes_at p = exps + value_group<D, P>(n) * step;
+        const bytes_at p = have ? exps + value_group<D, P>(n) * N : (bytes_at)kZeroCodes;
         if constexpr (EIGHT) load_codes<8>(x.e[P], p);
         else load_codes<1>(&x.e[P][j], p);
-        load_value_exps<D, EIGHT, P + 1>(x, j, exps, step, n);
+        load_value_exps<D, EIGHT, P + 1>(x, j, exps, have, N, n);
     }
 }
 
 // -> bit j: token t + 8g + j exists
 template <int D, bool EIGHT>
-__device__ inline uint32_t load_values(ValuesFp4<D, EIGHT>& x, const AttendArgs& a, const Fp4Pages& f, const SourceFp4& s, const Blocks<EIGHT>& b, uint32_t t, bool live, bool& bad) {
-    const uint32_t lane = threadIdx.x & 63, n = lane & 15, first = t + 8 * (lane >> 4);
-    const bytes_at zero = (bytes_at)kZeroCodes, pages = (bytes_at)s.v;
+__device__ inline uint32_t load_values(ValuesFp4<D, EIGHT>& x, const AttendArgs& a, const Fp4Pages& f, const SourceFp4& s, const Spots<EIGHT>& spots, uint32_t t, bool live, bool& bad) {
+    const uint32_t lane = threadIdx.x & 63, n = lane & 15, first = t + 8 * (lane >> 4), N = (uint32_t)a.g.N;
     if constexpr (EIGHT) {
-        const int32_t block = b.value(0);
-        const bool have = is_there(a, block, live && first < s.len, bad);
-        const uint32_t row = row_of(a, first);
-        bytes_at page = pages + block * f.block;
-        bytes_at codes = have ? page + row * (D / 2) : zero;
+        const Spot at = value_spot<EIGHT>(spots, 0);
+        const bool have = is_there(a, at.block, live && first < s.len, bad);
+        const bytes_at page = page_of(s.v, f, at.block), codes = have ? page + at.row * (D / 2) : (bytes_at)kZeroCodes;
 #pragma unroll
         for (int j = 0; j < 8; ++j) load_value_codes<D, true>(x, j, codes + j * (D / 2), n);
-        load_value_exps<D, true>(x, 0, have ? page + f.exps + row : zero, have ? (uint32_t)a.g.N : 0, n);
+        load_value_exps<D, true>(x, 0, page + f.exps + at.row, have, N, n);
         const uint32_t exist = s.len - min(first, s.len);
         return !have ? 0 : exist >= 8 ? 0xFF : ~(~0u << exist);
     } else {
         uint32_t there = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const int32_t block = b.value(j);
-            const bool have = is_there(a, block, live && first + j < s.len, bad);
-            const uint32_t row = row_of(a, first + j);
-            bytes_at page = pages + block * f.block;
+            const Spot at = value_spot<EIGHT>(spots, j);
+            const bool have = is_there(a, at.block, live && first + j < s.len, bad);
+            const bytes_at page = page_of(s.v, f, at.block);
             there |= have ? 1u << j : 0u;
-            load_value_codes<D, false>(x, j, have ? page + row * (D / 2) : zero, n);
-            load_value_exps<D, false>(x, j, have ? page + f.exps + row : zero, have ? (uint32_t)a.g.N : 0, n);
+            load_value_codes<D, false>(x, j, have ? page + at.row * (D / 2) : (bytes_at)kZeroCodes, n);
+            load_value_exps<D, false>(x, j, page + f.exps + at.row, have, N, n);
         }
         return there;
     }
 }
 
-// 2^e from its byte; 255 makes NaN of any code, as the conversion has it
-__device__ inline float power_of(uint32_t byte) { return __uint_as_float(byte << 23); }
+// 2^e, from byte `at` of a register: the conversion looks at nothing but bits 23 to 30 (a test compares all codes and exponents; 255 makes NaN of any code), so the byte is turned there and
+// its neighbours may be anywhere.
+__device__ inline float power_of(uint32_t bytes, uint32_t at) { return __uint_as_float(__builtin_amdgcn_alignbit(bytes, bytes, (8 * at + 9) & 31)); }
 
 // Eight channels of FP16, from a register of codes.
 __device__ inline uint4v eight_channels(uint32_t codes, float scale) {
@@ -197,21 +241,38 @@ __device__ inline void expand_keys(Tokens<D>& to, const KeysFp4<D>& x) {
         using Q = Piece<D, P>;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const float scale = power_of(EIGHT ? x.e[P][u] >> 8 * (threadIdx.x & 3) & 255 : x.e[P][u]);
+            const float scale = power_of(x.e[P][u], EIGHT ? threadIdx.x & 3 : 0);
 #pragma unroll
             for (int c = 0; c < Q::w / 2; ++c) to.k[u][Q::regs + c] = eight_channels(x.c[u][Q::regs + c], scale);
         }
         expand_keys<D, EIGHT, P + 1>(to, x);
     }
 }
-// Values of the tokens of `there`, bit j of token t + 8g + j; the others become zero.
+// Exponents of the tokens of `there` (bit j: token j of 8), in the place of the others zero, which makes zeros of their codes.
+template <int D, bool EIGHT>
+__device__ inline void keep_values(ValuesFp4<D, EIGHT>& x, uint32_t there) {
+    if constexpr (EIGHT) {
+        uint32_t mask[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) mask[i] = ((there >> 4 * i & 15) * 0x00204081u & 0x01010101u) * 255;  // (a bit to a byte)
+#pragma unroll
+        for (int p = 0; p < piece_count(D); ++p)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) x.e[p][i] &= mask[i];
+    } else {
+#pragma unroll
+        for (int p = 0; p < piece_count(D); ++p)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x.e[p][j] = there >> j & 1 ? x.e[p][j] : 0;
+    }
+}
 template <int D, bool EIGHT, int P = 0>
-__device__ inline void expand_values(Tokens<D>& to, const ValuesFp4<D, EIGHT>& x, uint32_t there) {
+__device__ inline void expand_values(Tokens<D>& to, const ValuesFp4<D, EIGHT>& x) {
     if constexpr (P < piece_count(D)) {
         using Q = Piece<D, P>;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const float scale = power_of(!(there >> j & 1) ? 0 : EIGHT ? x.e[P][EIGHT ? j / 4 : 0] >> 8 * (j % 4) & 255 : x.e[P][EIGHT ? 0 : j]);
+            const float scale = power_of(x.e[P][EIGHT ? j / 4 : j], EIGHT ? j % 4 : 0);
             to.v[j][Q::regs] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(x.c[j][P], scale, 0));
             if constexpr (Q::w > 2) to.v[j][Q::regs + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(x.c[j][P], scale, 1));
             if constexpr (Q::w > 4) {
@@ -219,7 +280,7 @@ __device__ inline void expand_values(Tokens<D>& to, const ValuesFp4<D, EIGHT>& x
                 to.v[j][Q::regs + 3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(x.c[j][P], scale, 3));
             }
         }
-        expand_values<D, EIGHT, P + 1>(to, x, there);
+        expand_values<D, EIGHT, P + 1>(to, x);
     }
 }
 

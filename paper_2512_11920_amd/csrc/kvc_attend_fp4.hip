@@ -14,24 +14,21 @@ struct TileFp4 {
     ValuesFp4<D, EIGHT> v;
     uint32_t there;
 
-    __device__ void load(const AttendFp4Args& x, const SourceFp4& s, const Blocks<EIGHT>& b, uint32_t t, bool live, bool& bad) {
-        load_keys<D, EIGHT>(k, x.a, x.f, s, b, t, live, bad);
-        there = load_values<D, EIGHT>(v, x.a, x.f, s, b, t, live, bad);
+    __device__ void load(const AttendFp4Args& x, const SourceFp4& s, const Spots<EIGHT>& spots, uint32_t t, bool live, bool& bad) {
+        load_keys<D, EIGHT>(k, x.a, x.f, s, spots, t, live, bad);
+        there = load_values<D, EIGHT>(v, x.a, x.f, s, spots, t, live, bad);
     }
 };
 
-// Whether a value of the tile may not be finite: exponents from 141 on, of which append writes NaN's.
+// Whether a value of the tile may not be finite: exponents from 141 on, of which append writes NaN's.  (Tokens that are not there have zeros.)
 template <int D, bool EIGHT>
-__device__ inline bool may_be_infinite(const TileFp4<D, EIGHT>& x) {
-    bool any = false;
+__device__ inline bool may_be_infinite(const ValuesFp4<D, EIGHT>& x) {
+    uint32_t any = 0;
 #pragma unroll
     for (int p = 0; p < piece_count(D); ++p)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const uint32_t byte = EIGHT ? x.v.e[p][EIGHT ? j / 4 : j] >> (EIGHT ? 8 * (j % 4) : 0) & 255 : x.v.e[p][j];
-            any = any || (x.there >> j & 1 && byte > 140);
-        }
-    return __any(any);
+        for (int i = 0; i < (EIGHT ? 2 : 8); ++i) any |= ((x.e[p][i] & 0x7F7F7F7Fu) + 0x73737373u) & x.e[p][i] & 0x80808080u;
+    return __any(any != 0);
 }
 
 // One piece's values of 8 tokens times the rows' weights; `mine`: rows for which the result is taken.
@@ -55,37 +52,79 @@ __device__ inline void add_values_of(Rows<D> (&r)[R], const Tokens<D>& x, const 
     }
 }
 
-// What a wave does with a tile.  Among the last n_q tokens some rows see values that others do not, and weight zero times one that is not finite is NaN: there, rows that see so many
-// of the tile's tokens are done by themselves, the other tokens' values being zero.
 template <int D, int R, bool EIGHT>
-__device__ inline void add_tile_fp4(Rows<D> (&r)[R], const AttendFp4Args& x, const TileFp4<D, EIGHT>& tile, uint32_t t, uint32_t len, const uint32_t (&limit)[R]) {
+__device__ inline void make_scores(float4v (&s)[R][2], const Rows<D> (&r)[R], const KeysFp4<D>& k) {
     Tokens<D> tokens;
-    expand_keys<D, EIGHT>(tokens, tile.k);
+    expand_keys<D, EIGHT>(tokens, k);
+#pragma unroll
+    for (int j = 0; j < R; ++j) scores(s[j], r[j], tokens);
+}
+
+// Scores of tokens t + 8g.. become weights, as `weights` has it (kvc_attend.h); all: every row sees every token.
+template <int D>
+__device__ inline half8 weights_of(Rows<D>& r, const float4v (&s)[2], float scale_log2, bool all, uint32_t there, uint32_t t, uint32_t limit) {
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = s[j / 4][j % 4] * scale_log2;
+    if (!all) {
+        const uint32_t first = t + 8 * ((threadIdx.x & 63) >> 4), n = limit > first ? limit - first : 0, seen = there & (n >= 8 ? 0xFFu : ~(~0u << n));
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = seen >> j & 1 ? v[j] : -INFINITY;
+    }
+    float top = fmaxf(v[0], v[1]);
+#pragma unroll
+    for (int j = 2; j < 8; ++j) top = fmaxf(top, v[j]);
+    top = row_max(top);
+    if (__any(top > r.m + kLag)) {  // (a row's first token too: its reference is -infinity)
+        const float m = fmaxf(r.m, top), f = r.m == -INFINITY ? 0.f : power2(r.m - m);
+        r.m = m;
+        r.l *= f;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) r.o[i] *= f;
+    }
+    const float low = (r.m == -INFINITY ? 0.f : r.m) - kLift;
+    half8 p;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float w = power2(v[j] - low);
+        r.l += w;
+        p[j] = (_Float16)w;
+    }
+    return p;
+}
+
+// What a wave does with a tile's scores and values.  Among the last n_q tokens some rows see values that others do not, and weight zero times one that is not finite is NaN: there, rows that see
+// so many of the tile's tokens are done by themselves, the other tokens' values being zero.  seen_by_all: tokens that every row sees.
+template <int D, int R, bool EIGHT>
+__device__ inline void add_tile_fp4(Rows<D> (&r)[R], const AttendFp4Args& x, TileFp4<D, EIGHT>& tile, const float4v (&s)[R][2], uint32_t t, uint32_t seen_by_all, const uint32_t (&limit)[R]) {
+    const bool all = t + kTile <= seen_by_all && __all(tile.there == 0xFF);
     half8 p[R];
 #pragma unroll
-    for (int j = 0; j < R; ++j) {
-        float4v s[2];
-        scores(s, r[j], tokens);
-        p[j] = weights(r[j], s, x.a.scale_log2, tile.there, t, limit[j]);
-    }
-    if (x.a.n_q > 1 && t + kTile + x.a.n_q - 1 > len && may_be_infinite<D, EIGHT>(tile)) {
-        const uint32_t first = t + 8 * ((threadIdx.x & 63) >> 4);
+    for (int j = 0; j < R; ++j) p[j] = weights_of(r[j], s[j], x.a.scale_log2, all, tile.there, t, limit[j]);
+    Tokens<D> tokens;
+    if (!all) {
+        keep_values<D, EIGHT>(tile.v, tile.there);
+        if (x.a.n_q > 1 && t + kTile > seen_by_all && may_be_infinite<D, EIGHT>(tile.v)) {
+            const uint32_t first = t + 8 * ((threadIdx.x & 63) >> 4);
 #pragma nounroll
-        for (uint32_t cut = 1; cut <= kTile; ++cut) {  // rows that see the tile's first `cut` tokens, and no more
-            bool mine[R], any = false;
+            for (uint32_t cut = 1; cut <= kTile; ++cut) {  // rows that see the tile's first `cut` tokens, and no more
+                bool mine[R], any = false;
 #pragma unroll
-            for (int j = 0; j < R; ++j) {
-                mine[j] = min(limit[j] > t ? limit[j] - t : 0, (uint32_t)kTile) == cut;
-                any = any || mine[j];
+                for (int j = 0; j < R; ++j) {
+                    mine[j] = min(limit[j] > t ? limit[j] - t : 0, (uint32_t)kTile) == cut;
+                    any = any || mine[j];
+                }
+                if (!__any(any)) continue;
+                const uint32_t n = t + cut > first ? t + cut - first : 0;
+                ValuesFp4<D, EIGHT> v = tile.v;
+                keep_values<D, EIGHT>(v, n >= 8 ? 0xFFu : ~(~0u << n));
+                expand_values<D, EIGHT>(tokens, v);
+                add_values_of<D, R>(r, tokens, p, mine);
             }
-            if (!__any(any)) continue;
-            const uint32_t n = t + cut > first ? t + cut - first : 0;
-            expand_values<D, EIGHT>(tokens, tile.v, tile.there & (n >= 8 ? 0xFFu : ~(~0u << n)));
-            add_values_of<D, R>(r, tokens, p, mine);
+            return;
         }
-        return;
     }
-    expand_values<D, EIGHT>(tokens, tile.v, tile.there);
+    expand_values<D, EIGHT>(tokens, tile.v);
     add_values<D, R>(r, tokens, p);
 }
 
@@ -96,25 +135,22 @@ __device__ inline void own_part_fp4(const AttendFp4Args& x, Sums& sums, uint32_t
     const auto tiles_of = [&](uint32_t s) { return (own_length(a, s) + kTile - 1) / kTile; };
     add_up(sums, a.n_seq, tiles_of);
     if (worker < 4) write_starts(sums, a.own_start, a.n_seq, tiles_of);
-    const uint32_t units = a.n_kv * a.own_tiles, all = uniform(sums.all) * units, each = share(all, a.own_workers);
-    const uint32_t begin = worker * each, end = min(begin + each, all);
-    if (begin >= end) return;
+    const uint32_t units = a.n_kv * a.own_tiles, all = uniform(sums.all), each = share(all, a.own_workers / units), range = worker / units;
+    const uint32_t begin = range * each, end = min(begin + each, all);
+    if (worker >= a.own_workers || begin >= end) return;
 
     Place c;
     {
-        const Item it = find_item(sums, a.n_seq, begin / units, tiles_of);
+        const Item it = find_item(sums, a.n_seq, begin, tiles_of);
         c.s = uniform(it.i);
         c.len = uniform(own_length(a, c.s));
         c.tiles = (c.len + kTile - 1) / kTile;
-        const uint32_t rel = begin - uniform(it.start) * units;
-        c.u = rel / c.tiles;
-        c.t = rel - c.u * c.tiles;
+        c.u = worker - range * units;
+        c.t = begin - uniform(it.start);
     }
     const auto advance = [&](Place& p) {  // (there is a next tile)
         if (++p.t < p.tiles) return;
         p.t = 0;
-        if (++p.u < units) return;
-        p.u = 0;
         do {
             ++p.s;
             p.len = uniform(own_length(a, p.s));
@@ -128,8 +164,10 @@ __device__ inline void own_part_fp4(const AttendFp4Args& x, Sums& sums, uint32_t
 
     const uint32_t lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     Rows<D> r[R];
-    uint32_t limit[R];
+    uint32_t limit[R], seen_by_all = 0;
     const auto open = [&](const Place& p) {
+        const uint32_t len = uniform((uint32_t)a.lens[p.s]), later = (uint32_t)a.n_q - 1;
+        seen_by_all = min(len > later ? len - later : 0, p.len);
         const uint32_t h = p.u / a.own_tiles, rt = p.u - h * a.own_tiles;
 #pragma unroll
         for (int j = 0; j < R; ++j) {
@@ -137,8 +175,8 @@ __device__ inline void own_part_fp4(const AttendFp4Args& x, Sums& sums, uint32_t
             const uint32_t row = min((rt * R + j) * 16 + n, (uint32_t)a.rows - 1);  // (rows beyond the last are computed with it, and not stored)
             const uint32_t in = fast_div(row, a.by_n_q), i = row - in * a.n_q;
             load_query<D>(r[j].q, a.q + p.s * a.q_strides[0] + i * a.q_strides[1] + (h * a.group + in) * a.q_strides[2], g);
-            const uint32_t later = a.n_q - 1 - i, len = (uint32_t)a.lens[p.s];
-            limit[j] = min(len > later ? len - later : 0, p.len);
+            const uint32_t after = later - i;
+            limit[j] = min(len > after ? len - after : 0, p.len);
 #pragma unroll
             for (int k = 0; k < D / 32; ++k) asm volatile("" : "+v"(r[j].q[k]));  // (waited for here, not in every step)
         }
@@ -171,21 +209,25 @@ __device__ inline void own_part_fp4(const AttendFp4Args& x, Sums& sums, uint32_t
         if (left > ahead) advance(n);
         return n;
     };
-    const auto find = [&](const Place& p) { return look_up<EIGHT>(a, a.table + (int64_t)p.s * a.max_blocks, p.len, p.t * kTile); };
+    Finder<EIGHT> finder;
+    const auto find = [&](const Place& p, bool first) { return finder.find(a, a.table + (int64_t)p.s * a.max_blocks, p.len, p.t, first); };
     bool bad = false;
     TileFp4<D, EIGHT> tiles[3];
     Place c1 = next(c, 1), c2 = next(c1, 2);
-    Blocks<EIGHT> b = find(c), b1 = find(c1), b2 = find(c2);
+    const Spots<EIGHT> at = find(c, true), at1 = find(c1, c1.t == 0);
+    Spots<EIGHT> at2 = find(c2, c2.t == 0);
     open(c);
-    tiles[0].load(x, source(c), b, c.t * kTile, true, bad);
-    tiles[1].load(x, source(c1), b1, c1.t * kTile, left > 1, bad);
+    tiles[0].load(x, source(c), at, c.t * kTile, true, bad);
+    tiles[1].load(x, source(c1), at1, c1.t * kTile, left > 1, bad);
     const auto step = [&](TileFp4<D, EIGHT>& now, TileFp4<D, EIGHT>& then) {  // -> whether it was the last one
         const Place c3 = next(c2, 3);
-        const Blocks<EIGHT> b3 = find(c3);
+        const Spots<EIGHT> at3 = find(c3, c3.t == 0);
         __builtin_amdgcn_sched_barrier(0);
-        then.load(x, source(c2), b2, c2.t * kTile, left > 2, bad);
+        then.load(x, source(c2), at2, c2.t * kTile, left > 2, bad);
         __builtin_amdgcn_sched_barrier(0);
-        add_tile_fp4<D, R, EIGHT>(r, x, now, c.t * kTile, c.len, limit);
+        float4v s[R][2];
+        make_scores<D, R, EIGHT>(s, r, now.k);
+        add_tile_fp4<D, R, EIGHT>(r, x, now, s, c.t * kTile, seen_by_all, limit);
         if (left == 1 || c1.t == 0) {
             close(c, first_tile);
             if (left == 1) return true;
@@ -195,7 +237,7 @@ __device__ inline void own_part_fp4(const AttendFp4Args& x, Sums& sums, uint32_t
         c = c1;
         c1 = c2;
         c2 = c3;
-        b2 = b3;
+        at2 = at3;
         --left;
         return false;
     };
@@ -219,8 +261,9 @@ __global__ __launch_bounds__(64 * kDirectWaves, D * R <= 128 ? 2 : 1) void k_dir
     const uint32_t lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4, wave = uniform(threadIdx.x / 64);
     const uint32_t units = a.n_kv * a.own_tiles, s = blockIdx.x / units, u = blockIdx.x - s * units, h = u / a.own_tiles, rt = u - h * a.own_tiles;
     SourceFp4 src{a.table + (int64_t)s * a.max_blocks, (uint32_t)a.max_blocks * (uint32_t)a.g.N, x.k + (int64_t)h * x.f.page, x.v + (int64_t)h * x.f.page};
-    Blocks<EIGHT> b;
-    if (wave * kTile < src.len) b = look_up<EIGHT>(a, src.table, src.len, wave * kTile);  // (as far as the table's row goes)
+    Finder<EIGHT> finder;
+    Spots<EIGHT> spots;
+    if (wave * kTile < src.len) spots = finder.find(a, src.table, src.len, wave, true);  // (as far as the table's row goes)
     Rows<D> r[R];
     uint32_t later[R];
 #pragma unroll
@@ -236,13 +279,16 @@ __global__ __launch_bounds__(64 * kDirectWaves, D * R <= 128 ? 2 : 1) void k_dir
     const uint32_t tiles = (src.len + kTile - 1) / kTile;
     bool bad = false;
     for (uint32_t t = wave; t < tiles; t += kDirectWaves) {
-        if (t != wave) b = look_up<EIGHT>(a, src.table, src.len, t * kTile);
+        if (t != wave) spots = finder.find(a, src.table, src.len, t, true);
         TileFp4<D, EIGHT> tile;
-        tile.load(x, src, b, t * kTile, true, bad);
+        tile.load(x, src, spots, t * kTile, true, bad);
         uint32_t limit[R];
 #pragma unroll
         for (int j = 0; j < R; ++j) limit[j] = min(len > later[j] ? len - later[j] : 0, src.len);
-        add_tile_fp4<D, R, EIGHT>(r, x, tile, t * kTile, src.len, limit);
+        float4v sc[R][2];
+        make_scores<D, R, EIGHT>(sc, r, tile.k);
+        const uint32_t later_most = (uint32_t)a.n_q - 1;
+        add_tile_fp4<D, R, EIGHT>(r, x, tile, sc, t * kTile, min(len > later_most ? len - later_most : 0, src.len), limit);
     }
     if (bad) atomicOr(&a.st->status, KVC_ST_BAD_INDEX);
     const uint32_t workers = min(tiles, kDirectWaves);
@@ -280,7 +326,7 @@ static hipError_t launch_parts_fp4(const AttendFp4Args& x, hipStream_t s) {
     const bool eight = x.a.g.N % 8 == 0;
     if constexpr (direct_fits(D, R))
         if (x.a.direct) return launch_kernel(eight ? k_direct_fp4<D, R, true> : k_direct_fp4<D, R, false>, dim3((unsigned)x.a.n_seq * x.a.n_kv * x.a.own_tiles), dim3(64 * kDirectWaves), s, x);
-    return launch_kernel(eight ? k_own_fp4<D, R, true> : k_own_fp4<D, R, false>, dim3(x.a.own_workers / 4), dim3(256), s, x);
+    return launch_kernel(eight ? k_own_fp4<D, R, true> : k_own_fp4<D, R, false>, dim3((x.a.own_workers + 3) / 4), dim3(256), s, x);
 }
 
 template <>
@@ -289,7 +335,7 @@ hipError_t launch_attend_fp4<KVC_HEAD_DIM>(const AttendFp4Args& x, hipStream_t s
     hipError_t e;
     if constexpr (D <= 192) e = x.a.own_rows == 32 ? launch_parts_fp4<D, 2>(x, s) : launch_parts_fp4<D, 1>(x, s);
     else e = launch_parts_fp4<D, 1>(x, s);
-    return e != hipSuccess || x.a.direct ? e : launch_join<D>(x.a, s);
+    return e != hipSuccess || x.a.direct ? e : launch_join<D>(x.a, true, s);
 }
 
 }  // namespace kvc

@@ -165,6 +165,6 @@ template <int D>
 hipError_t launch_attend(const AttendArgs& a, hipStream_t s);
 // its second launch, which joins the pieces that the first left in the workspace
 template <int D>
-hipError_t launch_join(const AttendArgs& a, hipStream_t s);
+hipError_t launch_join(const AttendArgs& a, bool by_unit, hipStream_t s);
 
 }  // namespace kvc

@@ -7,6 +7,10 @@
 using namespace kvc;
 
 static Fp4Pages pages_of(const kvc_ctx* ctx) { return fp4_pages(ctx->g.N, ctx->g.d, ctx->g.ppb); }
+// A block's bytes, and strides of FP16 in steps of 8, are counted in 32 bits.
+static bool blocks_ok(const kvc_ctx* ctx, bool fp4) {
+    return fp4 ? pages_of(ctx).block <= UINT32_MAX : ctx->g.block_stride / 8 <= UINT32_MAX && ctx->g.row_stride / 8 <= UINT32_MAX;
+}
 // where values begin: `v`, or behind the key pages of `k`
 static const uint8_t* values_fp4(const Fp4Pages& f, const void* k, const void* v, int32_t n_kv) {
     return v ? static_cast<const uint8_t*>(v) : static_cast<const uint8_t*>(k) + (int64_t)n_kv * f.page;
@@ -122,7 +126,7 @@ int kvc_attend_fp4(kvc_ctx* ctx, const kvc_attend_t* p, void* stream) {
     if (!p->d_q || !p->d_out || !p->d_k_cache || (!p->d_block_table && p->max_blocks) || !p->d_lens) return KVC_ERR_ARG;
     if (!aligned(p->d_q, 16) || !aligned(p->d_out, 16) || !aligned(p->d_k_cache, 16) || !aligned(p->d_v_cache, 16)) return KVC_ERR_ARG;
     if (!strides_ok(p->q_strides) || !strides_ok(p->out_strides)) return KVC_ERR_ARG;
-    if (!rows_ok(p->n_seq, p->n_q, p->n_heads, ctx->g.d) || !tokens_ok(ctx, p->max_blocks)) return KVC_ERR_ARG;
+    if (!rows_ok(p->n_seq, p->n_q, p->n_heads, ctx->g.d) || !tokens_ok(ctx, p->max_blocks) || !blocks_ok(ctx, true)) return KVC_ERR_ARG;
     const AttendPlan plan = plan_attend_fp4(p->n_seq, p->n_q, p->n_heads, p->n_kv_heads, ctx->g.d);
     const int64_t own_tokens = (int64_t)p->max_blocks * ctx->g.N, rows = (int64_t)(p->n_heads / p->n_kv_heads) * p->n_q, own_tiles = (rows + plan.own_rows - 1) / plan.own_rows;
     if (!product_ok(own_tiles * p->n_kv_heads, p->n_seq, own_tokens / 32 + 1)) return KVC_ERR_ARG;
@@ -171,7 +175,7 @@ int kvc_weigh(kvc_ctx* ctx, const kvc_weigh_t* p, void* stream) {
     if (!p->d_q || !p->d_k_cache || (!p->d_block_table && p->max_blocks) || !p->d_lens || !p->d_lse || !p->d_seen) return KVC_ERR_ARG;
     if (p->width && (!p->d_weights || !p->d_weights_out || !p->d_positions)) return KVC_ERR_ARG;
     if (!aligned(p->d_q, 16) || !aligned(p->d_k_cache, 16) || !strides_ok(p->q_strides)) return KVC_ERR_ARG;
-    if (!rows_ok(p->n_seq, p->n_q, p->n_heads, ctx->g.d) || !tokens_ok(ctx, p->max_blocks) || p->width > INT32_MAX - 256) return KVC_ERR_ARG;
+    if (!rows_ok(p->n_seq, p->n_q, p->n_heads, ctx->g.d) || !tokens_ok(ctx, p->max_blocks) || !blocks_ok(ctx, p->fp4) || p->width > INT32_MAX - 256) return KVC_ERR_ARG;
     if (!product_ok(p->n_kv_heads, p->n_seq, (int64_t)p->max_blocks * ctx->g.N / 32 + 1)) return KVC_ERR_ARG;
     if (!std::isfinite(p->scale * 1.44269504088896341f)) return KVC_ERR_ARG;
     const uint64_t bytes = (uint64_t)p->n_seq * p->n_kv_heads * p->width * 4;

@@ -28,21 +28,23 @@ struct KeyTile {
     uint4v keys[2][D / 32];
     uint32_t there;  // bit u
 
-    __device__ void load(const WeighArgs& x, const SourceFp4& s, const Blocks<EIGHT>& b, uint32_t t, bool live, bool& bad) {
+    __device__ void load(const WeighArgs& x, const SourceFp4& s, const Spots<EIGHT>& spots, uint32_t t, bool live, bool& bad) {
         const uint32_t lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4, first = t + 8 * (n >> 2) + (n & 3);
         there = 0;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const int32_t block = b.key(u);
-            const bool have = is_there(x.a, block, live && first + 4 * u < s.len, bad);
+            const Spot at = key_spot<EIGHT>(spots, u);
+            const bool have = is_there(x.a, at.block, live && first + 4 * u < s.len, bad);
             there |= have ? 1u << u : 0u;
             if constexpr (!FP4) {
-                bytes_at row = have ? (bytes_at)s.k + 2 * place(x.a, block, first + 4 * u) : (bytes_at)kZeroRow;
+                // (strides are multiples of 8 elements, and counted in these)
+                const uint64_t chunk = (uint64_t)(uint32_t)at.block * (uint32_t)(x.a.g.block_stride / 8) + (uint64_t)at.row * (uint32_t)(x.a.g.row_stride / 8);
+                const bytes_at row = have ? (bytes_at)s.k + 16 * chunk : (bytes_at)kZeroRow;
 #pragma unroll
                 for (int c = 0; c < D / 32; ++c) keys[u][c] = load_from<uint4v>(row + 64 * c + 16 * g);
             }
         }
-        if constexpr (FP4) load_keys<D, EIGHT>(packed, x.a, x.f, s, b, t, live, bad);
+        if constexpr (FP4) load_keys<D, EIGHT>(packed, x.a, x.f, s, spots, t, live, bad);
     }
     __device__ void expand(uint4v (&to)[2][D / 32]) const {
         if constexpr (FP4) {
@@ -202,9 +204,10 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_weigh(WeighArgs x) {
         float had;
     };
     bool bad = false;
-    const auto find = [&](const Place& p) { return look_up<EIGHT>(a, a.table + (int64_t)p.s * a.max_blocks, p.len, p.t * kTile); };
-    const auto load = [&](Ahead& to, const Place& p, const Blocks<EIGHT>& b, bool live) {
-        to.keys.load(x, keys_of(x, p.s, p.u, p.len), b, p.t * kTile, live, bad);
+    Finder<EIGHT> finder;
+    const auto find = [&](const Place& p, bool first) { return finder.find(a, a.table + (int64_t)p.s * a.max_blocks, p.len, p.t, first); };
+    const auto load = [&](Ahead& to, const Place& p, const Spots<EIGHT>& spots, bool live) {
+        to.keys.load(x, keys_of(x, p.s, p.u, p.len), spots, p.t * kTile, live, bad);
         to.had = load_from<float>((bytes_at)(x.before + ((int64_t)p.s * a.n_kv + p.u) * x.width + min(Result::token(p.t * kTile), p.len - 1)));
     };
 
@@ -223,15 +226,16 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_weigh(WeighArgs x) {
     // c: the tile computed; c1 and c2: those on their way; c3: the one whose blocks are looked up
     Ahead tiles[3];
     Place c1 = next(c, 1), c2 = next(c1, 2);
-    Blocks<EIGHT> b = find(c), b1 = find(c1), b2 = find(c2);
+    const Spots<EIGHT> at = find(c, true), at1 = find(c1, c1.t == 0);
+    Spots<EIGHT> at2 = find(c2, c2.t == 0);
     open(c);
-    load(tiles[0], c, b, true);
-    load(tiles[1], c1, b1, left > 1);
+    load(tiles[0], c, at, true);
+    load(tiles[1], c1, at1, left > 1);
     const auto step = [&](Ahead& now, Ahead& then) {  // -> whether it was the last one
         const Place c3 = next(c2, 3);
-        const Blocks<EIGHT> b3 = find(c3);
+        const Spots<EIGHT> at3 = find(c3, c3.t == 0);
         __builtin_amdgcn_sched_barrier(0);
-        load(then, c2, b2, left > 2);
+        load(then, c2, at2, left > 2);
         __builtin_amdgcn_sched_barrier(0);
         const uint32_t t = c.t * kTile, token = t + 8 * ((lane & 15) >> 2) + (lane & 3);
         uint4v keys[2][D / 32];
@@ -254,7 +258,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_weigh(WeighArgs x) {
         c = c1;
         c1 = c2;
         c2 = c3;
-        b2 = b3;
+        at2 = at3;
         --left;
         return false;
     };
@@ -263,24 +267,27 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_weigh(WeighArgs x) {
     if (bad) atomicOr(&a.st->status, KVC_ST_BAD_INDEX);
 }
 
-// ---- many queries: bound by the products and the powers.  A workgroup takes 128 tokens of a sequence and head, 32 to a wave, whose keys stay in registers; 16 queries at a time come to LDS for all waves, the
+// ---- many queries: bound by the products and the powers.  A workgroup takes 128 tokens of a sequence and head, 32 to a wave, whose keys stay in registers; 64 queries at a time (32 of wide heads) come to LDS for all waves, the
 // next ones on their way meanwhile, with their -lse and the tokens they see.
 constexpr uint32_t kChunk = 4 * kTile;
 template <int D, bool FP4, bool EIGHT>
 __global__ __launch_bounds__(256, 2) void k_weigh_many(WeighArgs x) {
     constexpr uint32_t kStride = 2 * D + 16;  // bytes of a query in LDS: 16 lanes that read the same channels of 16 queries meet in no bank
-    constexpr uint32_t kPieces = (16 * D / 8 + 255) / 256;  // of 16 bytes, of a thread
+    constexpr uint32_t kRows = D <= 128 ? 64 : 32;
+    constexpr uint32_t kAll = kRows * D / 8, kPieces = (kAll + 255) / 256;  // of 16 bytes, and of a thread
     __shared__ Sums sums;
-    __shared__ __align__(16) uint8_t queries[2][16 * kStride];
-    __shared__ __align__(16) float lows[2][16];
-    __shared__ __align__(16) uint32_t limits[2][16];
+    __shared__ __align__(16) uint8_t queries[2][kRows * kStride];
+    __shared__ __align__(16) float lows[2][kRows];
+    __shared__ __align__(16) uint32_t limits[2][kRows];
     const AttendArgs& a = x.a;
-    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform(tid / 64), n = lane & 15, g = lane >> 4, row_tiles = (a.rows + 15) / 16;
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform(tid / 64), n = lane & 15, g = lane >> 4, stages = (a.rows + kRows - 1) / kRows;
     const auto chunks_of = [&](uint32_t s) { return (weighed_length(x, s) + kChunk - 1) / kChunk; };
     add_up(sums, a.n_seq, chunks_of);
     const uint32_t all = uniform(sums.all) * a.n_kv;
     bool bad = false;
-    for (uint32_t chunk = blockIdx.x; chunk < all; chunk += gridDim.x) {
+    // (workgroups go to the XCDs in turn: an XCD's take neighbouring chunks, whose queries are the same)
+    const uint32_t of_xcd = (all + 7) / 8, first = blockIdx.x % 8 * of_xcd, last = min(first + of_xcd, all);
+    for (uint32_t chunk = first + blockIdx.x / 8; chunk < last; chunk += gridDim.x / 8) {
         const Item it = find_item(sums, a.n_seq, chunk / a.n_kv, chunks_of);
         const uint32_t s = uniform(it.i), len = uniform(weighed_length(x, s)), chunks = (len + kChunk - 1) / kChunk, rel = chunk - uniform(it.start) * a.n_kv, h = rel / chunks;
         const uint32_t begin = (rel - h * chunks) * kChunk, t = begin + wave * kTile, full = uniform((uint32_t)a.lens[s]);
@@ -288,14 +295,14 @@ __global__ __launch_bounds__(256, 2) void k_weigh_many(WeighArgs x) {
         uint4v ahead[kPieces];
         float low_ahead = 0.f;
         uint32_t limit_ahead = 0;
-        const auto ask = [&](uint32_t rt) {
+        const auto ask = [&](uint32_t stage) {
 #pragma unroll
             for (uint32_t k = 0; k < kPieces; ++k) {
-                const uint32_t i = min(tid + 256 * k, 16u * D / 8 - 1), row = min(rt * 16 + i / (D / 8), (uint32_t)a.rows - 1);
+                const uint32_t i = min(tid + 256 * k, kAll - 1), row = min(stage * kRows + i / (D / 8), (uint32_t)a.rows - 1);
                 ahead[k] = load_from<uint4v>((bytes_at)(Row(a, h, row).query(a, s) + 8 * (i % (D / 8))));
             }
-            if (tid < 16) {
-                const uint32_t row = rt * 16 + tid;
+            if (tid < kRows) {
+                const uint32_t row = stage * kRows + tid;
                 const Row of(a, h, min(row, (uint32_t)a.rows - 1));
                 low_ahead = of.low(a, s);
                 limit_ahead = row < (uint32_t)a.rows ? of.limit(a, full, len) : 0;
@@ -305,14 +312,14 @@ __global__ __launch_bounds__(256, 2) void k_weigh_many(WeighArgs x) {
 #pragma unroll
             for (uint32_t k = 0; k < kPieces; ++k) {
                 const uint32_t i = tid + 256 * k;
-                if (i < 16 * D / 8) *reinterpret_cast<uint4v*>(&queries[buffer][i / (D / 8) * kStride + i % (D / 8) * 16]) = ahead[k];
+                if (i < kAll) *reinterpret_cast<uint4v*>(&queries[buffer][i / (D / 8) * kStride + i % (D / 8) * 16]) = ahead[k];
             }
-            if (tid < 16) lows[buffer][tid] = low_ahead, limits[buffer][tid] = limit_ahead;
+            if (tid < kRows) lows[buffer][tid] = low_ahead, limits[buffer][tid] = limit_ahead;
         };
         const SourceFp4 src = keys_of(x, s, h, len);
-        const Blocks<EIGHT> b = look_up<EIGHT>(a, src.table, len, t);
+        Finder<EIGHT> finder;
         KeyTile<D, FP4, EIGHT> tile;
-        tile.load(x, src, b, t, live, bad);
+        tile.load(x, src, finder.find(a, src.table, len, t / kTile, true), t, live, bad);
         ask(0);
         uint4v keys[2][D / 32];
         tile.expand(keys);
@@ -321,27 +328,31 @@ __global__ __launch_bounds__(256, 2) void k_weigh_many(WeighArgs x) {
         // (queries that see all of the chunk, and exist, need no comparison)
         const bool all_seen = begin + kChunk + a.n_q <= full + 1 && begin + kChunk <= len;
         float sum[2] = {0.f, 0.f};
-        for (uint32_t rt = 0; rt < row_tiles; ++rt) {
-            const uint32_t buffer = rt & 1;
+        for (uint32_t stage = 0; stage < stages; ++stage) {
+            const uint32_t buffer = stage & 1;
             put(buffer);  // (the waves that read this buffer are past the last barrier)
             __syncthreads();
-            if (rt + 1 < row_tiles) ask(rt + 1);
-            uint4v q[D / 32];
-            if constexpr (FP4) {
-                const uint8_t* row = &queries[buffer][n * kStride];
-                load_query<D>(q, reinterpret_cast<const uint16_t*>(row), g);
-            } else {
+            if (stage + 1 < stages) ask(stage + 1);
+            const bool all_rows = all_seen && (stage + 1) * kRows <= (uint32_t)a.rows;
 #pragma unroll
-                for (int c = 0; c < D / 32; ++c) q[c] = *reinterpret_cast<const uint4v*>(&queries[buffer][n * kStride + 64 * c + 16 * g]);
+            for (uint32_t r = 0; r < kRows; r += 16) {
+                uint4v q[D / 32];
+                const uint8_t* row = &queries[buffer][(r + n) * kStride];
+                if constexpr (FP4) {
+                    load_query<D>(q, reinterpret_cast<const uint16_t*>(row), g);
+                } else {
+#pragma unroll
+                    for (int c = 0; c < D / 32; ++c) q[c] = *reinterpret_cast<const uint4v*>(row + 64 * c + 16 * g);
+                }
+                const float4v l = *reinterpret_cast<const float4v*>(&lows[buffer][r + 4 * g]);
+                const float low[4] = {l[0], l[1], l[2], l[3]};
+                float4v sc[2];
+                score<D>(sc, q, keys);
+                const uint4v m = *reinterpret_cast<const uint4v*>(&limits[buffer][r + 4 * g]);
+                const uint32_t limit[4] = {m[0], m[1], m[2], m[3]};
+                if (all_rows) add_weights<true>(sum, sc, a.scale_log2, low, limit, token);
+                else add_weights<false>(sum, sc, a.scale_log2, low, limit, token);
             }
-            const float4v l = *reinterpret_cast<const float4v*>(&lows[buffer][4 * g]);
-            const uint4v m = *reinterpret_cast<const uint4v*>(&limits[buffer][4 * g]);
-            const float low[4] = {l[0], l[1], l[2], l[3]};
-            const uint32_t limit[4] = {m[0], m[1], m[2], m[3]};
-            float4v sc[2];
-            score<D>(sc, q, keys);
-            if (all_seen && 16 * rt + 16 <= (uint32_t)a.rows) add_weights<true>(sum, sc, a.scale_log2, low, limit, token);
-            else add_weights<false>(sum, sc, a.scale_log2, low, limit, token);
         }
         __syncthreads();  // (the buffers are used again)
         result_of(x, s, h).store(sum, tile.there, had, x, t, full, len, x.seen[s]);
