@@ -16,56 +16,223 @@ __device__ inline uint32_t order_of(float w) {
     return b >> 31 ? ~b : b | 0x80000000u;
 }
 
+template <int N>
+struct Number {
+    static constexpr int value = N;
+};
+
 // set bits of lanes before this one
 __device__ inline uint32_t before_lane(uint64_t lanes) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(lanes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)lanes, 0)); }
 
-struct SelectLds {
+__device__ inline uint32_t key_of(float w, int32_t position, int64_t safe_from) { return position >= safe_from ? 0xFFFFFFFFu : order_of(w); }
+
+// The sum over a wave's lanes up to this one.  (Within rows of 16 lanes, then rows 0 and 2 into 1 and 3, then the first half into the second; without LDS.)
+template <int CONTROL, int ROWS>
+__device__ inline uint32_t plus_lane(uint32_t v) { return v + (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CONTROL, ROWS, 0xF, false); }
+__device__ inline uint32_t sum_upto(uint32_t v) {
+    v = plus_lane<0x111, 0xF>(v);  // one lane back, two, four, eight
+    v = plus_lane<0x112, 0xF>(v);
+    v = plus_lane<0x114, 0xF>(v);
+    v = plus_lane<0x118, 0xF>(v);
+    v = plus_lane<0x142, 0xA>(v);  // lane 15 of the row before
+    return plus_lane<0x143, 0xC>(v);  // lane 31
+}
+// Sums of what the waves left in LDS: before this one's, and of all.
+struct Before {
+    uint32_t here, all;
+    __device__ Before(const uint32_t (&of_wave)[kSelectWaves], uint32_t wave) {
+        const int v = (int)of_wave[threadIdx.x % kSelectWaves];
+        here = all = 0;
+#pragma unroll
+        for (uint32_t k = 0; k < kSelectWaves; ++k) {
+            const uint32_t n = (uint32_t)__builtin_amdgcn_readlane(v, k);
+            here += k < wave ? n : 0;
+            all += n;
+        }
+    }
+};
+
+// What a workgroup of the selection has: a sequence and head.
+struct Unit {
+    uint32_t s, len, keep;  // len: 0 where it is below zero
+    int32_t given;
+    int64_t safe_from;
+    const float* weights;
+    const int32_t* positions;
+    float* weights_out;
+    int32_t* positions_out;
+
+    __device__ explicit Unit(const EvictArgs& a) {
+        s = fast_div(blockIdx.x, a.by_n_kv);
+        given = a.lens[s];
+        len = (uint32_t)max(given, 0);
+        keep = (uint32_t)max(a.keep[s], 0);
+        safe_from = (int64_t)a.seen[s] - min((uint32_t)a.recent, keep);
+        const int64_t at = (int64_t)blockIdx.x * a.width;
+        weights = a.weights + at;
+        positions = a.positions + at;
+        weights_out = a.weights_out + at;
+        positions_out = a.positions_out + at;
+    }
+    // Whether nothing leaves: there are no more tokens than stay, or one has no block or no weight; what is kept for them is then copied as it is.  Called by all threads.
+    __device__ bool settled(const EvictArgs& a) const {
+        bool bad = given > a.width || (int64_t)given > (int64_t)a.max_blocks * a.g.N;
+        if (!bad)
+            for (uint32_t i = threadIdx.x; (int64_t)i * a.g.N < len; i += kSelectThreads) {
+                const int32_t block = a.table[(int64_t)s * a.max_blocks + i];
+                bad = bad || block < 0 || block >= a.n_cache_blocks;
+            }
+        bad = __syncthreads_or(bad);
+        const bool all = bad || len <= keep;
+        if (threadIdx.x == 0) {
+            if (bad) atomicOr(&a.st->status, KVC_ST_BAD_INDEX);
+            if (all) a.counts[blockIdx.x] = 0;
+            if (blockIdx.x == s * a.n_kv) a.left[s] = bad ? given : (int32_t)min(len, keep);
+        }
+        if (all) {
+            const uint32_t n = min(len, (uint32_t)a.width);
+            if (weights_out != weights)
+                for (uint32_t t = threadIdx.x; t < n; t += kSelectThreads) weights_out[t] = weights[t];
+            if (positions_out != positions)
+                for (uint32_t t = threadIdx.x; t < n; t += kSelectThreads) positions_out[t] = positions[t];
+        }
+        return all;
+    }
+};
+
+// ---- which tokens leave: a workgroup per sequence and head, whose waves have slots in a row each, up to I * 64 of them in registers.  The key of the heaviest that leaves is found 11 bits at a time, by
+// counting; of equal keys the lowest slots leave.  Slots that leave below `keep`, and those from there on that stay, are numbered in order, and meet in LDS.
+template <int I>
+__global__ __launch_bounds__(kSelectThreads, I <= 9 ? 8 : 4) void k_select(EvictArgs a) {
+    constexpr int kBins = 2048;
+    __shared__ uint32_t bins[kBins], sums[kSelectWaves], fillers_of[kSelectWaves], digit, next_rank;
+    __shared__ uint16_t hole_of[I * kSelectThreads / 2];
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform(tid / 64);
+    const Unit u(a);
+    const uint32_t part = (u.len + kSelectThreads - 1) / kSelectThreads * 64, from = wave * part + lane;
+    float w[I];
+    int32_t position[I];
+#pragma unroll
+    for (int i = 0; i < I; ++i) {  // (all at once, before anything is known of the sequence; behind the last slot the last one again)
+        const int64_t at = min(from + 64 * i, (uint32_t)a.width - 1);
+        w[i] = a.width ? u.weights[at] : 0.f;
+        position[i] = a.width ? u.positions[at] : 0;
+    }
+    if (u.settled(a)) return;
+    const uint32_t len = u.len, keep = u.keep;
+    uint32_t key[I];
+    bool mine[I];
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+        mine[i] = 64u * i < part && from + 64 * i < len;
+        key[i] = key_of(w[i], position[i], u.safe_from);
+    }
+    uint32_t prefix = 0, rank = len - keep;  // the rank-th smallest (from 1) of the keys that begin as prefix does
+    const auto pass = [&](auto shift_, auto bits_) {
+        constexpr int shift = decltype(shift_)::value, bits = decltype(bits_)::value;
+        bins[tid] = 0;
+        bins[tid + kSelectThreads] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < I; ++i)
+            if (mine[i] && (shift + bits == 32 || (key[i] ^ prefix) >> (shift + bits & 31) == 0)) atomicAdd(&bins[key[i] >> shift & (1u << bits) - 1], 1u);
+        __syncthreads();
+        const uint32_t n0 = bins[2 * tid], n = n0 + bins[2 * tid + 1];
+        uint32_t upto = sum_upto(n);
+        if (lane == 63) sums[wave] = upto;
+        __syncthreads();
+        upto += Before(sums, wave).here;
+        const uint32_t before = upto - n;
+        if (before < rank && rank <= upto) {  // (one thread)
+            const bool second = before + n0 < rank;
+            digit = 2 * tid + (second ? 1 : 0);
+            next_rank = rank - before - (second ? n0 : 0);
+        }
+        __syncthreads();
+        prefix |= digit << shift;
+        rank = next_rank;
+    };
+    pass(Number<21>(), Number<11>());
+    pass(Number<10>(), Number<11>());
+    pass(Number<0>(), Number<10>());
+    // keys below `prefix` leave, and the first `rank` that equal it
+    uint32_t equal = 0;
+#pragma unroll
+    for (int i = 0; i < I; ++i) equal += __popcll(__ballot(mine[i] && key[i] == prefix));
+    if (lane == 0) sums[wave] = equal;
+    __syncthreads();
+    uint32_t seen = Before(sums, wave).here;
+    bool hole[I], filler[I];
+    uint32_t holes = 0, fillers = 0;
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+        const uint64_t same = __ballot(mine[i] && key[i] == prefix);
+        const bool leaves = mine[i] && (key[i] < prefix || (key[i] == prefix && seen + before_lane(same) < rank));
+        seen += __popcll(same);
+        hole[i] = leaves && from + 64 * i < keep;
+        filler[i] = mine[i] && !leaves && from + 64 * i >= keep;
+        holes += __popcll(__ballot(hole[i]));
+        fillers += __popcll(__ballot(filler[i]));
+    }
+    __syncthreads();  // (the sums are used again)
+    if (lane == 0) sums[wave] = holes, fillers_of[wave] = fillers;
+    __syncthreads();
+    const Before holes_before(sums, wave);
+    uint32_t hole_at = holes_before.here, filler_at = Before(fillers_of, wave).here;
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+        const uint32_t t = from + 64 * i;
+        const uint64_t all = __ballot(hole[i]);
+        if (hole[i]) hole_of[hole_at + before_lane(all)] = (uint16_t)t;
+        hole_at += __popcll(all);
+        if (!hole[i] && mine[i] && t < keep) {
+            if (u.weights_out != u.weights) u.weights_out[t] = w[i];
+            if (u.positions_out != u.positions) u.positions_out[t] = position[i];
+        }
+    }
+    if (tid == 0) a.counts[blockIdx.x] = (int32_t)holes_before.all;
+    __syncthreads();
+    int32_t* hole_list = a.holes + (int64_t)blockIdx.x * a.most;
+    int32_t* filler_list = a.fillers + (int64_t)blockIdx.x * a.most;
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+        const uint64_t all = __ballot(filler[i]);
+        if (filler[i]) {
+            const uint32_t j = filler_at + before_lane(all), to = hole_of[j];
+            hole_list[j] = (int32_t)to;
+            filler_list[j] = (int32_t)(from + 64 * i);
+            u.weights_out[to] = w[i];
+            u.positions_out[to] = position[i];
+        }
+        filler_at += __popcll(all);
+    }
+}
+
+struct LongLds {
     uint32_t keys[kKeysKept];
     uint32_t bins[256];
     uint32_t ties[kSelectWaves], holes[kSelectWaves], fillers[kSelectWaves];
     uint32_t digit, rank;
 };
 
-// ---- which tokens leave: a workgroup per sequence and head.  The weight of the heaviest that leaves is found 8 bits at a time, of equal ones the lowest slots leave; then the lists of slots are
-// written in order.
-__global__ __launch_bounds__(kSelectThreads) void k_select(EvictArgs a) {
-    __shared__ SelectLds lds;
-    const uint32_t unit = blockIdx.x, s = fast_div(unit, a.by_n_kv), tid = threadIdx.x, lane = tid & 63, wave = uniform(tid / 64);
-    const int32_t given = a.lens[s], keep = max(a.keep[s], 0);
-    const uint32_t len = (uint32_t)max(given, 0);
-    const float* weights = a.weights + (int64_t)unit * a.width;
-    const int32_t* positions = a.positions + (int64_t)unit * a.width;
-    float* weights_out = a.weights_out + (int64_t)unit * a.width;
-    int32_t* positions_out = a.positions_out + (int64_t)unit * a.width;
-    // a sequence with a token that has no block, or no weight, is left as it is
-    bool bad = given > a.width || (int64_t)given > (int64_t)a.max_blocks * a.g.N;
-    if (!bad)
-        for (uint32_t i = tid; (int64_t)i * a.g.N < len; i += kSelectThreads) {
-            const int32_t block = a.table[(int64_t)s * a.max_blocks + i];
-            bad = bad || block < 0 || block >= a.n_cache_blocks;
-        }
-    bad = __syncthreads_or(bad);
-    if (bad && tid == 0) atomicOr(&a.st->status, KVC_ST_BAD_INDEX);
-    const bool stays_all = bad || len <= (uint32_t)keep;
-    if (tid == 0) {
-        if (stays_all) a.counts[unit] = 0;
-        if (unit == s * a.n_kv) a.left[s] = bad ? given : min((int32_t)len, keep);
-    }
-    if (stays_all) {
-        const uint32_t n = min(len, (uint32_t)a.width);
-        if (weights_out != weights)
-            for (uint32_t t = tid; t < n; t += kSelectThreads) weights_out[t] = weights[t];
-        if (positions_out != positions)
-            for (uint32_t t = tid; t < n; t += kSelectThreads) positions_out[t] = positions[t];
-        return;
-    }
-    const int64_t safe_from = (int64_t)a.seen[s] - min(a.recent, keep);
-    const auto make_key = [&](uint32_t t) { return (int64_t)positions[t] >= safe_from ? 0xFFFFFFFFu : order_of(weights[t]); };
+// ---- more than 16,384 slots: the same, with keys that are made again each time they are needed, 8 bits at a time.
+__global__ __launch_bounds__(kSelectThreads) void k_select_long(EvictArgs a) {
+    __shared__ LongLds lds;
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform(tid / 64);
+    const Unit u(a);
+    if (u.settled(a)) return;
+    const uint32_t len = u.len, keep = u.keep;
+    const float* weights = u.weights;
+    const int32_t* positions = u.positions;
+    float* weights_out = u.weights_out;
+    int32_t* positions_out = u.positions_out;
+    const int64_t unit = blockIdx.x;
+    const auto make_key = [&](uint32_t t) { return key_of(weights[t], positions[t], u.safe_from); };
     const bool kept = len <= kKeysKept;
     const auto key = [&](uint32_t t) { return kept ? lds.keys[t] : make_key(t); };
     if (kept)
         for (uint32_t t = tid; t < len; t += kSelectThreads) lds.keys[t] = make_key(t);
-    uint32_t prefix = 0, rank = len - (uint32_t)keep;  // the rank-th smallest (from 1) of the keys that begin as prefix does
+    uint32_t prefix = 0, rank = len - keep;  // the rank-th smallest (from 1) of the keys that begin as prefix does
     for (int shift = 24; shift >= 0; shift -= 8) {
         if (tid < 256) lds.bins[tid] = 0;
         __syncthreads();
@@ -111,7 +278,7 @@ __global__ __launch_bounds__(kSelectThreads) void k_select(EvictArgs a) {
             const uint64_t equal = __ballot(t < to && k == prefix);
             const bool leaves = t < to && (k < prefix || (k == prefix && seen + before_lane(equal) < rank));
             seen += __popcll(equal);
-            const bool hole = leaves && t < (uint32_t)keep, filler = t < to && !leaves && t >= (uint32_t)keep;
+            const bool hole = leaves && t < keep, filler = t < to && !leaves && t >= keep;
             each(t, hole, filler, __ballot(hole), __ballot(filler));
         }
     };
@@ -124,14 +291,14 @@ __global__ __launch_bounds__(kSelectThreads) void k_select(EvictArgs a) {
         if (w < wave) hole_at += lds.holes[w], filler_at += lds.fillers[w];
         count += lds.holes[w];
     }
-    int32_t* hole_list = a.holes + (int64_t)unit * a.most;
-    int32_t* filler_list = a.fillers + (int64_t)unit * a.most;
+    int32_t* hole_list = a.holes + unit * a.most;
+    int32_t* filler_list = a.fillers + unit * a.most;
     walk([&](uint32_t t, bool hole, bool filler, uint64_t h, uint64_t f) {
         if (hole) hole_list[hole_at + before_lane(h)] = (int32_t)t;
         if (filler) filler_list[filler_at + before_lane(f)] = (int32_t)t;
         hole_at += __popcll(h);
         filler_at += __popcll(f);
-        if (!hole && t < to && t < (uint32_t)keep) {
+        if (!hole && t < to && t < keep) {
             if (weights_out != weights) weights_out[t] = weights[t];
             if (positions_out != positions) positions_out[t] = positions[t];
         }
@@ -218,7 +385,7 @@ __global__ __launch_bounds__(256) void k_move_rows(EvictArgs a) {
 #pragma unroll
             for (uint32_t j = 0; j < kAtOnce; ++j)
                 if (to[j]) {
-                    *reinterpret_cast<uint4v*>(to[j]) = r[j];
+                    __builtin_nontemporal_store(r[j], reinterpret_cast<uint4v*>(to[j]));
                     if (FP4) *exp_to[j] = e[j];
                 }
         }
@@ -226,7 +393,11 @@ __global__ __launch_bounds__(256) void k_move_rows(EvictArgs a) {
 }
 
 hipError_t launch_evict(const EvictArgs& a, hipStream_t s) {
-    const hipError_t e = launch_kernel(k_select, dim3((unsigned)a.n_seq * (unsigned)a.n_kv), dim3(kSelectThreads), s, a);
+    // (as few registers as there are slots: up to 9,216 of them two workgroups are on a compute unit)
+    constexpr int per = (int)kSelectThreads;
+    const auto select = a.width <= per ? k_select<1> : a.width <= 2 * per ? k_select<2> : a.width <= 3 * per ? k_select<3> : a.width <= 5 * per ? k_select<5> : a.width <= 9 * per ? k_select<9> :
+                        a.width <= 16 * per ? k_select<16> : k_select_long;
+    const hipError_t e = launch_kernel(select, dim3((unsigned)a.n_seq * (unsigned)a.n_kv), dim3(kSelectThreads), s, a);
     return e != hipSuccess ? e : launch_kernel(a.fp4 ? k_move_rows<true> : k_move_rows<false>, dim3(kMoveGroups), dim3(256), s, a);
 }
 

@@ -278,10 +278,26 @@ def test_eviction_of_weights_of_every_kind(kind, keep, recent):
     _check_evict(_evict_case(1, 16, 32, 3, LENS, keep, kind=kind), recent, apart=False)
 
 
-@pytest.mark.parametrize("n", [1023, 1024, 1025, 5000, 16384, 16385, 20001])
+@pytest.mark.parametrize("n", [1023, 1024, 1025, 2000, 5000, 9000, 16300, 16384, 16385, 20001])
 def test_eviction_of_long_sequences(n):
     for kind, keep in (("heavy", n - 1), ("ties", n // 3), ("heavy", n // 2)):
         _check_evict(_evict_case(n, 16, 32, 1, [n, 7], keep, kind=kind), 100)
+
+
+def test_long_tables_of_short_sequences():
+    """Slots for 20,000 tokens, and fewer in most sequences."""
+    _check_evict(_evict_case(12, 16, 32, 2, [20001, 5000, 100, 16384], 3000), 100, apart=False)
+    _check_evict(_evict_case(13, 16, 32, 2, [9001, 5000, 100, 70], 60, kind="ties"), 10)
+
+
+def test_no_slots():
+    """Sequences of no tokens need none; of others none has a weight, and they stay."""
+    codec = _codec(16, 64, 4)
+    cache = torch.zeros((4, 4, 16, 64), dtype=torch.float16, device=DEV)
+    none, lens = torch.empty((2, 2, 0), device=DEV), _dev(np.array([0, 20], np.int32))
+    new = torch.full_like(lens, -1)
+    codec.evict(cache, _dev(np.array([[0, 1], [2, 3]], np.int32)), lens, lens // 2, 0, none, none.int(), lens, new, torch.empty(kvc.evict_workspace(2, 2, 0), dtype=torch.uint8, device=DEV))
+    assert new.tolist() == [0, 20] and codec.stats()["status"] == kvc.ST_BAD_INDEX
 
 
 def test_a_budget_for_each_sequence():
