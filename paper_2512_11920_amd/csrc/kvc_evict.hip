@@ -6,7 +6,7 @@
 
 namespace kvc {
 
-constexpr uint32_t kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
+constexpr uint32_t kSelectThreads = 512, kSelectWaves = kSelectThreads / 64;
 constexpr uint32_t kKeysKept = 16384;  // in LDS, 64 KB, so that two workgroups are on a compute unit
 
 // Weights in the order of whole numbers: -infinity..., zeros of either sign alike, ...infinity, NaN, and tokens that are safe.
@@ -103,8 +103,8 @@ struct Unit {
 // ---- which tokens leave: a workgroup per sequence and head, whose waves have slots in a row each, up to I * 64 of them in registers.  The key of the heaviest that leaves is found 11 bits at a time, by
 // counting; of equal keys the lowest slots leave.  Slots that leave below `keep`, and those from there on that stay, are numbered in order, and meet in LDS.
 template <int I>
-__global__ __launch_bounds__(kSelectThreads, I <= 9 ? 8 : 4) void k_select(EvictArgs a) {
-    constexpr int kBins = 2048;
+__global__ __launch_bounds__(kSelectThreads, I <= 17 ? 4 : 2) void k_select(EvictArgs a) {
+    constexpr uint32_t kBins = 2048, kEach = kBins / kSelectThreads;
     __shared__ uint32_t bins[kBins], sums[kSelectWaves], fillers_of[kSelectWaves], digit, next_rank;
     __shared__ uint16_t hole_of[I * kSelectThreads / 2];
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform(tid / 64);
@@ -130,23 +130,28 @@ __global__ __launch_bounds__(kSelectThreads, I <= 9 ? 8 : 4) void k_select(Evict
     uint32_t prefix = 0, rank = len - keep;  // the rank-th smallest (from 1) of the keys that begin as prefix does
     const auto pass = [&](auto shift_, auto bits_) {
         constexpr int shift = decltype(shift_)::value, bits = decltype(bits_)::value;
-        bins[tid] = 0;
-        bins[tid + kSelectThreads] = 0;
+#pragma unroll
+        for (uint32_t k = 0; k < kEach; ++k) bins[tid + k * kSelectThreads] = 0;
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < I; ++i)
             if (mine[i] && (shift + bits == 32 || (key[i] ^ prefix) >> (shift + bits & 31) == 0)) atomicAdd(&bins[key[i] >> shift & (1u << bits) - 1], 1u);
         __syncthreads();
-        const uint32_t n0 = bins[2 * tid], n = n0 + bins[2 * tid + 1];
-        uint32_t upto = sum_upto(n);
+        uint32_t n[kEach], here = 0;
+#pragma unroll
+        for (uint32_t k = 0; k < kEach; ++k) here += n[k] = bins[kEach * tid + k];
+        uint32_t upto = sum_upto(here);
         if (lane == 63) sums[wave] = upto;
         __syncthreads();
         upto += Before(sums, wave).here;
-        const uint32_t before = upto - n;
+        uint32_t before = upto - here;
         if (before < rank && rank <= upto) {  // (one thread)
-            const bool second = before + n0 < rank;
-            digit = 2 * tid + (second ? 1 : 0);
-            next_rank = rank - before - (second ? n0 : 0);
+            uint32_t k = 0;
+#pragma unroll
+            for (uint32_t j = 0; j + 1 < kEach; ++j)
+                if (k == j && before + n[j] < rank) before += n[j], k = j + 1;
+            digit = kEach * tid + k;
+            next_rank = rank - before;
         }
         __syncthreads();
         prefix |= digit << shift;
@@ -393,10 +398,8 @@ __global__ __launch_bounds__(256) void k_move_rows(EvictArgs a) {
 }
 
 hipError_t launch_evict(const EvictArgs& a, hipStream_t s) {
-    // (as few registers as there are slots: up to 9,216 of them two workgroups are on a compute unit)
     constexpr int per = (int)kSelectThreads;
-    const auto select = a.width <= per ? k_select<1> : a.width <= 2 * per ? k_select<2> : a.width <= 3 * per ? k_select<3> : a.width <= 5 * per ? k_select<5> : a.width <= 9 * per ? k_select<9> :
-                        a.width <= 16 * per ? k_select<16> : k_select_long;
+    const auto select = a.width <= 2 * per ? k_select<2> : a.width <= 5 * per ? k_select<5> : a.width <= 9 * per ? k_select<9> : a.width <= 17 * per ? k_select<17> : a.width <= 32 * per ? k_select<32> : k_select_long;
     const hipError_t e = launch_kernel(select, dim3((unsigned)a.n_seq * (unsigned)a.n_kv), dim3(kSelectThreads), s, a);
     return e != hipSuccess ? e : launch_kernel(a.fp4 ? k_move_rows<true> : k_move_rows<false>, dim3(kMoveGroups), dim3(256), s, a);
 }

@@ -19,11 +19,16 @@ inline Fp4Pages fp4_pages(int N, int d, int64_t ppb) {
     return f;
 }
 
+constexpr uint32_t kTurn = 4;
+
 struct AppendFp4Args {
     uint8_t* k_cache;
     uint8_t* v_cache;  // already at the first value page
     Fp4Pages f;
     AppendArgs a;      // (its caches are not looked at)
+    bool wide;         // kTurn new tokens to a workgroup, else one
+    uint32_t turns;    // workgroups of a sequence
+    FastDiv by_turns;
 };
 
 struct UnpackFp4Args {

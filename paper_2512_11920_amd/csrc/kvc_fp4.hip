@@ -18,50 +18,84 @@ __device__ inline uint32_t exponent_byte(uint32_t m) {
     return m == 0 ? 0 : min(e, 140u);
 }
 
-// ---- append: a workgroup per new token, a lane per 16 bytes of its K and V rows, four lanes to a group of 32 channels.
+// What 8 channels of a row become: codes, and the exponent of the 32 channels that four lanes have.
+struct Packed {
+    uint32_t codes, exp;
+};
+__device__ inline Packed packed(const uint4v& r) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) m = max(m, max(r[j] & 0x7FFFu, r[j] >> 16 & 0x7FFFu));
+    m = max(m, (uint32_t)__shfl_xor((int)m, 1));
+    m = max(m, (uint32_t)__shfl_xor((int)m, 2));
+    const bool finite = m < 0x7C00;
+    Packed p;
+    p.exp = finite ? exponent_byte(m) : 255;
+    const float scale = __uint_as_float(finite && m ? p.exp << 23 : 127u << 23);
+    p.codes = 0;
+    p.codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(p.codes, pair(r[0]), scale, 0);
+    p.codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(p.codes, pair(r[1]), scale, 1);
+    p.codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(p.codes, pair(r[2]), scale, 2);
+    p.codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(p.codes, pair(r[3]), scale, 3);
+    p.codes = finite ? p.codes : 0;
+    return p;
+}
+
+// ---- append: a workgroup per T new tokens of a sequence, a lane per 16 bytes of their K and V rows, four lanes to a group of 32 channels.  The rows are asked for first of all, as where they go takes two
+// reads that follow from each other (the length, the table).
+template <uint32_t T>
 __global__ __launch_bounds__(256) void k_append_fp4(AppendFp4Args x) {
     const AppendArgs& a = x.a;
-    const uint32_t s = fast_div(blockIdx.x, a.by_n_new), i = blockIdx.x - s * (uint32_t)a.n_new;
-    const int64_t t = (int64_t)a.lens[s] - a.n_new + i;
-    if (t < 0) return;
-    const uint32_t at = fast_div((uint32_t)t, a.by_N), row = (uint32_t)t - at * (uint32_t)a.g.N;
-    if (at >= (uint32_t)a.max_blocks) {
-        if (threadIdx.x == 0) atomicOr(&a.st->status, KVC_ST_BAD_INDEX);
-        return;
-    }
-    const int32_t block = a.table[(int64_t)s * a.max_blocks + at];
-    if (block < 0) return;
-    if (block >= a.n_cache_blocks) {
-        if (threadIdx.x == 0) atomicOr(&a.st->status, KVC_ST_BAD_INDEX);
-        return;
-    }
-    const uint32_t each = (uint32_t)(a.n_kv * a.g.lpr);  // (a multiple of 4, so a group's lanes are there together)
-    for (uint32_t c = threadIdx.x; c < 2 * each; c += blockDim.x) {
+    __shared__ int64_t block_at[T];  // bytes from the beginning of a cache to the token's block; -1: no place
+    __shared__ uint32_t row_at[T];
+    const uint32_t s = fast_div(blockIdx.x, x.by_turns), i0 = (blockIdx.x - s * x.turns) * T, tid = threadIdx.x, n = min(T, (uint32_t)a.n_new - i0);
+    const uint32_t each = (uint32_t)(a.n_kv * a.g.lpr), N = (uint32_t)a.g.N;  // (a multiple of 4, so a group's lanes are there together)
+    for (uint32_t c0 = 0; c0 < 2 * each; c0 += blockDim.x) {
+        const uint32_t c = c0 + tid;
         const bool v = c >= each;
         const uint32_t e = v ? c - each : c, h = fast_div(e, a.by_lpr), k = e - h * (uint32_t)a.g.lpr;
-        const uint16_t* from = v ? a.v_new + s * a.v_strides[0] + i * a.v_strides[1] + h * a.v_strides[2]
-                                 : a.k_new + s * a.k_strides[0] + i * a.k_strides[1] + h * a.k_strides[2];
-        const uint4v r = reinterpret_cast<const uint4v*>(from)[k];
-        uint32_t m = 0;
+        const int64_t* strides = v ? a.v_strides : a.k_strides;
+        const uint16_t* from = (v ? a.v_new : a.k_new) + s * strides[0] + h * strides[2] + 8 * k;
+        uint4v r[T];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) m = max(m, max(r[j] & 0x7FFFu, r[j] >> 16 & 0x7FFFu));
-        m = max(m, (uint32_t)__shfl_xor((int)m, 1));
-        m = max(m, (uint32_t)__shfl_xor((int)m, 2));
-        const bool finite = m < 0x7C00;
-        const uint32_t exp = finite ? exponent_byte(m) : 255;
-        const float scale = __uint_as_float(finite && m ? exp << 23 : 127u << 23);
-        uint32_t codes = 0;
-        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(codes, pair(r[0]), scale, 0);
-        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(codes, pair(r[1]), scale, 1);
-        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(codes, pair(r[2]), scale, 2);
-        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(codes, pair(r[3]), scale, 3);
-        uint8_t* page = (v ? x.v_cache : x.k_cache) + block * x.f.block + (int64_t)h * x.f.page;
-        reinterpret_cast<uint32_t*>(page + row * (uint32_t)(a.g.d / 2))[k] = finite ? codes : 0;
-        if ((k & 3) == 0) page[x.f.exps + (k / 4) * (uint32_t)a.g.N + row] = (uint8_t)exp;
+        for (uint32_t i = 0; i < T; ++i) {
+            r[i] = uint4v{0, 0, 0, 0};
+            if (c < 2 * each && i < n) r[i] = *reinterpret_cast<const uint4v*>(from + (i0 + i) * strides[1]);
+        }
+        if (c0 == 0) {
+            if (tid < n) {
+                const int64_t t = (int64_t)a.lens[s] - a.n_new + i0 + tid;
+                int64_t at = -1;
+                if (t >= 0) {
+                    const uint32_t entry = fast_div((uint32_t)t, a.by_N);
+                    row_at[tid] = (uint32_t)t - entry * N;
+                    const bool beyond = entry >= (uint32_t)a.max_blocks;
+                    const int32_t block = beyond ? -1 : a.table[(int64_t)s * a.max_blocks + entry];
+                    if (beyond || block >= a.n_cache_blocks) atomicOr(&a.st->status, KVC_ST_BAD_INDEX);
+                    else if (block >= 0) at = block * x.f.block;
+                }
+                block_at[tid] = at;
+            }
+            __syncthreads();
+        }
+        if (c >= 2 * each) break;
+        uint8_t* pages = (v ? x.v_cache : x.k_cache) + (int64_t)h * x.f.page;
+#pragma unroll
+        for (uint32_t i = 0; i < T; ++i) {
+            if (i >= n || block_at[i] < 0) continue;  // (for all lanes alike)
+            const Packed p = packed(r[i]);
+            uint8_t* page = pages + block_at[i];
+            *reinterpret_cast<uint32_t*>(page + row_at[i] * (uint32_t)(a.g.d / 2) + 4 * k) = p.codes;
+            if ((k & 3) == 0) page[x.f.exps + k / 4 * N + row_at[i]] = (uint8_t)p.exp;
+        }
     }
 }
 
-// ---- unpack: a workgroup per 16 KB of FP16, a lane per 8 channels, four of them on their way before the first store.
+constexpr int64_t kUnpackKept = 32 << 20;  // bytes of a call whose stores the caches keep
+
+// ---- unpack: a workgroup per 16 KB of FP16, a lane per 8 channels, four of them on their way before the first store.  PAST: stores go past the caches, where there are many: a prompt chunk's 64 MB behind an
+// append 22.4 us with it, 25.9 without, 59 MB in two calls 17.9 and 17.8, 256 KB 11.3 and 9.7.
+template <bool PAST>
 __global__ __launch_bounds__(256) void k_unpack_fp4(UnpackFp4Args a) {
     const uint32_t i = fast_div(blockIdx.x, a.by_pieces), piece = blockIdx.x - i * (uint32_t)a.pieces;
     const int32_t src = a.src ? a.src[i] : (int32_t)i, dst = a.dst ? a.dst[i] : (int32_t)i;
@@ -95,16 +129,19 @@ __global__ __launch_bounds__(256) void k_unpack_fp4(UnpackFp4Args a) {
         r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes[k], scale, 1));
         r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes[k], scale, 2));
         r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes[k], scale, 3));
-        if (at[k] >= 0) *reinterpret_cast<uint4v*>(y + at[k]) = r;
+        if (at[k] < 0) continue;
+        if (PAST) __builtin_nontemporal_store(r, reinterpret_cast<uint4v*>(y + at[k]));
+        else *reinterpret_cast<uint4v*>(y + at[k]) = r;
     }
 }
 
 hipError_t launch_append_fp4(const AppendFp4Args& a, hipStream_t s) {
     const unsigned threads = (unsigned)std::min<int64_t>(256, (2ll * a.a.n_kv * a.a.g.lpr + 63) / 64 * 64);
-    return launch_kernel(k_append_fp4, dim3((unsigned)(a.a.n_seq * a.a.n_new)), dim3(threads), s, a);
+    return launch_kernel(a.wide ? k_append_fp4<kTurn> : k_append_fp4<1>, dim3((unsigned)a.a.n_seq * a.turns), dim3(threads), s, a);
 }
 hipError_t launch_unpack_fp4(const UnpackFp4Args& a, hipStream_t s) {
-    return launch_kernel(k_unpack_fp4, dim3((unsigned)a.pieces * (unsigned)a.n), dim3(256), s, a);
+    const bool past = (int64_t)a.n * a.chunks * 16 > kUnpackKept;
+    return launch_kernel(past ? k_unpack_fp4<true> : k_unpack_fp4<false>, dim3((unsigned)a.pieces * (unsigned)a.n), dim3(256), s, a);
 }
 
 }  // namespace kvc

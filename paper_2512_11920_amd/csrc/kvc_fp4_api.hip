@@ -17,6 +17,8 @@ static const uint8_t* values_fp4(const Fp4Pages& f, const void* k, const void* v
 }
 // Tokens of a table's row are counted in 31 bits.
 static bool tokens_ok(const kvc_ctx* ctx, int32_t max_blocks) { return (int64_t)max_blocks * ctx->g.N <= INT32_MAX - 256; }
+// New tokens of a call from which on several of a sequence share a workgroup.
+constexpr int64_t kManyNew = 2048;
 static bool product_ok(int64_t a, int64_t b, int64_t c) { return (__int128)a * b * c <= INT32_MAX; }
 
 // What attention and the weighing of tokens have in common.
@@ -81,6 +83,9 @@ int kvc_append_fp4(kvc_ctx* ctx, const kvc_append_t* p, void* stream) {
     a.by_n_new = make_fast_div((uint32_t)p->n_new);
     a.by_lpr = make_fast_div((uint32_t)ctx->g.lpr);
     a.st = ctx->st;
+    x.wide = (int64_t)p->n_seq * p->n_new >= kManyNew && p->n_new > 1;
+    x.turns = x.wide ? ((uint32_t)p->n_new + kTurn - 1) / kTurn : (uint32_t)p->n_new;
+    x.by_turns = make_fast_div(x.turns);
     return launched(launch_append_fp4(x, static_cast<hipStream_t>(stream)));
 }
 
