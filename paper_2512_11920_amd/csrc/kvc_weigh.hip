@@ -267,18 +267,19 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_weigh(WeighArgs x) {
     if (bad) atomicOr(&a.st->status, KVC_ST_BAD_INDEX);
 }
 
-// ---- many queries: bound by the products and the powers.  A workgroup takes 128 tokens of a sequence and head, 32 to a wave, whose keys stay in registers; 64 queries at a time (32 of wide heads) come to LDS for all waves, the
-// next ones on their way meanwhile, with their -lse and the tokens they see.
-constexpr uint32_t kChunk = 4 * kTile;
+// ---- many queries: bound by the products and the powers.  A workgroup takes 64 tokens of a sequence and head, waves 0 and 2 the first 32 and waves 1 and 3 the others, whose keys stay in registers; 64 queries at
+// a time (32 of wide heads) come to LDS for all waves, the next ones on their way meanwhile, with their -lse and the tokens they see, and waves 0 and 1 take the first 16 of 32, waves 2 and 3 the others.
+constexpr uint32_t kChunk = 2 * kTile;
 template <int D, bool FP4, bool EIGHT>
-__global__ __launch_bounds__(256, 2) void k_weigh_many(WeighArgs x) {
+__global__ __launch_bounds__(256, D <= 128 ? 3 : 2) void k_weigh_many(WeighArgs x) {
     constexpr uint32_t kStride = 2 * D + 16;  // bytes of a query in LDS: 16 lanes that read the same channels of 16 queries meet in no bank
     constexpr uint32_t kRows = D <= 128 ? 64 : 32;
-    constexpr uint32_t kAll = kRows * D / 8, kPieces = (kAll + 255) / 256;  // of 16 bytes, and of a thread
+    constexpr uint32_t kLanes = 256 / kRows, kPieces = (D / 8 + kLanes - 1) / kLanes;  // threads that load a query, and pieces of 16 bytes of each
     __shared__ Sums sums;
     __shared__ __align__(16) uint8_t queries[2][kRows * kStride];
     __shared__ __align__(16) float lows[2][kRows];
     __shared__ __align__(16) uint32_t limits[2][kRows];
+    __shared__ float other[2][2][64];  // [half of the tokens][score tile][lane]: sums of waves 2 and 3
     const AttendArgs& a = x.a;
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform(tid / 64), n = lane & 15, g = lane >> 4, stages = (a.rows + kRows - 1) / kRows;
     const auto chunks_of = [&](uint32_t s) { return (weighed_length(x, s) + kChunk - 1) / kChunk; };
@@ -290,17 +291,14 @@ __global__ __launch_bounds__(256, 2) void k_weigh_many(WeighArgs x) {
     for (uint32_t chunk = first + blockIdx.x / 8; chunk < last; chunk += gridDim.x / 8) {
         const Item it = find_item(sums, a.n_seq, chunk / a.n_kv, chunks_of);
         const uint32_t s = uniform(it.i), len = uniform(weighed_length(x, s)), chunks = (len + kChunk - 1) / kChunk, rel = chunk - uniform(it.start) * a.n_kv, h = rel / chunks;
-        const uint32_t begin = (rel - h * chunks) * kChunk, t = begin + wave * kTile, full = uniform((uint32_t)a.lens[s]);
-        const bool live = t < len;
+        const uint32_t begin = (rel - h * chunks) * kChunk, t = begin + (wave & 1) * kTile, full = uniform((uint32_t)a.lens[s]);
         uint4v ahead[kPieces];
         float low_ahead = 0.f;
         uint32_t limit_ahead = 0;
         const auto ask = [&](uint32_t stage) {
+            const bytes_at from = (bytes_at)Row(a, h, min(stage * kRows + tid / kLanes, (uint32_t)a.rows - 1)).query(a, s);
 #pragma unroll
-            for (uint32_t k = 0; k < kPieces; ++k) {
-                const uint32_t i = min(tid + 256 * k, kAll - 1), row = min(stage * kRows + i / (D / 8), (uint32_t)a.rows - 1);
-                ahead[k] = load_from<uint4v>((bytes_at)(Row(a, h, row).query(a, s) + 8 * (i % (D / 8))));
-            }
+            for (uint32_t k = 0; k < kPieces; ++k) ahead[k] = load_from<uint4v>(from + 16 * min(kLanes * k + tid % kLanes, D / 8 - 1u));
             if (tid < kRows) {
                 const uint32_t row = stage * kRows + tid;
                 const Row of(a, h, min(row, (uint32_t)a.rows - 1));
@@ -311,15 +309,15 @@ __global__ __launch_bounds__(256, 2) void k_weigh_many(WeighArgs x) {
         const auto put = [&](uint32_t buffer) {
 #pragma unroll
             for (uint32_t k = 0; k < kPieces; ++k) {
-                const uint32_t i = tid + 256 * k;
-                if (i < kAll) *reinterpret_cast<uint4v*>(&queries[buffer][i / (D / 8) * kStride + i % (D / 8) * 16]) = ahead[k];
+                const uint32_t c = kLanes * k + tid % kLanes;
+                if (c < D / 8) *reinterpret_cast<uint4v*>(&queries[buffer][tid / kLanes * kStride + c * 16]) = ahead[k];
             }
             if (tid < kRows) lows[buffer][tid] = low_ahead, limits[buffer][tid] = limit_ahead;
         };
         const SourceFp4 src = keys_of(x, s, h, len);
         Finder<EIGHT> finder;
         KeyTile<D, FP4, EIGHT> tile;
-        tile.load(x, src, finder.find(a, src.table, len, t / kTile, true), t, live, bad);
+        tile.load(x, src, finder.find(a, src.table, len, t / kTile, true), t, t < len, bad);
         ask(0);
         uint4v keys[2][D / 32];
         tile.expand(keys);
@@ -335,7 +333,8 @@ __global__ __launch_bounds__(256, 2) void k_weigh_many(WeighArgs x) {
             if (stage + 1 < stages) ask(stage + 1);
             const bool all_rows = all_seen && (stage + 1) * kRows <= (uint32_t)a.rows;
 #pragma unroll
-            for (uint32_t r = 0; r < kRows; r += 16) {
+            for (uint32_t r0 = 0; r0 < kRows; r0 += 32) {
+                const uint32_t r = r0 + 16 * (wave >> 1);
                 uint4v q[D / 32];
                 const uint8_t* row = &queries[buffer][(r + n) * kStride];
                 if constexpr (FP4) {
@@ -354,8 +353,13 @@ __global__ __launch_bounds__(256, 2) void k_weigh_many(WeighArgs x) {
                 else add_weights<false>(sum, sc, a.scale_log2, low, limit, token);
             }
         }
-        __syncthreads();  // (the buffers are used again)
-        result_of(x, s, h).store(sum, tile.there, had, x, t, full, len, x.seen[s]);
+        if (wave >= 2) other[wave & 1][0][lane] = sum[0], other[wave & 1][1][lane] = sum[1];
+        __syncthreads();  // (and the buffers are used again)
+        if (wave < 2) {
+            sum[0] += other[wave][0][lane];
+            sum[1] += other[wave][1][lane];
+            result_of(x, s, h).store(sum, tile.there, had, x, t, full, len, x.seen[s]);
+        }
     }
     if (bad) atomicOr(&a.st->status, KVC_ST_BAD_INDEX);
 }
