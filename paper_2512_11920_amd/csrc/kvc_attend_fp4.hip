@@ -262,8 +262,8 @@ __global__ __launch_bounds__(64 * kDirectWaves, D * R <= 128 ? 2 : 1) void k_dir
     const uint32_t units = a.n_kv * a.own_tiles, s = blockIdx.x / units, u = blockIdx.x - s * units, h = u / a.own_tiles, rt = u - h * a.own_tiles;
     SourceFp4 src{a.table + (int64_t)s * a.max_blocks, (uint32_t)a.max_blocks * (uint32_t)a.g.N, x.k + (int64_t)h * x.f.page, x.v + (int64_t)h * x.f.page};
     Finder<EIGHT> finder;
-    Spots<EIGHT> spots;
-    if (wave * kTile < src.len) spots = finder.find(a, src.table, src.len, wave, true);  // (as far as the table's row goes)
+    Spots<EIGHT> spots = {};
+    if (a.max_blocks) spots = finder.find(a, src.table, src.len, wave, true);  // (as far as the table's row goes)
     Rows<D> r[R];
     uint32_t later[R];
 #pragma unroll
@@ -278,17 +278,43 @@ __global__ __launch_bounds__(64 * kDirectWaves, D * R <= 128 ? 2 : 1) void k_dir
     src.len = uniform(own_length(a, s));
     const uint32_t tiles = (src.len + kTile - 1) / kTile;
     bool bad = false;
-    for (uint32_t t = wave; t < tiles; t += kDirectWaves) {
-        if (t != wave) spots = finder.find(a, src.table, src.len, t, true);
-        TileFp4<D, EIGHT> tile;
-        tile.load(x, src, spots, t * kTile, true, bad);
+    if (wave < tiles) {
         uint32_t limit[R];
 #pragma unroll
         for (int j = 0; j < R; ++j) limit[j] = min(len > later[j] ? len - later[j] : 0, src.len);
-        float4v sc[R][2];
-        make_scores<D, R, EIGHT>(sc, r, tile.k);
-        const uint32_t later_most = (uint32_t)a.n_q - 1;
-        add_tile_fp4<D, R, EIGHT>(r, x, tile, sc, t * kTile, min(len > later_most ? len - later_most : 0, src.len), limit);
+        const uint32_t later_most = (uint32_t)a.n_q - 1, seen_by_all = min(len > later_most ? len - later_most : 0, src.len);
+        uint32_t t = wave;
+        if constexpr (D * R <= 128) {
+            // the next tile is on its way while this one is computed, its place in the table looked up before
+            TileFp4<D, EIGHT> here, next;
+            here.load(x, src, spots, t * kTile, true, bad);
+            spots = finder.find(a, src.table, src.len, t + kDirectWaves, true);
+            const auto step = [&](TileFp4<D, EIGHT>& now, TileFp4<D, EIGHT>& then) {  // -> whether it was the last one
+                const Spots<EIGHT> at = finder.find(a, src.table, src.len, t + 2 * kDirectWaves, true);
+                __builtin_amdgcn_sched_barrier(0);
+                then.load(x, src, spots, (t + kDirectWaves) * kTile, t + kDirectWaves < tiles, bad);
+                __builtin_amdgcn_sched_barrier(0);
+                float4v sc[R][2];
+                make_scores<D, R, EIGHT>(sc, r, now.k);
+                add_tile_fp4<D, R, EIGHT>(r, x, now, sc, t * kTile, seen_by_all, limit);
+                spots = at;
+                t += kDirectWaves;
+                return t >= tiles;
+            };
+            while (!step(here, next) && !step(next, here)) {
+            }
+        } else {  // (there are no registers for two)
+            for (;;) {
+                TileFp4<D, EIGHT> tile;
+                tile.load(x, src, spots, t * kTile, true, bad);
+                float4v sc[R][2];
+                make_scores<D, R, EIGHT>(sc, r, tile.k);
+                add_tile_fp4<D, R, EIGHT>(r, x, tile, sc, t * kTile, seen_by_all, limit);
+                t += kDirectWaves;
+                if (t >= tiles) break;
+                spots = finder.find(a, src.table, src.len, t, true);
+            }
+        }
     }
     if (bad) atomicOr(&a.st->status, KVC_ST_BAD_INDEX);
     const uint32_t workers = min(tiles, kDirectWaves);

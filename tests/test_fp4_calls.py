@@ -69,8 +69,12 @@ def test_calls_that_are_taken_and_calls_that_are_refused():
         assert code == kvc.ERR_ARG and n == 0, (c, code, n)
 
 
-def test_short_tables_take_one_launch():
-    assert answers([_attend(max_blocks=32)]) == [(kvc.OK, 1)] and answers([_attend(max_blocks=33)]) == [(kvc.OK, 2)]
+def test_calls_of_few_tokens_and_units_take_one_launch():
+    """A workgroup for every unit: up to 512 units of tables of 512 tokens, and longer ones where heads are narrow and units are many enough."""
+    calls = [(_attend(max_blocks=64), 1), (_attend(max_blocks=65), 2), (_attend(max_blocks=65, n_seq=32), 1), (_attend(max_blocks=128, n_seq=512), 1), (_attend(max_blocks=32, n_seq=513), 2),
+             (_attend(max_blocks=512, n_seq=256), 1), (_attend(max_blocks=512, n_seq=128), 2), (_attend(max_blocks=512, n_seq=257), 2), (_attend(max_blocks=513, n_seq=256), 2),
+             (_attend(max_blocks=32, n_heads=20), 1), (_attend(max_blocks=33, n_heads=20), 2), (_attend(max_blocks=32, d=224), 1), (_attend(max_blocks=33, d=224), 2), (_attend(max_blocks=1, d=256), 2)]
+    assert answers([dict(c) for c, _ in calls]) == [(kvc.OK, n) for _, n in calls]
 
 
 def test_calls_without_a_context_are_refused():

@@ -221,6 +221,20 @@ def test_attention_of_wide_tables(d, N, kv, group, nq):
     _check(_case(d + N, N, d, kv, group, nq, [0, 700, 1, 0, 33, 512, 1037, 5], separate=d % 64 == 0, width=-(-1100 // N), holes=nq > 1), strided=True)
 
 
+@pytest.mark.parametrize("d", [32, 96, 128])
+@pytest.mark.parametrize("N", [16, 5])
+@pytest.mark.parametrize("group,nq", [(1, 1), (4, 3)])
+def test_attention_of_middling_tables(d, N, group, nq):
+    """One launch, several tiles to a wave."""
+    _check(_case(d + N, N, d, 2, group, nq, [0, 900, 257, 512, 3, 1000, 511, 769], width=1020 // N, holes=nq > 1))
+
+
+def test_one_launch_of_long_sequences():
+    """256 units of up to 4,096 tokens."""
+    c = _case(20, 16, 32, 64, 1, 1, [4000, 100, 0, 2100])
+    _check(c)
+
+
 def test_one_long_sequence():
     _check(_case(1, 16, 128, 1, 8, 1, [20011]))
 
