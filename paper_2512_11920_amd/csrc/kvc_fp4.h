@@ -95,9 +95,9 @@ struct EvictArgs {
 // unit (a KV head and its row tiles), which takes one range of the sequences' tiles; one at least.
 inline AttendPlan plan_attend_fp4(int64_t n_seq, int64_t n_q, int64_t n_heads, int64_t n_kv, int d) {
     AttendPlan p = plan_attend(n_seq, n_q, n_heads, n_kv, d, 0);
-    const int64_t workers = (d * p.own_rows / 16 <= 128 ? 2 : 1) * kOwnWorkers, units = n_kv * ((n_heads / n_kv * n_q + p.own_rows - 1) / p.own_rows);
-    p.own_workers = (uint32_t)(std::max<int64_t>(1, workers / units) * units);
-    p.slots = p.rows + 2ull * p.own_workers * p.own_rows;
+    const int64_t workers = (d * p.own_rows / 16 <= 128 ? 2 : 1) * kOwnWorkers, units = n_kv * ((n_heads / n_kv * n_q + p.own_rows - 1) / p.own_rows), ranges = std::max<int64_t>(1, workers / units);
+    p.own_workers = (uint32_t)(ranges * units);
+    p.slots = p.rows + (ranges > 1 ? 2ull * p.own_workers * p.own_rows : 0);  // (of one range nothing is shared)
     p.bytes = p.starts + round_256(p.slots * 8) + p.slots * (uint64_t)d * 4;
     return p;
 }

@@ -267,9 +267,10 @@ def test_lengths_beyond_the_table_and_blocks_beyond_the_cache():
 @pytest.mark.parametrize("width", [None, 70])
 @pytest.mark.parametrize("nq", [1, 4])
 @pytest.mark.parametrize("N", [16, 5])
-def test_groups_that_are_nan_reach_only_the_queries_that_see_them(width, nq, N):
+@pytest.mark.parametrize("group", [2, 8])
+def test_groups_that_are_nan_reach_only_the_queries_that_see_them(width, nq, N, group):
     """A NaN group of keys makes the rows that see it NaN, one of values its channels of them; among the last tokens, of some queries and not of others."""
-    c = _case(7, N, 64, 1, 2, nq, [60, 100, 33], width=width)
+    c = _case(7, N, 64, 1, group, nq, [60, 100, 33], width=width)
     k, v = ref.parts(c["caches"][0], N, 64, 2), ref.parts(c["caches"][0], N, 64, 2)
     t = 99
     v[1][c["table"][1, t // N], 1, t % N, 1] = 255
