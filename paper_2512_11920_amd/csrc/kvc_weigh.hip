@@ -72,11 +72,9 @@ struct Row {
         head = h * a.group + in;
     }
     __device__ const uint16_t* query(const AttendArgs& a, uint32_t s) const { return a.q + s * a.q_strides[0] + i * a.q_strides[1] + head * a.q_strides[2]; }
+    __device__ float lse(const AttendArgs& a, uint32_t s) const { return a.lse[((int64_t)s * a.n_q + i) * a.n_heads + head]; }
     // -lse in powers of two; a query that sees nothing gives weights of zero
-    __device__ float low(const AttendArgs& a, uint32_t s) const {
-        const float lse = a.lse[((int64_t)s * a.n_q + i) * a.n_heads + head];
-        return lse == -INFINITY ? -INFINITY : -lse * 1.44269504088896341f;
-    }
+    __device__ static float low(float lse) { return lse == -INFINITY ? -INFINITY : -lse * 1.44269504088896341f; }
     // tokens it sees
     __device__ uint32_t limit(const AttendArgs& a, uint32_t full, uint32_t len) const {
         const uint32_t later = a.n_q - 1 - i;
@@ -108,7 +106,7 @@ struct Queries {
         for (int r = 0; r < 4; ++r) {
             const uint32_t row = rt * 16 + 4 * g + r;
             const Row of(a, h, min(row, last));
-            low[r] = of.low(a, s);
+            low[r] = Row::low(of.lse(a, s));
             limit[r] = row <= last ? of.limit(a, full, len) : 0;
         }
     }
@@ -133,6 +131,11 @@ __device__ inline void add_weights(float (&sum)[2], const float4v (&s)[2], float
             sum[u] += ALL || token + 4 * u < limit[r] ? w : 0.f;
         }
 }
+
+template <bool B>
+struct Flag {
+    static constexpr bool value = B;
+};
 
 // What a lane's tokens got, added to what they had, and positions of those that are new.
 struct Result {
@@ -293,7 +296,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 3 : 2) void k_weigh_many(WeighArgs 
         const uint32_t s = uniform(it.i), len = uniform(weighed_length(x, s)), chunks = (len + kChunk - 1) / kChunk, rel = chunk - uniform(it.start) * a.n_kv, h = rel / chunks;
         const uint32_t begin = (rel - h * chunks) * kChunk, t = begin + (wave & 1) * kTile, full = uniform((uint32_t)a.lens[s]);
         uint4v ahead[kPieces];
-        float low_ahead = 0.f;
+        float lse_ahead = 0.f;
         uint32_t limit_ahead = 0;
         const auto ask = [&](uint32_t stage) {
             const bytes_at from = (bytes_at)Row(a, h, min(stage * kRows + tid / kLanes, (uint32_t)a.rows - 1)).query(a, s);
@@ -302,7 +305,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 3 : 2) void k_weigh_many(WeighArgs 
             if (tid < kRows) {
                 const uint32_t row = stage * kRows + tid;
                 const Row of(a, h, min(row, (uint32_t)a.rows - 1));
-                low_ahead = of.low(a, s);
+                lse_ahead = of.lse(a, s);  // (and no more, which would be to wait for it here)
                 limit_ahead = row < (uint32_t)a.rows ? of.limit(a, full, len) : 0;
             }
         };
@@ -312,7 +315,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 3 : 2) void k_weigh_many(WeighArgs 
                 const uint32_t c = kLanes * k + tid % kLanes;
                 if (c < D / 8) *reinterpret_cast<uint4v*>(&queries[buffer][tid / kLanes * kStride + c * 16]) = ahead[k];
             }
-            if (tid < kRows) lows[buffer][tid] = low_ahead, limits[buffer][tid] = limit_ahead;
+            if (tid < kRows) lows[buffer][tid] = Row::low(lse_ahead), limits[buffer][tid] = limit_ahead;
         };
         const SourceFp4 src = keys_of(x, s, h, len);
         Finder<EIGHT> finder;
@@ -331,27 +334,29 @@ __global__ __launch_bounds__(256, D <= 128 ? 3 : 2) void k_weigh_many(WeighArgs 
             put(buffer);  // (the waves that read this buffer are past the last barrier)
             __syncthreads();
             if (stage + 1 < stages) ask(stage + 1);
-            const bool all_rows = all_seen && (stage + 1) * kRows <= (uint32_t)a.rows;
+            const auto add = [&](auto all_) {
 #pragma unroll
-            for (uint32_t r0 = 0; r0 < kRows; r0 += 32) {
-                const uint32_t r = r0 + 16 * (wave >> 1);
-                uint4v q[D / 32];
-                const uint8_t* row = &queries[buffer][(r + n) * kStride];
-                if constexpr (FP4) {
-                    load_query<D>(q, reinterpret_cast<const uint16_t*>(row), g);
-                } else {
+                for (uint32_t r0 = 0; r0 < kRows; r0 += 32) {
+                    const uint32_t r = r0 + 16 * (wave >> 1);
+                    uint4v q[D / 32];
+                    const uint8_t* row = &queries[buffer][(r + n) * kStride];
+                    if constexpr (FP4) {
+                        load_query<D>(q, reinterpret_cast<const uint16_t*>(row), g);
+                    } else {
 #pragma unroll
-                    for (int c = 0; c < D / 32; ++c) q[c] = *reinterpret_cast<const uint4v*>(row + 64 * c + 16 * g);
+                        for (int c = 0; c < D / 32; ++c) q[c] = *reinterpret_cast<const uint4v*>(row + 64 * c + 16 * g);
+                    }
+                    const float4v l = *reinterpret_cast<const float4v*>(&lows[buffer][r + 4 * g]);
+                    const float low[4] = {l[0], l[1], l[2], l[3]};
+                    const uint4v m = *reinterpret_cast<const uint4v*>(&limits[buffer][r + 4 * g]);
+                    const uint32_t limit[4] = {m[0], m[1], m[2], m[3]};
+                    float4v sc[2];
+                    score<D>(sc, q, keys);
+                    add_weights<decltype(all_)::value>(sum, sc, a.scale_log2, low, limit, token);
                 }
-                const float4v l = *reinterpret_cast<const float4v*>(&lows[buffer][r + 4 * g]);
-                const float low[4] = {l[0], l[1], l[2], l[3]};
-                float4v sc[2];
-                score<D>(sc, q, keys);
-                const uint4v m = *reinterpret_cast<const uint4v*>(&limits[buffer][r + 4 * g]);
-                const uint32_t limit[4] = {m[0], m[1], m[2], m[3]};
-                if (all_rows) add_weights<true>(sum, sc, a.scale_log2, low, limit, token);
-                else add_weights<false>(sum, sc, a.scale_log2, low, limit, token);
-            }
+            };
+            if (all_seen && (stage + 1) * kRows <= (uint32_t)a.rows) add(Flag<true>());
+            else add(Flag<false>());
         }
         if (wave >= 2) other[wave & 1][0][lane] = sum[0], other[wave & 1][1][lane] = sum[1];
         __syncthreads();  // (and the buffers are used again)
