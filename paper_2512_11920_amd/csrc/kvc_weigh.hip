@@ -270,19 +270,19 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_weigh(WeighArgs x) {
     if (bad) atomicOr(&a.st->status, KVC_ST_BAD_INDEX);
 }
 
-// ---- many queries: bound by the products and the powers.  A workgroup takes 64 tokens of a sequence and head, waves 0 and 2 the first 32 and waves 1 and 3 the others, whose keys stay in registers; 64 queries at
-// a time (32 of wide heads) come to LDS for all waves, the next ones on their way meanwhile, with their -lse and the tokens they see, and waves 0 and 1 take the first 16 of 32, waves 2 and 3 the others.
+// ---- many queries: bound by the products, the powers and reading LDS.  A workgroup takes 64 tokens of a sequence and head, whose keys stay in the registers of every wave; 64 queries at a time come to LDS, the next
+// ones on their way meanwhile, with their -lse and the tokens they see, and each wave takes 16 of them.
 constexpr uint32_t kChunk = 2 * kTile;
 template <int D, bool FP4, bool EIGHT>
 __global__ __launch_bounds__(256, D <= 128 ? 3 : 2) void k_weigh_many(WeighArgs x) {
     constexpr uint32_t kStride = 2 * D + 16;  // bytes of a query in LDS: 16 lanes that read the same channels of 16 queries meet in no bank
-    constexpr uint32_t kRows = D <= 128 ? 64 : 32;
+    constexpr uint32_t kRows = 64;
     constexpr uint32_t kLanes = 256 / kRows, kPieces = (D / 8 + kLanes - 1) / kLanes;  // threads that load a query, and pieces of 16 bytes of each
     __shared__ Sums sums;
     __shared__ __align__(16) uint8_t queries[2][kRows * kStride];
     __shared__ __align__(16) float lows[2][kRows];
     __shared__ __align__(16) uint32_t limits[2][kRows];
-    __shared__ float other[2][2][64];  // [half of the tokens][score tile][lane]: sums of waves 2 and 3
+    __shared__ float of_waves[4][4][64];  // [wave][score tile][lane]: sums
     const AttendArgs& a = x.a;
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform(tid / 64), n = lane & 15, g = lane >> 4, stages = (a.rows + kRows - 1) / kRows;
     const auto chunks_of = [&](uint32_t s) { return (weighed_length(x, s) + kChunk - 1) / kChunk; };
@@ -294,7 +294,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 3 : 2) void k_weigh_many(WeighArgs 
     for (uint32_t chunk = first + blockIdx.x / 8; chunk < last; chunk += gridDim.x / 8) {
         const Item it = find_item(sums, a.n_seq, chunk / a.n_kv, chunks_of);
         const uint32_t s = uniform(it.i), len = uniform(weighed_length(x, s)), chunks = (len + kChunk - 1) / kChunk, rel = chunk - uniform(it.start) * a.n_kv, h = rel / chunks;
-        const uint32_t begin = (rel - h * chunks) * kChunk, t = begin + (wave & 1) * kTile, full = uniform((uint32_t)a.lens[s]);
+        const uint32_t t = (rel - h * chunks) * kChunk, full = uniform((uint32_t)a.lens[s]);
         uint4v ahead[kPieces];
         float lse_ahead = 0.f;
         uint32_t limit_ahead = 0;
@@ -319,52 +319,63 @@ __global__ __launch_bounds__(256, D <= 128 ? 3 : 2) void k_weigh_many(WeighArgs 
         };
         const SourceFp4 src = keys_of(x, s, h, len);
         Finder<EIGHT> finder;
-        KeyTile<D, FP4, EIGHT> tile;
-        tile.load(x, src, finder.find(a, src.table, len, t / kTile, true), t, t < len, bad);
+        KeyTile<D, FP4, EIGHT> tile[2];
+        const Spots<EIGHT> at = finder.find(a, src.table, len, t / kTile, true), at1 = finder.find(a, src.table, len, t / kTile + 1, false);
+        tile[0].load(x, src, at, t, true, bad);
+        tile[1].load(x, src, at1, t + kTile, t + kTile < len, bad);
         ask(0);
-        uint4v keys[2][D / 32];
-        tile.expand(keys);
+        uint4v keys[2][2][D / 32];
+        float had[2], sum[2][2] = {};
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            tile[j].expand(keys[j]);
+            had[j] = load_from<float>((bytes_at)(x.before + ((int64_t)s * a.n_kv + h) * x.width + min(Result::token(t + j * kTile), len - 1)));
+        }
         const uint32_t token = t + 8 * (n >> 2) + (n & 3);
-        const float had = load_from<float>((bytes_at)(x.before + ((int64_t)s * a.n_kv + h) * x.width + min(Result::token(t), len - 1)));
         // (queries that see all of the chunk, and exist, need no comparison)
-        const bool all_seen = begin + kChunk + a.n_q <= full + 1 && begin + kChunk <= len;
-        float sum[2] = {0.f, 0.f};
+        const bool all_seen = t + kChunk + a.n_q <= full + 1 && t + kChunk <= len;
         for (uint32_t stage = 0; stage < stages; ++stage) {
             const uint32_t buffer = stage & 1;
             put(buffer);  // (the waves that read this buffer are past the last barrier)
             __syncthreads();
             if (stage + 1 < stages) ask(stage + 1);
             const auto add = [&](auto all_) {
+                const uint32_t r = 16 * wave;
+                uint4v q[D / 32];
+                const uint8_t* row = &queries[buffer][(r + n) * kStride];
+                if constexpr (FP4) {
+                    load_query<D>(q, reinterpret_cast<const uint16_t*>(row), g);
+                } else {
 #pragma unroll
-                for (uint32_t r0 = 0; r0 < kRows; r0 += 32) {
-                    const uint32_t r = r0 + 16 * (wave >> 1);
-                    uint4v q[D / 32];
-                    const uint8_t* row = &queries[buffer][(r + n) * kStride];
-                    if constexpr (FP4) {
-                        load_query<D>(q, reinterpret_cast<const uint16_t*>(row), g);
-                    } else {
-#pragma unroll
-                        for (int c = 0; c < D / 32; ++c) q[c] = *reinterpret_cast<const uint4v*>(row + 64 * c + 16 * g);
-                    }
-                    const float4v l = *reinterpret_cast<const float4v*>(&lows[buffer][r + 4 * g]);
-                    const float low[4] = {l[0], l[1], l[2], l[3]};
-                    const uint4v m = *reinterpret_cast<const uint4v*>(&limits[buffer][r + 4 * g]);
-                    const uint32_t limit[4] = {m[0], m[1], m[2], m[3]};
-                    float4v sc[2];
-                    score<D>(sc, q, keys);
-                    add_weights<decltype(all_)::value>(sum, sc, a.scale_log2, low, limit, token);
+                    for (int c = 0; c < D / 32; ++c) q[c] = *reinterpret_cast<const uint4v*>(row + 64 * c + 16 * g);
                 }
+                const float4v l = *reinterpret_cast<const float4v*>(&lows[buffer][r + 4 * g]);
+                const float low[4] = {l[0], l[1], l[2], l[3]};
+                const uint4v m = *reinterpret_cast<const uint4v*>(&limits[buffer][r + 4 * g]);
+                const uint32_t limit[4] = {m[0], m[1], m[2], m[3]};
+                float4v sc[2][2];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) score<D>(sc[j], q, keys[j]);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) add_weights<decltype(all_)::value>(sum[j], sc[j], a.scale_log2, low, limit, token + j * kTile);
             };
             if (all_seen && (stage + 1) * kRows <= (uint32_t)a.rows) add(Flag<true>());
             else add(Flag<false>());
         }
-        if (wave >= 2) other[wave & 1][0][lane] = sum[0], other[wave & 1][1][lane] = sum[1];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) of_waves[wave][k][lane] = sum[k / 2][k % 2];
         __syncthreads();  // (and the buffers are used again)
-        if (wave < 2) {
-            sum[0] += other[wave][0][lane];
-            sum[1] += other[wave][1][lane];
-            result_of(x, s, h).store(sum, tile.there, had, x, t, full, len, x.seen[s]);
+        if (wave < 2) {  // a wave for each half of the tokens
+            float all_waves[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const uint32_t k = 2 * wave + u;
+                all_waves[u] = (of_waves[0][k][lane] + of_waves[1][k][lane]) + (of_waves[2][k][lane] + of_waves[3][k][lane]);
+            }
+            if (wave == 0) result_of(x, s, h).store(all_waves, tile[0].there, had[0], x, t, full, len, x.seen[s]);
+            else result_of(x, s, h).store(all_waves, tile[1].there, had[1], x, t + kTile, full, len, x.seen[s]);
         }
+        __syncthreads();
     }
     if (bad) atomicOr(&a.st->status, KVC_ST_BAD_INDEX);
 }
