@@ -95,7 +95,8 @@ struct EvictArgs {
 // unit (a KV head and its row tiles), which takes one range of the sequences' tiles; one at least.
 inline AttendPlan plan_attend_fp4(int64_t n_seq, int64_t n_q, int64_t n_heads, int64_t n_kv, int d) {
     AttendPlan p = plan_attend(n_seq, n_q, n_heads, n_kv, d, 0);
-    const int64_t workers = (d * p.own_rows / 16 <= 128 ? 2 : 1) * kOwnWorkers, units = n_kv * ((n_heads / n_kv * n_q + p.own_rows - 1) / p.own_rows), ranges = std::max<int64_t>(1, workers / units);
+    // (waves on a SIMD, as registers are enough for: 64 sequences of 4,096 to 16,384 tokens, 8 x 32, 88.0 us with two, 80.2 with three; 8 x 64 100.7 and 110.8)
+    const int64_t workers = (d * p.own_rows / 16 <= 32 ? 3 : d * p.own_rows / 16 <= 128 ? 2 : 1) * kOwnWorkers, units = n_kv * ((n_heads / n_kv * n_q + p.own_rows - 1) / p.own_rows), ranges = std::max<int64_t>(1, workers / units);
     p.own_workers = (uint32_t)(ranges * units);
     p.slots = p.rows + (ranges > 1 ? 2ull * p.own_workers * p.own_rows : 0);  // (of one range nothing is shared)
     p.bytes = p.starts + round_256(p.slots * 8) + p.slots * (uint64_t)d * 4;
@@ -112,7 +113,12 @@ inline bool direct_fp4(int d, int row_tiles, int64_t units, int64_t tokens) {
     if (tokens <= (int64_t)kDirectTiles * 32) return true;
     return d * row_tiles <= 128 && (tokens <= 1024 || (tokens <= 2048 && units >= 32) || (tokens <= 8192 && units > 128 && units <= 256));
 }
-constexpr uint32_t kWeighWorkers = 2048, kWeighGroups = 768, kManyRows = 64;
+// Waves that weigh a few queries' tokens.  64 sequences of 1,024 to 8,192 tokens, 8 KV heads, 8 query heads each, us with 2,048, 3,072, 4,096: 128 channels in 4 bits 47.2, 44.1, 53.4, in FP16 126.0, 124.1, 124.6; 64 in 4 bits 36.7,
+// 32.9, 31.5, in FP16 69.0, 70.8, 70.7; 32 34.6, 30.9, 29.8 and 43.6, 40.8, 41.7.  Workgroups that weigh many: three to a compute unit, which is what LDS has room for of 128 channels.
+constexpr uint32_t kWeighWorkers = 3072, kWeighGroups = 768;
+// Queries of a sequence and KV head beyond which they share a workgroup's keys.  64 sequences of 512 to 4,096 tokens, the same heads, us, few / many: 24 rows, 128 channels 111 / 183, in 4 bits 57 / 97; 64 rows 182 / 182, 95 / 95 (64
+// channels 88 / 118, 71 / 75; 32 sequences of 256 channels 204 / 247, 95 / 143); 128 rows 320 / 201, 166 / 120 (144 / 132, 125 / 93; 352 / 239, 174 / 170).
+constexpr uint32_t kManyRows = 64;
 
 hipError_t launch_append_fp4(const AppendFp4Args& a, hipStream_t s);
 hipError_t launch_unpack_fp4(const UnpackFp4Args& a, hipStream_t s);
