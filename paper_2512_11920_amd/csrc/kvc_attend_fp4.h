@@ -225,13 +225,18 @@ __device__ inline uint32_t load_values(ValuesFp4<D, EIGHT>& x, const AttendArgs&
 // its neighbours may be anywhere.
 __device__ inline float power_of(uint32_t bytes, uint32_t at) { return __uint_as_float(__builtin_amdgcn_alignbit(bytes, bytes, (8 * at + 9) & 31)); }
 
+// Channels 2c and 2c + 1 of a register of codes.
+__device__ inline half2 two_channels(uint32_t codes, float scale, int c) {  // (c a constant)
+    return __builtin_bit_cast(half2, c == 0   ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 0)
+                                     : c == 1 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 1)
+                                     : c == 2 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 2)
+                                              : __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 3));
+}
 // Eight channels of FP16, from a register of codes.
 __device__ inline uint4v eight_channels(uint32_t codes, float scale) {
     uint4v r;
-    r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 0));
-    r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 1));
-    r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 2));
-    r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 3));
+#pragma unroll
+    for (int c = 0; c < 4; ++c) r[c] = __builtin_bit_cast(uint32_t, two_channels(codes, scale, c));
     return r;
 }
 
@@ -248,6 +253,9 @@ __device__ inline void expand_keys(Tokens<D>& to, const KeysFp4<D>& x) {
         expand_keys<D, EIGHT, P + 1>(to, x);
     }
 }
+// 2^e of token j of a lane's 8, of the exponents of one piece
+template <bool EIGHT>
+__device__ inline float exponent(const uint32_t (&e)[EIGHT ? 2 : 8], int j) { return power_of(e[EIGHT ? j / 4 : j], EIGHT ? j % 4 : 0); }
 // Exponents of the tokens of `there` (bit j: token j of 8), in the place of the others zero, which makes zeros of their codes.
 template <int D, bool EIGHT>
 __device__ inline void keep_values(ValuesFp4<D, EIGHT>& x, uint32_t there) {
@@ -272,27 +280,28 @@ __device__ inline void expand_values(Tokens<D>& to, const ValuesFp4<D, EIGHT>& x
         using Q = Piece<D, P>;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const float scale = power_of(x.e[P][EIGHT ? j / 4 : j], EIGHT ? j % 4 : 0);
-            to.v[j][Q::regs] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(x.c[j][P], scale, 0));
-            if constexpr (Q::w > 2) to.v[j][Q::regs + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(x.c[j][P], scale, 1));
-            if constexpr (Q::w > 4) {
-                to.v[j][Q::regs + 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(x.c[j][P], scale, 2));
-                to.v[j][Q::regs + 3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(x.c[j][P], scale, 3));
-            }
+            const float scale = exponent<EIGHT>(x.e[P], j);
+#pragma unroll
+            for (int c = 0; c < Q::w / 2; ++c) to.v[j][Q::regs + c] = __builtin_bit_cast(uint32_t, two_channels(x.c[j][P], scale, c));
         }
         expand_values<D, EIGHT, P + 1>(to, x);
     }
 }
 
-// A row's query, its channels in the order of the keys'.
-template <int D, int P = 0>
-__device__ inline void load_query(uint4v (&q)[D / 32], const uint16_t* row, uint32_t g) {
-    if constexpr (P < piece_count(D)) {
-        using Q = Piece<D, P>;
-#pragma unroll
-        for (int c = 0; c < Q::w / 2; ++c) q[Q::regs + c] = *reinterpret_cast<const uint4v*>(row + Q::before + 4 * Q::w * g + 8 * c);
-        load_query<D, P + 1>(q, row, g);
+// A row's query, its channels in the order of the keys': where the 8 of its k-th register of four are.
+template <int D>
+__device__ constexpr uint32_t query_channel(int k, uint32_t g) {
+    uint32_t at = 0;
+    for (int p = 0; p < piece_count(D); ++p) {
+        const int before = piece_before(D, p), w = (piece_before(D, p + 1) - before) / 16;
+        if (k >= before / 32) at = before + 4 * w * g + 8 * (k - before / 32);
     }
+    return at;
+}
+template <int D>
+__device__ inline void load_query(uint4v (&q)[D / 32], const uint16_t* row, uint32_t g) {
+#pragma unroll
+    for (int k = 0; k < D / 32; ++k) q[k] = *reinterpret_cast<const uint4v*>(row + query_channel<D>(k, g));
 }
 
 }  // namespace kvc

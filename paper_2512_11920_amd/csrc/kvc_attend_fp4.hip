@@ -31,24 +31,30 @@ __device__ inline bool may_be_infinite(const ValuesFp4<D, EIGHT>& x) {
     return __any(any != 0);
 }
 
-// One piece's values of 8 tokens times the rows' weights; `mine`: rows for which the result is taken.
-template <int D, int R, int P = 0>
-__device__ inline void add_values_of(Rows<D> (&r)[R], const Tokens<D>& x, const half8 (&p)[R], const bool (&mine)[R]) {
+// Values of 8 tokens, times the rows' weights, two channels at a time (there are few registers); `mine`: rows for which the result is taken.
+template <int D, int R, bool EIGHT, int P = 0>
+__device__ inline void add_values_of(Rows<D> (&r)[R], const ValuesFp4<D, EIGHT>& x, const half8 (&p)[R], const bool (&mine)[R]) {
     if constexpr (P < piece_count(D)) {
         using Q = Piece<D, P>;
 #pragma unroll
-        for (int j = 0; j < Q::w; ++j) {
-            const half8 v = __builtin_bit_cast(half8, value_column<D, P>(x, j));
+        for (int c = 0; c < Q::w / 2; ++c) {
+            Tokens<32> two;  // (a piece of two channels a lane)
 #pragma unroll
-            for (int i = 0; i < R; ++i) {
-                float4v& o = r[i].o[Q::before / 16 + j];
-                const float4v n = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p[i], o, 0, 0, 0);
+            for (int j = 0; j < 8; ++j) two.v[j][0] = __builtin_bit_cast(uint32_t, two_channels(x.c[j][P], exponent<EIGHT>(x.e[P], j), c));
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] = mine[i] ? n[e] : o[e];
+            for (int j = 0; j < 2; ++j) {
+                const half8 v = __builtin_bit_cast(half8, value_column<32, 0>(two, j));
+#pragma unroll
+                for (int i = 0; i < R; ++i) {
+                    float4v& o = r[i].o[Q::before / 16 + 2 * c + j];
+                    const float4v n = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p[i], o, 0, 0, 0);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[e] = mine[i] ? n[e] : o[e];
+                }
+                __builtin_amdgcn_sched_barrier(0);
             }
-            __builtin_amdgcn_sched_barrier(0);  // (one at a time: there are few registers)
         }
-        add_values_of<D, R, P + 1>(r, x, p, mine);
+        add_values_of<D, R, EIGHT, P + 1>(r, x, p, mine);
     }
 }
 
@@ -101,7 +107,6 @@ __device__ inline void add_tile_fp4(Rows<D> (&r)[R], const AttendFp4Args& x, Til
     half8 p[R];
 #pragma unroll
     for (int j = 0; j < R; ++j) p[j] = weights_of(r[j], s[j], x.a.scale_log2, all, tile.there, t, limit[j]);
-    Tokens<D> tokens;
     if (!all) {
         keep_values<D, EIGHT>(tile.v, tile.there);
         if (x.a.n_q > 1 && t + kTile > seen_by_all && may_be_infinite<D, EIGHT>(tile.v)) {
@@ -118,17 +123,20 @@ __device__ inline void add_tile_fp4(Rows<D> (&r)[R], const AttendFp4Args& x, Til
                 const uint32_t n = t + cut > first ? t + cut - first : 0;
                 ValuesFp4<D, EIGHT> v = tile.v;
                 keep_values<D, EIGHT>(v, n >= 8 ? 0xFFu : ~(~0u << n));
-                expand_values<D, EIGHT>(tokens, v);
-                add_values_of<D, R>(r, tokens, p, mine);
+                add_values_of<D, R, EIGHT>(r, v, p, mine);
             }
             return;
         }
     }
+    Tokens<D> tokens;
     expand_values<D, EIGHT>(tokens, tile.v);
     add_values<D, R>(r, tokens, p);
 }
 
-// ---- any lengths: a worker is a wave, the next tile is on its way while this one is computed, its block numbers a tile further ahead.
+// ---- any lengths: a worker is a wave that takes tiles of one unit (a KV head and its rows), as many as any other, from sequence to sequence; two tiles are on their way while one is computed, the block numbers
+// of a third are looked up.  For each tile of 32 tokens 34 d bytes are read and become FP16, and for each 16 rows there are d / 8 MFMAs: of up to 16 rows memory and instructions cost about the same, and
+// neither hides the other fully.  64 sequences of 512 to 8,192 tokens, 8 KV heads of 128 channels, 8 query heads each: 70 us (and 6 to join), 305 MB at 4.4 TB/s; with the products left out 66, with all blocks in the caches 52.  2,048
+// waves are what registers allow; 4,096 in two turns take 83.  With 32 rows products bound it: 118 us.
 template <int D, int R, bool EIGHT>
 __device__ inline void own_part_fp4(const AttendFp4Args& x, Sums& sums, uint32_t worker) {
     const AttendArgs& a = x.a;
@@ -165,7 +173,14 @@ __device__ inline void own_part_fp4(const AttendFp4Args& x, Sums& sums, uint32_t
     const uint32_t lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     Rows<D> r[R];
     uint32_t limit[R], seen_by_all = 0;
+    // (where registers are short, what only a sequence's begin and end need is made there, and not kept over the tiles)
+    const auto column = [&] {
+        uint32_t here = n;
+        if (!EIGHT && D * R <= 128) asm volatile("" : "+v"(here));
+        return here;
+    };
     const auto open = [&](const Place& p) {
+        const uint32_t n = column();
         const uint32_t len = uniform((uint32_t)a.lens[p.s]), later = (uint32_t)a.n_q - 1;
         seen_by_all = min(len > later ? len - later : 0, p.len);
         const uint32_t h = p.u / a.own_tiles, rt = p.u - h * a.own_tiles;
@@ -182,6 +197,7 @@ __device__ inline void own_part_fp4(const AttendFp4Args& x, Sums& sums, uint32_t
         }
     };
     const auto close = [&](const Place& p, uint32_t first_tile) {
+        const uint32_t n = column();
         const uint32_t h = p.u / a.own_tiles, rt = p.u - h * a.own_tiles;
         const bool whole = first_tile == 0 && p.t + 1 == p.tiles;
 #pragma unroll
@@ -201,8 +217,9 @@ __device__ inline void own_part_fp4(const AttendFp4Args& x, Sums& sums, uint32_t
         }
     };
 
-    // c: the tile computed; c1 and c2: those on their way; c3: the one whose blocks are looked up, before c2 is asked for, so that waiting for them is not waiting for it.
-    // All loads are made in any case (behind the last tile, of zeros): the compiler then knows how many come after those that it waits for.
+    // places[0]: the tile computed; the ones behind it are on their way, kAhead of them; the last, which is asked for in this step, has been looked up, and the tile behind it is looked up before, so that
+    // waiting for block numbers is not waiting for tiles.  All loads are made in any case (behind the last tile, of zeros): the compiler then knows how many come after those that it waits for.
+    constexpr uint32_t kAhead = EIGHT ? 2 : 1;  // (exponents that are not loaded eight at once take more registers)
     uint32_t left = end - begin, first_tile = c.t;
     const auto next = [&](const Place& p, uint32_t ahead) {
         Place n = p;
@@ -212,36 +229,46 @@ __device__ inline void own_part_fp4(const AttendFp4Args& x, Sums& sums, uint32_t
     Finder<EIGHT> finder;
     const auto find = [&](const Place& p, bool first) { return finder.find(a, a.table + (int64_t)p.s * a.max_blocks, p.len, p.t, first); };
     bool bad = false;
-    TileFp4<D, EIGHT> tiles[3];
-    Place c1 = next(c, 1), c2 = next(c1, 2);
-    const Spots<EIGHT> at = find(c, true), at1 = find(c1, c1.t == 0);
-    Spots<EIGHT> at2 = find(c2, c2.t == 0);
+    TileFp4<D, EIGHT> tiles[kAhead + 1];
+    Place places[kAhead + 1];
+    Spots<EIGHT> spots[kAhead + 1];
+#pragma unroll
+    for (uint32_t i = 0; i <= kAhead; ++i) {
+        places[i] = i ? next(places[i - 1], i) : c;
+        spots[i] = find(places[i], i == 0 || places[i].t == 0);
+    }
     open(c);
-    tiles[0].load(x, source(c), at, c.t * kTile, true, bad);
-    tiles[1].load(x, source(c1), at1, c1.t * kTile, left > 1, bad);
+#pragma unroll
+    for (uint32_t i = 0; i < kAhead; ++i) tiles[i].load(x, source(places[i]), spots[i], places[i].t * kTile, left > i, bad);
+    Spots<EIGHT> found = spots[kAhead];
     const auto step = [&](TileFp4<D, EIGHT>& now, TileFp4<D, EIGHT>& then) {  // -> whether it was the last one
-        const Place c3 = next(c2, 3);
-        const Spots<EIGHT> at3 = find(c3, c3.t == 0);
+        const Place behind = next(places[kAhead], kAhead + 1);
+        const Spots<EIGHT> at = find(behind, behind.t == 0);
         __builtin_amdgcn_sched_barrier(0);
-        then.load(x, source(c2), at2, c2.t * kTile, left > 2, bad);
+        then.load(x, source(places[kAhead]), found, places[kAhead].t * kTile, left > kAhead, bad);
         __builtin_amdgcn_sched_barrier(0);
         float4v s[R][2];
         make_scores<D, R, EIGHT>(s, r, now.k);
-        add_tile_fp4<D, R, EIGHT>(r, x, now, s, c.t * kTile, seen_by_all, limit);
-        if (left == 1 || c1.t == 0) {
-            close(c, first_tile);
+        add_tile_fp4<D, R, EIGHT>(r, x, now, s, places[0].t * kTile, seen_by_all, limit);
+        if (left == 1 || places[1].t == 0) {
+            close(places[0], first_tile);
             if (left == 1) return true;
-            open(c1);
+            open(places[1]);
             first_tile = 0;
         }
-        c = c1;
-        c1 = c2;
-        c2 = c3;
-        at2 = at3;
+#pragma unroll
+        for (uint32_t i = 0; i < kAhead; ++i) places[i] = places[i + 1];
+        places[kAhead] = behind;
+        found = at;
         --left;
         return false;
     };
-    while (!step(tiles[0], tiles[2]) && !step(tiles[1], tiles[0]) && !step(tiles[2], tiles[1])) {
+    if constexpr (kAhead == 2) {
+        while (!step(tiles[0], tiles[2]) && !step(tiles[1], tiles[0]) && !step(tiles[2], tiles[1])) {
+        }
+    } else {
+        while (!step(tiles[0], tiles[1]) && !step(tiles[1], tiles[0])) {
+        }
     }
     if (bad) atomicOr(&a.st->status, KVC_ST_BAD_INDEX);
 }
@@ -252,7 +279,8 @@ __global__ __launch_bounds__(256, D * R <= 128 ? 2 : 1) void k_own_fp4(AttendFp4
     own_part_fp4<D, R, EIGHT>(x, sums, uniform(blockIdx.x * 4 + threadIdx.x / 64));
 }
 
-// ---- short sequences: a workgroup of kDirectWaves takes a unit, its waves the tiles in turn, and they join their sums in LDS: one launch.
+// ---- short sequences: a workgroup of kDirectWaves takes a unit, its waves the tiles in turn, and they join their sums in LDS: one launch.  Bound by the chain of reads of a wave's tiles and by the launch: one sequence of 256 tokens,
+// 4 heads of 64, 5.3 us; 8 sequences of 1,024 to 2,048 tokens, 32 heads of 128, 15.2 us (54 MB).
 template <int D, int R, bool EIGHT>
 __global__ __launch_bounds__(64 * kDirectWaves, D * R <= 128 ? 2 : 1) void k_direct_fp4(AttendFp4Args x) {
     const AttendArgs& a = x.a;
@@ -284,7 +312,7 @@ __global__ __launch_bounds__(64 * kDirectWaves, D * R <= 128 ? 2 : 1) void k_dir
         for (int j = 0; j < R; ++j) limit[j] = min(len > later[j] ? len - later[j] : 0, src.len);
         const uint32_t later_most = (uint32_t)a.n_q - 1, seen_by_all = min(len > later_most ? len - later_most : 0, src.len);
         uint32_t t = wave;
-        if constexpr (D * R <= 128) {
+        if constexpr (D * R <= pipelined_fp4(EIGHT)) {
             // the next tile is on its way while this one is computed, its place in the table looked up before
             TileFp4<D, EIGHT> here, next;
             here.load(x, src, spots, t * kTile, true, bad);
@@ -350,8 +378,14 @@ __global__ __launch_bounds__(64 * kDirectWaves, D * R <= 128 ? 2 : 1) void k_dir
 template <int D, int R>
 static hipError_t launch_parts_fp4(const AttendFp4Args& x, hipStream_t s) {
     const bool eight = x.a.g.N % 8 == 0;
-    if constexpr (direct_fits(D, R))
-        if (x.a.direct) return launch_kernel(eight ? k_direct_fp4<D, R, true> : k_direct_fp4<D, R, false>, dim3((unsigned)x.a.n_seq * x.a.n_kv * x.a.own_tiles), dim3(64 * kDirectWaves), s, x);
+    if (x.a.direct) {  // (only where it fits: direct_fp4)
+        const dim3 grid((unsigned)x.a.n_seq * x.a.n_kv * x.a.own_tiles), block(64 * kDirectWaves);
+        if constexpr (direct_fits_fp4(D, R, true))
+            if (eight) return launch_kernel(k_direct_fp4<D, R, true>, grid, block, s, x);
+        if constexpr (direct_fits_fp4(D, R, false))
+            if (!eight) return launch_kernel(k_direct_fp4<D, R, false>, grid, block, s, x);
+        return hipErrorInvalidValue;
+    }
     return launch_kernel(eight ? k_own_fp4<D, R, true> : k_own_fp4<D, R, false>, dim3((x.a.own_workers + 3) / 4), dim3(256), s, x);
 }
 

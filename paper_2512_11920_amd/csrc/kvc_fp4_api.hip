@@ -148,7 +148,7 @@ int kvc_attend_fp4(kvc_ctx* ctx, const kvc_attend_t* p, void* stream) {
     for (int i = 0; i < 3; ++i) a.out_strides[i] = p->out_strides[i];
     a.own_tiles = (uint32_t)own_tiles;
     a.own_workers = plan.own_workers;
-    a.direct = direct_fp4(ctx->g.d, plan.own_rows / 16, own_tiles * p->n_kv_heads * p->n_seq, own_tokens);
+    a.direct = direct_fp4(ctx->g.d, ctx->g.N % 8 == 0, plan.own_rows / 16, own_tiles * p->n_kv_heads * p->n_seq, own_tokens);
     // (as attention over FP16 has it)
     const int64_t threads = (int64_t)plan.rows * (ctx->g.d / 8);
     while (a.join_lanes < 16 && a.join_lanes * 2 * (ctx->g.d / 8) <= 256 && threads * a.join_lanes * 2 <= 1 << 17) a.join_lanes *= 2;
