@@ -24,7 +24,8 @@ struct Number {
 // set bits of lanes before this one
 __device__ inline uint32_t before_lane(uint64_t lanes) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(lanes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)lanes, 0)); }
 
-__device__ inline uint32_t key_of(float w, int32_t position, int64_t safe_from) { return position >= safe_from ? 0xFFFFFFFFu : order_of(w); }
+constexpr uint32_t kSafe = 0xFFFFFFFFu;
+__device__ inline uint32_t key_of(float w, int32_t position, int64_t safe_from) { return position >= safe_from ? kSafe : order_of(w); }
 
 // The sum over a wave's lanes up to this one.  (Within rows of 16 lanes, then rows 0 and 2 into 1 and 3, then the first half into the second; without LDS.)
 template <int CONTROL, int ROWS>
@@ -102,12 +103,12 @@ struct Unit {
 
 // ---- which tokens leave: a workgroup per sequence and head, whose waves have slots in a row each, up to I * 64 of them in registers.  The key of the heaviest that leaves is found 11 bits at a time, by
 // counting; of equal keys the lowest slots leave.  Slots that leave below `keep`, and those from there on that stay, are numbered in order, and meet in LDS.
-// Bound by barriers, of which each of the three counts has four, and by how late the weights arrive: 512 heads of 4,097 slots 16.9 us, of 8,192 27.1.  (512 threads: one token of 4,097 leaves in 21.2 us with the moves, with 256 in
+// Bound by barriers, of which each of up to three counts has three, and by how late the weights arrive: 512 heads of 4,097 slots 16.9 us, of 8,192 27.1.  (512 threads: one token of 4,097 leaves in 21.2 us with the moves, with 256 in
 // 23.5, with 1,024 in 25.6.)
 template <int I>
 __global__ __launch_bounds__(kSelectThreads, I <= 17 ? 4 : 2) void k_select(EvictArgs a) {
     constexpr uint32_t kBins = 2048, kEach = kBins / kSelectThreads;
-    __shared__ uint32_t bins[kBins], sums[kSelectWaves], fillers_of[kSelectWaves], digit, next_rank;
+    __shared__ uint32_t bins[kBins], sums[kSelectWaves], fillers_of[kSelectWaves], digit, next_rank, whole;
     __shared__ uint16_t hole_of[I * kSelectThreads / 2];
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform(tid / 64);
     const Unit u(a);
@@ -120,7 +121,9 @@ __global__ __launch_bounds__(kSelectThreads, I <= 17 ? 4 : 2) void k_select(Evic
         w[i] = a.width ? u.weights[at] : 0.f;
         position[i] = a.width ? u.positions[at] : 0;
     }
-    if (u.settled(a)) return;
+#pragma unroll
+    for (uint32_t k = 0; k < kEach; ++k) bins[tid + k * kSelectThreads] = 0;
+    if (u.settled(a)) return;  // (past a barrier)
     const uint32_t len = u.len, keep = u.keep;
     uint32_t key[I];
     bool mine[I];
@@ -130,38 +133,48 @@ __global__ __launch_bounds__(kSelectThreads, I <= 17 ? 4 : 2) void k_select(Evic
         key[i] = key_of(w[i], position[i], u.safe_from);
     }
     uint32_t prefix = 0, rank = len - keep;  // the rank-th smallest (from 1) of the keys that begin as prefix does
-    const auto pass = [&](auto shift_, auto bits_) {
+    const auto pass = [&](auto shift_, auto bits_) {  // -> whether all keys that begin with the digits found leave: no more of them are needed, prefix is the key behind those
         constexpr int shift = decltype(shift_)::value, bits = decltype(bits_)::value;
 #pragma unroll
-        for (uint32_t k = 0; k < kEach; ++k) bins[tid + k * kSelectThreads] = 0;
-        __syncthreads();
-#pragma unroll
         for (int i = 0; i < I; ++i)
-            if (mine[i] && (shift + bits == 32 || (key[i] ^ prefix) >> (shift + bits & 31) == 0)) atomicAdd(&bins[key[i] >> shift & (1u << bits) - 1], 1u);
+            if (mine[i] && key[i] != kSafe && (shift + bits == 32 || (key[i] ^ prefix) >> (shift + bits & 31) == 0)) atomicAdd(&bins[key[i] >> shift & (1u << bits) - 1], 1u);
         __syncthreads();
         uint32_t n[kEach], here = 0;
 #pragma unroll
-        for (uint32_t k = 0; k < kEach; ++k) here += n[k] = bins[kEach * tid + k];
+        for (uint32_t k = 0; k < kEach; ++k) {
+            here += n[k] = bins[kEach * tid + k];
+            bins[kEach * tid + k] = 0;  // (for the next one, two barriers from here)
+        }
         uint32_t upto = sum_upto(here);
         if (lane == 63) sums[wave] = upto;
         __syncthreads();
-        upto += Before(sums, wave).here;
+        const Before others(sums, wave);
+        if (rank > others.all) {  // tokens that are safe leave too (and are not counted: they are in a row, and would wait for each other)
+            prefix = kSafe;
+            rank -= others.all;
+            __syncthreads();  // (the sums are used again)
+            return true;
+        }
+        upto += others.here;
         uint32_t before = upto - here;
         if (before < rank && rank <= upto) {  // (one thread)
-            uint32_t k = 0;
+            uint32_t k = 0, count = n[0];
 #pragma unroll
             for (uint32_t j = 0; j + 1 < kEach; ++j)
-                if (k == j && before + n[j] < rank) before += n[j], k = j + 1;
+                if (k == j && before + n[j] < rank) before += n[j], k = j + 1, count = n[j + 1];
             digit = kEach * tid + k;
             next_rank = rank - before;
+            whole = count == rank - before;
         }
         __syncthreads();
         prefix |= digit << shift;
         rank = next_rank;
+        if (!whole) return false;
+        prefix += (1u << shift) - (prefix >> shift == kSafe >> shift ? 1 : 0);  // (the last such keys end below kSafe)
+        rank = 0;
+        return true;
     };
-    pass(Number<21>(), Number<11>());
-    pass(Number<10>(), Number<11>());
-    pass(Number<0>(), Number<10>());
+    if (!pass(Number<21>(), Number<11>()) && !pass(Number<10>(), Number<11>())) pass(Number<0>(), Number<10>());
     // keys below `prefix` leave, and the first `rank` that equal it
     uint32_t equal = 0;
 #pragma unroll

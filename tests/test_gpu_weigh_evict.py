@@ -389,6 +389,27 @@ def test_the_binding_refuses(what):
         codec.weigh(**dict(w, **bad))
 
 
+@pytest.mark.parametrize("keep", [1, 40, 100, 199])
+def test_eviction_of_keys_that_share_their_first_bits(keep):
+    """The last to leave is found by its first 11 bits, the next 11, the last 10: weights that differ in some of these only, or end in zeros or ones."""
+    c = _evict_case(14, 16, 32, 4, [200, 200, 64], keep)
+    rng = np.random.default_rng(14)
+    bits = rng.choice(np.array([0x3F800000, 0x3FA00000, 0x40000000], np.uint32), c["weights"].shape) | rng.choice(np.array([0, 0x400, 0x1FFC00, 0x1FF800], np.uint32), c["weights"].shape) \
+        | rng.choice(np.array([0, 1, 0x3FE, 0x3FF], np.uint32), c["weights"].shape)
+    bits[:, 1] |= 0x1FFFFF
+    bits[:, 2] &= 0xFFE00000
+    c["weights"] = bits.view(np.float32)
+    c["weights"][:, 3] *= -1
+    _check_evict(c, 3)
+
+
+def test_fewer_slots_than_tokens():
+    """A sequence of more tokens than weights are kept for stays, and is reported; the others lose theirs."""
+    c = _evict_case(15, 16, 64, 2, [100, 90, 70], 40)
+    c["weights"], c["positions"] = (np.ascontiguousarray(c[k][:, :, :95]) for k in ("weights", "positions"))
+    _check_evict(c, 5, apart=False, status=4)
+
+
 def test_another_stream_and_nothing_to_do():
     s = torch.cuda.Stream()
     _check_evict(_evict_case(8, 16, 64, 2, [100, 3], 40), 5, stream=s)
