@@ -66,7 +66,8 @@ __device__ inline void make_scores(float4v (&s)[R][2], const Rows<D> (&r)[R], co
     for (int j = 0; j < R; ++j) scores(s[j], r[j], tokens);
 }
 
-// Scores of tokens t + 8g.. become weights, as `weights` has it (kvc_attend.h); all: every row sees every token.
+// Scores of tokens t + 8g.. become weights, as `weights` has it (kvc_attend.h); all: every row sees every token.  Whether a row's reference has to follow is asked lane by lane: its maximum over the four
+// lanes is needed only then.  (A score is scaled first and made relative then, each rounded: in one step, against a reference that was rounded, the largest of scores beyond 2^27 would not be its own reference.)
 template <int D>
 __device__ inline half8 weights_of(Rows<D>& r, const float4v (&s)[2], float scale_log2, bool all, uint32_t there, uint32_t t, uint32_t limit) {
     float v[8];
@@ -80,22 +81,22 @@ __device__ inline half8 weights_of(Rows<D>& r, const float4v (&s)[2], float scal
     float top = fmaxf(v[0], v[1]);
 #pragma unroll
     for (int j = 2; j < 8; ++j) top = fmaxf(top, v[j]);
-    top = row_max(top);
     if (__any(top > r.m + kLag)) {  // (a row's first token too: its reference is -infinity)
-        const float m = fmaxf(r.m, top), f = r.m == -INFINITY ? 0.f : power2(r.m - m);
+        const float m = fmaxf(r.m, row_max(top)), f = r.m == -INFINITY ? 0.f : power2(r.m - m);
         r.m = m;
         r.l *= f;
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) r.o[i] *= f;
     }
     const float low = (r.m == -INFINITY ? 0.f : r.m) - kLift;
+    float w[8];
     half8 p;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        const float w = power2(v[j] - low);
-        r.l += w;
-        p[j] = (_Float16)w;
+        w[j] = power2(v[j] - low);
+        p[j] = (_Float16)w[j];
     }
+    r.l += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
     return p;
 }
 
@@ -135,7 +136,7 @@ __device__ inline void add_tile_fp4(Rows<D> (&r)[R], const AttendFp4Args& x, Til
 
 // ---- any lengths: a worker is a wave that takes tiles of one unit (a KV head and its rows), as many as any other, from sequence to sequence; two tiles are on their way while one is computed, the block numbers
 // of a third are looked up.  For each tile of 32 tokens 34 d bytes are read and become FP16, and for each 16 rows there are d / 8 MFMAs: of up to 16 rows memory and instructions cost about the same, and
-// neither hides the other fully.  64 sequences of 512 to 8,192 tokens, 8 KV heads of 128 channels, 8 query heads each: 70 us (and 6 to join), 305 MB at 4.4 TB/s; with the products left out 66, with all blocks in the caches 52.  2,048
+// neither hides the other fully.  64 sequences of 512 to 8,192 tokens, 8 KV heads of 128 channels, 8 query heads each: 65 us (and 6 to join), 305 MB at 4.7 TB/s, some 5 of them a chain of reads before the first tile (lengths, table, rows); on an earlier step that took 70, 66 with the products left out, 52 with all blocks in the caches.  2,048
 // waves are what registers allow; 4,096 in two turns take 83.  With 32 rows products bound it: 118 us.
 template <int D, int R, bool EIGHT>
 __device__ inline void own_part_fp4(const AttendFp4Args& x, Sums& sums, uint32_t worker) {

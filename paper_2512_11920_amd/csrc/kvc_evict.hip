@@ -103,8 +103,8 @@ struct Unit {
 
 // ---- which tokens leave: a workgroup per sequence and head, whose waves have slots in a row each, up to I * 64 of them in registers.  The key of the heaviest that leaves is found 11 bits at a time, by
 // counting; of equal keys the lowest slots leave.  Slots that leave below `keep`, and those from there on that stay, are numbered in order, and meet in LDS.
-// Bound by barriers, of which each of up to three counts has three, and by how late the weights arrive: 512 heads of 4,097 slots 16.9 us, of 8,192 27.1.  (512 threads: one token of 4,097 leaves in 21.2 us with the moves, with 256 in
-// 23.5, with 1,024 in 25.6.)
+// Bound by barriers, of which each of up to three counts has three, and by how late the weights arrive: 512 heads of 4,097 slots 15.9 us, of 8,192 27.0.  (512 threads: one token of 4,097 left in 21.2 us with the moves on an earlier
+// step, with 256 in 23.5, with 1,024 in 25.6.)
 template <int I>
 __global__ __launch_bounds__(kSelectThreads, I <= 17 ? 4 : 2) void k_select(EvictArgs a) {
     constexpr uint32_t kBins = 2048, kEach = kBins / kSelectThreads;
@@ -334,7 +334,7 @@ __global__ __launch_bounds__(kSelectThreads) void k_select_long(EvictArgs a) {
 
 // ---- the rows move: the moves of all sequences and heads, in equal shares to the workgroups, 64 at a time: a thread each finds where they go from and to, then the workgroup moves them, a lane per 16 bytes
 // of keys or values (and the exponent that belongs to them).  Bound by memory: half of 8,192 tokens of 64 sequences, 8 KV heads of 128 channels, 0.54 GB that are read and written in rows of 256
-// bytes, 229 us, 4.7 TB/s; one token of each head 4.2 us.
+// bytes, 226 us, 4.7 TB/s; one token of each head 4.2 us.
 constexpr uint32_t kMoveGroups = 2048, kMoves = 64;
 
 template <bool FP4>

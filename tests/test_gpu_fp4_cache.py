@@ -249,6 +249,30 @@ def test_scales(scale):
         _check(_case(3, 16, 64, 2, 3, 2, [77, 300, 3], width=width), scale=scale)
 
 
+@pytest.mark.parametrize("N", [16, 5])
+@pytest.mark.parametrize("width", [None, 70])
+def test_rows_with_a_score_beyond_32_bits_are_nan(width, N):
+    """Whether the tile has a mask or not; rows that stay within 32 bits have the value of their largest score, as all others are far below it."""
+    c = _case(11, N, 64, 2, 6, 1, [96, 128, 40], width=width)
+    scale = 8e36
+    out, lse, _ = _run(c, scale)
+    k, v, first = _values(c)
+    seen = []
+    for s, n in enumerate(c["lens"]):
+        rows = [(c["table"][s, t // N], t % N) for t in range(n)]
+        for h in range(c["q"].shape[2]):
+            x = np.array([k[b, h // 6, r].astype(np.float64) @ c["q"][s, 0, h].astype(np.float64) for b, r in rows]) * scale / np.log(2)
+            top, best = x.max(), x.argmax()
+            assert abs(top / 2.0 ** 128 - 1) > 1e-4 and np.sort(x)[-2] < top * (1 - 1e-4)  # (sums are off by 64 * 2^-24 of their magnitudes' at most, here 1.5e-5 of the largest score)
+            seen.append(top > 2.0 ** 128)
+            if seen[-1]:
+                assert np.isnan(out[s, 0, h]).all() and np.isnan(lse[s, 0, h])
+            else:
+                b, r = rows[best]
+                assert np.array_equal(out[s, 0, h], v[b, first + h // 6, r])
+    assert any(seen) and not all(seen)
+
+
 def test_lengths_beyond_the_table_and_blocks_beyond_the_cache():
     for width in (None, 70):
         c = _case(4, 16, 96, 2, 2, 2, [40, 90, 64], width=width)
