@@ -213,9 +213,10 @@ int kvc_weigh(kvc_ctx* ctx, const kvc_weigh_t* p, void* stream) {
     return KVC_ERR_UNSUPPORTED;
 }
 
-// Workspace: moves of every sequence and head and how many they are, and tokens that stay.
+// Workspace: moves of every sequence and head and how many they are, and tokens that stay.  (Slots are counted in 31 bits, moves too; a workgroup of 512 threads has a sequence and head.)
 uint64_t kvc_evict_workspace(int32_t n_seq, int32_t n_kv_heads, int32_t width) {
-    if (n_seq < 0 || n_kv_heads < 1 || width < 0 || !product_ok(n_seq, n_kv_heads, width / 2 + 1)) return 0;
+    if (n_seq < 0 || n_kv_heads < 1 || width < 0 || width > INT32_MAX - 256 || !product_ok(n_seq, n_kv_heads, width / 2 + 1)) return 0;
+    if ((int64_t)n_seq * n_kv_heads > kMaxGroups / 4) return 0;
     const uint64_t units = (uint64_t)n_seq * n_kv_heads;
     return round_256(units * 4) + round_256((uint64_t)n_seq * 4) + 2 * round_256(units * (uint64_t)(width / 2) * 4) + 256;
 }
@@ -224,13 +225,13 @@ int kvc_evict(kvc_ctx* ctx, const kvc_evict_t* p, void* stream) {
     if (!ctx || !p || p->n_seq < 0 || p->max_blocks < 0 || p->n_cache_blocks < 0 || p->width < 0 || p->recent < 0) return KVC_ERR_ARG;
     if (!heads_ok(ctx, p->d_v_cache, p->n_kv_heads)) return KVC_ERR_ARG;
     const uint64_t need = kvc_evict_workspace(p->n_seq, p->n_kv_heads, p->width);
-    if (!need || (int64_t)p->n_seq * p->n_kv_heads > kMaxGroups / 4) return KVC_ERR_ARG;
+    if (!need) return KVC_ERR_ARG;
     if (p->n_seq == 0) return KVC_OK;
     if (!on_ctx_device(ctx)) return KVC_ERR_ARG;
     if (!p->d_k_cache || (!p->d_block_table && p->max_blocks) || !p->d_lens || !p->d_keep || !p->d_seen || !p->d_new_lens) return KVC_ERR_ARG;
     if (p->width && (!p->d_weights || !p->d_weights_out || !p->d_positions || !p->d_positions_out)) return KVC_ERR_ARG;
     if (!aligned(p->d_k_cache, 16) || !aligned(p->d_v_cache, 16)) return KVC_ERR_ARG;
-    if (!tokens_ok(ctx, p->max_blocks) || p->width > INT32_MAX - 256) return KVC_ERR_ARG;
+    if (!tokens_ok(ctx, p->max_blocks)) return KVC_ERR_ARG;
     if (!p->d_work || !aligned(p->d_work, 256) || p->work_bytes < need) return KVC_ERR_ARG;
     const uint64_t bytes = (uint64_t)p->n_seq * p->n_kv_heads * p->width * 4;
     const Buffer w = {p->d_weights, bytes}, wo = {p->d_weights_out, bytes}, o = {p->d_positions, bytes}, oo = {p->d_positions_out, bytes};
