@@ -337,7 +337,7 @@ uint64_t kvc_attend_workspace(int32_t n_seq, int32_t n_q, int32_t n_heads, int32
  * pages_per_block pages in a row, a cache blocks in a row, whatever kvc_set_cache_layout says; 16-byte aligned. */
 uint64_t kvc_fp4_block_bytes(int32_t tokens_per_block, int32_t head_dim, int32_t pages_per_block); /* 0: a shape that kvc_create refuses */
 
-/* kvc_append into a cache in 4 bits: the caches of *a are in 4 bits, the new rows are FP16. */
+/* kvc_append into a cache in 4 bits: the caches of *a are in 4 bits, the new rows are FP16.  Refused: heads whose rows of one token, K and V, are 2^31 pieces of 16 bytes or more. */
 int kvc_append_fp4(kvc_ctx* ctx, const kvc_append_t* a, void* stream);
 
 /* Blocks of a cache in 4 bits, in FP16: block src[i] of d_cache goes to block dst[i] of d_out (NULL: i), i < n.  d_out has the context's geometry and layout; no block

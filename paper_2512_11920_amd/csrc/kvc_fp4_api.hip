@@ -62,7 +62,7 @@ int kvc_append_fp4(kvc_ctx* ctx, const kvc_append_t* p, void* stream) {
     if (!p->d_k_cache || (!p->d_block_table && p->max_blocks) || !p->d_lens || !p->d_k_new || !p->d_v_new) return KVC_ERR_ARG;
     if (!aligned(p->d_k_cache, 16) || !aligned(p->d_v_cache, 16) || !aligned(p->d_k_new, 16) || !aligned(p->d_v_new, 16)) return KVC_ERR_ARG;
     if (!strides_ok(p->k_strides) || !strides_ok(p->v_strides)) return KVC_ERR_ARG;
-    if ((int64_t)p->n_seq * p->n_new > kMaxGroups) return KVC_ERR_ARG;
+    if ((int64_t)p->n_seq * p->n_new > kMaxGroups || !product_ok(2, p->n_kv_heads, ctx->g.lpr)) return KVC_ERR_ARG;
     AppendFp4Args x = {};
     x.f = pages_of(ctx);
     x.k_cache = static_cast<uint8_t*>(p->d_k_cache);
