@@ -331,7 +331,7 @@ uint64_t kvc_attend_workspace(int32_t n_seq, int32_t n_q, int32_t n_heads, int32
 /* A cache in 4 bits: the values of the same pages, in about a quarter of the memory.  32 neighbouring channels of a token share a power of two 2^e, and each is one of
  * 0, 0.5, 1, 1.5, 2, 3, 4, 6 of it, with a sign.  e is the smallest whole number with max |x| <= 7 * 2^e, and at most 13; a magnitude becomes the nearest of the eight,
  * halfway the one of even number, beyond 6 * 2^e that.  (So nothing is off by more than 2^e, but for magnitudes beyond 57,344 = 7 * 2^13, which become 49,152.)  32
- * channels of which one is infinite or NaN are all NaN.  What a code stands for is an FP16 number.
+ * channels of which one is infinite or NaN are all NaN.  What is written so stands for FP16 numbers; of other codes and exponents (half of 2^-26, 6 * 2^14) the nearest FP16 value, or infinity.
  * A page is N * d/2 bytes of codes (token by token, channel 2i in the low half of byte i; the sign is the code's highest bit, the rest the
  * number of the magnitude), N bytes of e + 127 for every 32 channels in turn (0 where all are zero, 255 for NaN), and 0 to 15 bytes that make a multiple of 16.  A block is
  * pages_per_block pages in a row, a cache blocks in a row, whatever kvc_set_cache_layout says; 16-byte aligned. */
@@ -379,7 +379,8 @@ int kvc_weigh(kvc_ctx* ctx, const kvc_weigh_t* a, void* stream);
  * others the ones with the largest weights; of equal weights the lowest slots leave first, and NaN is larger than all.  (If more than keep[s] are at such positions, the highest slots of them stay.)  The slots t < keep[s] hold what stays: a token that stays below
  * keep[s] keeps its slot, and those from there on go, in order, to the slots that were left, in order.  Keys, values, weights and positions go with the token, each head for itself; new_lens[s]
  * is what stays.  Attention does not look at the order, and positions say which token is where.  What lies from new_lens[s] on is not touched.
- * Blocks are written in place: those that hold slots below keep[s] must be the sequence's alone.  A sequence with a token that has no block, or lies beyond its table's row or `width`,
+ * Blocks are written in place: those that hold slots below keep[s] must be the sequence's alone (copies of FP16 blocks: kvc_copy_blocks; blocks in 4 bits are kvc_fp4_block_bytes bytes in a row, and copied as
+ * such).  A sequence with a token that has no block, or lies beyond its table's row or `width`,
  * stays as it is, and sets KVC_ST_BAD_INDEX.  weights_out may be weights, positions_out positions, new_lens lens. */
 typedef struct {
     void* d_k_cache;
@@ -404,7 +405,7 @@ int kvc_evict(kvc_ctx* ctx, const kvc_evict_t* a, void* stream);
 /* (0: sizes that kvc_evict refuses) */
 uint64_t kvc_evict_workspace(int32_t n_seq, int32_t n_kv_heads, int32_t width);
 
-/* Copy of cache blocks: in every layer l < n_layers, block l*blocks_per_layer + src[i] is copied to block
+/* Copy of blocks of an FP16 cache: in every layer l < n_layers, block l*blocks_per_layer + src[i] is copied to block
  * l*blocks_per_layer + dst[i] of the same cache, i < n.  One block may be copied to several; no block may be
  * both source and destination, nor destination twice. */
 int kvc_copy_blocks(kvc_ctx* ctx, void* d_cache, int64_t n_cache_blocks, const int32_t* d_src_ids, const int32_t* d_dst_ids, int32_t n,

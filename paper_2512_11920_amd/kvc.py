@@ -448,7 +448,7 @@ class Codec:
             _check(rc, "kvc_evict")
 
     def copy_blocks(self, cache, src_ids, dst_ids, n_layers: int = 1, blocks_per_layer: int | None = None, stream=None):
-        """In every layer, cache block src_ids[i] is copied to block dst_ids[i].  blocks_per_layer: default all there are."""
+        """In every layer, block src_ids[i] of an FP16 cache is copied to block dst_ids[i].  blocks_per_layer: default all there are."""
         rc = _call.copy(self._ctx.value, self._block_stride, self._span, cache, src_ids, dst_ids, n_layers, blocks_per_layer,
                         _stream_now() if stream is None else stream.cuda_stream)
         if rc:
