@@ -1,5 +1,5 @@
-// A wave's 32 tokens of a cache in 4 bits.  What a lane holds of them becomes what attention over FP16 works with (kvc_attend.h) by conversions alone: a code and its exponent are
-// an FP16 number exactly, so nothing is lost on the way.
+// A wave's 32 tokens of a cache in 4 bits.  What a lane holds of them becomes what attention over FP16 works with (kvc_attend.h) by conversions alone: a code and an exponent that
+// append wrote are an FP16 number exactly, so nothing is lost on the way.
 //
 // As sums over channels take their terms in any order, lane group g = lane / 16 has the channels 4w*g..4w*g+4w-1 of a piece of 16w: 2w bytes in a row, all of one
 // exponent.  (FP16 keys are taken 8 channels at a time: 4 * w/8 times 16 bytes.)  Values are as there: channels w*n..w*n+w-1 of 8 tokens, w/2 bytes of each row.
@@ -221,7 +221,7 @@ __device__ inline uint32_t load_values(ValuesFp4<D, EIGHT>& x, const AttendArgs&
     }
 }
 
-// 2^e, from byte `at` of a register: the conversion looks at nothing but bits 23 to 30 (a test compares all codes and exponents; 255 makes NaN of any code), so the byte is turned there and
+// 2^e, from byte `at` of a register: the conversion looks at nothing but bits 23 to 30 (a test compares all codes under all exponents that append writes, beside any others; 255 makes NaN of any code), so the byte is turned there and
 // its neighbours may be anywhere.
 __device__ inline float power_of(uint32_t bytes, uint32_t at) { return __uint_as_float(__builtin_amdgcn_alignbit(bytes, bytes, (8 * at + 9) & 31)); }
 

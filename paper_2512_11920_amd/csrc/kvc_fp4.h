@@ -110,7 +110,8 @@ constexpr int pipelined_fp4(bool eight) { return eight ? 128 : 64; }
 // 23.3; 32 units 13.6 / 9.8, 16.0 / 14.6, 17.5 / 23.6; 128 units 17.0 / 10.6, 20.0 / 15.1, 25.4 / 24.2, of 8,192 41.2 / 43.1; 256 units 19.6 / 11.4, 25.0 / 16.5, 40.7 / 30.8, 65.2 / 55.9; 512 units 24.9 / 20.9, 41.2 / 34.8;
 // 1,024 units of 128 16.2 / 18.6, of 448 23.4 / 27.7; 2,048 units 17.6 / 34.8, 34.7 / 56.3.  Sequences of a sixteenth of that length and more: 256 units of up to 8,192 tokens 46.0 / 43.8, 512 units of up to 2,048 28.5 / 26.4,
 // of up to 8,192 75.1 / 76.5 (heads of 96 70.5 / 82.1).  32 rows of 128 channels, or 8 of 192, for which there are no registers for a tile on its way: 128 units of 448 19.2 / 11.9, 14.9 / 9.1; 512 units 28.0 / 22.6, 21.0 / 17.6; 1,024
-// units 31.3 / 44.4, 28.5 / 34.2.
+// units 31.3 / 44.4, 28.5 / 34.2.  Lengths are on the device, and the rule goes by the table alone: where one sequence is long among short ones its workgroup is what the call waits for.  32 sequences, 256 units: one of 8,192 tokens
+// and 31 of 256 19.8 / 40.2, one of 4,096 16.3 / 23.2 (a table one block wider than 8,192 tokens has them divided); 64 sequences, 512 units, one of 2,048 and 63 of 128 15.6 / 14.4.
 inline bool direct_fp4(int d, bool eight, int row_tiles, int64_t units, int64_t tokens) {
     if (!direct_fits_fp4(d, row_tiles, eight) || units > 512) return false;
     if (tokens <= (int64_t)kDirectTiles * 32) return true;
@@ -119,8 +120,9 @@ inline bool direct_fp4(int d, bool eight, int row_tiles, int64_t units, int64_t 
 // Waves that weigh a few queries' tokens.  64 sequences of 1,024 to 8,192 tokens, 8 KV heads, 8 query heads each, us with two, three and four waves on a SIMD: 128 channels in 4 bits 47.2, 44.1, 53.4, in FP16 126.0, 124.1, 124.6; 64 in 4 bits 36.7,
 // 32.9, 31.5, in FP16 69.0, 70.8, 70.7; 32 34.6, 30.9, 29.8 and 43.6, 40.8, 41.7.  Workgroups that weigh many: three to a compute unit, which is what LDS has room for of 128 channels.
 constexpr uint32_t kWeighWorkers = 3 * 1024, kWeighGroups = 3 * 256;
-// Queries of a sequence and KV head beyond which they share a workgroup's keys.  64 sequences of 512 to 4,096 tokens, the same heads, us, few / many: 24 rows, 128 channels 111 / 183, in 4 bits 57 / 97; 64 rows 182 / 182, 95 / 95 (64
-// channels 88 / 118, 71 / 75; 32 sequences of 256 channels 204 / 247, 95 / 143); 128 rows 320 / 201, 166 / 120 (144 / 132, 125 / 93; 352 / 239, 174 / 170).
+// Queries of a sequence and KV head beyond which they share a workgroup's keys.  64 sequences of 512 to 4,096 tokens, the same heads, inputs that change from call to call, us, few / many: 24 rows, 128 channels 141 / 178, in 4 bits
+// 52 / 97; 64 rows 230 / 178, 92 / 96 (64 channels 80 / 118, 66 / 75; 32 sequences of 256 channels 212 / 233, 108 / 121); 128 rows 398 / 198, 169 / 121 (128 / 132, 115 / 94; 360 / 254, 191 / 157).  So FP16 keys of 128
+// channels would rather share from fewer rows on than the others.  (Few: the rows' queries are read again for every tile.)
 constexpr uint32_t kManyRows = 64;
 
 hipError_t launch_append_fp4(const AppendFp4Args& a, hipStream_t s);

@@ -1,7 +1,8 @@
 // Rows into a cache held in 4 bits, and its blocks back to FP16.
 //
 // A magnitude is one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 times 2^e, e of 32 channels of a token.  gfx950 converts pairs both ways in one instruction, to the nearest (halfway to the even
-// code), beyond 6 to 6; a test compares them with the definition for every FP16 value.  2^e times a code is an FP16 number, as e is 13 at most and FP16 values are multiples of 2^-24.
+// code), beyond 6 to 6; a test compares them with the definition for every finite FP16 value.  2^e times a code that comes out is an FP16 number, as e is 13 at most and FP16 values are
+// multiples of 2^-24, of which the smallest make codes of 1, 2, 3, 4 and 6 alone.
 #include "kvc_fp4.h"
 
 namespace kvc {

@@ -272,7 +272,8 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void k_weigh(WeighArgs x) {
 
 // ---- many queries: bound by the products, the powers and reading LDS.  A workgroup takes 64 tokens of a sequence and head, whose keys stay in the registers of every wave; 64 queries at a time come to LDS, the next
 // ones on their way meanwhile, with their -lse and the tokens they see, and each wave takes 16 of them.
-// 256 queries of 64 heads, 4 prompts of 1,024 to 2,048 tokens, 8 KV heads of 128 channels in 4 bits: 43 us, 600 TFLOP/s with one power for every 256 FLOP.
+// 256 queries of 64 heads, 4 prompts of 1,024 to 2,048 tokens, 8 KV heads of 128 channels in 4 bits: 42 us among other calls, 610 TFLOP/s with one power for every
+// 256 FLOP; 44 to 48 where such calls follow each other with nothing between them, as the clock falls then.
 constexpr uint32_t kChunk = 2 * kTile;
 template <int D, bool FP4, bool EIGHT>
 __global__ __launch_bounds__(256, D <= 128 && (EIGHT || !FP4 || D <= 96) ? 3 : 2) void k_weigh_many(WeighArgs x) {

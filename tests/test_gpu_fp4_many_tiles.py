@@ -195,10 +195,10 @@ def _check_weigh(c, apart):
 @pytest.mark.parametrize("N,d,most", [(16, 32, 1800), (5, 64, 1800), (16, 128, 1500), (8, 96, 1500), (3, 192, 1500), (16, 256, 1500)])
 @pytest.mark.parametrize("fp4", [False, True])
 def test_weights_by_waves_of_many_tiles(N, d, most, group, nq, fp4):
-    """Up to 64 rows: 3,072 waves share the tiles of all sequences and heads."""
+    """Up to 64 rows: three waves on a SIMD share the tiles of all sequences and heads."""
     kv, lens = 64, _lens(np.random.default_rng(d), 10, most)
     tiles = -(-lens // 32)
-    share = -(-int(tiles.sum()) * kv // 3072)
+    share = -(-int(tiles.sum()) * kv // (3 * 1024))
     assert share >= 4 and tiles.max() > share and (tiles % share).any()
     c = _weigh_case(d + nq, N, d, kv, group, nq, lens, fp4, holes=nq > 1, token_major=not fp4 and N == 16)
     _check_weigh(c, apart=nq != 7)
