@@ -137,8 +137,8 @@ __device__ inline void add_tile_fp4(Rows<D> (&r)[R], const AttendFp4Args& x, Til
 // ---- any lengths: a worker is a wave that takes tiles of one unit (a KV head and its rows), as many as any other, from sequence to sequence; two tiles are on their way while one is computed, the block numbers
 // of a third are looked up.  For each tile of 32 tokens 34 d bytes are read and become FP16, and for each 16 rows there are d / 8 MFMAs: of up to 16 rows memory and instructions cost about the same, and
 // neither hides the other fully.  64 sequences of 512 to 8,192 tokens, 8 KV heads of 128 channels, 8 query heads each: 65 us (and 6 to join), 305 MB at 4.7 TB/s, some 5 of them a chain of reads before the first tile (lengths, table, rows); on an earlier step that took 70, 66 with the products left out, 52 with all blocks in the caches.  2,048
-// waves are what registers allow; 4,096 in two turns take 83.  With 17 to 32 rows it takes 103 to 112 (109 and 111 with the
-// join among other calls, of 24 and 32): the registers leave one wave on a SIMD, whose conversions and products follow each other with nothing beside them; the products alone would take 28, the bytes 55.
+// waves are what registers allow; 4,096 in two turns take 83.  With 24 and 32 rows it takes 104 and 106 at
+// best, 110 and 114 on average in a row of calls: the registers leave one wave on a SIMD, whose conversions and products follow each other with nothing beside them; the products alone would take 28, the bytes 55.
 template <int D, int R, bool EIGHT>
 __device__ inline void own_part_fp4(const AttendFp4Args& x, Sums& sums, uint32_t worker) {
     const AttendArgs& a = x.a;
